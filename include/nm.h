@@ -180,6 +180,44 @@ int nm_matmul_host(const void *A_host, const void *B, void *C_host, void *A_stag
 int nm_matmul_static(const void *A, const void *B, void *C, int M, int N, int K,
                      nm_dtype dtype, nm_layout layout_B, nm_stream stream);
 
+/* ---- narrow product with 4-bit weights ------------------------------------------------------------- */
+
+/*
+ * C[M x N] = A[M x K] * W,  W[k][n] = (code[n][k] - 8) * scale[n][k / group],  1 <= M <= 16: the same product as nm_matmul with
+ * the resident weights in 4 bits, a quarter of the bytes (the paper has no counterpart: its weights are bf16).
+ *
+ *   dtype    NM_BF16, NM_BF16_F32OUT: A and scales bf16; NM_F16: A and scales fp16.  NM_F32: NM_ERR_UNSUPPORTED
+ *   group    32, 64, 128 or 256 consecutive k share a scale; the last group may be short
+ *   N, K     any >= 1
+ *   lda, ldc elements between rows of A (>= K) and C (>= N)
+ * Codes enter the products as exact integers, a group's sum is fp32, the scale multiplies that sum, and the result is rounded
+ * once.  A row of A that starts on 16 bytes (A 16-byte aligned, lda and K multiples of 8) is read in 16-byte loads, any other
+ * element by element.  No workspace: k-splits meet in the shared memory of a cluster, in a fixed order, so equal calls give
+ * equal bits and concurrent calls share nothing.  Honours nm_set_programmatic_launch.
+ *
+ * Storage, written by nm_w4_quantize (or by the caller): blocks of 16 columns n x 64 k, 512 bytes each, the blocks of one
+ * 16-column strip behind each other along k; nm_w4_packed_bytes in all, 16-byte aligned.  Byte 4 * (4 * (4 g + t) + j) + b of
+ * a block holds two codes: the low nibble that of column g, the high nibble that of column g + 8, both at
+ * k = 32 * (j >> 1) + 8 * t + 4 * (j & 1) + 2 * (b & 1) + (b >> 1)   (g 0..7; t, j, b 0..3).
+ * scales: [ceil(K / group)][ceil(N / 16)][8][2], the pair being columns g and g + 8 of the strip; nm_w4_scale_count
+ * elements, 4-byte aligned.  Codes and scales of columns >= N and codes of k >= K may hold anything.
+ */
+int nm_matmul_w4(const void *A, const void *packed, const void *scales, void *C, int M, int N, int K, int group, long lda,
+                 long ldc, nm_dtype dtype, nm_stream stream);
+
+size_t nm_w4_packed_bytes(int N, int K);
+size_t nm_w4_scale_count(int N, int K, int group);        /* 16-bit elements */
+
+/*
+ * Dense weights (B: K x N in NM_ROW_MAJOR or NM_COL_MAJOR, bf16 or fp16 by dtype) to 4 bits, and back.  Per column and group:
+ *   scale = round16(max |w| / 7),  code = clamp(round(w / scale), -8, 7) + 8  (8 where scale is 0),  back = round16((code - 8) * scale)
+ * round to nearest even throughout; a NaN weight becomes code 0.  Columns and k beyond N and K are stored as zero weights.
+ */
+int nm_w4_quantize(const void *B, void *packed, void *scales, int N, int K, int group, nm_dtype dtype, nm_layout layout_B,
+                   nm_stream stream);
+int nm_w4_dequantize(const void *packed, const void *scales, void *B, int N, int K, int group, nm_dtype dtype,
+                     nm_layout layout_B, nm_stream stream);
+
 /* ---- single-token MLA decode step ------------------------------------------------------------------ */
 
 /*

@@ -57,6 +57,13 @@ _lib.nm_matmul_batched.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _l, _l, _l, _l
 _lib.nm_matmul_batched_ws.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _l, _l, _l, _l, _l, _i, _i, _vp, _sz, _vp]
 _lib.nm_matmul_host.argtypes = [_vp, _vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _vp, _sz, _vp]
 _lib.nm_matmul_static.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _i, _vp]
+_lib.nm_matmul_w4.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _l, _l, _i, _vp]
+_lib.nm_w4_packed_bytes.restype = _sz
+_lib.nm_w4_packed_bytes.argtypes = [_i, _i]
+_lib.nm_w4_scale_count.restype = _sz
+_lib.nm_w4_scale_count.argtypes = [_i, _i, _i]
+_lib.nm_w4_quantize.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _i, _vp]
+_lib.nm_w4_dequantize.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _i, _vp]
 _lib.nm_debug_set_plan.argtypes = [_i, _i]
 _lib.nm_debug_set_kernel.argtypes = [_i, _i]
 _lib.nm_set_tensor_core_min_m.argtypes = [_i]
@@ -206,6 +213,28 @@ def nm_matmul_static(A, B, C_out, M, N, K, dtype, layout_B, stream=None) -> None
     should come before any stream capture."""
     _check(_lib.nm_matmul_static(_ptr(A), _ptr(B), _ptr(C_out), M, N, K, dtype, layout_B, _stream(stream)),
            "nm_matmul_static")
+
+
+def nm_matmul_w4(A, packed, scales, C_out, M, N, K, group, dtype, lda=None, ldc=None, stream=None) -> None:
+    """nm_matmul with the weights in 4 bits (nm_w4_quantize); lda / ldc default to dense rows."""
+    _check(_lib.nm_matmul_w4(_ptr(A), _ptr(packed), _ptr(scales), _ptr(C_out), M, N, K, group, K if lda is None else lda,
+                             N if ldc is None else ldc, dtype, _stream(stream)), "nm_matmul_w4")
+
+
+def nm_w4_packed_bytes(N, K) -> int:
+    return int(_lib.nm_w4_packed_bytes(N, K))
+
+
+def nm_w4_scale_count(N, K, group) -> int:
+    return int(_lib.nm_w4_scale_count(N, K, group))
+
+
+def nm_w4_quantize(B, packed, scales, N, K, group, dtype=BF16, layout_B=ROW_MAJOR, stream=None) -> None:
+    _check(_lib.nm_w4_quantize(_ptr(B), _ptr(packed), _ptr(scales), N, K, group, dtype, layout_B, _stream(stream)), "nm_w4_quantize")
+
+
+def nm_w4_dequantize(packed, scales, B_out, N, K, group, dtype=BF16, layout_B=ROW_MAJOR, stream=None) -> None:
+    _check(_lib.nm_w4_dequantize(_ptr(packed), _ptr(scales), _ptr(B_out), N, K, group, dtype, layout_B, _stream(stream)), "nm_w4_dequantize")
 
 
 def nm_debug_set_plan(tile_n: int = 0, nsplit: int = 0) -> None:

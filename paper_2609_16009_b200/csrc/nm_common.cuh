@@ -162,6 +162,9 @@ int matmul_enqueue(const void *A, const void *B, void *C, int M, int N, int K, i
 // force one of its products without touching what other host threads see.
 void set_thread_plan_override(bool active, int tile_n, int nsplit, int stages);
 
+// The process-wide nm_set_programmatic_launch setting.
+bool programmatic_launch_enabled();
+
 // How the row-major bf16 product K x N (H heads) at this M will be split: k-rows per split and splits.
 void matmul_row_major_split(int M, int N, int K, int H, int *k_rows_per_split, int *nsplit, bool chained = false);
 

@@ -81,6 +81,12 @@ static void refresh_tuning()
     if (g_plan_override.active) { g_t.force_tn = g_plan_override.tn; g_t.force_split = g_plan_override.split; g_t.force_stages = g_plan_override.stages; }
 }
 
+bool programmatic_launch_enabled()
+{
+    std::lock_guard<std::mutex> lock(g_tuning_mutex);
+    return g_tuning_shared.use_pdl != 0;
+}
+
 void set_thread_plan_override(bool active, int tile_n, int nsplit, int stages)
 {
     g_plan_override.active = active; g_plan_override.tn = tile_n; g_plan_override.split = nsplit; g_plan_override.stages = stages;
