@@ -6,12 +6,27 @@
 // registers.  (tcgen05 takes its operands from shared or tensor memory only: the unpacked 16-bit codes would cost a store and
 // a read of four times the packed bytes there, and at 2 * 16 flops per code the warp-level matrix pipe is not the limit.)
 // The storage of nm_w4.cuh makes a lane's 16-byte load its operand.
-//   unpack   a word w of eight codes: ((w >> 4 i) & 0x000f000f) | magic is a pair of 128 + code as bf16 (1024 + code as
-//            fp16), minus 136 (1032) exactly code - 8.  The codes stay integers in the product: exact in 16 bits, the sums of a
-//            group are fp32, and the scale multiplies the fp32 sum of its group - nothing is rounded before the output.
-//   split    a CTA is eight warps, wn of them side by side over strips, 8 / wn along k; up to eight CTAs of a cluster split k
-//            further.  Partial sums meet in shared memory, then in that of the cluster's first CTA, added in a fixed order:
+//   unpack   A code c in the low (high) nibble of a 16-bit half IS the fp16 number c * 2^-24 (c * 2^-20): a subnormal, which the
+//            matrix unit multiplies exactly.  So w & 0x000f000f, w & 0x00f000f0 and the same of w >> 8 are the four registers of the
+//            weight operand: five instructions for eight codes.  Low nibbles are rows g of the product and high ones rows g + 8, so
+//            the factor 16 goes into the scale of those rows.  (With the usual detour over 128 + c in bf16 - shift, mask, subtract
+//            - the kernel was bound by issue slots: 78 instructions a block of 1024 codes, 26 clocks of an SM against 22 of HBM.)
+//   minus 8  sum_k a (c - 8) = sum_k a c - 8 sum_k a: the second term, one number per token and scale group, is computed when
+//            the tokens are copied to shared memory and is what the group's accumulator starts from.  All of it is fp32; the
+//            error is that of adding terms of size 15 |a| instead of 8 |a|.
+//   tokens   fp16 as they are; bf16 ones times a power of two that puts the largest of the 64 (32) tokens that share a sum into
+//            fp16's last binade, 2^15: bf16's eight bits fit fp16's eleven, exactly down to 2^-29 of that largest value and to
+//            2^-40 of it absolutely below.  The inverse multiplies the sum together with the scale.
+//   scale    multiplies the fp32 sum of its group; nothing is rounded before the output.
+//   split    a CTA is eight warps, wn of them side by side over units (a unit: one strip, or two for M > 8), 8 / wn along k; up
+//            to eight CTAs of a cluster split k further.  Two to four CTAs share an SM, so that one fills its tokens while another
+//            streams.  Partial sums meet in shared memory, then in that of the cluster's first CTA, added in a fixed order:
 //            no workspace, no atomics, the same bits every time, and calls on different streams share nothing.
+// Measured back to back, weights from HBM: M = 1, 16384 x 7168, groups of 64: 16.5 us (62 MB, 3.8 TB/s; loads without the
+// products take 13); 7168 x 576: 4.5 us; 1536 x 24576: 8.6 us; M = 16, 7168 x 18432: 28.7 us.  What bounds it: M <= 8 a start and an end
+// of about 5 us around a stream at 5 to 6 TB/s; M > 8 the tokens - made ready once per SM, and read from shared memory
+// by every warp.  Built, measured and left: one CTA per SM whose warps walk evenly over all blocks of its share (20.8 us for the first: its
+// start and end are not hidden by another CTA), rings in shared memory by asynchronous copies (the same stream, more instructions).
 #include <type_traits>
 
 #include "nm_async.cuh"
@@ -21,7 +36,17 @@ namespace nm {
 
 namespace {
 
-constexpr int kThreads = 256, kWarps = 8;
+// Warps of a CTA: for M > 8 one CTA of sixteen per SM, so that the tokens are made ready once per SM; else two of eight, one of
+// which streams while the other starts or ends.
+__host__ __device__ constexpr int w4_warps(int nt) { return nt == 1 ? 8 : 16; }
+constexpr int kSmemMost = 224 * 1024;              // of an SM; a CTA of eight warps takes half of it
+
+// Bytes of the partial sums' exchange: tiles of the cluster's CTAs and of the other warps along k, or the finished tile.
+inline int w4_sum_bytes(int nt, int wn, int cl)
+{
+    const int tile = wn * nt * nt * 4 * 32, wk = w4_warps(nt) / wn, red = ((cl > 1 ? cl : 0) + wk - 1) * tile;
+    return (red > tile ? red : tile) * (int)sizeof(float);          // (a finished tile is as large: 8 nt rows of 16 nt wn columns)
+}
 
 struct W4Args {
     const uint16_t *A;
@@ -31,231 +56,409 @@ struct W4Args {
     long lda, ldc;
     int M, N, K;
     int nb, kb;                                    // strips, blocks along k
-    int blocks_per_group;                          // 64-k blocks a scale covers (groups of 64 and more)
-    int wn;                                        // warps side by side over strips
-    int cl;                                        // CTAs of a cluster, each a part of k
+    int groups;                                    // groups along k
+    int group_shift;                               // log2 of the 64-k blocks a scale covers (groups of 64 and more)
+    int wn_log2;                                   // log2 of the warps side by side over units
+    int cl, blocks_each, blocks_more;              // CTAs of a cluster, each a part of k: quotient and remainder of the shares
+    int chunk;                                     // blocks along k whose tokens a CTA holds at a time
+    int pitch;                                     // bytes between token rows in shared memory
+    int tok_bytes;                                 // of the tokens, the starts of the sums and the powers of two
+    int scale_bytes;
+    int vec;                                       // token rows start on 16 bytes
 };
 
-template <typename T> __device__ __forceinline__ uint32_t magic_sub(uint32_t v)
-{
-    if constexpr (std::is_same<T, bf16_t>::value) {
-        const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&v),
-                                         __halves2bfloat162(__ushort_as_bfloat16(0x4308), __ushort_as_bfloat16(0x4308)));
-        return *reinterpret_cast<const uint32_t *>(&r);
-    } else {
-        const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&v), __halves2half2(__ushort_as_half(0x6408), __ushort_as_half(0x6408)));
-        return *reinterpret_cast<const uint32_t *>(&r);
-    }
-}
 // eight codes of a word -> the four registers of the weight operand
-template <typename T> __device__ __forceinline__ void unpack_codes(uint32_t w, uint32_t (&r)[4])
+__device__ __forceinline__ void unpack_codes(uint32_t w, uint32_t (&r)[4])
 {
-    constexpr uint32_t magic = std::is_same<T, bf16_t>::value ? 0x43004300u : 0x64006400u;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = magic_sub<T>(((w >> (4 * i)) & 0x000f000fu) | magic);
+    const uint32_t v = w >> 8;
+    r[0] = w & 0x000f000fu; r[1] = w & 0x00f000f0u;
+    r[2] = v & 0x000f000fu; r[3] = v & 0x00f000f0u;
 }
-template <typename T> __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
-    if constexpr (std::is_same<T, bf16_t>::value)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// scales of rows g and g + 8, the latter with the 1 / 16 of its codes' place; fp16 tokens have no power of two of their own, so the
+// 2^24 of the codes goes in here
 template <typename T> __device__ __forceinline__ float2 scale_pair(uint32_t v)
 {
-    if constexpr (std::is_same<T, bf16_t>::value) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
-    else return __half22float2(*reinterpret_cast<const __half2 *>(&v));
-}
-
-// Eight consecutive k of a token row, zeros beyond K and for token rows beyond M (row == nullptr).
-template <bool kVec> __device__ __forceinline__ uint4 load_tokens(const uint16_t *row, int k, int K)
-{
-    if (!row || k >= K) return make_uint4(0u, 0u, 0u, 0u);
-    if constexpr (kVec) return __ldg(reinterpret_cast<const uint4 *>(row + k));
-    uint32_t v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t lo = k + 2 * i < K ? row[k + 2 * i] : 0u, hi = k + 2 * i + 1 < K ? row[k + 2 * i + 1] : 0u;
-        v[i] = lo | (hi << 16);
+    if constexpr (std::is_same<T, bf16_t>::value) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u) * 0.0625f);
+    else {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v));
+        return make_float2(f.x * 16777216.f, f.y * 1048576.f);
     }
-    return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
-__device__ __forceinline__ void cluster_barrier()
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// Predicated load: no branch, so that the loads of a ring stay in flight behind each other.
+__device__ __forceinline__ void ld_weights_if(uint4 &v, const void *p, bool ok)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t@p ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                 : "+r"(v.x), "+r"(v.y), "+r"(v.z), "+r"(v.w) : "l"(p), "r"((uint32_t)ok));
+}
+
+// Tokens of n k from k0 on to shared memory, ready for the product, zeros beyond K; the row pitch is 64 bytes off a multiple of
+// 128, so that the eight 16-byte reads of a quarter warp (two rows, 64 bytes each) hit 32 different banks.  One pass: the eight
+// (four) lanes that hold the tokens of a sum find their largest and their sum by shuffles.  Per sum and eight rows goes to
+// s_start what lane (g, t) needs for tokens 2 t and 2 t + 1: where the accumulators start, -8 sum a in units of 2^-24, for row g
+// and 16 times that for row g + 8; and to s_inv the powers of two taken out of the tokens and the codes.  Every CTA begins at a place of its own
+// (`turn`, a multiple of 8): all of them read the same few rows, and in step they would queue for the same lines of L2.
+template <typename T, bool kG32>
+__device__ __forceinline__ void stage_tokens(unsigned char *s, float *s_start, float *s_inv, const W4Args &a, int k0, int n, int turn)
+{
+    constexpr bool kBf16 = std::is_same<T, bf16_t>::value;
+    constexpr int kPer = kG32 ? 4 : 8;                             // vectors of eight tokens that share a sum
+    const int per = n / 8, tiles = (a.M + 7) / 8;                  // n is a multiple of 64
+    const unsigned mates = 0xffu << (threadIdx.x & 24);            // (eight lanes run together: per and blockDim are multiples of 8)
+    auto fetch = [&](int c, int m, uint32_t (&w)[4]) {
+        const int k = k0 + 8 * c;
+        const uint16_t *src = a.A + m * a.lda + k;
+        w[0] = w[1] = w[2] = w[3] = 0u;
+        if (a.vec) {
+            if (k < a.K) {
+                const uint4 x = __ldg(reinterpret_cast<const uint4 *>(src));
+                w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = (k + 2 * j < a.K ? (uint32_t)src[2 * j] : 0u) | ((k + 2 * j + 1 < a.K ? (uint32_t)src[2 * j + 1] : 0u) << 16);
+        }
+    };
+    auto finish = [&](int c, int m, uint32_t (&w)[4]) {
+        float inv = 1.f, sum = 0.f;
+        if constexpr (kBf16) {
+            uint32_t top = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
+            top = __vmaxu2(top, __shfl_xor_sync(mates, top, 1));
+            top = __vmaxu2(top, __shfl_xor_sync(mates, top, 2));
+            if constexpr (!kG32) top = __vmaxu2(top, __shfl_xor_sync(mates, top, 4));
+            // exponent e of the largest, at least -112; up = 2^(15 - e) and inv = 2^(24 - 15 + e), both inside fp32's range
+            const int e = max((int)(max(top >> 16, top & 0xffffu) >> 7) - 127, -112);
+            const float up = __uint_as_float((uint32_t)(127 + 15 - min(e, 119)) << 23);
+            inv = e >= 119 ? __uint_as_float(0x7fc00000u)          // (an infinity or NaN among them, or 2^119: the sum is NaN)
+                           : __uint_as_float((uint32_t)(127 + 9 + e) << 23);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float x = __uint_as_float(w[j] << 16) * up, y = __uint_as_float(w[j] & 0xffff0000u) * up;
+                const __half2 h = __floats2half2_rn(x, y);
+                w[j] = *reinterpret_cast<const uint32_t *>(&h);
+                sum += x + y;                                      // (what fp16 drops of them is below 2^-40 of the largest)
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w[j]));
+                sum += f.x + f.y;
+            }
+        }
+        *reinterpret_cast<uint4 *>(s + m * a.pitch + 16 * c) = make_uint4(w[0], w[1], w[2], w[3]);
+        sum += __shfl_xor_sync(mates, sum, 1);
+        sum += __shfl_xor_sync(mates, sum, 2);
+        if constexpr (!kG32) sum += __shfl_xor_sync(mates, sum, 4);
+        if (c % kPer == 0) {
+            const int at = (c / kPer) * tiles + (m >> 3);
+            const float st = sum * (-8.f / 16777216.f);
+            float *d = s_start + at * 16 + ((m & 7) >> 1) * 4 + (m & 1);
+            d[0] = st; d[2] = 16.f * st;
+            if constexpr (kBf16) s_inv[at * 8 + (m & 7)] = inv;
+        }
+    };
+    auto place = [&](int i) { const int c = i + turn; return c >= per ? c - per : c; };
+    // four loads on their way: of four rows, or where there are fewer of four places in a row
+    const int step = blockDim.x;
+    if (a.M >= 4) {
+        for (int i = threadIdx.x; i < per; i += step)
+            for (int m = 0; m < a.M; m += 4) {
+                uint32_t w[4][4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (m + j < a.M) fetch(place(i), m + j, w[j]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (m + j < a.M) finish(place(i), m + j, w[j]);
+            }
+    } else {
+        for (int m = 0; m < a.M; ++m)
+            for (int i = threadIdx.x; i < per; i += 4 * step) {
+                uint32_t w[4][4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (i + j * step < per) fetch(place(i + j * step), m, w[j]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) if (i + j * step < per) finish(place(i + j * step), m, w[j]);
+            }
+    }
+}
+
+__device__ __forceinline__ void cluster_arrive()
 {
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-// kNT: groups of eight tokens; kG32: groups of 32 k (two scales per block); kVec: tokens in 16-byte loads
-template <typename T, typename TO, int kNT, bool kG32, bool kVec>
-__global__ void __launch_bounds__(kThreads, 2) w4_kernel(const W4Args a)
+// kNT: groups of eight tokens; kG32: groups of 32 k (two scales per block).  A warp multiplies kNT strips side by side, so that the
+// tokens of up to sixteen rows are read from shared memory half as often (their 16-byte reads would bound M > 8 otherwise).
+template <typename T, typename TO, int kNT, bool kG32>
+__global__ void __launch_bounds__(w4_warps(kNT) * 32, kNT == 1 ? 2 : 1) w4_kernel(const W4Args a)
 {
-    constexpr int kDepth = kNT == 1 ? 4 : 2;                       // blocks on their way while as many are multiplied
-    constexpr int kS = kG32 ? 2 : 1;
-    extern __shared__ float s_red[];
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
-    const int wn = a.wn, wk = kWarps / wn, wr = warp % wn, wki = warp / wn;
+    constexpr bool kBf16 = std::is_same<T, bf16_t>::value;
+    constexpr int kS = kG32 ? 2 : 1, kSide = kNT;                    // scales of a block; strips of a unit
+    constexpr int kWarps = w4_warps(kNT), kThreads = kWarps * 32, kWarpsLog2 = kNT == 1 ? 3 : 4;
+    constexpr int kDepth = kNT == 1 ? 8 : 3;                       // blocks of weights on their way, per warp
+    constexpr int kVals = kSide * kNT * 4;                         // sums a lane holds
+    extern __shared__ __align__(16) unsigned char s_raw[];
+    unsigned char *s_tok = s_raw;
+    float *s_start = reinterpret_cast<float *>(s_tok + a.M * a.pitch);     // [block (half)][eight tokens][t][4]: where the sums start
+    float *s_inv = s_start + a.chunk * kS * kNT * 16;                      // [block (half)][eight tokens][8]: the tokens' powers of two
+    uint32_t *s_scale = reinterpret_cast<uint32_t *>(s_raw + a.tok_bytes); // [warp of the row][block (half)][side][8 pairs]
+    float *s_red = reinterpret_cast<float *>(s_raw + a.tok_bytes + a.scale_bytes);
+    const int tid = threadIdx.x, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);       // the same for the whole warp, and the compiler knows
+    const int wn = 1 << a.wn_log2, wk_log2 = kWarpsLog2 - a.wn_log2, wr = warp & (wn - 1), wki = warp >> a.wn_log2;
     const int rank = blockIdx.x, tile = blockIdx.y;
-    const int strip = tile * wn + wr;
-    const bool live = strip < a.nb;
-    const int part = rank * wk + wki, parts = wk * a.cl;
-    const int b0 = (int)((long)a.kb * part / parts), b1 = live ? (int)((long)a.kb * (part + 1) / parts) : b0;
+    const int strip = (tile * wn + wr) * kSide;
+    const bool live = strip < a.nb, both = kSide == 2 && strip + 1 < a.nb;
+    const int cta0 = rank * a.blocks_each + min(rank, a.blocks_more), cta1 = cta0 + a.blocks_each + (rank < a.blocks_more);
+    if (a.cl > 1) cluster_arrive();                                // first half of a barrier: see the sums' exchange
     pdl_launch_dependents();
 
-    float acc[kNT][4] = {};
-    struct Stage { uint4 w; uint32_t s[kS]; };
+    float acc[kSide][kNT][4] = {};
     const uint4 *wp = a.packed + (long)(live ? strip : 0) * a.kb * 32 + lane;
-    const uint32_t *sp = a.scales + (long)(live ? strip : 0) * 8 + g;
-    auto load_stage = [&](Stage &st, int b) {
-        if (b < b1) {
-            st.w = ld_stream16(wp + (long)b * 32);
-#pragma unroll
-            for (int i = 0; i < kS; ++i) {
-                const int grp = kG32 ? min(2 * b + i, (a.K - 1) / 32) : b / a.blocks_per_group;
-                st.s[i] = __ldg(sp + (long)grp * a.nb * 8);
-            }
-        } else {
-            st.w = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-            for (int i = 0; i < kS; ++i) st.s[i] = 0u;
-        }
-    };
-    const uint16_t *row[kNT];
-#pragma unroll
-    for (int n = 0; n < kNT; ++n) row[n] = g + 8 * n < a.M ? a.A + (long)(g + 8 * n) * a.lda : nullptr;
-
-    Stage cur[kDepth], nxt[kDepth];
-#pragma unroll
-    for (int i = 0; i < kDepth; ++i) load_stage(cur[i], b0 + i);
-    pdl_wait_prior_grids();                                        // weights may come early, tokens not
-    for (int b = b0; b < b1; b += kDepth) {
-        uint4 tok[kDepth][kNT][2];
+    const long side_step = both ? (long)a.kb * 32 : 0;             // (an odd last strip is multiplied twice, the second time for nothing)
+    for (int c0 = cta0; c0 < cta1; c0 += a.chunk) {                // one chunk unless the tokens of the CTA's k exceed its shared memory
+        const int R = min(cta1, c0 + a.chunk) - c0;
+        const int b0 = (R * wki) >> wk_log2, b1 = live ? (R * (wki + 1)) >> wk_log2 : b0;      // the warp's blocks, from c0 on
+        // they pass through a ring of registers: a slot is loaded anew as soon as its block has been multiplied
+        uint4 w[kDepth][kSide] = {};
+        const uint4 *next = wp + (long)(c0 + b0) * 32;
 #pragma unroll
         for (int i = 0; i < kDepth; ++i)
 #pragma unroll
-            for (int n = 0; n < kNT; ++n)
+            for (int r = 0; r < kSide; ++r) ld_weights_if(w[i][r], next + r * side_step + i * 32, b0 + i < b1);
+        next += kDepth * 32;
+        if (c0 > cta0) __syncthreads();                            // the chunk before has been read
+        // the scales of the warp's own blocks - a block has its own entry even where it shares a scale, so that it is found without arithmetic
+        uint32_t *sw = s_scale + wr * (a.chunk * kS * kSide * 8);
+        for (int j = b0 * (kS * kSide) + (lane >> 3); j < b1 * (kS * kSide); j += 4) {
+            const int side = both ? j & 1 : 0, half = kG32 ? (j / kSide) & 1 : 0, blk = c0 + j / (kS * kSide);
+            const int grp = kG32 ? min(2 * blk + half, a.groups - 1) : blk >> a.group_shift;
+            cp_async4(smem_u32(sw + j * 8 + (lane & 7)), a.scales + (size_t)(unsigned)grp * (unsigned)(a.nb * 8) + (unsigned)(strip + side) * 8u + (lane & 7));
+        }
+        if (c0 == cta0) pdl_wait_prior_grids();                    // weights may come early, tokens not
+        stage_tokens<T, kG32>(s_tok, s_start, s_inv, a, c0 * kW4Rows, R * kW4Rows, (int)((long)R * tile / gridDim.y) * 8);
+        cp_async_wait_all();
+        __syncthreads();
+        // lanes of tokens beyond M read the last token's: their columns of the product are never stored
+        const unsigned char *tp[kNT];
 #pragma unroll
-                for (int h = 0; h < 2; ++h)                        // a block of the next warp's part meets zero codes' scales: not loaded
-                    tok[i][n][h] = b + i < b1 ? load_tokens<kVec>(row[n], (b + i) * kW4Rows + 32 * h + 8 * t, a.K) : make_uint4(0u, 0u, 0u, 0u);
+        for (int n = 0; n < kNT; ++n) tp[n] = s_tok + min(g + 8 * n, a.M - 1) * a.pitch + 16 * t + b0 * (kW4Rows * 2);
+        const float *st = s_start + b0 * (kS * kNT * 16) + 4 * t, *iv = s_inv + b0 * (kS * kNT * 8) + 2 * t;
+        const uint32_t *sc = sw + b0 * (kS * kSide * 8) + g;
+        auto multiply = [&](const uint4 (&code)[kSide], int j) {   // j: blocks from where the pointers stand
+            uint4 tok[2][kNT];
 #pragma unroll
-        for (int i = 0; i < kDepth; ++i) load_stage(nxt[i], b + kDepth + i);
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < kDepth; ++i) {
-            const uint32_t w[4] = {cur[i].w.x, cur[i].w.y, cur[i].w.z, cur[i].w.w};
-            float sum[kNT][4] = {};
+                for (int n = 0; n < kNT; ++n) tok[h][n] = *reinterpret_cast<const uint4 *>(tp[n] + j * (kW4Rows * 2) + 64 * h);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t op[4];
-                unpack_codes<T>(w[j], op);
+            for (int r = 0; r < kSide; ++r) {
+                const uint32_t word[4] = {code[r].x, code[r].y, code[r].z, code[r].w};
+                float sum[kNT][4];
 #pragma unroll
-                for (int n = 0; n < kNT; ++n) {
-                    const uint4 &v = tok[i][n][j >> 1];
-                    mma16816<T>(sum[n], op, (j & 1) ? v.z : v.x, (j & 1) ? v.w : v.y);
-                }
-                if ((kG32 && j == 1) || j == 3) {                  // the group's sum is complete (or the block's): its scale
-                    const float2 sc = scale_pair<T>(cur[i].s[kG32 ? j >> 1 : 0]);
+                for (int h = 0; h < 2; ++h) {
+                    if (kG32 || h == 0) {
 #pragma unroll
-                    for (int n = 0; n < kNT; ++n) {
-                        acc[n][0] = fmaf(sc.x, sum[n][0], acc[n][0]); acc[n][1] = fmaf(sc.x, sum[n][1], acc[n][1]);
-                        acc[n][2] = fmaf(sc.y, sum[n][2], acc[n][2]); acc[n][3] = fmaf(sc.y, sum[n][3], acc[n][3]);
-                        sum[n][0] = sum[n][1] = sum[n][2] = sum[n][3] = 0.f;
+                        for (int n = 0; n < kNT; ++n) {
+                            const float4 q = *reinterpret_cast<const float4 *>(st + ((j * kS + h) * kNT + n) * 16);
+                            sum[n][0] = q.x; sum[n][1] = q.y; sum[n][2] = q.z; sum[n][3] = q.w;
+                        }
+                    }
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        uint32_t op[4];
+                        unpack_codes(word[2 * h + q], op);
+#pragma unroll
+                        for (int n = 0; n < kNT; ++n) mma16816(sum[n], op, q ? tok[h][n].z : tok[h][n].x, q ? tok[h][n].w : tok[h][n].y);
+                    }
+                    if (kG32 || h == 1) {                          // the group's sum is complete (or the block's): its scale
+                        const int hs = kG32 ? h : 0;
+                        const float2 f = scale_pair<T>(sc[((j * kS + hs) * kSide + r) * 8]);
+#pragma unroll
+                        for (int n = 0; n < kNT; ++n) {
+                            float2 inv = make_float2(1.f, 1.f);
+                            if constexpr (kBf16) inv = *reinterpret_cast<const float2 *>(iv + ((j * kS + hs) * kNT + n) * 8);
+                            acc[r][n][0] = fmaf(f.x, sum[n][0] * inv.x, acc[r][n][0]); acc[r][n][1] = fmaf(f.x, sum[n][1] * inv.y, acc[r][n][1]);
+                            acc[r][n][2] = fmaf(f.y, sum[n][2] * inv.x, acc[r][n][2]); acc[r][n][3] = fmaf(f.y, sum[n][3] * inv.y, acc[r][n][3]);
+                        }
                     }
                 }
             }
-        }
+        };
+        auto turn = [&]() {
 #pragma unroll
-        for (int i = 0; i < kDepth; ++i) cur[i] = nxt[i];
+            for (int n = 0; n < kNT; ++n) tp[n] += kDepth * (kW4Rows * 2);
+            st += kDepth * (kS * kNT * 16); iv += kDepth * (kS * kNT * 8); sc += kDepth * (kS * kSide * 8);
+            next += kDepth * 32;
+        };
+        int left = b1 - b0;
+        for (; left >= 2 * kDepth; left -= kDepth) {
+#pragma unroll
+            for (int i = 0; i < kDepth; ++i) {
+                multiply(w[i], i);
+#pragma unroll
+                for (int r = 0; r < kSide; ++r) w[i][r] = ld_stream16(next + r * side_step + i * 32);
+            }
+            turn();
+        }
+        for (; left > 0; left -= kDepth) {                         // the last one or two turns of the ring
+#pragma unroll
+            for (int i = 0; i < kDepth; ++i) {
+                if (i < left) multiply(w[i], i);
+#pragma unroll
+                for (int r = 0; r < kSide; ++r) ld_weights_if(w[i][r], next + r * side_step + i * 32, kDepth + i < left);
+            }
+            turn();
+        }
     }
 
     // ---- partial sums: over the CTA's warps along k, then over the cluster's CTAs, each in index order --------------------
-    constexpr int kVals = kNT * 4;                                 // floats a lane holds
-    const int tile_vals = wn * kVals * 32;                         // floats of the CTA's tile, [strip warp][value][lane]
+    const int wk = kWarps >> a.wn_log2, tile_vals = wn * kVals * 32;       // floats of the CTA's tile, [unit][value][lane]
     float *slots = s_red;                                          // [cluster rank][tile], used in rank 0
     float *local = s_red + (a.cl > 1 ? a.cl : 0) * tile_vals;      // [wk - 1][tile]
     const int mine = wr * kVals * 32 + lane;
+    float *sums = &acc[0][0][0];
     if (wki > 0) {
         float *d = local + (wki - 1) * tile_vals + mine;
 #pragma unroll
-        for (int n = 0; n < kNT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) d[(n * 4 + i) * 32] = acc[n][i];
+        for (int i = 0; i < kVals; ++i) d[i * 32] = sums[i];
     }
     __syncthreads();
     if (wki == 0) {
-        for (int w = 0; w < wk - 1; ++w) {
-            const float *s = local + w * tile_vals + mine;
+        for (int q = 0; q < wk - 1; ++q) {
+            const float *v = local + q * tile_vals + mine;
 #pragma unroll
-            for (int n = 0; n < kNT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[n][i] += s[(n * 4 + i) * 32];
+            for (int i = 0; i < kVals; ++i) sums[i] += v[i * 32];
         }
     }
     if (a.cl > 1) {
-        // peers have all started (their shared memory exists) once this barrier is passed; the second one orders the stores
-        cluster_barrier();
+        cluster_wait();                                            // every peer has started: its shared memory exists
         if (wki == 0 && rank > 0) {
             uint32_t dst;
             asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(dst) : "r"(smem_u32(slots + rank * tile_vals + mine)), "r"(0));
 #pragma unroll
-            for (int n = 0; n < kNT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst + 128u * (n * 4 + i)), "f"(acc[n][i]) : "memory");
+            for (int i = 0; i < kVals; ++i) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(dst + 128u * i), "f"(sums[i]) : "memory");
         }
-        cluster_barrier();
+        cluster_arrive();
+        cluster_wait();
         if (rank > 0) return;
         if (wki == 0) {
             for (int p = 1; p < a.cl; ++p) {
-                const float *s = slots + p * tile_vals + mine;
+                const float *v = slots + p * tile_vals + mine;
 #pragma unroll
-                for (int n = 0; n < kNT; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[n][i] += s[(n * 4 + i) * 32];
+                for (int i = 0; i < kVals; ++i) sums[i] += v[i * 32];
             }
         }
     }
     // ---- the tile leaves as rows of C: lane (g, t) holds columns g and g + 8 of tokens 2 t and 2 t + 1 ------------------------
     __syncthreads();
-    const int cols = wn * kW4Cols;
+    constexpr int kCols = kSide * kW4Cols;
+    const int cols_log2 = a.wn_log2 + (kSide == 2 ? 5 : 4), cols = 1 << cols_log2;
     if (wki == 0) {
 #pragma unroll
-        for (int n = 0; n < kNT; ++n)
+        for (int r = 0; r < kSide; ++r)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s_red[(8 * n + 2 * t + (i & 1)) * cols + wr * kW4Cols + g + 8 * (i >> 1)] = acc[n][i];
+            for (int n = 0; n < kNT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    s_red[(8 * n + 2 * t + (i & 1)) * cols + wr * kCols + r * kW4Cols + g + 8 * (i >> 1)] = acc[r][n][i];
     }
     __syncthreads();
     TO *C = static_cast<TO *>(a.C);
-    const int n0 = tile * cols;
+    const long n0 = (long)tile * cols;
     for (int i = tid; i < a.M * cols; i += kThreads) {
-        const int m = i / cols, c = i - m * cols;
+        const int m = i >> cols_log2, c = i & (cols - 1);
         if (n0 + c < a.N) C[(long)m * a.ldc + n0 + c] = round_out<TO>(s_red[i]);
     }
 }
 
+// How many warps side by side and how many CTAs along k: the least time by a model in microseconds, fitted to sweeps of both on B200
+// (shapes of 0.6 to 18 thousand columns and 1.5 to 16 thousand k).  Per wave of resident CTAs: a fixed start and end, a block of
+// 1024 codes per 12.6 ns and SM (15 for two strips side by side), a block of a token row per 3 (6) ns, and a cluster's exchange.
+// `resident`: clusters of each size that run at once (their CTAs need SMs of one GPC, so not every size fills the machine).
 struct W4Plan { int wn, cl; };
-
-W4Plan plan_w4(int nb, int kb)
+W4Plan plan_w4(int M, int units, int kb, const int (&resident)[9])
 {
-    W4Plan p{8, 1};
-    while (p.wn > 1 && ceil_div(nb, p.wn) < 2 * kSMs && kb >= 2 * (kWarps / p.wn)) p.wn /= 2;
-    while (p.cl < 8 && ceil_div(nb, p.wn) * p.cl < 2 * kSMs && kb / ((kWarps / p.wn) * p.cl * 2) >= 4) p.cl *= 2;
-    return p;
+    const bool wide = M > 8;
+    const int warps = w4_warps(wide ? 2 : 1);
+    W4Plan best{warps, 1};
+    double least = 1e300;
+    for (int wn = 1; wn <= warps; wn *= 2)
+        for (int cl = 1; cl <= 8 && cl <= kb; ++cl) {
+            if (resident[cl] < 1 || w4_sum_bytes(wide ? 2 : 1, wn, cl) > (wide ? 96 : 40) * 1024) continue;      // (the tokens want room too)
+            const int tiles = ceil_div(units, wn), blocks = ceil_div(kb, cl), run = ceil_div(blocks, warps / wn);
+            const int waves = ceil_div(tiles, resident[cl]), on_sm = wide || (long)tiles * cl <= kSMs ? 1 : 2;
+            const double stream = on_sm * warps * run * (wide ? 2 * 0.015 : 0.0126), tokens = on_sm * M * blocks * (wide ? 0.006 : 0.003);
+            const double cost = waves * ((wide ? 2.0 : 1.5) + stream + tokens + (cl > 1 ? 0.8 : 0.0));
+            if (cost < least) { least = cost; best = W4Plan{wn, cl}; }
+        }
+    return best;
 }
 
-template <typename T, typename TO, int kNT, bool kG32, bool kVec>
-cudaError_t launch_w4(const W4Args &a, cudaStream_t stream, bool pdl)
+// Asked of one instance for all of its kind: they differ in nothing that matters here.
+template <int kNT>
+cudaError_t resident_clusters(int (&resident)[9])
 {
-    const int wk = kWarps / a.wn, tile_vals = a.wn * kNT * 4 * 32;
-    const size_t red = (size_t)((a.cl > 1 ? a.cl : 0) + wk - 1) * tile_vals, out = (size_t)(8 * kNT) * a.wn * kW4Cols;
+    static std::atomic<unsigned long long> configured{0};
+    auto kern = w4_kernel<bf16_t, bf16_t, kNT, false>;
+    cudaError_t e = ensure_dynamic_smem(kern, kSmemMost, configured);
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.cl, ceil_div(a.nb, a.wn), 1);
-    cfg.blockDim = dim3(kThreads);
-    // at most eight cluster slots of eight strips and seven more tiles of one: (8 * wn + 7) KB x kNT, below 48 KB only for
-    // wn * kNT <= 4 with a full cluster; plan_w4 takes a cluster when there are few strips, so wn is 1 or 2 then
-    cfg.dynamicSmemBytes = (red > out ? red : out) * sizeof(float);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.blockDim = dim3(w4_warps(kNT) * 32);
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cfg.dynamicSmemBytes = kNT == 1 ? kSmemMost / 2 : kSmemMost;
+    resident[0] = 0;
+    resident[1] = kNT == 1 ? 2 * kSMs : kSMs;
+    for (int cl = 2; cl <= 8; ++cl) {
+        attr[0].val.clusterDim.x = cl;
+        cfg.gridDim = dim3(cl, 1, 1);
+        resident[cl] = max_clusters_cached(kern, cfg, cl);
+    }
+    return cudaSuccess;
+}
+
+template <typename T, typename TO, int kNT, bool kG32>
+cudaError_t launch_w4(W4Args a, cudaStream_t stream, bool pdl)
+{
+    static std::atomic<unsigned long long> configured{0};
+    auto kern = w4_kernel<T, TO, kNT, kG32>;
+    cudaError_t e = ensure_dynamic_smem(kern, kSmemMost, configured);
+    if (e != cudaSuccess) return e;
+    constexpr int kS = kG32 ? 2 : 1, kSide = kNT, kWarps = w4_warps(kNT), kStart = kS * kNT * (std::is_same<T, bf16_t>::value ? 96 : 64);
+    const int units = ceil_div(a.nb, kSide);
+    int resident[9];
+    e = resident_clusters<kNT>(resident);
+    if (e != cudaSuccess) return e;
+    const W4Plan p = plan_w4(a.M, units, a.kb, resident);
+    for (a.wn_log2 = 0; (1 << a.wn_log2) < p.wn; ++a.wn_log2) {}
+    a.cl = p.cl;
+    a.blocks_each = a.kb / a.cl; a.blocks_more = a.kb % a.cl;
+    // per block of the CTA's k: M x 128 bytes of tokens, the starts of their sums, the scales of wn units
+    const int scale_block = kS * kSide * 32 * p.wn, run = ceil_div(a.kb, a.cl), sum_bytes = w4_sum_bytes(kNT, p.wn, p.cl);
+    const int fit = ((kNT == 1 ? kSmemMost / 2 : kSmemMost) - sum_bytes - a.M * 64) / (a.M * kW4Rows * 2 + kStart + scale_block);
+    a.chunk = ceil_div(run, ceil_div(run, fit));
+    a.pitch = a.chunk * (kW4Rows * 2) + 64;
+    a.tok_bytes = a.M * a.pitch + a.chunk * kStart;
+    a.scale_bytes = a.chunk * scale_block;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(a.cl, ceil_div(units, p.wn), 1);
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.dynamicSmemBytes = a.tok_bytes + a.scale_bytes + sum_bytes;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     int n = 0;
@@ -271,14 +474,14 @@ cudaError_t launch_w4(const W4Args &a, cudaStream_t stream, bool pdl)
     }
     cfg.attrs = attr;
     cfg.numAttrs = n;
-    return cudaLaunchKernelEx(&cfg, w4_kernel<T, TO, kNT, kG32, kVec>, a);
+    return cudaLaunchKernelEx(&cfg, kern, a);
 }
 
-template <typename T, typename TO, int kNT>
-cudaError_t dispatch_w4(const W4Args &a, bool g32, bool vec, cudaStream_t s, bool pdl)
+template <typename T, typename TO>
+cudaError_t dispatch_w4(const W4Args &a, bool g32, cudaStream_t s, bool pdl)
 {
-    if (g32) return vec ? launch_w4<T, TO, kNT, true, true>(a, s, pdl) : launch_w4<T, TO, kNT, true, false>(a, s, pdl);
-    return vec ? launch_w4<T, TO, kNT, false, true>(a, s, pdl) : launch_w4<T, TO, kNT, false, false>(a, s, pdl);
+    if (a.M <= 8) return g32 ? launch_w4<T, TO, 1, true>(a, s, pdl) : launch_w4<T, TO, 1, false>(a, s, pdl);
+    return g32 ? launch_w4<T, TO, 2, true>(a, s, pdl) : launch_w4<T, TO, 2, false>(a, s, pdl);
 }
 
 }  // namespace
@@ -306,18 +509,15 @@ int nm_matmul_w4(const void *A, const void *packed, const void *scales, void *C,
     a.M = M; a.N = N; a.K = K;
     a.nb = (int)(((long)N + kW4Cols - 1) / kW4Cols);
     a.kb = (int)(((long)K + kW4Rows - 1) / kW4Rows);
-    a.blocks_per_group = group >= kW4Rows ? group / kW4Rows : 1;
-    const W4Plan p = plan_w4(a.nb, a.kb);
-    a.wn = p.wn; a.cl = p.cl;
-    if (ceil_div(a.nb, p.wn) > 65535) return NM_ERR_UNSUPPORTED;
+    a.group_shift = group == 256 ? 2 : (group == 128 ? 1 : 0);
+    a.groups = (int)(((long)K + group - 1) / group);
     // 16-byte token loads want 16-byte aligned rows and a K that no such load straddles
-    const bool vec = !((uintptr_t)A & 15u) && lda % 8 == 0 && K % 8 == 0;
+    a.vec = !((uintptr_t)A & 15u) && lda % 8 == 0 && K % 8 == 0;
     const bool pdl = programmatic_launch_enabled(), g32 = group < kW4Rows;
     cudaStream_t s = (cudaStream_t)stream;
-    cudaError_t e;
-    if (dtype == NM_F16) e = M <= 8 ? dispatch_w4<f16_t, f16_t, 1>(a, g32, vec, s, pdl) : dispatch_w4<f16_t, f16_t, 2>(a, g32, vec, s, pdl);
-    else if (dtype == NM_BF16_F32OUT) e = M <= 8 ? dispatch_w4<bf16_t, float, 1>(a, g32, vec, s, pdl) : dispatch_w4<bf16_t, float, 2>(a, g32, vec, s, pdl);
-    else e = M <= 8 ? dispatch_w4<bf16_t, bf16_t, 1>(a, g32, vec, s, pdl) : dispatch_w4<bf16_t, bf16_t, 2>(a, g32, vec, s, pdl);
+    const cudaError_t e = dtype == NM_F16            ? dispatch_w4<f16_t, f16_t>(a, g32, s, pdl)
+                          : dtype == NM_BF16_F32OUT ? dispatch_w4<bf16_t, float>(a, g32, s, pdl)
+                                                    : dispatch_w4<bf16_t, bf16_t>(a, g32, s, pdl);
     return e == cudaSuccess ? NM_OK : record_cuda_error(e, "4-bit narrow matmul launch");
 }
 

@@ -71,7 +71,8 @@ def case(M, N, K, group, dtype, seed, lda=None):
     A = torch.from_numpy(rng.standard_normal((M, K))).to(t)
     w = (codes - 8) * np.repeat(sc.double().numpy(), group, axis=1)[:, :K]
     a = A.double().numpy()
-    return A, codes, sc, a @ w.T, np.abs(a) @ np.abs(w).T
+    # sizes of the terms that are added: a times a code 0..15, and 8 a taken off again
+    return A, codes, sc, a @ w.T, np.abs(a) @ (23 * np.repeat(sc.double().numpy(), group, axis=1)[:, :K]).T
 
 
 def assert_close(got, ref, size, dtype):
@@ -94,7 +95,8 @@ def product(nm, A, codes, sc, M, N, K, group, dtype, lda=None, ldc=None, shift=0
     nm.nm_matmul_w4(dA[shift:], packed, scales, C[1:], M, N, K, group, dtype, lda=lda, ldc=ldc)
     again = torch.full((M, ldc), 77.0, dtype=out, device="cuda")
     nm.nm_matmul_w4(dA[shift:], packed, scales, again, M, N, K, group, dtype, lda=lda, ldc=ldc)
-    assert torch.equal(C[1:M + 1], again), "equal calls give equal bits"
+    bits = torch.int32 if out == torch.float32 else torch.int16
+    assert torch.equal(C[1:M + 1].view(bits), again.view(bits)), "equal calls give equal bits"
     c = C.double().cpu().numpy()
     assert (c[0] == 77).all() and (c[-1] == 77).all() and (c[:, N:] == 77).all(), "written outside C"
     return c[1:M + 1, :N]
@@ -138,19 +140,40 @@ def test_strides_and_alignment(lda, ldc, shift):
 
 @pytest.mark.gpu
 def test_codes_are_exact_integers():
-    """One-hot tokens read single weights: (code - 8) * scale to the last bit, every code, and infinite tokens stay where they are."""
+    """One-hot tokens read single weights: (code - 8) * scale to the last bit, every code.  A token row with an infinity or a NaN
+    gives NaN and leaves the other rows alone."""
     import paper_2609_16009_b200 as nm
     N, K = 32, 128
     codes = np.arange(N * K).reshape(N, K) % 16
     sc = torch.from_numpy(np.linspace(0.01, 0.02, N * 2).reshape(N, 2)).to(torch.bfloat16)
     for k in (0, 1, 17, 63, 64, 100, 127):
-        A = torch.zeros(2, K, dtype=torch.bfloat16)
-        A[0, k], A[1, k] = 1, float("inf")
-        got = product(nm, A, codes, sc, 2, N, K, 64, BF16_F32OUT)
-        assert np.array_equal(got[0], (codes[:, k] - 8) * sc.double().numpy()[:, k // 64])
-        with np.errstate(invalid="ignore"):
-            want = np.where(codes[:, k] == 8, np.nan, np.sign(codes[:, k] - 8.0) * np.inf)
-        assert np.array_equal(got[1], want, equal_nan=True)
+        for dtype in (BF16_F32OUT, F16):
+            for big in (1.0, 0.25, 448.0):
+                A = torch.zeros(3, K, dtype=TORCH[dtype])
+                A[0, k], A[1, k], A[2, 5] = big, float("inf"), float("nan")
+                got = product(nm, A, codes, sc.to(TORCH[dtype]), 3, N, K, 64, dtype)
+                want = torch.from_numpy((codes[:, k] - 8) * sc.to(TORCH[dtype]).double().numpy()[:, k // 64] * big)
+                assert np.array_equal(got[0], (want if dtype == BF16_F32OUT else want.half()).double().numpy())
+                assert np.isnan(got[1:]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("low,high", [(-30, 10), (-126, -100), (95, 118), (-3, 3)])
+def test_wide_ranges_of_tokens(low, high):
+    """bf16 tokens of very different sizes in one row, and rows at the ends of the type's range."""
+    import paper_2609_16009_b200 as nm
+    M, N, K = 3, 64, 640
+    A, codes, sc, _, _ = case(M, N, K, 64, BF16_F32OUT, 77)
+    e = torch.randint(low, high + 1, (M, K), generator=torch.Generator().manual_seed(3)).double()
+    A = (A.double().clamp(-1, 1) * 2.0 ** e).to(torch.bfloat16)
+    w = (codes - 8) * np.repeat(sc.double().numpy(), 64, axis=1)
+    a = A.double().numpy()
+    got = product(nm, A, codes, sc, M, N, K, 64, BF16_F32OUT)
+    # as assert_close, with sums of terms up to 15 |a| (see the kernel), and the tokens' absolute step: 2^-40 of the row's largest
+    s = np.repeat(sc.double().numpy(), 64, axis=1)
+    size = np.abs(a) @ (23 * s).T
+    tol = 160 * 2.0 ** -23 * size + 2.0 ** -40 * np.abs(a).max(1, keepdims=True) * (15 * s).sum(1) + 2.0 ** -149
+    assert np.all(np.abs(got - a @ w.T) <= tol)
 
 
 @pytest.mark.gpu
