@@ -260,6 +260,30 @@ int nm_mla_attention_combine(const void *Q, const void *kv_cache, void *o_bf16, 
                              int n_rows, long extra_row, int kv_lora, int rope, float scale,
                              void *workspace, size_t workspace_bytes, nm_stream stream);
 
+/* ---- quantised latent cache ------------------------------------------------------------------------------------
+ *
+ * A cache row in 8 bits: kv_lora e4m3 codes | rope bf16 | one fp32 scale s | 12 bytes of zeros, nm_mla_q8_row_bytes in all (656 for
+ * 512 + 64, against 1152 in bf16); row = s * (codes | bf16 part).  s is a power of two, 2^e with the least e in [-32, 32] that
+ * keeps the latent part within 448 * 2^e (1 for a latent part of zeros), so the bf16 part loses nothing by it (short of its
+ * type's range).  Dimensions: kv_lora a multiple of 16 up to 1024, rope a multiple of 8 up to 256 (0: no key part).
+ *
+ * nm_mla_cache_write_q8: T rows x = ckr + t * ckr_stride (elements, a multiple of 8), bf16 (latent | key) as W_DKVKR leaves them:
+ *   latent  RMSNorm(x[:kv_lora]; gamma, eps), gamma [kv_lora] bf16; NULL: taken as it is
+ *   key     RoPE(x[kv_lora:]) by cos_sin [T][rope] fp32 (rows of nm_rope_table); NULL: taken as it is
+ *   then quantised - each value rounded once, from fp32 - and stored as record rows[t] (device, 64-bit) of the cache.  A rows[t] outside
+ *   [0, n_cache_rows) writes nothing (padding tokens); rows NULL means row t.  The rows named in one call must differ from
+ *   each other: what a row named twice holds afterwards is unspecified.  A NaN stays a NaN, an infinite or too large
+ *   latent value becomes +-448 s.
+ * nm_mla_cache_read_q8: records rows[i] (NULL: i) as bf16 rows out + i * out_stride (elements, a multiple of 8): (latent | key), exact but
+ *   for the range of bf16; zeros where rows[i] is outside [0, n_cache_rows).  The same row may be read any number of times.
+ * ckr, gamma, cache and out are 16-byte aligned, cos_sin and rows 8-byte.  Both honour nm_set_programmatic_launch.
+ */
+size_t nm_mla_q8_row_bytes(int kv_lora, int rope);
+int nm_mla_cache_write_q8(const void *ckr, long ckr_stride, const void *gamma, const float *cos_sin, const int64_t *rows, void *cache,
+                          long n_cache_rows, int T, int kv_lora, int rope, float eps, nm_stream stream);
+int nm_mla_cache_read_q8(const void *cache, long n_cache_rows, const int64_t *rows, void *out, long out_stride, int n, int kv_lora,
+                         int rope, nm_stream stream);
+
 /*
  * One decode step for one token (DeepSeek-V3-style MLA, absorbed form).  Stages, each rounded to
  * bf16 as the paper rounds MatMul 2's output before RoPE / RMSNorm (Algorithm 2, output cast):

@@ -102,6 +102,10 @@ _lib.nm_mla_attention_workspace_bytes.argtypes = [_i, _i, _i]
 _lib.nm_mla_attention.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _l, _i, _i, C.c_float, _vp, _sz, _vp]
 _lib.nm_mla_attention_partial.argtypes = [_vp, _vp, _i, _i, _i, _i, C.c_float, _vp, _sz, _vp]
 _lib.nm_mla_attention_combine.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _l, _i, _i, C.c_float, _vp, _sz, _vp]
+_lib.nm_mla_q8_row_bytes.restype = _sz
+_lib.nm_mla_q8_row_bytes.argtypes = [_i, _i]
+_lib.nm_mla_cache_write_q8.argtypes = [_vp, _l, _vp, _vp, _vp, _vp, _l, _i, _i, _i, C.c_float, _vp]
+_lib.nm_mla_cache_read_q8.argtypes = [_vp, _l, _vp, _vp, _l, _i, _i, _i, _vp]
 _lib.nm_mla_workspace_bytes.restype = _sz
 _lib.nm_mla_workspace_bytes.argtypes = [C.POINTER(MlaParams)]
 _lib.nm_mla_decode_step.argtypes = [C.POINTER(MlaParams), _vp, _vp]
@@ -306,6 +310,21 @@ def nm_mla_attention_combine(Q, kv_cache, o_bf16, o_f32, H, n_rows, extra_row, k
     _check(_lib.nm_mla_attention_combine(_ptr(Q), _ptr(kv_cache), _ptr(o_bf16), _ptr(o_f32), H, n_rows, extra_row, kv_lora,
                                          rope, scale, _ptr(workspace), workspace.numel() * workspace.element_size(),
                                          _stream(stream)), "nm_mla_attention_combine")
+
+
+def nm_mla_q8_row_bytes(kv_lora, rope) -> int:
+    return int(_lib.nm_mla_q8_row_bytes(kv_lora, rope))
+
+
+def nm_mla_cache_write_q8(ckr, gamma, cos_sin, rows, cache, n_cache_rows, T, kv_lora, rope, eps=1e-6, ckr_stride=None, stream=None) -> None:
+    """gamma, cos_sin and rows (int64) may be None; ckr_stride defaults to dense rows."""
+    _check(_lib.nm_mla_cache_write_q8(_ptr(ckr), kv_lora + rope if ckr_stride is None else ckr_stride, _ptr(gamma), _ptr(cos_sin), _ptr(rows),
+                                      _ptr(cache), n_cache_rows, T, kv_lora, rope, eps, _stream(stream)), "nm_mla_cache_write_q8")
+
+
+def nm_mla_cache_read_q8(cache, n_cache_rows, rows, out, n, kv_lora, rope, out_stride=None, stream=None) -> None:
+    _check(_lib.nm_mla_cache_read_q8(_ptr(cache), n_cache_rows, _ptr(rows), _ptr(out), kv_lora + rope if out_stride is None else out_stride, n,
+                                     kv_lora, rope, _stream(stream)), "nm_mla_cache_read_q8")
 
 
 def mla_params(dims: dict, seq_len: int, tensors: dict, rms_eps=1e-6, softmax_scale=None, layout_dense=ROW_MAJOR,
