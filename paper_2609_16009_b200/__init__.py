@@ -142,8 +142,8 @@ def _ptr(t) -> int | None:
 
 
 def _stream(stream) -> int:
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream
+    if stream is None:                             # the raw handle of torch's current stream, without building a Stream object
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
