@@ -285,6 +285,32 @@ int nm_mla_cache_read_q8(const void *cache, long n_cache_rows, const int64_t *ro
                          int rope, nm_stream stream);
 
 /*
+ * Latent attention of a batch over the quantised cache: T sequences, one query token each, that share a prefix and have rows of
+ * their own,
+ *   s[t,h,j] = scale * <Q[t,h,:], row_j>,  p = softmax_j(s),  o[t,h,:] = sum_j p[t,h,j] * row_j[:kv_lora]
+ * with j over the prefix_rows records of `prefix` (read once for all heads that share the matrix unit, not once per sequence), then
+ * the seq_lens[t] records at cache + t * cache_stride.  nm_mla_attention over 8-bit records, for a batch and any number of heads.
+ *   T            1..NM_MAX_Q8_BATCH;  H  1..128 heads;  kv_lora 512, rope 64
+ *   Q            [T][H][kv_lora+rope] bf16, token t at Q + t * q_stride (elements, a multiple of 8, >= H * (kv_lora+rope))
+ *   prefix       prefix_rows records (may be 0; prefix may be NULL then)
+ *   seq_lens     HOST array [T]: own records of each sequence (>= 0); cache may be NULL where all are 0
+ *   cache_stride BYTES between the caches of consecutive sequences (a multiple of 16; >= the longest, for T > 1)
+ *   o_bf16, o_f32, lse  [T][H][kv_lora], [T][H][kv_lora], [T][H] (natural log of sum_j exp(s)); any may be NULL.  A sequence
+ *                without any row gets zeros and minus infinity.
+ * Nothing behind the rows named here is read into a result, whatever it holds.  A head whose query holds an infinity or a NaN, and a
+ * sequence (or all, in the prefix) with a NaN record, gets NaN.  Weights p keep at least eight bits, whatever their size down to 2^-24
+ * of the largest; sums are fp32.  Equal calls give equal bits.
+ * Q, prefix, cache, o_f32 and the workspace are 16-byte aligned, o_bf16 8-byte.  Workspace:
+ * nm_mla_attention_q8_workspace_bytes, whatever the lengths; nothing in it has to be cleared, and it keeps nothing from one call for the
+ * next; calls that overlap on the GPU (two captured graphs among them) need workspaces of their own.
+ */
+#define NM_MAX_Q8_BATCH 64
+size_t nm_mla_attention_q8_workspace_bytes(int T, int H);
+int nm_mla_attention_q8(const void *Q, long q_stride, const void *prefix, long prefix_rows, const void *cache, long cache_stride,
+                        const int *seq_lens, void *o_bf16, float *o_f32, float *lse, int T, int H, int kv_lora, int rope, float scale,
+                        void *workspace, size_t workspace_bytes, nm_stream stream);
+
+/*
  * One decode step for one token (DeepSeek-V3-style MLA, absorbed form).  Stages, each rounded to
  * bf16 as the paper rounds MatMul 2's output before RoPE / RMSNorm (Algorithm 2, output cast):
  *   c_q = h*W_DQ; c_qn = RMSNorm(c_q; gamma_q); q = c_qn*W_UQR ([H][nope+rope]);

@@ -106,6 +106,9 @@ _lib.nm_mla_q8_row_bytes.restype = _sz
 _lib.nm_mla_q8_row_bytes.argtypes = [_i, _i]
 _lib.nm_mla_cache_write_q8.argtypes = [_vp, _l, _vp, _vp, _vp, _vp, _l, _i, _i, _i, C.c_float, _vp]
 _lib.nm_mla_cache_read_q8.argtypes = [_vp, _l, _vp, _vp, _l, _i, _i, _i, _vp]
+_lib.nm_mla_attention_q8_workspace_bytes.restype = _sz
+_lib.nm_mla_attention_q8_workspace_bytes.argtypes = [_i, _i]
+_lib.nm_mla_attention_q8.argtypes = [_vp, _l, _vp, _l, _vp, _l, _vp, _vp, _vp, _vp, _i, _i, _i, _i, C.c_float, _vp, _sz, _vp]
 _lib.nm_mla_workspace_bytes.restype = _sz
 _lib.nm_mla_workspace_bytes.argtypes = [C.POINTER(MlaParams)]
 _lib.nm_mla_decode_step.argtypes = [C.POINTER(MlaParams), _vp, _vp]
@@ -325,6 +328,19 @@ def nm_mla_cache_write_q8(ckr, gamma, cos_sin, rows, cache, n_cache_rows, T, kv_
 def nm_mla_cache_read_q8(cache, n_cache_rows, rows, out, n, kv_lora, rope, out_stride=None, stream=None) -> None:
     _check(_lib.nm_mla_cache_read_q8(_ptr(cache), n_cache_rows, _ptr(rows), _ptr(out), kv_lora + rope if out_stride is None else out_stride, n,
                                      kv_lora, rope, _stream(stream)), "nm_mla_cache_read_q8")
+
+
+def nm_mla_attention_q8_workspace_bytes(T, H) -> int:
+    return int(_lib.nm_mla_attention_q8_workspace_bytes(T, H))
+
+
+def nm_mla_attention_q8(Q, prefix, prefix_rows, cache, cache_stride, seq_lens, o_bf16, o_f32, lse, H, kv_lora, rope, scale, workspace, q_stride=None,
+                        stream=None) -> None:
+    """seq_lens: a host sequence of ints (own rows of each sequence); cache_stride in bytes; q_stride defaults to dense tokens."""
+    T = len(seq_lens)
+    _check(_lib.nm_mla_attention_q8(_ptr(Q), H * (kv_lora + rope) if q_stride is None else q_stride, _ptr(prefix), prefix_rows, _ptr(cache), cache_stride,
+                                    (_i * T)(*seq_lens), _ptr(o_bf16), _ptr(o_f32), _ptr(lse), T, H, kv_lora, rope, scale, _ptr(workspace),
+                                    workspace.numel() * workspace.element_size(), _stream(stream)), "nm_mla_attention_q8")
 
 
 def mla_params(dims: dict, seq_len: int, tensors: dict, rms_eps=1e-6, softmax_scale=None, layout_dense=ROW_MAJOR,

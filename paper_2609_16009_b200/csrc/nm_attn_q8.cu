@@ -1,0 +1,642 @@
+// Latent attention of a batch over the quantised cache (records: nm_mla_q8.cuh), with a prefix that all sequences share.
+//
+//   o[t,h] = sum_j p_j row_j[:512],  p = softmax_j(scale <Q[t,h], row_j>),  row_j = s_j (k_j | r_j),  j over the prefix rows, then t's own
+//
+// Three launches: the queries are split and laid out (one warp per head), the pass over the rows (tcgen05), the merge of its parts.
+//
+// The pass.  A work item is up to 128 rows of the query matrix [T * H] x a run of cache rows: over the prefix the heads of several
+// sequences fill the 128 rows of the matrix unit, so its records are read once per 128 heads, not once per sequence; a sequence's own
+// rows meet its H heads.  Two CTAs per item, one per half of the 512 output columns (O[128 x 256] fp32 is half of TMEM, see
+// nm_attn_wide.cu; the scores are computed by both).  The stored bytes ARE the matrix operands - nothing is unpacked:
+//   scores   q' = q 2^-a (a per head) is two e4m3 terms, hi = round(q'), lo = round(q' - hi): a bf16's eight bits exactly down to 2^-10
+//            of the head's largest, and 2^-19 of that absolutely below.  S = hi k^T + lo k^T (kind::f8f6f4, K = 32) + the key part in bf16
+//            (kind::f16), 36 MMAs M128 N96.  Each k block serves as K-major operand here and as MN-major operand of P * V.
+//   P * V    the weight of row j is p_j s_j: with t_j = score_j + log2 s_j, w_j = 2^(t_j - m + 14), m the running maximum of t (moved, and O
+//            rescaled, only when it grows by more than 1).  w goes to fp16 - eleven bits, 2^-24 to 2^15, so a row 2^-30 below the largest
+//            still counts, which in e4m3 it would not: many small weights beside one large one are what long caches have - and
+//            from there into three e5m2 terms (fp16's upper byte is e5m2): truncate, subtract exactly, again, round the last; nine bits and
+//            more.  18 MMAs M128 N128 K32 a tile, P from TMEM, fp32 accumulation.  The sum of p_j = w_j / s_j stays fp32.
+// What is resident: the lo terms, half of the hi terms and the key part of Q in 112 KB of shared memory, the other half of hi in 64 columns of
+// TMEM; nine 12 KB slots of [96 rows x 128 bytes] for the records.  96 rows a tile: two score buffers of 96 columns fit TMEM beside O
+// and Q, so the scores of the next tile run while this one's exponentials do, and an MMA of N = 96 is still at its full rate
+// (max(50, N / 2) clocks).  Bound by the tensor pipe: 36 * 50 + 18 * 64 = 2950 clocks a tile and CTA.
+#include <algorithm>
+
+#include <cuda_fp8.h>
+
+#include "nm_async.cuh"
+#include "nm_mla_q8.cuh"
+#include "nm_tcgen05.cuh"
+
+namespace nm {
+
+namespace {
+
+constexpr int kKv = 512, kRope = 64, kRec = 656;
+constexpr int kM = 128;                            // query rows of an item
+constexpr int kR = 96;                             // cache rows of a tile
+constexpr int kQRow = 2 * kKv + 2 * kRope;         // bytes of a prepared query: hi | lo | key part
+constexpr int kQBlock = kM * 128, kSlotBytes = kR * 128, kSlots = 9;
+constexpr int kQBytes = 7 * kQBlock;               // lo 0-3, hi of this half's two blocks, key part
+constexpr int kTableBytes = 2 * kR * 16;
+constexpr int kSmemBytes = 1024 + kQBytes + kSlots * kSlotBytes + kTableBytes + 256;
+static_assert(kSmemBytes <= 232448, "shared memory");
+constexpr int kThreads = 192;                      // TMA, MMA, four softmax warps
+constexpr uint32_t kColO = 0, kColS = 256, kColQ = 448;
+constexpr float kHeadroom = 14.f, kLazy = 1.f;     // log2: weights are at most 2^(14 + 1)
+constexpr int kMaxT = NM_MAX_Q8_BATCH, kPairs = kSMs / 2, kMaxItems = 4 * kPairs;
+
+struct Item {
+    int q_row, n_q;                                // query rows
+    int source;                                    // 0: the prefix, 1 + t: sequence t
+    int row0, row1;                                // cache rows
+    int out_row;                                   // where its partial results start
+};
+struct PassArgs {
+    CUtensorMap q;                                 // [rows][1152] bytes, boxes of 128 x 128
+    CUtensorMap k[1 + kMaxT];                      // records as bytes, boxes of 128 x 96
+    const unsigned char *records[1 + kMaxT];
+    const unsigned char *q_rows;
+    const float *q_mult;
+    float *ml, *O;
+    unsigned *status;
+    int total_q;
+    Item items[kMaxItems];
+};
+struct MergeArgs {
+    const float *ml, *O;
+    uint16_t *o_bf16;
+    float *o_f32, *lse;
+    int H, n_prefix, tile_rows;                    // parts of the prefix, query rows of a prefix item
+    int own_row[kMaxT], own_n[kMaxT];              // first partial row and parts of each sequence
+};
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// ---- queries ---------------------------------------------------------------------------------------------------------
+__global__ void __launch_bounds__(128) q8_prepare_kernel(const uint16_t *__restrict__ Q, long q_stride, int T, int H, unsigned char *__restrict__ q_rows,
+                                                         float *__restrict__ q_mult, float scale_log2)
+{
+    pdl_launch_dependents();
+    const int row = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (row >= T * H) return;
+    const int t = row / H, h = row - t * H;
+    const uint16_t *q = Q + t * q_stride + (long)h * (kKv + kRope);
+    const uint4 a = *reinterpret_cast<const uint4 *>(q + 16 * lane), b = *reinterpret_cast<const uint4 *>(q + 16 * lane + 8);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    const uint32_t key = *reinterpret_cast<const uint32_t *>(q + kKv + 2 * lane);
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) top = __vmaxu2(top, w[j] & 0x7fff7fffu);
+    uint32_t top_key = key & 0x7fff7fffu;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, o));
+        top_key = __vmaxu2(top_key, __shfl_xor_sync(0xffffffffu, top_key, o));
+    }
+    const uint32_t most = max(top >> 16, top & 0xffffu), most_key = max(top_key >> 16, top_key & 0xffffu);       // the largest magnitudes' bits
+    const bool odd = max(most, most_key) >= 0x7f80u;
+    // least exponent with |q| <= 448 * 2^e, 448 = 1.75 * 2^8 (bf16: mantissa 0x60), kept where 2^-e is a normal number and the key part
+    // times 2^-e stays in range
+    int e = 0;
+    if (most) e = max((int)(most >> 7) - 127 - 8 + ((most & 0x7fu) > 0x60u), -112);
+    e = max(e, (int)(most_key >> 7) - 127 - 100);
+    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
+    unsigned char *out = q_rows + (long)row * kQRow;
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float x[4] = {__uint_as_float(w[2 * j] << 16) * inv, __uint_as_float(w[2 * j] & 0xffff0000u) * inv, __uint_as_float(w[2 * j + 1] << 16) * inv,
+                      __uint_as_float(w[2 * j + 1] & 0xffff0000u) * inv};
+        hi[j] = lo[j] = 0;
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            const uint32_t c = __nv_cvt_float2_to_fp8x2(make_float2(x[2 * p], x[2 * p + 1]), __NV_SATFINITE, __NV_E4M3);
+            const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)c, __NV_E4M3);
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&r));
+            hi[j] |= c << (16 * p);
+            lo[j] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(x[2 * p] - f.x, x[2 * p + 1] - f.y), __NV_SATFINITE, __NV_E4M3) << (16 * p);
+        }
+    }
+    *reinterpret_cast<uint4 *>(out + 16 * lane) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint4 *>(out + kKv + 16 * lane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    const float k0 = __uint_as_float(key << 16) * inv, k1 = __uint_as_float(key & 0xffff0000u) * inv;
+    *reinterpret_cast<uint32_t *>(out + 2 * kKv + 4 * lane) =
+        (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(k0)) | ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(k1)) << 16);
+    // an infinity or a NaN in a head makes its scores NaN (and nobody else's)
+    if (lane == 0) q_mult[row] = odd ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(127 + e) << 23) * scale_log2;
+}
+
+// ---- the pass ----------------------------------------------------------------------------------------------------------
+// Instruction descriptor, kind::f8f6f4: a_format e4m3 (0) or e5m2 (1), B e4m3, fp32 accumulation.
+__host__ __device__ constexpr uint32_t instr_desc_f8(int m, int n, int a_format, bool b_mn_major)
+{
+    return (1u << 4) | ((uint32_t)a_format << 7) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+__device__ __forceinline__ void mma_f8_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(0u) : "memory");
+}
+__device__ __forceinline__ void mma_f8_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(0u) : "memory");
+}
+
+__global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_constant__ PassArgs a)
+{
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t raw_addr = smem_u32(smem_raw), base = (raw_addr + 1023u) & ~1023u;      // swizzle atoms want 1024-byte alignment
+    unsigned char *smem = smem_raw + (base - raw_addr);
+    const uint32_t q_addr = base, ring = base + kQBytes;
+    float4 *s_table = reinterpret_cast<float4 *>(smem + kQBytes + kSlots * kSlotBytes);    // [2][96]: s, log2 s, 1 / s of a tile's rows
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + kQBytes + kSlots * kSlotBytes + kTableBytes);
+    const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * kSlots, bar_q = bar_empty + 8 * kSlots, bar_qt = bar_q + 8,
+                   bar_s = bar_qt + 8, bar_p = bar_s + 16, bar_pv = bar_p + 16;
+    __shared__ uint32_t s_tmem;
+    __shared__ int s_abort;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, half = blockIdx.x & 1;
+    const Item &it = a.items[blockIdx.x >> 1];
+    const int row0 = it.row0, row1 = it.row1, ntiles = ceil_div(row1 - row0, kR), source = it.source;
+    const CUtensorMap *map_k = &a.k[source];
+    if (tid == 0) {
+        s_abort = 0;
+        for (int i = 0; i < kSlots; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
+        mbar_init(bar_q, 1);
+        mbar_init(bar_qt, 128);
+        for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_p + 8 * i, 128); }
+        mbar_init(bar_pv, 1);
+        mbar_init_fence();
+    }
+    if (warp == 1) tmem_alloc(&s_tmem, 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    pdl_launch_dependents();
+
+    // A tile's five blocks in ring order: the other half's two latent blocks, the key part, this half's two latent blocks (the last
+    // ones to be given back: they are also V).  x: byte offset in the record.
+    const int other = 2 * (half ^ 1), mine = 2 * half;
+    auto block_x = [&](int j) { return j < 2 ? 128 * (other + j) : (j == 2 ? kKv : 128 * (mine + j - 3)); };
+
+    if (warp == 0) {
+        if (lane == 0) {
+            tma_prefetch_descriptor(&a.q);
+            tma_prefetch_descriptor(map_k);
+            const uint64_t keep = l2_policy_evict_last();
+            auto load = [&](int item) {
+                const int slot = item % kSlots, t = item / 5;
+                mbar_arrive_expect_tx(bar_full + 8 * slot, kSlotBytes);
+                tma_load_2d(ring + slot * kSlotBytes, map_k, block_x(item - 5 * t), row0 + t * kR, bar_full + 8 * slot, keep);
+            };
+            const int total = 5 * ntiles, early = min(kSlots, total);
+            for (int i = 0; i < early; ++i) load(i);               // the records were written before the queries' kernel began
+            pdl_wait_prior_grids();
+            mbar_arrive_expect_tx(bar_q, kQBytes);
+            for (int i = 0; i < 7; ++i)                            // lo 0-3, hi of this half, key part
+                tma_load_2d(q_addr + i * kQBlock, &a.q, i < 4 ? kKv + 128 * i : (i < 6 ? 128 * (mine + i - 4) : 2 * kKv), it.q_row, bar_q, keep);
+            for (int i = early; i < total; ++i) {
+                const uint32_t bar = bar_empty + 8 * (i % kSlots), par = ((i / kSlots) - 1) & 1;
+                if (!mbar_try_wait(bar, par) && !mbar_wait(bar, par, &s_abort, a.status)) break;
+                load(i);
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            constexpr uint32_t idesc_s = instr_desc_f8(kM, kR, 0, false), idesc_key = instr_desc(kM, kR, false, false), idesc_o = instr_desc_f8(kM, 128, 1, true);
+            bool ok = mbar_wait(bar_q, 0, &s_abort, a.status) && mbar_wait(bar_qt, 0, &s_abort, a.status);
+            auto scores = [&](int t) {
+                const uint32_t d = tmem + kColS + kR * (t & 1);
+                for (int j = 0; j < 5 && ok; ++j) {
+                    const int item = 5 * t + j, slot = item % kSlots;
+                    ok = mbar_try_wait(bar_full + 8 * slot, (item / kSlots) & 1) || mbar_wait(bar_full + 8 * slot, (item / kSlots) & 1, &s_abort, a.status);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint64_t k = smem_desc(ring + slot * kSlotBytes, 16, 1024);
+                    if (j == 2) {
+                        const uint64_t q = smem_desc(q_addr + 6 * kQBlock, 16, 1024);
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk) mma_ss(d, q + 2 * kk, k + 2 * kk, idesc_key, true);
+                    } else {
+                        const int blk = j < 2 ? other + j : mine + j - 3;
+                        const uint64_t lo = smem_desc(q_addr + blk * kQBlock, 16, 1024), hi = smem_desc(q_addr + (j < 2 ? 0 : 4 + j - 3) * kQBlock, 16, 1024);
+#pragma unroll
+                        for (int kk = 0; kk < 4; ++kk) {           // 32 latent dimensions: 32 bytes in shared memory, 8 columns of TMEM
+                            if (j < 2) mma_f8_ts(d, tmem + kColQ + 32 * j + 8 * kk, k + 2 * kk, idesc_s, (j | kk) != 0);
+                            else mma_f8_ss(d, hi + 2 * kk, k + 2 * kk, idesc_s, true);
+                            mma_f8_ss(d, lo + 2 * kk, k + 2 * kk, idesc_s, true);
+                        }
+                    }
+                    if (j < 3) mma_commit(bar_empty + 8 * slot);
+                }
+                if (ok) mma_commit(bar_s + 8 * (t & 1));
+            };
+            tc_fence_after();
+            if (ok) scores(0);
+            for (int t = 0; t < ntiles && ok; ++t) {
+                if (t + 1 < ntiles) scores(t + 1);
+                if (!ok) break;
+                ok = mbar_try_wait(bar_p + 8 * (t & 1), (t >> 1) & 1) || mbar_wait(bar_p + 8 * (t & 1), (t >> 1) & 1, &s_abort, a.status);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t p = tmem + kColS + kR * (t & 1);
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                    const int slot = (5 * t + 3 + v) % kSlots;
+#pragma unroll
+                    for (int kk = 0; kk < 3; ++kk) {               // 32 rows: four groups of eight, 1024 bytes apart
+                        const uint64_t b = smem_desc(ring + slot * kSlotBytes + kk * 4096, 1024, 1024);
+#pragma unroll
+                        for (int term = 0; term < 3; ++term) mma_f8_ts(tmem + kColO + 128 * v, p + 32 * kk + 8 * term, b, idesc_o, (t | kk | term) != 0);
+                    }
+                    mma_commit(bar_empty + 8 * slot);
+                }
+                mma_commit(bar_pv);
+            }
+        }
+    } else {
+        // ---- softmax: one thread per query row; warp w may touch the TMEM lanes of quarter w % 4 -----------------------------------
+        const int quad = warp & 3, r = quad * 32 + lane;
+        const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
+        const unsigned char *records = a.records[source];
+        auto row_entry = [&](int t, float s) {                     // (thread r < 96: row r of tile t)
+            const bool there = row0 + t * kR + r < row1;
+            s = s == 0.f ? 0x1p-60f : s;                           // (a record of zeros is a row of zeros, and has its weight)
+            return there ? make_float4(s, __log2f(s), 1.f / s, 0.f) : make_float4(0.f, -INFINITY, 0.f, 0.f);       // past the end: no weight
+        };
+        auto row_scale = [&](int t) {
+            const int row = row0 + t * kR + r;
+            return r < kR && row < row1 ? __ldg(reinterpret_cast<const float *>(records + (long)row * kRec + kKv + 2 * kRope)) : 0.f;
+        };
+        const float s0 = row_scale(0);
+        pdl_wait_prior_grids();
+        {
+            // the hi terms of the other half's columns to TMEM, 256 bytes a row; rows past the last query are zeros
+            const int q_row = it.q_row + r;
+            const uint4 *src = reinterpret_cast<const uint4 *>(a.q_rows + (long)min(q_row, a.total_q - 1) * kQRow + 128 * other);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t v[16];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint4 u = q_row < a.total_q ? src[4 * i + j] : make_uint4(0u, 0u, 0u, 0u);
+                    v[4 * j] = u.x; v[4 * j + 1] = u.y; v[4 * j + 2] = u.z; v[4 * j + 3] = u.w;
+                }
+                tmem_st16(lanes + kColQ + 16 * i, v);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(bar_qt);
+        }
+        const float mult = r < it.n_q ? a.q_mult[it.q_row + r] : 0.f;
+        if (r < kR) s_table[r] = row_entry(0, s0);
+        named_barrier_sync(1, 128);
+        float m = -INFINITY, l = 0.f;
+        for (int t = 0; t < ntiles; ++t) {
+            const float s_next = t + 1 < ntiles ? row_scale(t + 1) : 0.f;
+            const float4 *table = s_table + kR * (t & 1);
+            const uint32_t col = lanes + kColS + kR * (t & 1);
+            // (after an expired wait every later wait returns at once: the loop runs on, so that the threads keep meeting at the
+            // named barrier below, and ends with a result that the status word disowns)
+            mbar_wait(bar_s + 8 * (t & 1), (t >> 1) & 1, &s_abort, a.status);
+            tc_fence_after();
+            uint32_t raw[3][32];
+#pragma unroll
+            for (int c = 0; c < 3; ++c) tmem_ld32(col + 32 * c, raw[c]);
+            tmem_wait_ld();
+            float mx = -1e30f, mx1 = -1e30f;                       // (two chains; the start keeps a row without any finite score from becoming NaN)
+#pragma unroll
+            for (int c = 0; c < 3; ++c)
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) {
+                    const float4 e0 = table[32 * c + i], e1 = table[32 * c + i + 1];
+                    const float x0 = fmaf(__uint_as_float(raw[c][i]), mult * e0.x, e0.y), x1 = fmaf(__uint_as_float(raw[c][i + 1]), mult * e1.x, e1.y);
+                    raw[c][i] = __float_as_uint(x0); raw[c][i + 1] = __float_as_uint(x1);
+                    mx = fmaxf(mx, x0); mx1 = fmaxf(mx1, x1);
+                }
+            mx = fmaxf(mx, mx1);
+            const bool grow = t == 0 || mx > m + kLazy;
+            if (t > 0 && __any_sync(0xffffffffu, grow)) {
+                // the previous tile's P * V has to be through before O is touched
+                mbar_wait(bar_pv, (t - 1) & 1, &s_abort, a.status);
+                tc_fence_after();
+                const float f = grow ? ex2(m - mx) : 1.f;
+                for (int c = 0; c < 16; ++c) {
+                    uint32_t o[16];
+                    tmem_ld16(lanes + kColO + 16 * c, o);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                    tmem_st16(lanes + kColO + 16 * c, o);
+                }
+                l *= f;
+            }
+            if (grow) m = mx;
+            const float ref = m - kHeadroom;
+            float l1 = 0.f;
+#pragma unroll
+            for (int c = 0; c < 3; ++c) {
+                uint32_t hi[8], mid[8], lo[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    uint32_t h[2], h1[2], h2[2];
+#pragma unroll
+                    for (int p = 0; p < 2; ++p) {
+                        const int i = 4 * q + 2 * p;
+                        const float w0 = ex2(__uint_as_float(raw[c][i]) - ref), w1 = ex2(__uint_as_float(raw[c][i + 1]) - ref);
+                        l = fmaf(w0, table[32 * c + i].z, l); l1 = fmaf(w1, table[32 * c + i + 1].z, l1);
+                        const __half2 x = __floats2half2_rn(w0, w1);
+                        h[p] = *reinterpret_cast<const uint32_t *>(&x);
+                        const uint32_t top = h[p] & 0xff00ff00u;
+                        const __half2 x1 = __hsub2(x, *reinterpret_cast<const __half2 *>(&top));
+                        h1[p] = *reinterpret_cast<const uint32_t *>(&x1);
+                        const uint32_t top1 = h1[p] & 0xff00ff00u;
+                        const __half2 x2 = __hsub2(x1, *reinterpret_cast<const __half2 *>(&top1));
+                        h2[p] = *reinterpret_cast<const uint32_t *>(&x2) + 0x00800080u;
+                    }
+                    hi[q] = __byte_perm(h[0], h[1], 0x7531); mid[q] = __byte_perm(h1[0], h1[1], 0x7531); lo[q] = __byte_perm(h2[0], h2[1], 0x7531);
+                }
+                // over the columns of S that this thread alone has read
+                tmem_st8(col + 32 * c, hi);
+                tmem_st8(col + 32 * c + 8, mid);
+                tmem_st8(col + 32 * c + 16, lo);
+            }
+            l += l1;
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(bar_p + 8 * (t & 1));
+            if (t + 1 < ntiles) {
+                if (r < kR) s_table[kR * ((t + 1) & 1) + r] = row_entry(t + 1, s_next);
+                named_barrier_sync(1, 128);                        // the next tile's table is written, this one's has been read by all
+            }
+        }
+        mbar_wait(bar_pv, (ntiles - 1) & 1, &s_abort, a.status);
+        tc_fence_after();
+        // ---- out: the warp's 32 rows, 64 columns at a time through its own corner of the ring (every copy into it has been used), so
+        //      that the stores run along the rows ------------------------------------------------------------------------------------
+        if (half == 0 && r < it.n_q) {
+            float *ml = a.ml + 2 * (long)(it.out_row + r);
+            ml[0] = m; ml[1] = l;
+        }
+        float4 *corner = reinterpret_cast<float4 *>(smem + kQBytes + quad * 8192);        // [32 rows][16 float4], the index XOR-ed with row & 15
+        for (int c0 = 0; c0 < 256; c0 += 64) {
+            uint32_t o[2][32];
+            tmem_ld32(lanes + kColO + c0, o[0]);
+            tmem_ld32(lanes + kColO + c0 + 32, o[1]);
+            tmem_wait_ld();
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const uint32_t *v = &o[i >> 3][4 * (i & 7)];
+                corner[lane * 16 + (i ^ (lane & 15))] = make_float4(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3]));
+            }
+            __syncwarp();
+            for (int i = lane; i < 32 * 16; i += 32) {
+                const int rr = i >> 4, f = i & 15, q = quad * 32 + rr;
+                if (q < it.n_q)
+                    *reinterpret_cast<float4 *>(a.O + (long)(it.out_row + q) * kKv + 256 * half + c0 + 4 * f) = corner[rr * 16 + (f ^ (rr & 15))];
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (s_abort && tid == 0) {
+        // a wait expired: give copies already issued a bounded chance to land before the CTA exits
+        for (int i = 0; i < (1 << 16) && !mbar_try_wait(bar_full, 0); ++i) {}
+        for (int i = 0; i < (1 << 16) && !mbar_try_wait(bar_q, 0); ++i) {}
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// ---- the merge: one CTA per head of a sequence, four columns a thread ---------------------------------------------------------
+__global__ void __launch_bounds__(128) q8_merge_kernel(const __grid_constant__ MergeArgs a)
+{
+    __shared__ float s_w[2 * kMaxItems];
+    __shared__ int s_row[2 * kMaxItems];
+    __shared__ float s_red[2][4];
+    pdl_launch_dependents();
+    pdl_wait_prior_grids();
+    const int t = blockIdx.x / a.H, h = blockIdx.x - t * a.H, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int n = a.n_prefix + a.own_n[t];
+    float mx = -INFINITY;
+    for (int i = tid; i < n; i += 128) {
+        // prefix: item (tile of query rows, part); own: item (sequence, part)
+        const int row = i < a.n_prefix ? (blockIdx.x / kM * a.n_prefix + i) * a.tile_rows + blockIdx.x % kM : a.own_row[t] + (i - a.n_prefix) * a.H + h;
+        s_row[i] = row;
+        s_w[i] = a.ml[2 * (long)row];
+        mx = fmaxf(mx, s_w[i]);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    if (lane == 0) s_red[0][warp] = mx;
+    __syncthreads();
+    mx = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float total = 0.f;
+    for (int i = tid; i < n; i += 128) s_w[i] = ex2(s_w[i] - mx);
+    __syncthreads();
+    // (every thread adds the same sums in the same order)
+#pragma unroll 4
+    for (int i = 0; i < n; ++i) {
+        const float w = s_w[i];
+        const float4 v = *reinterpret_cast<const float4 *>(a.O + (long)s_row[i] * kKv + 4 * tid);
+        total = fmaf(w, a.ml[2 * (long)s_row[i] + 1], total);
+        acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y); acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
+    }
+    const float inv = n > 0 ? 1.f / total : 0.f;                   // no rows: zeros, and minus infinity below
+    const long at = (long)blockIdx.x * kKv + 4 * tid;
+    acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
+    if (a.o_f32) *reinterpret_cast<float4 *>(a.o_f32 + at) = acc;
+    if (a.o_bf16) {
+        const uint32_t lo = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(acc.x)) | ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(acc.y)) << 16);
+        const uint32_t hi = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(acc.z)) | ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(acc.w)) << 16);
+        *reinterpret_cast<uint2 *>(a.o_bf16 + at) = make_uint2(lo, hi);
+    }
+    if (a.lse && tid == 0) a.lse[blockIdx.x] = n > 0 ? (mx - kHeadroom + log2f(total)) * 0.6931471805599453f : -INFINITY;
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------------------
+struct Layout { size_t q_rows, mult, ml, O, total; };
+Layout layout_of(int T, int H, long part_rows)
+{
+    auto up = [](size_t x) { return (x + 1023) & ~(size_t)1023; };
+    Layout l;
+    l.q_rows = 0;
+    l.mult = up((size_t)T * H * kQRow);
+    l.ml = l.mult + up((size_t)T * H * sizeof(float));
+    l.O = l.ml + up((size_t)part_rows * 2 * sizeof(float));
+    l.total = l.O + (size_t)part_rows * kKv * sizeof(float);
+    return l;
+}
+
+// How the rows are split: tiles of every (query tile or sequence, source) are cut into parts of at most `most` tiles.  Few waves of
+// CTA pairs, each part as long as that allows: a part costs about three tiles beside its own (queries in, partial results out and
+// merged), so one wave is taken unless the units are too uneven for it.
+int parts_of(int tiles, int most) { return (tiles + most - 1) / most; }
+int choose_part(const int *tiles, const int *count, int n)         // `count[i]` units of `tiles[i]` tiles
+{
+    constexpr double kPart = 3.0;
+    long work = 0, units = 0, longest = 1;
+    for (int i = 0; i < n; ++i) { work += (long)tiles[i] * count[i]; units += count[i]; longest = std::max<long>(longest, tiles[i]); }
+    int best = (int)longest;
+    double least = 1e300;
+    for (int waves = 1; waves <= kMaxItems / kPairs; ++waves) {
+        if (units > (long)waves * kPairs) continue;
+        long lo = 1, hi = longest;                                 // least part length with at most waves * kPairs parts
+        while (lo < hi) {
+            const long mid = (lo + hi) / 2;
+            long parts = 0;
+            for (int i = 0; i < n; ++i) parts += (long)parts_of(tiles[i], (int)mid) * count[i];
+            if (parts <= (long)waves * kPairs) hi = mid; else lo = mid + 1;
+        }
+        long parts = 0;
+        for (int i = 0; i < n; ++i) parts += (long)parts_of(tiles[i], (int)lo) * count[i];
+        // one wave ends with its longest part; more of them even out, but for about half a part at the end
+        const double cost = waves == 1 ? lo + kPart : (work + kPart * parts) / kPairs + 0.5 * lo;
+        if (cost < least) { least = cost; best = (int)lo; }
+    }
+    return best;
+}
+
+bool encode_bytes_map(CUtensorMap *map, const void *ptr, long rows, long pitch, int box_rows)
+{
+    EncodeTiledFn enc = tensor_map_encoder();
+    if (!enc) return false;
+    const cuuint64_t dims[2] = {(cuuint64_t)pitch, (cuuint64_t)rows};
+    const cuuint64_t strides[1] = {(cuuint64_t)pitch};
+    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+    return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <typename Kern, typename... Args>
+cudaError_t launch_after(Kern kern, unsigned grid, unsigned threads, size_t smem, cudaStream_t stream, Args... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
+}  // namespace
+
+}  // namespace nm
+
+using namespace nm;
+
+extern "C" {
+#pragma GCC visibility push(default)
+
+size_t nm_mla_attention_q8_workspace_bytes(int T, int H)
+{
+    if (T < 1 || T > kMaxT || H < 1 || H > kM) return 0;
+    return layout_of(T, H, (long)kMaxItems * std::min(kM, T * H)).total;
+}
+
+int nm_mla_attention_q8(const void *Q, long q_stride, const void *prefix, long prefix_rows, const void *cache, long cache_stride, const int *seq_lens,
+                        void *o_bf16, float *o_f32, float *lse, int T, int H, int kv_lora, int rope, float scale, void *workspace,
+                        size_t workspace_bytes, nm_stream stream)
+{
+    if (!Q || !seq_lens || T < 1 || T > kMaxT || H < 1 || prefix_rows < 0 || prefix_rows > 0x7fffff00L || (prefix_rows > 0 && !prefix) ||
+        q_stride < (long)H * (kv_lora + rope))
+        return NM_ERR_INVALID_ARG;
+    if (kv_lora != kKv || rope != kRope || H > kM) return NM_ERR_UNSUPPORTED;
+    int longest = 0;
+    for (int t = 0; t < T; ++t) {
+        if (seq_lens[t] < 0 || seq_lens[t] > 0x7fffff00) return NM_ERR_INVALID_ARG;
+        longest = std::max(longest, seq_lens[t]);
+    }
+    if (longest > 0 && (!cache || (T > 1 && cache_stride < (long)longest * kRec))) return NM_ERR_INVALID_ARG;
+    if (((uintptr_t)Q & 15u) || q_stride % 8 || ((uintptr_t)prefix & 15u) || ((uintptr_t)cache & 15u) || cache_stride % 16 || ((uintptr_t)o_bf16 & 7u) ||
+        ((uintptr_t)o_f32 & 15u) || ((uintptr_t)lse & 3u))
+        return NM_ERR_ALIGNMENT;
+    if (!workspace || workspace_bytes < nm_mla_attention_q8_workspace_bytes(T, H)) return NM_ERR_WORKSPACE;
+    if ((uintptr_t)workspace & 15u) return NM_ERR_ALIGNMENT;
+
+    // units: the prefix once per tile of query rows, each sequence's own rows once
+    const int total_q = T * H, q_tiles = ceil_div(total_q, kM), prefix_tiles = (int)((prefix_rows + kR - 1) / kR);
+    int tiles[1 + kMaxT], count[1 + kMaxT], n = 0;
+    if (prefix_tiles) { tiles[n] = prefix_tiles; count[n++] = q_tiles; }
+    for (int t = 0; t < T; ++t)
+        if (seq_lens[t]) { tiles[n] = ceil_div(seq_lens[t], kR); count[n++] = 1; }
+    const int most = n ? choose_part(tiles, count, n) : 1;
+
+    cudaStream_t s = (cudaStream_t)stream;
+    const Layout lay = layout_of(T, H, (long)kMaxItems * std::min(kM, total_q));
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    PassArgs pa{};
+    MergeArgs ma{};
+    pa.q_rows = ws + lay.q_rows;
+    pa.q_mult = reinterpret_cast<float *>(ws + lay.mult);
+    pa.ml = reinterpret_cast<float *>(ws + lay.ml);
+    pa.O = reinterpret_cast<float *>(ws + lay.O);
+    pa.total_q = total_q;
+    ma.ml = pa.ml; ma.O = pa.O;
+    ma.o_bf16 = static_cast<uint16_t *>(o_bf16); ma.o_f32 = o_f32; ma.lse = lse;
+    ma.H = H;
+    ma.tile_rows = std::min(kM, total_q);
+    int items = 0, out_row = 0;
+    auto add_unit = [&](int source, int q_row, int n_q, int unit_tiles, int rows, int row_step) {
+        const int parts = parts_of(unit_tiles, most);
+        for (int p = 0; p < parts; ++p) {
+            Item &i = pa.items[items++];
+            i.q_row = q_row; i.n_q = n_q; i.source = source;
+            i.row0 = (int)((long)unit_tiles * p / parts) * kR;
+            i.row1 = std::min(rows, (int)((long)unit_tiles * (p + 1) / parts) * kR);
+            i.out_row = out_row;
+            out_row += row_step;
+        }
+        return parts;
+    };
+    if (prefix_tiles)
+        for (int q = 0; q < q_tiles; ++q) ma.n_prefix = add_unit(0, q * kM, std::min(kM, total_q - q * kM), prefix_tiles, (int)prefix_rows, ma.tile_rows);
+    for (int t = 0; t < T; ++t) {
+        ma.own_row[t] = out_row;
+        ma.own_n[t] = seq_lens[t] ? add_unit(1 + t, t * H, H, ceil_div(seq_lens[t], kR), seq_lens[t], H) : 0;
+    }
+    if (items) {
+        pa.status = device_status_ptr();
+        if (!encode_bytes_map(&pa.q, pa.q_rows, total_q, kQRow, kM)) return record_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+        // The maps cover exactly the rows attended: what lies behind them reads as zeros (and has no weight), whatever it holds.
+        for (int i = 0; i <= T; ++i) {
+            const long rows = i == 0 ? prefix_rows : seq_lens[i - 1];
+            const unsigned char *p = i == 0 ? static_cast<const unsigned char *>(prefix) : static_cast<const unsigned char *>(cache) + (long)(i - 1) * cache_stride;
+            pa.records[i] = p;
+            if (rows && !encode_bytes_map(&pa.k[i], p, rows, kRec, kR)) return record_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
+        }
+        // the longest parts first: the last wave then ends evenly
+        std::sort(pa.items, pa.items + items, [](const Item &x, const Item &y) { return x.row1 - x.row0 > y.row1 - y.row0; });
+        static std::atomic<unsigned long long> configured{0};
+        cudaError_t e = ensure_dynamic_smem(attn_q8_kernel, kSmemBytes, configured);
+        if (e != cudaSuccess) return record_cuda_error(e, "quantised attention kernel attribute");
+        q8_prepare_kernel<<<ceil_div(total_q, 4), 128, 0, s>>>(static_cast<const uint16_t *>(Q), q_stride, T, H, ws + lay.q_rows,
+                                                              reinterpret_cast<float *>(ws + lay.mult), scale * 1.4426950408889634f);
+        e = cudaGetLastError();
+        if (e == cudaSuccess) e = launch_after(attn_q8_kernel, 2 * items, kThreads, kSmemBytes, s, pa);
+        if (e != cudaSuccess) return record_cuda_error(e, "quantised attention launch");
+    }
+    const cudaError_t e = launch_after(q8_merge_kernel, (unsigned)total_q, 128, 0, s, ma);
+    return e == cudaSuccess ? NM_OK : record_cuda_error(e, "quantised attention merge launch");
+}
+
+#pragma GCC visibility pop
+}  // extern "C"
