@@ -264,7 +264,7 @@ int nm_mla_attention_combine(const void *Q, const void *kv_cache, void *o_bf16, 
  *
  * A cache row in 8 bits: kv_lora e4m3 codes | rope bf16 | one fp32 scale s | 12 bytes of zeros, nm_mla_q8_row_bytes in all (656 for
  * 512 + 64, against 1152 in bf16); row = s * (codes | bf16 part).  s is a power of two, 2^e with the least e in [-32, 32] that
- * keeps the latent part within 448 * 2^e (1 for a latent part of zeros), so the bf16 part loses nothing by it (short of its
+ * keeps the latent part within 448 * 2^e (1 for a latent part of zeros; readers take it for a power of two), so the bf16 part loses nothing by it (short of its
  * type's range).  Dimensions: kv_lora a multiple of 16 up to 1024, rope a multiple of 8 up to 256 (0: no key part).
  *
  * nm_mla_cache_write_q8: T rows x = ckr + t * ckr_stride (elements, a multiple of 8), bf16 (latent | key) as W_DKVKR leaves them:
@@ -298,7 +298,7 @@ int nm_mla_cache_read_q8(const void *cache, long n_cache_rows, const int64_t *ro
  *   o_bf16, o_f32, lse  [T][H][kv_lora], [T][H][kv_lora], [T][H] (natural log of sum_j exp(s)); any may be NULL.  A sequence
  *                without any row gets zeros and minus infinity.
  * Nothing behind the rows named here is read into a result, whatever it holds.  A head whose query holds an infinity or a NaN, and a
- * sequence (or all, in the prefix) with a NaN record, gets NaN.  Weights p keep at least eight bits, whatever their size down to 2^-24
+ * sequence (or all, in the prefix) with a NaN record, gets NaN.  Weights p keep at least eight bits, whatever their size down to 2^-20
  * of the largest; sums are fp32.  Equal calls give equal bits.
  * Q, prefix, cache, o_f32 and the workspace are 16-byte aligned, o_bf16 8-byte.  Workspace:
  * nm_mla_attention_q8_workspace_bytes, whatever the lengths; nothing in it has to be cleared, and it keeps nothing from one call for the

@@ -11,8 +11,8 @@
 //   scores   q' = q 2^-a (a per head) is two e4m3 terms, hi = round(q'), lo = round(q' - hi): a bf16's eight bits exactly down to 2^-10
 //            of the head's largest, and 2^-19 of that absolutely below.  S = hi k^T + lo k^T (kind::f8f6f4, K = 32) + the key part in bf16
 //            (kind::f16), 36 MMAs M128 N96.  Each k block serves as K-major operand here and as MN-major operand of P * V.
-//   P * V    the weight of row j is p_j s_j: with t_j = score_j + log2 s_j, w_j = 2^(t_j - m + 14), m the running maximum of t (moved, and O
-//            rescaled, only when it grows by more than 1).  w goes to fp16 - eleven bits, 2^-24 to 2^15, so a row 2^-30 below the largest
+//   P * V    the weight of row j is p_j s_j: with t_j = score_j + log2 s_j, w_j = 2^(t_j - m + 11), m the running maximum of t (moved, and O
+//            rescaled, only when it grows by more than 4).  w goes to fp16 - eleven bits, 2^-24 to 2^15, so a row 2^-27 below the largest
 //            still counts, which in e4m3 it would not: many small weights beside one large one are what long caches have - and
 //            from there into three e5m2 terms (fp16's upper byte is e5m2): truncate, subtract exactly, again, round the last; nine bits and
 //            more.  18 MMAs M128 N128 K32 a tile, P from TMEM, fp32 accumulation.  The sum of p_j = w_j / s_j stays fp32.
@@ -38,12 +38,12 @@ constexpr int kR = 96;                             // cache rows of a tile
 constexpr int kQRow = 2 * kKv + 2 * kRope;         // bytes of a prepared query: hi | lo | key part
 constexpr int kQBlock = kM * 128, kSlotBytes = kR * 128, kSlots = 9;
 constexpr int kQBytes = 7 * kQBlock;               // lo 0-3, hi of this half's two blocks, key part
-constexpr int kTableBytes = 2 * kR * 16;
+constexpr int kTableBytes = 2 * kR * 4;
 constexpr int kSmemBytes = 1024 + kQBytes + kSlots * kSlotBytes + kTableBytes + 256;
 static_assert(kSmemBytes <= 232448, "shared memory");
 constexpr int kThreads = 192;                      // TMA, MMA, four softmax warps
 constexpr uint32_t kColO = 0, kColS = 256, kColQ = 448;
-constexpr float kHeadroom = 14.f, kLazy = 1.f;     // log2: weights are at most 2^(14 + 1)
+constexpr float kHeadroom = 11.f, kLazy = 4.f;     // log2: weights are at most 2^(11 + 4)
 constexpr int kMaxT = NM_MAX_Q8_BATCH, kPairs = kSMs / 2, kMaxItems = 4 * kPairs;
 
 struct Item {
@@ -138,6 +138,12 @@ __host__ __device__ constexpr uint32_t instr_desc_f8(int m, int n, int a_format,
 {
     return (1u << 4) | ((uint32_t)a_format << 7) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
 __device__ __forceinline__ void mma_f8_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
 {
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
@@ -157,13 +163,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
     const uint32_t raw_addr = smem_u32(smem_raw), base = (raw_addr + 1023u) & ~1023u;      // swizzle atoms want 1024-byte alignment
     unsigned char *smem = smem_raw + (base - raw_addr);
     const uint32_t q_addr = base, ring = base + kQBytes;
-    float4 *s_table = reinterpret_cast<float4 *>(smem + kQBytes + kSlots * kSlotBytes);    // [2][96]: s, log2 s, 1 / s of a tile's rows
+    // [2][96]: s and log2 s of a tile's rows as two bf16 (s is a power of two: both exact) - four rows per 16-byte read, since the
+    // matrix unit wants shared memory's bandwidth for itself
+    uint32_t *s_table = reinterpret_cast<uint32_t *>(smem + kQBytes + kSlots * kSlotBytes);
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + kQBytes + kSlots * kSlotBytes + kTableBytes);
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * kSlots, bar_q = bar_empty + 8 * kSlots, bar_qt = bar_q + 8,
                    bar_s = bar_qt + 8, bar_p = bar_s + 16, bar_pv = bar_p + 16;
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, half = blockIdx.x & 1;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, half = blockIdx.x & 1;
     const Item &it = a.items[blockIdx.x >> 1];
     const int row0 = it.row0, row1 = it.row1, ntiles = ceil_div(row1 - row0, kR), source = it.source;
     const CUtensorMap *map_k = &a.k[source];
@@ -211,57 +219,77 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            constexpr uint32_t idesc_s = instr_desc_f8(kM, kR, 0, false), idesc_key = instr_desc(kM, kR, false, false), idesc_o = instr_desc_f8(kM, 128, 1, true);
-            bool ok = mbar_wait(bar_q, 0, &s_abort, a.status) && mbar_wait(bar_qt, 0, &s_abort, a.status);
-            auto scores = [&](int t) {
-                const uint32_t d = tmem + kColS + kR * (t & 1);
-                for (int j = 0; j < 5 && ok; ++j) {
-                    const int item = 5 * t + j, slot = item % kSlots;
-                    ok = mbar_try_wait(bar_full + 8 * slot, (item / kSlots) & 1) || mbar_wait(bar_full + 8 * slot, (item / kSlots) & 1, &s_abort, a.status);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint64_t k = smem_desc(ring + slot * kSlotBytes, 16, 1024);
+        // The whole warp walks, one elected lane issues: descriptors and addresses are then uniform values, which an MMA takes as they are.
+        // (Computed by one lane in a branch of its own each MMA costs 100 to 170 clocks of issue; so, N = 96 from shared memory 57,
+        // from TMEM 49, N = 128 from TMEM 65 - shared memory's and the pipe's own times.)
+        constexpr uint32_t idesc_s = instr_desc_f8(kM, kR, 0, false), idesc_key = instr_desc(kM, kR, false, false), idesc_o = instr_desc_f8(kM, 128, 1, true);
+        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), sm = __shfl_sync(0xffffffffu, base, 0);
+        const bool leader = elect_one();
+        auto wait = [&](uint32_t bar, uint32_t par) {
+            const bool there = mbar_try_wait(bar, par) || mbar_wait(bar, par, &s_abort, a.status);
+            return __all_sync(0xffffffffu, there) != 0;
+        };
+        bool ok = wait(bar_q, 0) && wait(bar_qt, 0);
+        int full_slot = 0, full_par = 0;                           // the ring's next block
+        auto scores = [&](int t) {
+            const uint32_t d = tm + kColS + kR * (t & 1);
+#pragma unroll
+            for (int j = 0; j < 5; ++j) {
+                if (!ok) break;
+                ok = wait(bar_full + 8 * full_slot, full_par);
+                if (!ok) break;
+                tc_fence_after();
+                const uint64_t k = smem_desc(sm + kQBytes + full_slot * kSlotBytes, 16, 1024);
+                if (leader) {
                     if (j == 2) {
-                        const uint64_t q = smem_desc(q_addr + 6 * kQBlock, 16, 1024);
+                        const uint64_t q = smem_desc(sm + 6 * kQBlock, 16, 1024);
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk) mma_ss(d, q + 2 * kk, k + 2 * kk, idesc_key, true);
                     } else {
-                        const int blk = j < 2 ? other + j : mine + j - 3;
-                        const uint64_t lo = smem_desc(q_addr + blk * kQBlock, 16, 1024), hi = smem_desc(q_addr + (j < 2 ? 0 : 4 + j - 3) * kQBlock, 16, 1024);
+                        const uint64_t lo = smem_desc(sm + (j < 2 ? other + j : mine + j - 3) * kQBlock, 16, 1024);
+                        const uint64_t hi = smem_desc(sm + (j < 2 ? 0 : 4 + j - 3) * kQBlock, 16, 1024);
 #pragma unroll
                         for (int kk = 0; kk < 4; ++kk) {           // 32 latent dimensions: 32 bytes in shared memory, 8 columns of TMEM
-                            if (j < 2) mma_f8_ts(d, tmem + kColQ + 32 * j + 8 * kk, k + 2 * kk, idesc_s, (j | kk) != 0);
+                            if (j < 2) mma_f8_ts(d, tm + kColQ + 32 * j + 8 * kk, k + 2 * kk, idesc_s, (j | kk) != 0);
                             else mma_f8_ss(d, hi + 2 * kk, k + 2 * kk, idesc_s, true);
                             mma_f8_ss(d, lo + 2 * kk, k + 2 * kk, idesc_s, true);
                         }
                     }
-                    if (j < 3) mma_commit(bar_empty + 8 * slot);
+                    if (j < 3) mma_commit(bar_empty + 8 * full_slot);
+                    if (j == 4) mma_commit(bar_s + 8 * (t & 1));
                 }
-                if (ok) mma_commit(bar_s + 8 * (t & 1));
-            };
-            tc_fence_after();
-            if (ok) scores(0);
-            for (int t = 0; t < ntiles && ok; ++t) {
-                if (t + 1 < ntiles) scores(t + 1);
-                if (!ok) break;
-                ok = mbar_try_wait(bar_p + 8 * (t & 1), (t >> 1) & 1) || mbar_wait(bar_p + 8 * (t & 1), (t >> 1) & 1, &s_abort, a.status);
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t p = tmem + kColS + kR * (t & 1);
-#pragma unroll
-                for (int v = 0; v < 2; ++v) {
-                    const int slot = (5 * t + 3 + v) % kSlots;
-#pragma unroll
-                    for (int kk = 0; kk < 3; ++kk) {               // 32 rows: four groups of eight, 1024 bytes apart
-                        const uint64_t b = smem_desc(ring + slot * kSlotBytes + kk * 4096, 1024, 1024);
-#pragma unroll
-                        for (int term = 0; term < 3; ++term) mma_f8_ts(tmem + kColO + 128 * v, p + 32 * kk + 8 * term, b, idesc_o, (t | kk | term) != 0);
-                    }
-                    mma_commit(bar_empty + 8 * slot);
-                }
-                mma_commit(bar_pv);
+                __syncwarp();
+                if (++full_slot == kSlots) { full_slot = 0; full_par ^= 1; }
             }
+        };
+        tc_fence_after();
+        if (ok) scores(0);
+        int v_slot = 3;                                            // the tile's first V block
+        for (int t = 0; t < ntiles && ok; ++t) {
+            if (t + 1 < ntiles) scores(t + 1);
+            if (!ok) break;
+            ok = wait(bar_p + 8 * (t & 1), (t >> 1) & 1);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t p = tm + kColS + kR * (t & 1);
+            int slot = v_slot;
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                const uint64_t b0 = smem_desc(sm + kQBytes + slot * kSlotBytes, 1024, 1024);
+                if (leader) {
+#pragma unroll
+                    for (int kk = 0; kk < 3; ++kk)                 // 32 rows: four groups of eight, 1024 bytes apart
+#pragma unroll
+                        for (int term = 0; term < 3; ++term)
+                            mma_f8_ts(tm + kColO + 128 * v, p + 32 * kk + 8 * term, b0 + 256 * kk, idesc_o, t > 0 || (kk | term) != 0);
+                    mma_commit(bar_empty + 8 * slot);
+                    if (v == 1) mma_commit(bar_pv);
+                }
+                __syncwarp();
+                if (++slot == kSlots) slot = 0;
+            }
+            v_slot += 5;
+            if (v_slot >= kSlots) v_slot -= kSlots;
         }
     } else {
         // ---- softmax: one thread per query row; warp w may touch the TMEM lanes of quarter w % 4 -----------------------------------
@@ -271,7 +299,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
         auto row_entry = [&](int t, float s) {                     // (thread r < 96: row r of tile t)
             const bool there = row0 + t * kR + r < row1;
             s = s == 0.f ? 0x1p-60f : s;                           // (a record of zeros is a row of zeros, and has its weight)
-            return there ? make_float4(s, __log2f(s), 1.f / s, 0.f) : make_float4(0.f, -INFINITY, 0.f, 0.f);       // past the end: no weight
+            const uint32_t bits = __float_as_uint(s), e = __float_as_uint((float)((int)(bits >> 23) - 127));
+            return there ? (bits & 0xff800000u) | (e >> 16) : 0x0000ff80u;         // past the end: 0 and minus infinity, no weight
         };
         auto row_scale = [&](int t) {
             const int row = row0 + t * kR + r;
@@ -303,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
         float m = -INFINITY, l = 0.f;
         for (int t = 0; t < ntiles; ++t) {
             const float s_next = t + 1 < ntiles ? row_scale(t + 1) : 0.f;
-            const float4 *table = s_table + kR * (t & 1);
+            const uint4 *table = reinterpret_cast<const uint4 *>(s_table + kR * (t & 1));
             const uint32_t col = lanes + kColS + kR * (t & 1);
             // (after an expired wait every later wait returns at once: the loop runs on, so that the threads keep meeting at the
             // named barrier below, and ends with a result that the status word disowns)
@@ -317,11 +346,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
 #pragma unroll
             for (int c = 0; c < 3; ++c)
 #pragma unroll
-                for (int i = 0; i < 32; i += 2) {
-                    const float4 e0 = table[32 * c + i], e1 = table[32 * c + i + 1];
-                    const float x0 = fmaf(__uint_as_float(raw[c][i]), mult * e0.x, e0.y), x1 = fmaf(__uint_as_float(raw[c][i + 1]), mult * e1.x, e1.y);
-                    raw[c][i] = __float_as_uint(x0); raw[c][i + 1] = __float_as_uint(x1);
-                    mx = fmaxf(mx, x0); mx1 = fmaxf(mx1, x1);
+                for (int i = 0; i < 32; i += 4) {
+                    const uint4 e = table[8 * c + i / 4];
+                    const uint32_t ew[4] = {e.x, e.y, e.z, e.w};
+                    float x[4];
+#pragma unroll
+                    for (int p = 0; p < 4; ++p) {
+                        x[p] = fmaf(__uint_as_float(raw[c][i + p]), mult * __uint_as_float(ew[p] & 0xffff0000u), __uint_as_float(ew[p] << 16));
+                        raw[c][i + p] = __float_as_uint(x[p]);
+                    }
+                    mx = fmaxf(mx, fmaxf(x[0], x[1])); mx1 = fmaxf(mx1, fmaxf(x[2], x[3]));
                 }
             mx = fmaxf(mx, mx1);
             const bool grow = t == 0 || mx > m + kLazy;
@@ -349,11 +383,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
                     uint32_t h[2], h1[2], h2[2];
+                    const uint4 e = table[8 * c + q];
+                    const uint32_t ew[4] = {e.x, e.y, e.z, e.w};
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
                         const int i = 4 * q + 2 * p;
                         const float w0 = ex2(__uint_as_float(raw[c][i]) - ref), w1 = ex2(__uint_as_float(raw[c][i + 1]) - ref);
-                        l = fmaf(w0, table[32 * c + i].z, l); l1 = fmaf(w1, table[32 * c + i + 1].z, l1);
+                        // 1 / s of a power of two by its exponent (of s = 0: 2^127, times no weight)
+                        l = fmaf(w0, __uint_as_float(0x7f000000u - (ew[2 * p] & 0xffff0000u)), l);
+                        l1 = fmaf(w1, __uint_as_float(0x7f000000u - (ew[2 * p + 1] & 0xffff0000u)), l1);
                         const __half2 x = __floats2half2_rn(w0, w1);
                         h[p] = *reinterpret_cast<const uint32_t *>(&x);
                         const uint32_t top = h[p] & 0xff00ff00u;
