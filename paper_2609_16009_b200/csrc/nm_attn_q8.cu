@@ -38,10 +38,10 @@ constexpr int kR = 96;                             // cache rows of a tile
 constexpr int kQRow = 2 * kKv + 2 * kRope;         // bytes of a prepared query: hi | lo | key part
 constexpr int kQBlock = kM * 128, kSlotBytes = kR * 128, kSlots = 9;
 constexpr int kQBytes = 7 * kQBlock;               // lo 0-3, hi of this half's two blocks, key part
-constexpr int kTableBytes = 2 * kR * 4;
+constexpr int kTables = 4, kTableBytes = kTables * kR * 4;
 constexpr int kSmemBytes = 1024 + kQBytes + kSlots * kSlotBytes + kTableBytes + 256;
 static_assert(kSmemBytes <= 232448, "shared memory");
-constexpr int kThreads = 192;                      // TMA, MMA, four softmax warps
+constexpr int kSoftmax = 256, kThreads = 64 + kSoftmax;       // TMA, MMA, two softmax threads per query row
 constexpr uint32_t kColO = 0, kColS = 256, kColQ = 448;
 constexpr float kHeadroom = 11.f, kLazy = 4.f;     // log2: weights are at most 2^(11 + 4)
 constexpr int kMaxT = NM_MAX_Q8_BATCH, kPairs = kSMs / 2, kMaxItems = 4 * kPairs;
@@ -138,6 +138,10 @@ __host__ __device__ constexpr uint32_t instr_desc_f8(int m, int n, int a_format,
 {
     return (1u << 4) | ((uint32_t)a_format << 7) | ((b_mn_major ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
 }
+__device__ __forceinline__ void tmem_st4(uint32_t addr, const uint32_t (&r)[4])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
 __device__ __forceinline__ bool elect_one()
 {
     uint32_t r;
@@ -163,13 +167,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
     const uint32_t raw_addr = smem_u32(smem_raw), base = (raw_addr + 1023u) & ~1023u;      // swizzle atoms want 1024-byte alignment
     unsigned char *smem = smem_raw + (base - raw_addr);
     const uint32_t q_addr = base, ring = base + kQBytes;
-    // [2][96]: s and log2 s of a tile's rows as two bf16 (s is a power of two: both exact) - four rows per 16-byte read, since the
+    // [4][96]: s and log2 s of a tile's rows as two bf16 (s is a power of two: both exact) - four rows per 16-byte read, since the
     // matrix unit wants shared memory's bandwidth for itself
     uint32_t *s_table = reinterpret_cast<uint32_t *>(smem + kQBytes + kSlots * kSlotBytes);
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + kQBytes + kSlots * kSlotBytes + kTableBytes);
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * kSlots, bar_q = bar_empty + 8 * kSlots, bar_qt = bar_q + 8,
                    bar_s = bar_qt + 8, bar_p = bar_s + 16, bar_pv = bar_p + 16;
     __shared__ uint32_t s_tmem;
+    __shared__ float s_pair[2][kM];                                // what the two threads of a row tell each other
     __shared__ int s_abort;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, half = blockIdx.x & 1;
     const Item &it = a.items[blockIdx.x >> 1];
@@ -180,7 +185,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
         for (int i = 0; i < kSlots; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
         mbar_init(bar_q, 1);
         mbar_init(bar_qt, 128);
-        for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_p + 8 * i, 128); }
+        for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_p + 8 * i, kSoftmax); }
         mbar_init(bar_pv, 1);
         mbar_init_fence();
     }
@@ -292,23 +297,26 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
             if (v_slot >= kSlots) v_slot -= kSlots;
         }
     } else {
-        // ---- softmax: one thread per query row; warp w may touch the TMEM lanes of quarter w % 4 -----------------------------------
-        const int quad = warp & 3, r = quad * 32 + lane;
+        // ---- softmax: two threads per query row, each with 48 of a tile's cache rows (one alone needs 4000 clocks a tile, more than
+        //      the matrix unit's 3100); warp w may touch the TMEM lanes of quarter w % 4 ------------------------------------------
+        const int set = (warp - 2) >> 2, quad = warp & 3, r = quad * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
         const unsigned char *records = a.records[source];
-        auto row_entry = [&](int t, float s) {                     // (thread r < 96: row r of tile t)
-            const bool there = row0 + t * kR + r < row1;
+        const int entry = set == 0 ? r : kR;                       // the row of a tile whose scale this thread fetches, if there is one
+        auto row_entry = [&](int t, float s) {
+            const bool there = row0 + t * kR + entry < row1;
             s = s == 0.f ? 0x1p-60f : s;                           // (a record of zeros is a row of zeros, and has its weight)
             const uint32_t bits = __float_as_uint(s), e = __float_as_uint((float)((int)(bits >> 23) - 127));
             return there ? (bits & 0xff800000u) | (e >> 16) : 0x0000ff80u;         // past the end: 0 and minus infinity, no weight
         };
         auto row_scale = [&](int t) {
-            const int row = row0 + t * kR + r;
-            return r < kR && row < row1 ? __ldg(reinterpret_cast<const float *>(records + (long)row * kRec + kKv + 2 * kRope)) : 0.f;
+            const int row = row0 + t * kR + entry;
+            return entry < kR && row < row1 ? __ldg(reinterpret_cast<const float *>(records + (long)row * kRec + kKv + 2 * kRope)) : 0.f;
         };
-        const float s0 = row_scale(0);
+        const float s0 = row_scale(0), s1 = row_scale(1);
+        float s_next = row_scale(2);
         pdl_wait_prior_grids();
-        {
+        if (set == 0) {
             // the hi terms of the other half's columns to TMEM, 256 bytes a row; rows past the last query are zeros
             const int q_row = it.q_row + r;
             const uint4 *src = reinterpret_cast<const uint4 *>(a.q_rows + (long)min(q_row, a.total_q - 1) * kQRow + 128 * other);
@@ -327,27 +335,26 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
             mbar_arrive(bar_qt);
         }
         const float mult = r < it.n_q ? a.q_mult[it.q_row + r] : 0.f;
-        if (r < kR) s_table[r] = row_entry(0, s0);
-        named_barrier_sync(1, 128);
-        float m = -INFINITY, l = 0.f;
+        if (entry < kR) { s_table[entry] = row_entry(0, s0); s_table[kR + entry] = row_entry(1, s1); }
+        named_barrier_sync(1, kSoftmax);
+        float m = -INFINITY, l = 0.f, l1 = 0.f;
         for (int t = 0; t < ntiles; ++t) {
-            const float s_next = t + 1 < ntiles ? row_scale(t + 1) : 0.f;
-            const uint4 *table = reinterpret_cast<const uint4 *>(s_table + kR * (t & 1));
+            const uint4 *table = reinterpret_cast<const uint4 *>(s_table + kR * (t % kTables) + 48 * set);
             const uint32_t col = lanes + kColS + kR * (t & 1);
             // (after an expired wait every later wait returns at once: the loop runs on, so that the threads keep meeting at the
             // named barrier below, and ends with a result that the status word disowns)
             mbar_wait(bar_s + 8 * (t & 1), (t >> 1) & 1, &s_abort, a.status);
             tc_fence_after();
-            uint32_t raw[3][32];
+            uint32_t raw[3][16];                                   // three pieces of 16 cache rows
 #pragma unroll
-            for (int c = 0; c < 3; ++c) tmem_ld32(col + 32 * c, raw[c]);
+            for (int c = 0; c < 3; ++c) tmem_ld16(col + 48 * set + 16 * c, raw[c]);
             tmem_wait_ld();
             float mx = -1e30f, mx1 = -1e30f;                       // (two chains; the start keeps a row without any finite score from becoming NaN)
 #pragma unroll
             for (int c = 0; c < 3; ++c)
 #pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    const uint4 e = table[8 * c + i / 4];
+                for (int i = 0; i < 16; i += 4) {
+                    const uint4 e = table[4 * c + i / 4];
                     const uint32_t ew[4] = {e.x, e.y, e.z, e.w};
                     float x[4];
 #pragma unroll
@@ -357,14 +364,20 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
                     }
                     mx = fmaxf(mx, fmaxf(x[0], x[1])); mx1 = fmaxf(mx1, fmaxf(x[2], x[3]));
                 }
-            mx = fmaxf(mx, mx1);
+            // One barrier a tile.  Before it: this tile's scores are in registers (P may overwrite them), its maxima are told, and the
+            // table of the tile after next is written - into a buffer whose last readers passed the barrier before this one.
+            s_pair[set][r] = fmaxf(mx, mx1);
+            if (entry < kR) s_table[kR * ((t + 2) % kTables) + entry] = row_entry(t + 2, s_next);
+            named_barrier_sync(1, kSoftmax);
+            s_next = row_scale(t + 3);
+            mx = fmaxf(s_pair[0][r], s_pair[1][r]);
             const bool grow = t == 0 || mx > m + kLazy;
             if (t > 0 && __any_sync(0xffffffffu, grow)) {
-                // the previous tile's P * V has to be through before O is touched
+                // the previous tile's P * V has to be through before O is touched; each of the row's threads takes half of the columns
                 mbar_wait(bar_pv, (t - 1) & 1, &s_abort, a.status);
                 tc_fence_after();
                 const float f = grow ? ex2(m - mx) : 1.f;
-                for (int c = 0; c < 16; ++c) {
+                for (int c = 8 * set; c < 8 * set + 8; ++c) {
                     uint32_t o[16];
                     tmem_ld16(lanes + kColO + 16 * c, o);
                     tmem_wait_ld();
@@ -372,18 +385,17 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
                     for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
                     tmem_st16(lanes + kColO + 16 * c, o);
                 }
-                l *= f;
+                l *= f; l1 *= f;
             }
             if (grow) m = mx;
             const float ref = m - kHeadroom;
-            float l1 = 0.f;
 #pragma unroll
             for (int c = 0; c < 3; ++c) {
-                uint32_t hi[8], mid[8], lo[8];
+                uint32_t hi[4], mid[4], lo[4];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
+                for (int q = 0; q < 4; ++q) {
                     uint32_t h[2], h1[2], h2[2];
-                    const uint4 e = table[8 * c + q];
+                    const uint4 e = table[4 * c + q];
                     const uint32_t ew[4] = {e.x, e.y, e.z, e.w};
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
@@ -403,30 +415,28 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
                     }
                     hi[q] = __byte_perm(h[0], h[1], 0x7531); mid[q] = __byte_perm(h1[0], h1[1], 0x7531); lo[q] = __byte_perm(h2[0], h2[1], 0x7531);
                 }
-                // over the columns of S that this thread alone has read
-                tmem_st8(col + 32 * c, hi);
-                tmem_st8(col + 32 * c + 8, mid);
-                tmem_st8(col + 32 * c + 16, lo);
+                // 32 cache rows have 8 columns of each term, 16 rows half of them, over the columns of their scores
+                const int piece = 3 * set + c;
+                const uint32_t to = col + 32 * (piece >> 1) + 4 * (piece & 1);
+                tmem_st4(to, hi);
+                tmem_st4(to + 8, mid);
+                tmem_st4(to + 16, lo);
             }
-            l += l1;
             tmem_wait_st();
             tc_fence_before();
             mbar_arrive(bar_p + 8 * (t & 1));
-            if (t + 1 < ntiles) {
-                if (r < kR) s_table[kR * ((t + 1) & 1) + r] = row_entry(t + 1, s_next);
-                named_barrier_sync(1, 128);                        // the next tile's table is written, this one's has been read by all
-            }
         }
         mbar_wait(bar_pv, (ntiles - 1) & 1, &s_abort, a.status);
         tc_fence_after();
-        // ---- out: the warp's 32 rows, 64 columns at a time through its own corner of the ring (every copy into it has been used), so
-        //      that the stores run along the rows ------------------------------------------------------------------------------------
-        if (half == 0 && r < it.n_q) {
-            float *ml = a.ml + 2 * (long)(it.out_row + r);
-            ml[0] = m; ml[1] = l;
-        }
-        float4 *corner = reinterpret_cast<float4 *>(smem + kQBytes + quad * 8192);        // [32 rows][16 float4], the index XOR-ed with row & 15
-        for (int c0 = 0; c0 < 256; c0 += 64) {
+        // ---- out: the warp's 32 rows and its set's 128 columns, 64 at a time through its own corner of the ring (every copy into it has
+        //      been used), so that the stores run along the rows ----------------------------------------------------------------------
+        named_barrier_sync(1, kSoftmax);
+        s_pair[set][r] = l + l1;
+        named_barrier_sync(1, kSoftmax);
+        if (half == 0 && set == 0 && r < it.n_q)
+            *reinterpret_cast<float2 *>(a.ml + 2 * (long)(it.out_row + r)) = make_float2(m, s_pair[0][r] + s_pair[1][r]);
+        float4 *corner = reinterpret_cast<float4 *>(smem + kQBytes + (4 * set + quad) * 8192);        // [32 rows][16 float4], the index XOR-ed with row & 15
+        for (int c0 = 128 * set; c0 < 128 * set + 128; c0 += 64) {
             uint32_t o[2][32];
             tmem_ld32(lanes + kColO + c0, o[0]);
             tmem_ld32(lanes + kColO + c0 + 32, o[1]);
@@ -438,6 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
                 corner[lane * 16 + (i ^ (lane & 15))] = make_float4(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3]));
             }
             __syncwarp();
+#pragma unroll 4
             for (int i = lane; i < 32 * 16; i += 32) {
                 const int rr = i >> 4, f = i & 15, q = quad * 32 + rr;
                 if (q < it.n_q)
@@ -458,43 +469,52 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
     }
 }
 
-// ---- the merge: one CTA per head of a sequence, four columns a thread ---------------------------------------------------------
-__global__ void __launch_bounds__(128) q8_merge_kernel(const __grid_constant__ MergeArgs a)
+// ---- the merge: one CTA per head of a sequence, four columns a thread, four threads for every fourth part -----------------------
+constexpr int kMergeGroups = 4, kMergeThreads = kMergeGroups * 128;
+__global__ void __launch_bounds__(kMergeThreads) q8_merge_kernel(const __grid_constant__ MergeArgs a)
 {
-    __shared__ float s_w[2 * kMaxItems];
+    __shared__ float s_w[2 * kMaxItems], s_l[2 * kMaxItems];
     __shared__ int s_row[2 * kMaxItems];
-    __shared__ float s_red[2][4];
+    __shared__ float s_red[kMergeThreads / 32];
+    __shared__ float4 s_acc[kMergeGroups - 1][128];
     pdl_launch_dependents();
     pdl_wait_prior_grids();
-    const int t = blockIdx.x / a.H, h = blockIdx.x - t * a.H, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int t = blockIdx.x / a.H, h = blockIdx.x - t * a.H, tid = threadIdx.x, group = tid >> 7, x = tid & 127;
     const int n = a.n_prefix + a.own_n[t];
     float mx = -INFINITY;
-    for (int i = tid; i < n; i += 128) {
+    for (int i = tid; i < n; i += kMergeThreads) {
         // prefix: item (tile of query rows, part); own: item (sequence, part)
         const int row = i < a.n_prefix ? (blockIdx.x / kM * a.n_prefix + i) * a.tile_rows + blockIdx.x % kM : a.own_row[t] + (i - a.n_prefix) * a.H + h;
+        const float2 ml = *reinterpret_cast<const float2 *>(a.ml + 2 * (long)row);
         s_row[i] = row;
-        s_w[i] = a.ml[2 * (long)row];
-        mx = fmaxf(mx, s_w[i]);
+        s_w[i] = ml.x; s_l[i] = ml.y;
+        mx = fmaxf(mx, ml.x);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    if (lane == 0) s_red[0][warp] = mx;
+    if ((tid & 31) == 0) s_red[tid >> 5] = mx;
     __syncthreads();
-    mx = fmaxf(fmaxf(s_red[0][0], s_red[0][1]), fmaxf(s_red[0][2], s_red[0][3]));
+#pragma unroll
+    for (int w = 0; w < kMergeThreads / 32; ++w) mx = fmaxf(mx, s_red[w]);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float total = 0.f;
-    for (int i = tid; i < n; i += 128) s_w[i] = ex2(s_w[i] - mx);
-    __syncthreads();
-    // (every thread adds the same sums in the same order)
 #pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-        const float w = s_w[i];
-        const float4 v = *reinterpret_cast<const float4 *>(a.O + (long)s_row[i] * kKv + 4 * tid);
-        total = fmaf(w, a.ml[2 * (long)s_row[i] + 1], total);
+    for (int i = group; i < n; i += kMergeGroups) {
+        const float w = ex2(s_w[i] - mx);
+        const float4 v = *reinterpret_cast<const float4 *>(a.O + (long)s_row[i] * kKv + 4 * x);
         acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y); acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
     }
+    if (group > 0) s_acc[group - 1][x] = acc;
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int g = 0; g < kMergeGroups - 1; ++g) {
+        const float4 v = s_acc[g][x];
+        acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+    }
+    float total = 0.f;                                             // (every thread adds the same sums in the same order)
+    for (int i = 0; i < n; ++i) total = fmaf(ex2(s_w[i] - mx), s_l[i], total);
     const float inv = n > 0 ? 1.f / total : 0.f;                   // no rows: zeros, and minus infinity below
-    const long at = (long)blockIdx.x * kKv + 4 * tid;
+    const long at = (long)blockIdx.x * kKv + 4 * x;
     acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
     if (a.o_f32) *reinterpret_cast<float4 *>(a.o_f32 + at) = acc;
     if (a.o_bf16) {
@@ -672,7 +692,7 @@ int nm_mla_attention_q8(const void *Q, long q_stride, const void *prefix, long p
         if (e == cudaSuccess) e = launch_after(attn_q8_kernel, 2 * items, kThreads, kSmemBytes, s, pa);
         if (e != cudaSuccess) return record_cuda_error(e, "quantised attention launch");
     }
-    const cudaError_t e = launch_after(q8_merge_kernel, (unsigned)total_q, 128, 0, s, ma);
+    const cudaError_t e = launch_after(q8_merge_kernel, (unsigned)total_q, kMergeThreads, 0, s, ma);
     return e == cudaSuccess ? NM_OK : record_cuda_error(e, "quantised attention merge launch");
 }
 
