@@ -38,7 +38,7 @@ constexpr int kR = 96;                             // cache rows of a tile
 constexpr int kQRow = 2 * kKv + 2 * kRope;         // bytes of a prepared query: hi | lo | key part
 constexpr int kQBlock = kM * 128, kSlotBytes = kR * 128, kSlots = 9;
 constexpr int kQBytes = 7 * kQBlock;               // lo 0-3, hi of this half's two blocks, key part
-constexpr int kTables = 4, kTableBytes = kTables * kR * 4;
+constexpr int kTables = 4, kTableBytes = kTables * kR;
 constexpr int kSmemBytes = 1024 + kQBytes + kSlots * kSlotBytes + kTableBytes + 256;
 static_assert(kSmemBytes <= 232448, "shared memory");
 constexpr int kSoftmax = 256, kThreads = 64 + kSoftmax;       // TMA, MMA, two softmax threads per query row
@@ -167,9 +167,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
     const uint32_t raw_addr = smem_u32(smem_raw), base = (raw_addr + 1023u) & ~1023u;      // swizzle atoms want 1024-byte alignment
     unsigned char *smem = smem_raw + (base - raw_addr);
     const uint32_t q_addr = base, ring = base + kQBytes;
-    // [4][96]: s and log2 s of a tile's rows as two bf16 (s is a power of two: both exact) - four rows per 16-byte read, since the
-    // matrix unit wants shared memory's bandwidth for itself
-    uint32_t *s_table = reinterpret_cast<uint32_t *>(smem + kQBytes + kSlots * kSlotBytes);
+    // [4][96]: the biased exponents of a tile's scales, 16 to a read - the matrix unit wants shared memory's bandwidth for itself
+    unsigned char *s_table = smem + kQBytes + kSlots * kSlotBytes;
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + kQBytes + kSlots * kSlotBytes + kTableBytes);
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * kSlots, bar_q = bar_empty + 8 * kSlots, bar_qt = bar_q + 8,
                    bar_s = bar_qt + 8, bar_p = bar_s + 16, bar_pv = bar_p + 16;
@@ -303,11 +302,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
         const unsigned char *records = a.records[source];
         const int entry = set == 0 ? r : kR;                       // the row of a tile whose scale this thread fetches, if there is one
-        auto row_entry = [&](int t, float s) {
-            const bool there = row0 + t * kR + entry < row1;
-            s = s == 0.f ? 0x1p-60f : s;                           // (a record of zeros is a row of zeros, and has its weight)
-            const uint32_t bits = __float_as_uint(s), e = __float_as_uint((float)((int)(bits >> 23) - 127));
-            return there ? (bits & 0xff800000u) | (e >> 16) : 0x0000ff80u;         // past the end: 0 and minus infinity, no weight
+        auto row_entry = [&](float s) {                            // (a record of zeros is a row of zeros, and has its weight: 2^-60 will do for its s)
+            return (unsigned char)(s == 0.f ? 127 - 60 : __float_as_uint(s) >> 23);
         };
         auto row_scale = [&](int t) {
             const int row = row0 + t * kR + entry;
@@ -335,11 +331,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
             mbar_arrive(bar_qt);
         }
         const float mult = r < it.n_q ? a.q_mult[it.q_row + r] : 0.f;
-        if (entry < kR) { s_table[entry] = row_entry(0, s0); s_table[kR + entry] = row_entry(1, s1); }
+        if (entry < kR) { s_table[entry] = row_entry(s0); s_table[kR + entry] = row_entry(s1); }
         named_barrier_sync(1, kSoftmax);
         float m = -INFINITY, l = 0.f, l1 = 0.f;
         for (int t = 0; t < ntiles; ++t) {
-            const uint4 *table = reinterpret_cast<const uint4 *>(s_table + kR * (t % kTables) + 48 * set);
             const uint32_t col = lanes + kColS + kR * (t & 1);
             // (after an expired wait every later wait returns at once: the loop runs on, so that the threads keep meeting at the
             // named barrier below, and ends with a result that the status word disowns)
@@ -349,25 +344,38 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
 #pragma unroll
             for (int c = 0; c < 3; ++c) tmem_ld16(col + 48 * set + 16 * c, raw[c]);
             tmem_wait_ld();
+            // s as a number is its exponent in place; log2 s: the exponent below 2^23's last binary place, less 2^23 and the bias
+            uint32_t exps[12];
+#pragma unroll
+            for (int c = 0; c < 3; ++c) {
+                const uint4 e = reinterpret_cast<const uint4 *>(s_table + kR * (t % kTables) + 48 * set)[c];
+                exps[4 * c] = e.x; exps[4 * c + 1] = e.y; exps[4 * c + 2] = e.z; exps[4 * c + 3] = e.w;
+            }
             float mx = -1e30f, mx1 = -1e30f;                       // (two chains; the start keeps a row without any finite score from becoming NaN)
 #pragma unroll
             for (int c = 0; c < 3; ++c)
 #pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    const uint4 e = table[4 * c + i / 4];
-                    const uint32_t ew[4] = {e.x, e.y, e.z, e.w};
-                    float x[4];
-#pragma unroll
-                    for (int p = 0; p < 4; ++p) {
-                        x[p] = fmaf(__uint_as_float(raw[c][i + p]), mult * __uint_as_float(ew[p] & 0xffff0000u), __uint_as_float(ew[p] << 16));
-                        raw[c][i + p] = __float_as_uint(x[p]);
-                    }
-                    mx = fmaxf(mx, fmaxf(x[0], x[1])); mx1 = fmaxf(mx1, fmaxf(x[2], x[3]));
+                for (int i = 0; i < 16; ++i) {
+                    const uint32_t w = exps[4 * c + i / 4], e = __byte_perm(w, 0, 0x4440 + (i & 3));
+                    const float x = fmaf(__uint_as_float(raw[c][i]), mult * __uint_as_float(e << 23), __uint_as_float(0x4b000000u | e) - 8388735.f);
+                    raw[c][i] = __float_as_uint(x);
                 }
+            const int valid = row1 - (row0 + t * kR) - 48 * set;
+            if (valid < 48) {                                      // (the last tile) rows past the end: no weight
+#pragma unroll
+                for (int c = 0; c < 3; ++c)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (16 * c + i >= valid) raw[c][i] = 0xff800000u;
+            }
+#pragma unroll
+            for (int c = 0; c < 3; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; i += 2) { mx = fmaxf(mx, __uint_as_float(raw[c][i])); mx1 = fmaxf(mx1, __uint_as_float(raw[c][i + 1])); }
             // One barrier a tile.  Before it: this tile's scores are in registers (P may overwrite them), its maxima are told, and the
             // table of the tile after next is written - into a buffer whose last readers passed the barrier before this one.
             s_pair[set][r] = fmaxf(mx, mx1);
-            if (entry < kR) s_table[kR * ((t + 2) % kTables) + entry] = row_entry(t + 2, s_next);
+            if (entry < kR) s_table[kR * ((t + 2) % kTables) + entry] = row_entry(s_next);
             named_barrier_sync(1, kSoftmax);
             s_next = row_scale(t + 3);
             mx = fmaxf(s_pair[0][r], s_pair[1][r]);
@@ -377,13 +385,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
                 mbar_wait(bar_pv, (t - 1) & 1, &s_abort, a.status);
                 tc_fence_after();
                 const float f = grow ? ex2(m - mx) : 1.f;
-                for (int c = 8 * set; c < 8 * set + 8; ++c) {
-                    uint32_t o[16];
-                    tmem_ld16(lanes + kColO + 16 * c, o);
+#pragma unroll 1
+                for (int c = 128 * set; c < 128 * set + 128; c += 64) {
+                    uint32_t o[2][32];
+                    tmem_ld32(lanes + kColO + c, o[0]);
+                    tmem_ld32(lanes + kColO + c + 32, o[1]);
                     tmem_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                    tmem_st16(lanes + kColO + 16 * c, o);
+                    for (int i = 0; i < 32; ++i) {
+                        o[0][i] = __float_as_uint(__uint_as_float(o[0][i]) * f); o[1][i] = __float_as_uint(__uint_as_float(o[1][i]) * f);
+                    }
+                    tmem_st32(lanes + kColO + c, o[0]);
+                    tmem_st32(lanes + kColO + c + 32, o[1]);
                 }
                 l *= f; l1 *= f;
             }
@@ -395,15 +408,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     uint32_t h[2], h1[2], h2[2];
-                    const uint4 e = table[4 * c + q];
-                    const uint32_t ew[4] = {e.x, e.y, e.z, e.w};
+                    const uint32_t w = exps[4 * c + q];
 #pragma unroll
                     for (int p = 0; p < 2; ++p) {
                         const int i = 4 * q + 2 * p;
                         const float w0 = ex2(__uint_as_float(raw[c][i]) - ref), w1 = ex2(__uint_as_float(raw[c][i + 1]) - ref);
-                        // 1 / s of a power of two by its exponent (of s = 0: 2^127, times no weight)
-                        l = fmaf(w0, __uint_as_float(0x7f000000u - (ew[2 * p] & 0xffff0000u)), l);
-                        l1 = fmaf(w1, __uint_as_float(0x7f000000u - (ew[2 * p + 1] & 0xffff0000u)), l1);
+                        // 1 / s by its exponent (past the end, 0: 2^127, times no weight)
+                        l = fmaf(w0, __uint_as_float(0x7f000000u - (__byte_perm(w, 0, 0x4440 + 2 * p) << 23)), l);
+                        l1 = fmaf(w1, __uint_as_float(0x7f000000u - (__byte_perm(w, 0, 0x4441 + 2 * p) << 23)), l1);
                         const __half2 x = __floats2half2_rn(w0, w1);
                         h[p] = *reinterpret_cast<const uint32_t *>(&x);
                         const uint32_t top = h[p] & 0xff00ff00u;
@@ -426,6 +438,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
             tc_fence_before();
             mbar_arrive(bar_p + 8 * (t & 1));
         }
+        // (both of the last two: the scores of the last tile say that the P * V before these is through, not that the last but one is,
+        // and a wait by parity alone would take an older phase for the last)
+        if (ntiles > 1) mbar_wait(bar_pv, (ntiles - 2) & 1, &s_abort, a.status);
         mbar_wait(bar_pv, (ntiles - 1) & 1, &s_abort, a.status);
         tc_fence_after();
         // ---- out: the warp's 32 rows and its set's 128 columns, 64 at a time through its own corner of the ring (every copy into it has
