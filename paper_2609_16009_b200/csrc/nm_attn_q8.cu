@@ -44,7 +44,9 @@ static_assert(kSmemBytes <= 232448, "shared memory");
 constexpr int kSoftmax = 256, kThreads = 64 + kSoftmax;       // TMA, MMA, two softmax threads per query row
 constexpr uint32_t kColO = 0, kColS = 256, kColQ = 448;
 constexpr float kHeadroom = 11.f, kLazy = 4.f;     // log2: weights are at most 2^(11 + 4)
-constexpr int kMaxT = NM_MAX_Q8_BATCH, kPairs = kSMs / 2, kMaxItems = 4 * kPairs;
+constexpr int kMaxT = NM_MAX_Q8_BATCH, kPairs = kSMs / 2;
+constexpr int kMaxUnits = 2 * kMaxT;               // query tiles of the prefix (at most 64 * 128 / 128) and sequences
+constexpr int kMaxItems = kMaxUnits + kPairs;      // every unit once, and one more where a pair's share ends inside a unit
 
 struct Item {
     int q_row, n_q;                                // query rows
@@ -61,14 +63,16 @@ struct PassArgs {
     float *ml, *O;
     unsigned *status;
     int total_q;
+    short first[kPairs + 1];                       // items of each pair of CTAs
     Item items[kMaxItems];
 };
 struct MergeArgs {
     const float *ml, *O;
     uint16_t *o_bf16;
     float *o_f32, *lse;
-    int H, n_prefix, tile_rows;                    // parts of the prefix, query rows of a prefix item
-    int own_row[kMaxT], own_n[kMaxT];              // first partial row and parts of each sequence
+    int H, tile_rows;                              // query rows of a prefix item
+    int prefix_row[kMaxT], own_row[kMaxT];         // first partial row of each query tile of the prefix, of each sequence
+    short prefix_n[kMaxT], own_n[kMaxT];           // and their parts
 };
 
 __device__ __forceinline__ float ex2(float x)
@@ -148,17 +152,51 @@ __device__ __forceinline__ bool elect_one()
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
     return r != 0;
 }
-__device__ __forceinline__ void mma_f8_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate)
+// Matrix descriptors as their lower words - address / 16 and, above it, the leading stride / 16; the upper word (8 rows 1024 bytes
+// apart, version 1, 128-byte swizzle) is the same for all.  Put together inside the instruction's own assembly: as 64-bit arithmetic
+// the compiler repeats two dozen uniform instructions per MMA, and the issuing warp, not the pipe, sets the pace.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr, uint32_t lead_bytes) { return ((addr & 0x3ffffu) >> 4) | ((lead_bytes >> 4) << 16); }
+#define NM_Q8_MMA(KIND, A)                                                                                                            \
+    "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"                 \
+    "tcgen05.mma.cta_group::1.kind::" KIND " [%0], " A ", b, %3, p;\n\t}"
+__device__ __forceinline__ void mma_f8_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(0u) : "memory");
+    asm volatile(NM_Q8_MMA("f8f6f4", "a") ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(kDescHigh) : "memory");
 }
-__device__ __forceinline__ void mma_f8_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate)
+__device__ __forceinline__ void mma_f8_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(0u) : "memory");
+    asm volatile(NM_Q8_MMA("f8f6f4", "[%1]") ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(kDescHigh) : "memory");
+}
+__device__ __forceinline__ void mma_key_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool accumulate)
+{
+    asm volatile(NM_Q8_MMA("f16", "a") ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)accumulate), "r"(kDescHigh) : "memory");
+}
+#undef NM_Q8_MMA
+
+// The bounded wait of the issuing warp: no function call, and every decision is the warp's vote, so that its control flow stays uniform
+// to the compiler and the operands of the MMAs around it stay in uniform registers.
+__device__ __forceinline__ void wait_uniform(uint32_t bar, uint32_t par, volatile int *abort_flag, unsigned *status)
+{
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, par))) return;
+    const uint64_t t0 = global_timer_ns();
+#pragma unroll 1
+    for (;;) {
+        if (__all_sync(0xffffffffu, mbar_try_wait(bar, par))) return;
+        if (__any_sync(0xffffffffu, *abort_flag != 0)) return;
+        if (__any_sync(0xffffffffu, global_timer_ns() - t0 > kWaitLimitNs)) {
+            *abort_flag = 1;
+            if (status) atomicOr(status, kStatusWaitExpired);
+            return;
+        }
+    }
+}
+// A whole warp's wait: one lane polls (32 of them take shared memory's time from the matrix unit), the others meet it.
+__device__ __forceinline__ void warp_wait(uint32_t bar, uint32_t par, int lane, volatile int *abort_flag, unsigned *status)
+{
+    if (lane == 0 && !mbar_try_wait(bar, par)) mbar_wait(bar, par, abort_flag, status);
+    __syncwarp();
+    tc_fence_after();
 }
 
 __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_constant__ PassArgs a)
@@ -171,21 +209,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
     unsigned char *s_table = smem + kQBytes + kSlots * kSlotBytes;
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + kQBytes + kSlots * kSlotBytes + kTableBytes);
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * kSlots, bar_q = bar_empty + 8 * kSlots, bar_qt = bar_q + 8,
-                   bar_s = bar_qt + 8, bar_p = bar_s + 16, bar_pv = bar_p + 16;
+                   bar_s = bar_qt + 8, bar_p = bar_s + 16, bar_pv = bar_p + 16,
+                   bar_free = bar_pv + 8;
     __shared__ uint32_t s_tmem;
     __shared__ float s_pair[2][kM];                                // what the two threads of a row tell each other
     __shared__ int s_abort;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, half = blockIdx.x & 1;
-    const Item &it = a.items[blockIdx.x >> 1];
-    const int row0 = it.row0, row1 = it.row1, ntiles = ceil_div(row1 - row0, kR), source = it.source;
-    const CUtensorMap *map_k = &a.k[source];
+    const int pair = blockIdx.x >> 1, item0 = a.first[pair], item1 = a.first[pair + 1];
     if (tid == 0) {
         s_abort = 0;
         for (int i = 0; i < kSlots; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
         mbar_init(bar_q, 1);
         mbar_init(bar_qt, 128);
-        for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_p + 8 * i, kSoftmax); }
+        for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_p + 8 * i, kSoftmax / 32); }
         mbar_init(bar_pv, 1);
+        mbar_init(bar_free, kSoftmax / 32);
         mbar_init_fence();
     }
     if (warp == 1) tmem_alloc(&s_tmem, 512);
@@ -200,26 +238,45 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
     const int other = 2 * (half ^ 1), mine = 2 * half;
     auto block_x = [&](int j) { return j < 2 ? 128 * (other + j) : (j == 2 ? kKv : 128 * (mine + j - 3)); };
 
+    // The CTA takes its items one after another; the ring runs on from one to the next, so an item's records are on their way while the
+    // one before it is being finished.
     if (warp == 0) {
         if (lane == 0) {
             tma_prefetch_descriptor(&a.q);
-            tma_prefetch_descriptor(map_k);
             const uint64_t keep = l2_policy_evict_last();
-            auto load = [&](int item) {
-                const int slot = item % kSlots, t = item / 5;
-                mbar_arrive_expect_tx(bar_full + 8 * slot, kSlotBytes);
-                tma_load_2d(ring + slot * kSlotBytes, map_k, block_x(item - 5 * t), row0 + t * kR, bar_full + 8 * slot, keep);
+            int slot = 0, par = 1;                                 // (parity 1: a fresh barrier's phase before the first counts as complete)
+            bool ok = true;
+            auto load_queries = [&](int i) {                       // lo 0-3, hi of this half, key part
+                if (i > item0 && !mbar_try_wait(bar_free, (i - item0 - 1) & 1)) ok = mbar_wait(bar_free, (i - item0 - 1) & 1, &s_abort, a.status);
+                if (!ok) return;
+                mbar_arrive_expect_tx(bar_q, kQBytes);
+                for (int b = 0; b < 7; ++b)
+                    tma_load_2d(q_addr + b * kQBlock, &a.q, b < 4 ? kKv + 128 * b : (b < 6 ? 128 * (mine + b - 4) : 2 * kKv), a.items[i].q_row, bar_q, keep);
             };
-            const int total = 5 * ntiles, early = min(kSlots, total);
-            for (int i = 0; i < early; ++i) load(i);               // the records were written before the queries' kernel began
-            pdl_wait_prior_grids();
-            mbar_arrive_expect_tx(bar_q, kQBytes);
-            for (int i = 0; i < 7; ++i)                            // lo 0-3, hi of this half, key part
-                tma_load_2d(q_addr + i * kQBlock, &a.q, i < 4 ? kKv + 128 * i : (i < 6 ? 128 * (mine + i - 4) : 2 * kKv), it.q_row, bar_q, keep);
-            for (int i = early; i < total; ++i) {
-                const uint32_t bar = bar_empty + 8 * (i % kSlots), par = ((i / kSlots) - 1) & 1;
-                if (!mbar_try_wait(bar, par) && !mbar_wait(bar, par, &s_abort, a.status)) break;
-                load(i);
+            for (int i = item0; i < item1 && ok; ++i) {
+                const Item &it = a.items[i];
+                const CUtensorMap *map_k = &a.k[it.source];
+                tma_prefetch_descriptor(map_k);
+                const int total = 5 * ceil_div(it.row1 - it.row0, kR);
+                // An item's first tiles go ahead of its queries: these wait for the item before to be finished (the first item's for the
+                // kernel that prepares them - the records were written before that began)
+                const int ahead = min(total, 5);
+                for (int b = 0, x = 0, row = it.row0; b < total && ok; ++b) {
+                    if (b == ahead) {
+                        if (i == item0) pdl_wait_prior_grids();
+                        load_queries(i);
+                        if (!ok) break;
+                    }
+                    if (!mbar_try_wait(bar_empty + 8 * slot, par) && !mbar_wait(bar_empty + 8 * slot, par, &s_abort, a.status)) { ok = false; break; }
+                    mbar_arrive_expect_tx(bar_full + 8 * slot, kSlotBytes);
+                    tma_load_2d(ring + slot * kSlotBytes, map_k, block_x(x), row, bar_full + 8 * slot, keep);
+                    if (++slot == kSlots) { slot = 0; par ^= 1; }
+                    if (++x == 5) { x = 0; row += kR; }
+                }
+                if (ok && total <= ahead) {
+                    if (i == item0) pdl_wait_prior_grids();
+                    load_queries(i);
+                }
             }
         }
     } else if (warp == 1) {
@@ -229,78 +286,94 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
         constexpr uint32_t idesc_s = instr_desc_f8(kM, kR, 0, false), idesc_key = instr_desc(kM, kR, false, false), idesc_o = instr_desc_f8(kM, 128, 1, true);
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), sm = __shfl_sync(0xffffffffu, base, 0);
         const bool leader = elect_one();
+        const uint32_t q_low = desc_low(sm, 16), q_other = q_low + other * (kQBlock >> 4), q_mine = q_low + mine * (kQBlock >> 4);
+        // A block is waited for before the MMAs of the one before it are issued: the pipe queues only a few, and a wait between them
+        // would let it run dry.
+        // (An expired wait changes nothing here: the walk goes on, every operand in its place whatever it holds, so that the control
+        // flow stays uniform; the status word disowns the result.)
         auto wait = [&](uint32_t bar, uint32_t par) {
-            const bool there = mbar_try_wait(bar, par) || mbar_wait(bar, par, &s_abort, a.status);
-            return __all_sync(0xffffffffu, there) != 0;
+            wait_uniform(bar, par, &s_abort, a.status);
         };
-        bool ok = wait(bar_q, 0) && wait(bar_qt, 0);
-        int full_slot = 0, full_par = 0;                           // the ring's next block
-        auto scores = [&](int t) {
-            const uint32_t d = tm + kColS + kR * (t & 1);
+        int wait_slot = 0, wait_par = 0, slot = 0, v_slot = 3;     // the ring's block waited for next, issued next, and the next tile's first V block
+        int gs = 0, gp = 0;                                        // tiles of all items so far: scores issued, P * V issued
+        for (int i = item0; i < item1; ++i) {
+            const int ntiles = ceil_div(a.items[i].row1 - a.items[i].row0, kR), total = 5 * ntiles;
+            int waited = 0;
+            auto wait_block = [&]() {
+                if (waited < total) {
+                    wait(bar_full + 8 * wait_slot, wait_par);
+                    if (++wait_slot == kSlots) { wait_slot = 0; wait_par ^= 1; }
+                }
+                ++waited;
+            };
+            wait(bar_q, (i - item0) & 1);
+            wait(bar_qt, (i - item0) & 1);
+            tc_fence_after();                                      // (for what other threads did to TMEM; copies into shared memory need none)
+            wait_block();
+            auto scores = [&]() {
+                const uint32_t d = tm + kColS + kR * (gs & 1);
 #pragma unroll
-            for (int j = 0; j < 5; ++j) {
-                if (!ok) break;
-                ok = wait(bar_full + 8 * full_slot, full_par);
-                if (!ok) break;
-                tc_fence_after();
-                const uint64_t k = smem_desc(sm + kQBytes + full_slot * kSlotBytes, 16, 1024);
-                if (leader) {
-                    if (j == 2) {
-                        const uint64_t q = smem_desc(sm + 6 * kQBlock, 16, 1024);
+                for (int j = 0; j < 5; ++j) {
+                    wait_block();                                  // (the one after this)
+                    const uint32_t k = desc_low(sm + kQBytes, 16) + slot * (kSlotBytes >> 4);
+                    if (leader) {
+                        if (j == 2) {
+                            const uint32_t q = q_low + 6 * (kQBlock >> 4);
 #pragma unroll
-                        for (int kk = 0; kk < 4; ++kk) mma_ss(d, q + 2 * kk, k + 2 * kk, idesc_key, true);
-                    } else {
-                        const uint64_t lo = smem_desc(sm + (j < 2 ? other + j : mine + j - 3) * kQBlock, 16, 1024);
-                        const uint64_t hi = smem_desc(sm + (j < 2 ? 0 : 4 + j - 3) * kQBlock, 16, 1024);
+                            for (int kk = 0; kk < 4; ++kk) mma_key_ss(d, q + 2 * kk, k + 2 * kk, idesc_key, true);
+                        } else {
+                            const uint32_t lo = (j < 2 ? q_other + j * (kQBlock >> 4) : q_mine + (j - 3) * (kQBlock >> 4));
+                            const uint32_t hi = q_low + (j < 2 ? 0 : 4 + j - 3) * (kQBlock >> 4);
 #pragma unroll
-                        for (int kk = 0; kk < 4; ++kk) {           // 32 latent dimensions: 32 bytes in shared memory, 8 columns of TMEM
-                            if (j < 2) mma_f8_ts(d, tm + kColQ + 32 * j + 8 * kk, k + 2 * kk, idesc_s, (j | kk) != 0);
-                            else mma_f8_ss(d, hi + 2 * kk, k + 2 * kk, idesc_s, true);
-                            mma_f8_ss(d, lo + 2 * kk, k + 2 * kk, idesc_s, true);
+                            for (int kk = 0; kk < 4; ++kk) {       // 32 latent dimensions: 32 bytes in shared memory, 8 columns of TMEM
+                                if (j < 2) mma_f8_ts(d, tm + kColQ + 32 * j + 8 * kk, k + 2 * kk, idesc_s, (j | kk) != 0);
+                                else mma_f8_ss(d, hi + 2 * kk, k + 2 * kk, idesc_s, true);
+                                mma_f8_ss(d, lo + 2 * kk, k + 2 * kk, idesc_s, true);
+                            }
                         }
+                        if (j < 3) mma_commit(bar_empty + 8 * slot);
+                        if (j == 4) mma_commit(bar_s + 8 * (gs & 1));
                     }
-                    if (j < 3) mma_commit(bar_empty + 8 * full_slot);
-                    if (j == 4) mma_commit(bar_s + 8 * (t & 1));
+                    __syncwarp();
+                    if (++slot == kSlots) slot = 0;
                 }
-                __syncwarp();
-                if (++full_slot == kSlots) { full_slot = 0; full_par ^= 1; }
-            }
-        };
-        tc_fence_after();
-        if (ok) scores(0);
-        int v_slot = 3;                                            // the tile's first V block
-        for (int t = 0; t < ntiles && ok; ++t) {
-            if (t + 1 < ntiles) scores(t + 1);
-            if (!ok) break;
-            ok = wait(bar_p + 8 * (t & 1), (t >> 1) & 1);
-            if (!ok) break;
-            tc_fence_after();
-            const uint32_t p = tm + kColS + kR * (t & 1);
-            int slot = v_slot;
-#pragma unroll
-            for (int v = 0; v < 2; ++v) {
-                const uint64_t b0 = smem_desc(sm + kQBytes + slot * kSlotBytes, 1024, 1024);
+                ++gs;
+            };
+            scores();
+            for (int t = 0; t < ntiles; ++t, ++gp) {
+                if (t + 1 < ntiles) scores();
+                wait(bar_p + 8 * (gp & 1), (gp >> 1) & 1);
+                tc_fence_after();
+                const uint32_t p = tm + kColS + kR * (gp & 1);
+                const int v_next = v_slot + 1 == kSlots ? 0 : v_slot + 1;
+                const uint32_t v_low = desc_low(sm + kQBytes, 1024), b0 = v_low + v_slot * (kSlotBytes >> 4), b1 = v_low + v_next * (kSlotBytes >> 4);
                 if (leader) {
 #pragma unroll
-                    for (int kk = 0; kk < 3; ++kk)                 // 32 rows: four groups of eight, 1024 bytes apart
+                    for (int v = 0; v < 2; ++v) {
 #pragma unroll
-                        for (int term = 0; term < 3; ++term)
-                            mma_f8_ts(tm + kColO + 128 * v, p + 32 * kk + 8 * term, b0 + 256 * kk, idesc_o, t > 0 || (kk | term) != 0);
-                    mma_commit(bar_empty + 8 * slot);
-                    if (v == 1) mma_commit(bar_pv);
+                        for (int kk = 0; kk < 3; ++kk)             // 32 rows: four groups of eight, 1024 bytes apart
+#pragma unroll
+                            for (int term = 0; term < 3; ++term)
+                                mma_f8_ts(tm + kColO + 128 * v, p + 32 * kk + 8 * term, (v ? b1 : b0) + 256 * kk, idesc_o, t > 0 || (kk | term) != 0);
+                        mma_commit(bar_empty + 8 * (v ? v_next : v_slot));
+                    }
+                    mma_commit(bar_pv);
                 }
                 __syncwarp();
-                if (++slot == kSlots) slot = 0;
+                v_slot += 5;
+                if (v_slot >= kSlots) v_slot -= kSlots;
             }
-            v_slot += 5;
-            if (v_slot >= kSlots) v_slot -= kSlots;
         }
     } else {
         // ---- softmax: two threads per query row, each with 48 of a tile's cache rows (one alone needs 4000 clocks a tile, more than
         //      the matrix unit's 3100); warp w may touch the TMEM lanes of quarter w % 4 ------------------------------------------
         const int set = (warp - 2) >> 2, quad = warp & 3, r = quad * 32 + lane;
         const uint32_t lanes = tmem + ((uint32_t)(quad * 32) << 16);
-        const unsigned char *records = a.records[source];
+        int g = 0;                                                 // tiles of all items so far
+        for (int item = item0; item < item1; ++item) {
+        const Item &it = a.items[item];
+        const int row0 = it.row0, row1 = it.row1, ntiles = ceil_div(row1 - row0, kR);
+        const unsigned char *records = a.records[it.source];
         const int entry = set == 0 ? r : kR;                       // the row of a tile whose scale this thread fetches, if there is one
         auto row_entry = [&](float s) {                            // (a record of zeros is a row of zeros, and has its weight: 2^-60 will do for its s)
             return (unsigned char)(s == 0.f ? 127 - 60 : __float_as_uint(s) >> 23);
@@ -311,7 +384,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
         };
         const float s0 = row_scale(0), s1 = row_scale(1);
         float s_next = row_scale(2);
-        pdl_wait_prior_grids();
+        if (item == item0) pdl_wait_prior_grids();
         if (set == 0) {
             // the hi terms of the other half's columns to TMEM, 256 bytes a row; rows past the last query are zeros
             const int q_row = it.q_row + r;
@@ -334,12 +407,11 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
         if (entry < kR) { s_table[entry] = row_entry(s0); s_table[kR + entry] = row_entry(s1); }
         named_barrier_sync(1, kSoftmax);
         float m = -INFINITY, l = 0.f, l1 = 0.f;
-        for (int t = 0; t < ntiles; ++t) {
-            const uint32_t col = lanes + kColS + kR * (t & 1);
+        for (int t = 0; t < ntiles; ++t, ++g) {
+            const uint32_t col = lanes + kColS + kR * (g & 1);
             // (after an expired wait every later wait returns at once: the loop runs on, so that the threads keep meeting at the
             // named barrier below, and ends with a result that the status word disowns)
-            mbar_wait(bar_s + 8 * (t & 1), (t >> 1) & 1, &s_abort, a.status);
-            tc_fence_after();
+            warp_wait(bar_s + 8 * (g & 1), (g >> 1) & 1, lane, &s_abort, a.status);
             uint32_t raw[3][16];                                   // three pieces of 16 cache rows
 #pragma unroll
             for (int c = 0; c < 3; ++c) tmem_ld16(col + 48 * set + 16 * c, raw[c]);
@@ -382,8 +454,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
             const bool grow = t == 0 || mx > m + kLazy;
             if (t > 0 && __any_sync(0xffffffffu, grow)) {
                 // the previous tile's P * V has to be through before O is touched; each of the row's threads takes half of the columns
-                mbar_wait(bar_pv, (t - 1) & 1, &s_abort, a.status);
-                tc_fence_after();
+                warp_wait(bar_pv, (g - 1) & 1, lane, &s_abort, a.status);
                 const float f = grow ? ex2(m - mx) : 1.f;
 #pragma unroll 1
                 for (int c = 128 * set; c < 128 * set + 128; c += 64) {
@@ -436,21 +507,21 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
             }
             tmem_wait_st();
             tc_fence_before();
-            mbar_arrive(bar_p + 8 * (t & 1));
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_p + 8 * (g & 1));
         }
         // (both of the last two: the scores of the last tile say that the P * V before these is through, not that the last but one is,
         // and a wait by parity alone would take an older phase for the last)
-        if (ntiles > 1) mbar_wait(bar_pv, (ntiles - 2) & 1, &s_abort, a.status);
-        mbar_wait(bar_pv, (ntiles - 1) & 1, &s_abort, a.status);
-        tc_fence_after();
-        // ---- out: the warp's 32 rows and its set's 128 columns, 64 at a time through its own corner of the ring (every copy into it has
-        //      been used), so that the stores run along the rows ----------------------------------------------------------------------
+        if (ntiles > 1) warp_wait(bar_pv, g & 1, lane, &s_abort, a.status);
+        warp_wait(bar_pv, (g - 1) & 1, lane, &s_abort, a.status);
+        // ---- out: the warp's 32 rows and its set's 128 columns, 64 at a time through its own corner of the queries' place (the last
+        //      scores are through), so that the stores run along the rows ----------------------------------------------------------------------
         named_barrier_sync(1, kSoftmax);
         s_pair[set][r] = l + l1;
         named_barrier_sync(1, kSoftmax);
         if (half == 0 && set == 0 && r < it.n_q)
             *reinterpret_cast<float2 *>(a.ml + 2 * (long)(it.out_row + r)) = make_float2(m, s_pair[0][r] + s_pair[1][r]);
-        float4 *corner = reinterpret_cast<float4 *>(smem + kQBytes + (4 * set + quad) * 8192);        // [32 rows][16 float4], the index XOR-ed with row & 15
+        float4 *corner = reinterpret_cast<float4 *>(smem + (4 * set + quad) * 8192);        // [32 rows][16 float4], the index XOR-ed with row & 15
         for (int c0 = 128 * set; c0 < 128 * set + 128; c0 += 64) {
             uint32_t o[2][32];
             tmem_ld32(lanes + kColO + c0, o[0]);
@@ -470,6 +541,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
                     *reinterpret_cast<float4 *>(a.O + (long)(it.out_row + q) * kKv + 256 * half + c0 + 4 * f) = corner[rr * 16 + (f ^ (rr & 15))];
             }
         }
+        // the next item's queries may come: into the place just used, and (from this warp's threads) into TMEM
+        fence_proxy_async();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar_free);
+        }
     }
     tc_fence_before();
     __syncthreads();
@@ -488,18 +565,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
 constexpr int kMergeGroups = 4, kMergeThreads = kMergeGroups * 128;
 __global__ void __launch_bounds__(kMergeThreads) q8_merge_kernel(const __grid_constant__ MergeArgs a)
 {
-    __shared__ float s_w[2 * kMaxItems], s_l[2 * kMaxItems];
-    __shared__ int s_row[2 * kMaxItems];
+    __shared__ float s_w[2 * kPairs + 2], s_l[2 * kPairs + 2];
+    __shared__ int s_row[2 * kPairs + 2];
     __shared__ float s_red[kMergeThreads / 32];
     __shared__ float4 s_acc[kMergeGroups - 1][128];
     pdl_launch_dependents();
     pdl_wait_prior_grids();
     const int t = blockIdx.x / a.H, h = blockIdx.x - t * a.H, tid = threadIdx.x, group = tid >> 7, x = tid & 127;
-    const int n = a.n_prefix + a.own_n[t];
+    const int q_tile = blockIdx.x / kM, n_prefix = a.prefix_n[q_tile], n = n_prefix + a.own_n[t];
     float mx = -INFINITY;
     for (int i = tid; i < n; i += kMergeThreads) {
         // prefix: item (tile of query rows, part); own: item (sequence, part)
-        const int row = i < a.n_prefix ? (blockIdx.x / kM * a.n_prefix + i) * a.tile_rows + blockIdx.x % kM : a.own_row[t] + (i - a.n_prefix) * a.H + h;
+        const int row = i < n_prefix ? a.prefix_row[q_tile] + i * a.tile_rows + blockIdx.x % kM : a.own_row[t] + (i - n_prefix) * a.H + h;
         const float2 ml = *reinterpret_cast<const float2 *>(a.ml + 2 * (long)row);
         s_row[i] = row;
         s_w[i] = ml.x; s_l[i] = ml.y;
@@ -554,33 +631,35 @@ Layout layout_of(int T, int H, long part_rows)
     return l;
 }
 
-// How the rows are split: tiles of every (query tile or sequence, source) are cut into parts of at most `most` tiles.  Few waves of
-// CTA pairs, each part as long as that allows: a part costs about three tiles beside its own (queries in, partial results out and
-// merged), so one wave is taken unless the units are too uneven for it.
-int parts_of(int tiles, int most) { return (tiles + most - 1) / most; }
-int choose_part(const int *tiles, const int *count, int n)         // `count[i]` units of `tiles[i]` tiles
+// How the work is shared out: the tiles of all units (a tile of query rows over the prefix, a sequence over its own rows), one unit
+// after another, are cut into even shares for the pairs of CTAs; a share's piece of a unit is an item.  An item costs about as much
+// as three tiles beside its own (queries in, pipeline filled and drained, partial results out), so a piece is at least `cost` long:
+// three where the pairs have six tiles and more, one or none where there is less to do than that and latency counts (257 rows:
+// 12 us instead of 18).
+inline int item_cost(long work) { return work >= 6 * kPairs ? 3 : (work >= 2 * kPairs ? 1 : 0); }
+struct Unit { int source, q_row, n_q, tiles, rows, out_rows; };
+// The pairs that shares of `share` need; with `place`, every item is told to it: (unit, first tile, tiles, pair).
+template <typename Place>
+int share_out(const Unit *units, int n, int share, int cost, Place place)
 {
-    constexpr double kPart = 3.0;
-    long work = 0, units = 0, longest = 1;
-    for (int i = 0; i < n; ++i) { work += (long)tiles[i] * count[i]; units += count[i]; longest = std::max<long>(longest, tiles[i]); }
-    int best = (int)longest;
-    double least = 1e300;
-    for (int waves = 1; waves <= kMaxItems / kPairs; ++waves) {
-        if (units > (long)waves * kPairs) continue;
-        long lo = 1, hi = longest;                                 // least part length with at most waves * kPairs parts
-        while (lo < hi) {
-            const long mid = (lo + hi) / 2;
-            long parts = 0;
-            for (int i = 0; i < n; ++i) parts += (long)parts_of(tiles[i], (int)mid) * count[i];
-            if (parts <= (long)waves * kPairs) hi = mid; else lo = mid + 1;
+    int pair = 0, room = share;
+    for (int u = 0; u < n; ++u) {
+        for (int at = 0; at < units[u].tiles;) {
+            const int rest = units[u].tiles - at;
+            int take = room - cost;
+            if (take < rest && take < cost) {                 // not worth a piece: the next pair's
+                if (room < share) { ++pair; room = share; continue; }
+                take = cost;
+            }
+            if (take > rest) take = rest;
+            if (rest - take > 0 && rest - take < cost && rest <= share) take = rest;      // (nor is what would be left)
+            place(u, at, take, pair);
+            at += take;
+            room -= take + cost;
+            if (room <= cost) { ++pair; room = share; }
         }
-        long parts = 0;
-        for (int i = 0; i < n; ++i) parts += (long)parts_of(tiles[i], (int)lo) * count[i];
-        // one wave ends with its longest part; more of them even out, but for about half a part at the end
-        const double cost = waves == 1 ? lo + kPart : (work + kPart * parts) / kPairs + 0.5 * lo;
-        if (cost < least) { least = cost; best = (int)lo; }
     }
-    return best;
+    return pair + (room < share);
 }
 
 bool encode_bytes_map(CUtensorMap *map, const void *ptr, long rows, long pitch, int box_rows)
@@ -646,12 +725,23 @@ int nm_mla_attention_q8(const void *Q, long q_stride, const void *prefix, long p
     if ((uintptr_t)workspace & 15u) return NM_ERR_ALIGNMENT;
 
     // units: the prefix once per tile of query rows, each sequence's own rows once
-    const int total_q = T * H, q_tiles = ceil_div(total_q, kM), prefix_tiles = (int)((prefix_rows + kR - 1) / kR);
-    int tiles[1 + kMaxT], count[1 + kMaxT], n = 0;
-    if (prefix_tiles) { tiles[n] = prefix_tiles; count[n++] = q_tiles; }
+    const int total_q = T * H, q_tiles = ceil_div(total_q, kM), prefix_tiles = (int)((prefix_rows + kR - 1) / kR), tile_rows = std::min(kM, total_q);
+    Unit units[kMaxUnits];
+    int n = 0;
+    long work = 0;
+    if (prefix_tiles)
+        for (int q = 0; q < q_tiles; ++q) units[n++] = Unit{0, q * kM, std::min(kM, total_q - q * kM), prefix_tiles, (int)prefix_rows, tile_rows};
     for (int t = 0; t < T; ++t)
-        if (seq_lens[t]) { tiles[n] = ceil_div(seq_lens[t], kR); count[n++] = 1; }
-    const int most = n ? choose_part(tiles, count, n) : 1;
+        if (seq_lens[t]) units[n++] = Unit{1 + t, t * H, H, ceil_div(seq_lens[t], kR), seq_lens[t], H};
+    for (int u = 0; u < n; ++u) work += units[u].tiles;
+    // the least share that does with the pairs there are
+    const int cost = item_cost(work);
+    long lo = std::max<long>(2 * cost, 1), hi = work + (long)cost * (n + 3) + 1;
+    lo = std::max(lo, (work + (long)cost * n) / kPairs);
+    while (lo < hi) {
+        const long mid = (lo + hi) / 2;
+        if (share_out(units, n, (int)mid, cost, [](int, int, int, int) {}) <= kPairs) hi = mid; else lo = mid + 1;
+    }
 
     cudaStream_t s = (cudaStream_t)stream;
     const Layout lay = layout_of(T, H, (long)kMaxItems * std::min(kM, total_q));
@@ -666,26 +756,20 @@ int nm_mla_attention_q8(const void *Q, long q_stride, const void *prefix, long p
     ma.ml = pa.ml; ma.O = pa.O;
     ma.o_bf16 = static_cast<uint16_t *>(o_bf16); ma.o_f32 = o_f32; ma.lse = lse;
     ma.H = H;
-    ma.tile_rows = std::min(kM, total_q);
-    int items = 0, out_row = 0;
-    auto add_unit = [&](int source, int q_row, int n_q, int unit_tiles, int rows, int row_step) {
-        const int parts = parts_of(unit_tiles, most);
-        for (int p = 0; p < parts; ++p) {
-            Item &i = pa.items[items++];
-            i.q_row = q_row; i.n_q = n_q; i.source = source;
-            i.row0 = (int)((long)unit_tiles * p / parts) * kR;
-            i.row1 = std::min(rows, (int)((long)unit_tiles * (p + 1) / parts) * kR);
-            i.out_row = out_row;
-            out_row += row_step;
+    ma.tile_rows = tile_rows;
+    int items = 0, out_row = 0, pairs = 0, last_unit = -1;
+    share_out(units, n, (int)lo, cost, [&](int u, int at, int tiles, int pair) {
+        const Unit &w = units[u];
+        if (u != last_unit) {
+            last_unit = u;
+            (w.source ? ma.own_row[w.source - 1] : ma.prefix_row[w.q_row / kM]) = out_row;
         }
-        return parts;
-    };
-    if (prefix_tiles)
-        for (int q = 0; q < q_tiles; ++q) ma.n_prefix = add_unit(0, q * kM, std::min(kM, total_q - q * kM), prefix_tiles, (int)prefix_rows, ma.tile_rows);
-    for (int t = 0; t < T; ++t) {
-        ma.own_row[t] = out_row;
-        ma.own_n[t] = seq_lens[t] ? add_unit(1 + t, t * H, H, ceil_div(seq_lens[t], kR), seq_lens[t], H) : 0;
-    }
+        ++(w.source ? ma.own_n[w.source - 1] : ma.prefix_n[w.q_row / kM]);
+        while (pairs <= pair) pa.first[pairs++] = (short)items;
+        pa.items[items++] = Item{w.q_row, w.n_q, w.source, at * kR, std::min(w.rows, (at + tiles) * kR), out_row};
+        out_row += w.out_rows;
+    });
+    pa.first[pairs] = (short)items;
     if (items) {
         pa.status = device_status_ptr();
         if (!encode_bytes_map(&pa.q, pa.q_rows, total_q, kQRow, kM)) return record_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
@@ -696,15 +780,13 @@ int nm_mla_attention_q8(const void *Q, long q_stride, const void *prefix, long p
             pa.records[i] = p;
             if (rows && !encode_bytes_map(&pa.k[i], p, rows, kRec, kR)) return record_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
         }
-        // the longest parts first: the last wave then ends evenly
-        std::sort(pa.items, pa.items + items, [](const Item &x, const Item &y) { return x.row1 - x.row0 > y.row1 - y.row0; });
         static std::atomic<unsigned long long> configured{0};
         cudaError_t e = ensure_dynamic_smem(attn_q8_kernel, kSmemBytes, configured);
         if (e != cudaSuccess) return record_cuda_error(e, "quantised attention kernel attribute");
         q8_prepare_kernel<<<ceil_div(total_q, 4), 128, 0, s>>>(static_cast<const uint16_t *>(Q), q_stride, T, H, ws + lay.q_rows,
                                                               reinterpret_cast<float *>(ws + lay.mult), scale * 1.4426950408889634f);
         e = cudaGetLastError();
-        if (e == cudaSuccess) e = launch_after(attn_q8_kernel, 2 * items, kThreads, kSmemBytes, s, pa);
+        if (e == cudaSuccess) e = launch_after(attn_q8_kernel, 2 * pairs, kThreads, kSmemBytes, s, pa);
         if (e != cudaSuccess) return record_cuda_error(e, "quantised attention launch");
     }
     const cudaError_t e = launch_after(q8_merge_kernel, (unsigned)total_q, kMergeThreads, 0, s, ma);
