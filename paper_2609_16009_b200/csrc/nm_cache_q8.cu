@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
     const uint16_t *x = ckr + (long)t * stride;
     const int vecs = kv / 8;
     float y[kVecs][8];
-    float squares = 0.f;
+    double squares = 0.;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
         const int v = lane + 32 * i;
@@ -46,13 +46,18 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) { y[i][2 * j] = bf_lo(w[j]); y[i][2 * j + 1] = bf_hi(w[j]); }
+        if (gamma) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) squares = fmaf(y[i][j], y[i][j], squares);
+            for (int j = 0; j < 8; ++j) squares += (double)(y[i][j] * y[i][j]);       // (a bf16's square is exact in fp32)
+        }
     }
     if (gamma) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, o);
-        const float r = rsqrtf(squares / (float)kv + eps);
+        // The normaliser in 64 bits, and used as two fp32 terms on the exact products x * gamma: y is off by one rounding only.  A code
+        // next to a tie of e4m3 falls wrongly by whatever the value is off, and a code is worth 2^-4 of it; the row waits for memory anyway.
+        const double rd = 1. / sqrt(squares / (double)kv + (double)eps);
+        const float r = (float)rd, r_low = (float)(rd - (double)r);
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
             const int v = lane + 32 * i;
@@ -60,7 +65,10 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
             if (v < vecs) u = __ldg(reinterpret_cast<const uint4 *>(gamma + 8 * v));
             const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-            for (int j = 0; j < 4; ++j) { y[i][2 * j] = y[i][2 * j] * r * bf_lo(w[j]); y[i][2 * j + 1] = y[i][2 * j + 1] * r * bf_hi(w[j]); }
+            for (int j = 0; j < 4; ++j) {
+                const float a = y[i][2 * j] * bf_lo(w[j]), b = y[i][2 * j + 1] * bf_hi(w[j]);
+                y[i][2 * j] = fmaf(a, r, a * r_low); y[i][2 * j + 1] = fmaf(b, r, b * r_low);
+            }
         }
     }
     float top = 0.f;
