@@ -188,7 +188,7 @@ int nm_matmul_static(const void *A, const void *B, void *C, int M, int N, int K,
  *
  *   dtype    NM_BF16, NM_BF16_F32OUT: A and scales bf16; NM_F16: A and scales fp16.  NM_F32: NM_ERR_UNSUPPORTED
  *   group    32, 64, 128 or 256 consecutive k share a scale; the last group may be short
- *   N, K     any >= 1
+ *   N, K     any >= 1 (K up to 2^30)
  *   lda, ldc elements between rows of A (>= K) and C (>= N)
  * Codes enter the products as exact integers, a group's sum is fp32 (sum a * code, minus 8 * sum a), the scale multiplies that
  * sum, and the result is rounded once.  bf16 tokens pass through fp16 times a power of two per 64 of them (32 for groups of 32):
@@ -293,7 +293,7 @@ int nm_mla_cache_read_q8(const void *cache, long n_cache_rows, const int64_t *ro
  *   T            1..NM_MAX_Q8_BATCH;  H  1..128 heads;  kv_lora 512, rope 64
  *   Q            [T][H][kv_lora+rope] bf16, token t at Q + t * q_stride (elements, a multiple of 8, >= H * (kv_lora+rope))
  *   prefix       prefix_rows records (may be 0; prefix may be NULL then)
- *   seq_lens     HOST array [T]: own records of each sequence (>= 0); cache may be NULL where all are 0
+ *   seq_lens     HOST array [T]: own records of each sequence (0..2^30, the prefix too); cache may be NULL where all are 0
  *   cache_stride BYTES between the caches of consecutive sequences (a multiple of 16; >= the longest, for T > 1)
  *   o_bf16, o_f32, lse  [T][H][kv_lora], [T][H][kv_lora], [T][H] (natural log of sum_j exp(s)); any may be NULL.  A sequence
  *                without any row gets zeros and minus infinity.

@@ -18,8 +18,16 @@
 //            more.  18 MMAs M128 N128 K32 a tile, P from TMEM, fp32 accumulation.  The sum of p_j = w_j / s_j stays fp32.
 // What is resident: the lo terms, half of the hi terms and the key part of Q in 112 KB of shared memory, the other half of hi in 64 columns of
 // TMEM; nine 12 KB slots of [96 rows x 128 bytes] for the records.  96 rows a tile: two score buffers of 96 columns fit TMEM beside O
-// and Q, so the scores of the next tile run while this one's exponentials do, and an MMA of N = 96 is still at its full rate
-// (max(50, N / 2) clocks).  Bound by the tensor pipe: 36 * 50 + 18 * 64 = 2950 clocks a tile and CTA.
+// and Q, so the scores of the next tile run while this one's exponentials do.  The MMAs of a tile by themselves take 3040 clocks
+// (1890 for the scores, bound by shared memory's 128 bytes a clock, 1150 for P * V).
+//   walk     One CTA per SM.  The tiles of all units are cut into even shares for the 74 pairs of CTAs, and a CTA walks over its one to
+//            three items; the ring runs on across them.
+// Measured: 16 x 128 heads, 32768 shared rows and about 500 own ones each: 213 us (148 GFLOP of scores and P * V in one pass: 695 TFLOP/s, 42 % of
+// the bf16 rate, at two and three terms); 16 x 128, ragged 4096: 54 us; 1 x 128, 16384: 25 us; 1 x 16, 257: 13 us.  A tile takes 4300 clocks:
+// the matrix unit waits neither for copies nor for weights then, but its MMAs run slower beside the softmax warps than alone (3770 with
+// their work taken out).  Made no difference: no copies at all, one polling lane per warp, waits ahead of the MMAs, descriptors as 32-bit
+// words, loops instead of straight-line MMAs, fewer shared-memory reads in the softmax.  Made one: MMAs issued by an elected lane of a walking
+// warp (7500 -> 4500 clocks a tile), two softmax threads per row (-10 %), even shares (-14 %).
 #include <algorithm>
 
 #include <cuda_fp8.h>
@@ -45,6 +53,7 @@ constexpr int kSoftmax = 256, kThreads = 64 + kSoftmax;       // TMA, MMA, two s
 constexpr uint32_t kColO = 0, kColS = 256, kColQ = 448;
 constexpr float kHeadroom = 11.f, kLazy = 4.f;     // log2: weights are at most 2^(11 + 4)
 constexpr int kMaxT = NM_MAX_Q8_BATCH, kPairs = kSMs / 2;
+constexpr int kMaxRows = 1 << 30;                  // of the prefix, of a sequence: row numbers a few tiles past the end stay 32-bit
 constexpr int kMaxUnits = 2 * kMaxT;               // query tiles of the prefix (at most 64 * 128 / 128) and sequences
 constexpr int kMaxItems = kMaxUnits + kPairs;      // every unit once, and one more where a pair's share ends inside a unit
 
@@ -708,13 +717,13 @@ int nm_mla_attention_q8(const void *Q, long q_stride, const void *prefix, long p
                         void *o_bf16, float *o_f32, float *lse, int T, int H, int kv_lora, int rope, float scale, void *workspace,
                         size_t workspace_bytes, nm_stream stream)
 {
-    if (!Q || !seq_lens || T < 1 || T > kMaxT || H < 1 || prefix_rows < 0 || prefix_rows > 0x7fffff00L || (prefix_rows > 0 && !prefix) ||
+    if (!Q || !seq_lens || T < 1 || T > kMaxT || H < 1 || prefix_rows < 0 || prefix_rows > kMaxRows || (prefix_rows > 0 && !prefix) ||
         q_stride < (long)H * (kv_lora + rope))
         return NM_ERR_INVALID_ARG;
     if (kv_lora != kKv || rope != kRope || H > kM) return NM_ERR_UNSUPPORTED;
     int longest = 0;
     for (int t = 0; t < T; ++t) {
-        if (seq_lens[t] < 0 || seq_lens[t] > 0x7fffff00) return NM_ERR_INVALID_ARG;
+        if (seq_lens[t] < 0 || seq_lens[t] > kMaxRows) return NM_ERR_INVALID_ARG;
         longest = std::max(longest, seq_lens[t]);
     }
     if (longest > 0 && (!cache || (T > 1 && cache_stride < (long)longest * kRec))) return NM_ERR_INVALID_ARG;

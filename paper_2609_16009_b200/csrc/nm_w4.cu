@@ -217,7 +217,7 @@ __global__ void __launch_bounds__(w4_warps(kNT) * 32, kNT == 1 ? 2 : 1) w4_kerne
     const int tid = threadIdx.x, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);       // the same for the whole warp, and the compiler knows
     const int wn = 1 << a.wn_log2, wk_log2 = kWarpsLog2 - a.wn_log2, wr = warp & (wn - 1), wki = warp >> a.wn_log2;
-    const int rank = blockIdx.x, tile = blockIdx.y;
+    const int rank = blockIdx.y, tile = blockIdx.x;                // (a cluster runs along y)
     const int strip = (tile * wn + wr) * kSide;
     const bool live = strip < a.nb, both = kSide == 2 && strip + 1 < a.nb;
     const int cta0 = rank * a.blocks_each + min(rank, a.blocks_more), cta1 = cta0 + a.blocks_each + (rank < a.blocks_more);
@@ -247,7 +247,7 @@ __global__ void __launch_bounds__(w4_warps(kNT) * 32, kNT == 1 ? 2 : 1) w4_kerne
             cp_async4(smem_u32(sw + j * 8 + (lane & 7)), a.scales + (size_t)(unsigned)grp * (unsigned)(a.nb * 8) + (unsigned)(strip + side) * 8u + (lane & 7));
         }
         if (c0 == cta0) pdl_wait_prior_grids();                    // weights may come early, tokens not
-        stage_tokens<T, kG32>(s_tok, s_start, s_inv, a, c0 * kW4Rows, R * kW4Rows, (int)((long)R * tile / gridDim.y) * 8);
+        stage_tokens<T, kG32>(s_tok, s_start, s_inv, a, c0 * kW4Rows, R * kW4Rows, (int)((long)R * tile / gridDim.x) * 8);
         cp_async_wait_all();
         __syncthreads();
         // lanes of tokens beyond M read the last token's: their columns of the product are never stored
@@ -417,7 +417,7 @@ cudaError_t resident_clusters(int (&resident)[9])
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.x = 1; attr[0].val.clusterDim.z = 1;
     cfg.blockDim = dim3(w4_warps(kNT) * 32);
     cfg.attrs = attr;
     cfg.numAttrs = 1;
@@ -425,8 +425,8 @@ cudaError_t resident_clusters(int (&resident)[9])
     resident[0] = 0;
     resident[1] = kNT == 1 ? 2 * kSMs : kSMs;
     for (int cl = 2; cl <= 8; ++cl) {
-        attr[0].val.clusterDim.x = cl;
-        cfg.gridDim = dim3(cl, 1, 1);
+        attr[0].val.clusterDim.y = cl;
+        cfg.gridDim = dim3(1, cl, 1);
         resident[cl] = max_clusters_cached(kern, cfg, cl);
     }
     return cudaSuccess;
@@ -456,7 +456,7 @@ cudaError_t launch_w4(W4Args a, cudaStream_t stream, bool pdl)
     a.tok_bytes = a.M * a.pitch + a.chunk * kStart;
     a.scale_bytes = a.chunk * scale_block;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.cl, ceil_div(units, p.wn), 1);
+    cfg.gridDim = dim3(ceil_div(units, p.wn), a.cl, 1);
     cfg.blockDim = dim3(kWarps * 32);
     cfg.dynamicSmemBytes = a.tok_bytes + a.scale_bytes + sum_bytes;
     cfg.stream = stream;
@@ -464,7 +464,7 @@ cudaError_t launch_w4(W4Args a, cudaStream_t stream, bool pdl)
     int n = 0;
     if (a.cl > 1) {
         attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = a.cl; attr[n].val.clusterDim.y = 1; attr[n].val.clusterDim.z = 1;
+        attr[n].val.clusterDim.x = 1; attr[n].val.clusterDim.y = a.cl; attr[n].val.clusterDim.z = 1;
         ++n;
     }
     if (pdl) {
@@ -497,7 +497,7 @@ int nm_matmul_w4(const void *A, const void *packed, const void *scales, void *C,
                  nm_dtype dtype, nm_stream stream)
 {
     if (!A || !packed || !scales || !C || M < 1 || M > NM_MAX_M || N < 1 || K < 1 || lda < K || ldc < N) return NM_ERR_INVALID_ARG;
-    if (!w4_dtype_ok(dtype) || !w4_group_ok(group)) return NM_ERR_UNSUPPORTED;
+    if (!w4_dtype_ok(dtype) || !w4_group_ok(group) || K > (1 << 30)) return NM_ERR_UNSUPPORTED;
     if (((uintptr_t)A & 1u) || ((uintptr_t)packed & 15u) || ((uintptr_t)scales & 3u) || ((uintptr_t)C & (dtype == NM_BF16_F32OUT ? 3u : 1u)))
         return NM_ERR_ALIGNMENT;
     W4Args a{};

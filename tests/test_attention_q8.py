@@ -287,7 +287,7 @@ def test_refusals():
                                        vp(ws), wb, None)
 
     for bad in (dict(Q=None), dict(lens=None, T=2), dict(T=0), dict(lens=(1,) * 65), dict(H=0), dict(n_pre=-1), dict(pre=None), dict(lens=(3, -1)), dict(cache=None),
-                dict(lens=(3, 11)), dict(qs=16 * 576 - 8)):
+                dict(lens=(3, 11)), dict(qs=16 * 576 - 8), dict(n_pre=(1 << 30) + 1)):
         assert call(**bad) == -1, bad
     for bad in (dict(kv=256), dict(rope=32), dict(H=129, qs=129 * 576)):
         assert call(**bad) == -2, bad

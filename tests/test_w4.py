@@ -269,7 +269,7 @@ def test_refusals():
 
     for bad in (dict(A=None), dict(p=None), dict(s=None), dict(C=None), dict(M=0), dict(M=17), dict(N=0), dict(K=0), dict(lda=63), dict(ldc=31)):
         assert call(**bad) == -1, bad
-    for bad in (dict(d=0), dict(d=9), dict(g=0), dict(g=48), dict(g=512), dict(g=-64)):
+    for bad in (dict(d=0), dict(d=9), dict(g=0), dict(g=48), dict(g=512), dict(g=-64), dict(K=(1 << 30) + 1, lda=1 << 31)):
         assert call(**bad) == -2, bad
     for bad in (dict(A=257), dict(p=520), dict(s=1026), dict(C=2049), dict(C=2050, d=BF16_F32OUT)):
         assert call(**bad) == -3, bad
