@@ -1,9 +1,13 @@
 // Weights to 4 bits and back (storage: nm_w4.cuh).  Done once when weights are loaded; both are one pass over the weights.
 //   scale = round16(max |w| of the group / 7), code = clamp(round(w / scale), -8, 7) + 8 (8 where the scale is 0),
 //   back = round16((code - 8) * scale)
-// A CTA takes 64 columns x 256 k through shared memory, laid out there as it is in memory (k contiguous or columns contiguous), so
-// that either layout of the weights is read and written in 16-byte vectors, runs of 128 bytes and more, whichever way the codes
-// run.  Bound by HBM: 2 bytes in and half a byte out per weight, and the reverse.
+// A CTA takes 64 columns x 128 k (256 for groups of that many) through shared memory, laid out there as it is in memory (k
+// contiguous or columns contiguous), so that either layout of the weights is read and written in 16-byte vectors, runs of 128
+// bytes and more, whichever way the codes run.
+// Bound by HBM: 2 bytes in and half a byte out per weight, and the reverse; 45 us either way for 16384 x 7168 weights.  Measured
+// there (bf16): columns in groups of 64 are quantised in 77 us and brought back in 47, rows in 82 and 54, rows in groups of 256 in 79
+// and 56.  Pieces of 64 k for the groups up to 64 took 101 and 60.  What the quantisation spends above the floor are instructions,
+// some ten per weight: a division each and conversions to integers and back took 145 us.
 #include <type_traits>
 
 #include "nm_w4.cuh"
@@ -12,21 +16,49 @@ namespace nm {
 
 namespace {
 
-constexpr int kCols = 64, kRows = 256, kThreads = 256;             // a CTA's tile; kRows is a multiple of every group
+constexpr int kCols = 64, kThreads = 256;          // columns of a CTA's tile; its k are kRows, a multiple of the group
 
 template <typename T> __device__ __forceinline__ float widen16(uint16_t v) { T x; x.bits = v; return Elem<T>::widen(x); }
 
-// The tile in shared memory.  Pitches in elements: 264 puts the 16-byte vectors of eight columns into different banks, 66 the
-// 2-byte accesses of lanes (g, t) at (column g, k = 8 t).
-template <bool kColMajor> struct Tile {
+// Two elements at a time.  The largest of magnitudes passes over NaN, as fmaxf does.
+template <typename T> __device__ __forceinline__ uint32_t max_abs2(uint32_t a, uint32_t b)
+{
+    b &= 0x7fff7fffu;
+    if constexpr (std::is_same_v<T, f16_t>) {
+        const __half2 m = __hmax2(*reinterpret_cast<const __half2 *>(&a), *reinterpret_cast<const __half2 *>(&b));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    } else {
+        const __nv_bfloat162 m = __hmax2(*reinterpret_cast<const __nv_bfloat162 *>(&a), *reinterpret_cast<const __nv_bfloat162 *>(&b));
+        return *reinterpret_cast<const uint32_t *>(&m);
+    }
+}
+// (code - 8) * scale of the codes in the low nibbles of both halves: the code is put behind the leading bits of 1024 (fp16) or 128
+// (bf16), where a step is 1, so that the difference is exact; the product is rounded once.
+template <typename T> __device__ __forceinline__ uint32_t decode2(uint32_t codes, uint32_t scale2)
+{
+    codes &= 0x000f000fu;
+    if constexpr (std::is_same_v<T, f16_t>) {
+        const uint32_t u = codes | 0x64006400u;
+        const __half2 r = __hmul2_rn(__hsub2(*reinterpret_cast<const __half2 *>(&u), __float2half2_rn(1032.f)), *reinterpret_cast<const __half2 *>(&scale2));
+        return *reinterpret_cast<const uint32_t *>(&r);
+    } else {
+        const uint32_t u = codes | 0x43004300u;
+        const __nv_bfloat162 r = __hmul2_rn(__hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&u), __float2bfloat162_rn(136.f)), *reinterpret_cast<const __nv_bfloat162 *>(&scale2));
+        return *reinterpret_cast<const uint32_t *>(&r);
+    }
+}
+
+// The tile in shared memory.  Pitches in elements: 8 more than the k puts the 16-byte vectors of eight columns into different banks,
+// 66 the 2-byte accesses of lanes (g, t) at (column g, k = 8 t).
+template <bool kColMajor, int kRows> struct Tile {
     static constexpr int kPitch = kColMajor ? kRows + 8 : kCols + 2;
     uint16_t v[(kColMajor ? kCols : kRows) * kPitch];
     __device__ __forceinline__ uint16_t &at(int r, int c) { return v[kColMajor ? c * kPitch + r : r * kPitch + c]; }
 };
 
 // vec: every run of eight elements along the contiguous dimension starts on 16 bytes and ends inside the matrix
-template <bool kColMajor>
-__device__ __forceinline__ void load_tile(Tile<kColMajor> &s, const uint16_t *__restrict__ B, int n0, int k0, int N, int K, bool vec)
+template <bool kColMajor, int kRows>
+__device__ __forceinline__ void load_tile(Tile<kColMajor, kRows> &s, const uint16_t *__restrict__ B, int n0, int k0, int N, int K, bool vec)
 {
     constexpr int kInner = kColMajor ? kRows : kCols;
     if (vec) {
@@ -48,8 +80,8 @@ __device__ __forceinline__ void load_tile(Tile<kColMajor> &s, const uint16_t *__
         }
     }
 }
-template <bool kColMajor>
-__device__ __forceinline__ void store_tile(Tile<kColMajor> &s, uint16_t *__restrict__ B, int n0, int k0, int N, int K, bool vec)
+template <bool kColMajor, int kRows>
+__device__ __forceinline__ void store_tile(Tile<kColMajor, kRows> &s, uint16_t *__restrict__ B, int n0, int k0, int N, int K, bool vec)
 {
     constexpr int kInner = kColMajor ? kRows : kCols;
     if (vec) {
@@ -72,32 +104,33 @@ __device__ __forceinline__ void store_tile(Tile<kColMajor> &s, uint16_t *__restr
     }
 }
 
-template <typename T, bool kColMajor>
+template <typename T, bool kColMajor, int kRows>
 __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const uint16_t *__restrict__ B, uint4 *__restrict__ packed, uint16_t *__restrict__ scales, int N,
                                                                int K, int nb, int kb, int group, int vec)
 {
-    __shared__ __align__(16) Tile<kColMajor> s_w;
+    __shared__ __align__(16) Tile<kColMajor, kRows> s_w;
     __shared__ float s_max[kRows / 32][kCols + 1];                 // per 32 k: the largest, then the rounded scale of its group
     const int tid = threadIdx.x, n0 = blockIdx.y * kCols, k0 = blockIdx.x * kRows;
-    load_tile<kColMajor>(s_w, B, n0, k0, N, K, vec != 0);
+    load_tile<kColMajor, kRows>(s_w, B, n0, k0, N, K, vec != 0);
     __syncthreads();
-    for (int i = tid; i < kCols * (kRows / 32); i += kThreads) {
-        // (columns along the lanes where they are contiguous, 32-k pieces of a column otherwise)
-        const int c = kColMajor ? i / (kRows / 32) : i % kCols, q = kColMajor ? i % (kRows / 32) : i / kCols;
-        float m = 0.f;
+    for (int i = tid; i < (kColMajor ? kCols : kCols / 2) * (kRows / 32); i += kThreads) {
+        // (pairs of columns along the lanes where columns are contiguous, 32-k pieces of a column otherwise)
+        uint32_t m = 0u;
         if constexpr (kColMajor) {
+            const int c = i / (kRows / 32), q = i % (kRows / 32);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const uint4 u = *reinterpret_cast<const uint4 *>(&s_w.at(32 * q + 8 * r, c));
-                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) m = fmaxf(m, fmaxf(fabsf(widen16<T>((uint16_t)w[j])), fabsf(widen16<T>((uint16_t)(w[j] >> 16)))));
+                m = max_abs2<T>(max_abs2<T>(max_abs2<T>(max_abs2<T>(m, u.x), u.y), u.z), u.w);
             }
+            s_max[q][c] = fmaxf(widen16<T>((uint16_t)m), widen16<T>((uint16_t)(m >> 16)));
         } else {
+            const int c = 2 * (i % (kCols / 2)), q = i / (kCols / 2);
 #pragma unroll 8
-            for (int r = 0; r < 32; ++r) m = fmaxf(m, fabsf(widen16<T>(s_w.at(32 * q + r, c))));
+            for (int r = 0; r < 32; ++r) m = max_abs2<T>(m, *reinterpret_cast<const uint32_t *>(&s_w.at(32 * q + r, c)));
+            s_max[q][c] = widen16<T>((uint16_t)m);
+            s_max[q][c + 1] = widen16<T>((uint16_t)(m >> 16));
         }
-        s_max[q][c] = m;
     }
     __syncthreads();
     const int per = group / 32, groups = kRows / group;
@@ -116,7 +149,10 @@ __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const uint16_t *_
         const int lane = i % 32, blk = (i / 32) % (kRows / kW4Rows), st = i / (32 * (kRows / kW4Rows)), g = lane >> 2, t = lane & 3;
         const int strip = n0 / kW4Cols + st, kblk = k0 / kW4Rows + blk;
         if (strip >= nb || kblk >= kb) continue;
-        uint32_t w[4] = {0u, 0u, 0u, 0u};
+        // A quotient is rounded by adding 1.5 * 2^23 + 8, which leaves the code at the end of the sum's bits; the leading bits of the
+        // eight sums of a word are taken off beforehand, all arithmetic being modulo 2^32.
+        constexpr uint32_t kStart = 0u - 0x4b400000u * 0x11111111u;
+        uint32_t w[4] = {kStart, kStart, kStart, kStart};
 #pragma unroll
         for (int hi = 0; hi < 2; ++hi) {
             const int c = st * kW4Cols + g + 8 * hi;
@@ -124,11 +160,29 @@ __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const uint16_t *_
             for (int h = 0; h < 2; ++h) {                          // words 2 h and 2 h + 1: eight consecutive k from 32 h + 8 t on
                 const int r0 = blk * kW4Rows + 32 * h + 8 * t;
                 const float sc = s_max[r0 / 32][c];
+                float v[8];
+                if constexpr (kColMajor) Elem<T>::unpack(*reinterpret_cast<const uint4 *>(&s_w.at(r0, c)), v);
+                else
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) v[x] = widen16<T>(s_w.at(r0 + x, c));
+                // w / sc with one reciprocal for eight weights: a product, its exact error, the corrected quotient.  Quotients of two
+                // numbers of a 16-bit type are ties or at least 2^-13 of themselves away from one, and a tie is met exactly, so the
+                // code is that of the rounded quotient.  (At the ends of fp32's range the reciprocal or the error would leave it.)
+                if (sc > 0x1p-60f && sc < 0x1p60f) {
+                    const float inv = 1.f / sc;
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) {
+                        const float first = v[x] * inv;
+                        v[x] = fmaf(fmaf(-first, sc, v[x]), inv, first);
+                    }
+                } else {
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) v[x] = sc > 0.f ? __fdiv_rn(v[x], sc) : 0.f;
+                }
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {                      // k = r0 + 4 (j & 1) + 2 (b & 1) + (b >> 1)
                     const int j = 2 * h + (x >> 2), b = ((x >> 1) & 1) + 2 * (x & 1);
-                    const float q = sc > 0.f ? fminf(fmaxf(rintf(__fdiv_rn(widen16<T>(s_w.at(r0 + x, c)), sc)), -8.f), 7.f) : 0.f;
-                    w[j] |= (uint32_t)((int)q + 8) << (8 * b + 4 * hi);
+                    w[j] += __float_as_uint(fminf(fmaxf(v[x], -8.f), 7.f) + 12582920.f) << (8 * b + 4 * hi);
                 }
             }
         }
@@ -136,11 +190,11 @@ __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const uint16_t *_
     }
 }
 
-template <typename T, bool kColMajor>
+template <typename T, bool kColMajor, int kRows>
 __global__ void __launch_bounds__(kThreads) w4_dequantize_kernel(const uint4 *__restrict__ packed, const uint16_t *__restrict__ scales, uint16_t *__restrict__ B,
                                                                  int N, int K, int nb, int kb, int group, int vec)
 {
-    __shared__ __align__(16) Tile<kColMajor> s_w;
+    __shared__ __align__(16) Tile<kColMajor, kRows> s_w;
     const int tid = threadIdx.x, n0 = blockIdx.y * kCols, k0 = blockIdx.x * kRows;
     for (int i = tid; i < (kCols / kW4Cols) * (kRows / kW4Rows) * 32; i += kThreads) {
         const int lane = i % 32, blk = (i / 32) % (kRows / kW4Rows), st = i / (32 * (kRows / kW4Rows)), g = lane >> 2, t = lane & 3;
@@ -154,24 +208,20 @@ __global__ void __launch_bounds__(kThreads) w4_dequantize_kernel(const uint4 *__
             const uint32_t pair = *reinterpret_cast<const uint32_t *>(scales + ((long)(k32 < K ? k32 / group : 0) * nb + strip) * kW4Cols + 2 * g);
 #pragma unroll
             for (int hi = 0; hi < 2; ++hi) {
-                const float sc = widen16<T>((uint16_t)(hi ? pair >> 16 : pair));
+                const uint32_t sc = __byte_perm(pair, 0u, hi ? 0x3232 : 0x1010);
                 const int c = st * kW4Cols + g + 8 * hi;
-                uint32_t o[8];
+                uint32_t o[4];                                     // pairs of k: bytes b and b + 2 of a word
 #pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    const int j = 2 * h + (x >> 2), b = ((x >> 1) & 1) + 2 * (x & 1);
-                    o[x] = round_out<T>((float)((int)((w[j] >> (8 * b + 4 * hi)) & 15u) - 8) * sc).bits;
-                }
-                if constexpr (kColMajor)
-                    *reinterpret_cast<uint4 *>(&s_w.at(r0, c)) = make_uint4(o[0] | (o[1] << 16), o[2] | (o[3] << 16), o[4] | (o[5] << 16), o[6] | (o[7] << 16));
+                for (int x = 0; x < 4; ++x) o[x] = decode2<T>(w[2 * h + (x >> 1)] >> (8 * (x & 1) + 4 * hi), sc);
+                if constexpr (kColMajor) *reinterpret_cast<uint4 *>(&s_w.at(r0, c)) = make_uint4(o[0], o[1], o[2], o[3]);
                 else
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) s_w.at(r0 + x, c) = (uint16_t)o[x];
+                    for (int x = 0; x < 8; ++x) s_w.at(r0 + x, c) = (uint16_t)(o[x / 2] >> (16 * (x & 1)));
             }
         }
     }
     __syncthreads();
-    store_tile<kColMajor>(s_w, B, n0, k0, N, K, vec != 0);
+    store_tile<kColMajor, kRows>(s_w, B, n0, k0, N, K, vec != 0);
 }
 
 // whether the contiguous dimension runs in whole, aligned 16-byte vectors
@@ -212,12 +262,18 @@ int nm_w4_quantize(const void *B, void *packed, void *scales, int N, int K, int 
     const int rc = check_pack(B, packed, scales, N, K, group, dtype, layout_B);
     if (rc != NM_OK) return rc;
     const int nb = (int)(((long)N + kW4Cols - 1) / kW4Cols), kb = (int)(((long)K + kW4Rows - 1) / kW4Rows);
-    const dim3 grid((unsigned)(((long)K + kRows - 1) / kRows), (unsigned)(((long)N + kCols - 1) / kCols));
-    auto go = [&](auto kern) {
+    auto go = [&](auto rows, auto kern) {
+        const dim3 grid((unsigned)(((long)K + rows - 1) / rows), (unsigned)(((long)N + kCols - 1) / kCols));
         kern<<<grid, kThreads, 0, (cudaStream_t)stream>>>(static_cast<const uint16_t *>(B), static_cast<uint4 *>(packed), static_cast<uint16_t *>(scales), N, K, nb, kb, group, (int)pack_vec(B, N, K, layout_B));
     };
-    if (dtype == NM_F16) layout_B == NM_COL_MAJOR ? go(w4_quantize_kernel<f16_t, true>) : go(w4_quantize_kernel<f16_t, false>);
-    else layout_B == NM_COL_MAJOR ? go(w4_quantize_kernel<bf16_t, true>) : go(w4_quantize_kernel<bf16_t, false>);
+    auto by_rows = [&](auto t, auto col) {
+        using T = decltype(t);
+        constexpr bool kCol = decltype(col)::value;
+        if (group <= 128) go(128, w4_quantize_kernel<T, kCol, 128>);
+        else go(256, w4_quantize_kernel<T, kCol, 256>);
+    };
+    if (dtype == NM_F16) layout_B == NM_COL_MAJOR ? by_rows(f16_t{}, std::true_type{}) : by_rows(f16_t{}, std::false_type{});
+    else layout_B == NM_COL_MAJOR ? by_rows(bf16_t{}, std::true_type{}) : by_rows(bf16_t{}, std::false_type{});
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? NM_OK : record_cuda_error(e, "4-bit quantisation launch");
 }
@@ -227,12 +283,18 @@ int nm_w4_dequantize(const void *packed, const void *scales, void *B, int N, int
     const int rc = check_pack(B, packed, scales, N, K, group, dtype, layout_B);
     if (rc != NM_OK) return rc;
     const int nb = (int)(((long)N + kW4Cols - 1) / kW4Cols), kb = (int)(((long)K + kW4Rows - 1) / kW4Rows);
-    const dim3 grid((unsigned)(((long)K + kRows - 1) / kRows), (unsigned)(((long)N + kCols - 1) / kCols));
-    auto go = [&](auto kern) {
+    auto go = [&](auto rows, auto kern) {
+        const dim3 grid((unsigned)(((long)K + rows - 1) / rows), (unsigned)(((long)N + kCols - 1) / kCols));
         kern<<<grid, kThreads, 0, (cudaStream_t)stream>>>(static_cast<const uint4 *>(packed), static_cast<const uint16_t *>(scales), static_cast<uint16_t *>(B), N, K, nb, kb, group, (int)pack_vec(B, N, K, layout_B));
     };
-    if (dtype == NM_F16) layout_B == NM_COL_MAJOR ? go(w4_dequantize_kernel<f16_t, true>) : go(w4_dequantize_kernel<f16_t, false>);
-    else layout_B == NM_COL_MAJOR ? go(w4_dequantize_kernel<bf16_t, true>) : go(w4_dequantize_kernel<bf16_t, false>);
+    auto by_rows = [&](auto t, auto col) {
+        using T = decltype(t);
+        constexpr bool kCol = decltype(col)::value;
+        if (group <= 128) go(128, w4_dequantize_kernel<T, kCol, 128>);
+        else go(256, w4_dequantize_kernel<T, kCol, 256>);
+    };
+    if (dtype == NM_F16) layout_B == NM_COL_MAJOR ? by_rows(f16_t{}, std::true_type{}) : by_rows(f16_t{}, std::false_type{});
+    else layout_B == NM_COL_MAJOR ? by_rows(bf16_t{}, std::true_type{}) : by_rows(bf16_t{}, std::false_type{});
     const cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? NM_OK : record_cuda_error(e, "4-bit dequantisation launch");
 }
