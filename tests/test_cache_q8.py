@@ -116,6 +116,24 @@ def test_write_at_the_ends_of_the_range():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("power", [-12, 70, 100])
+def test_write_normalises_rows_of_any_size(power):
+    """Squares beyond fp32's range belong to the norm all the same."""
+    import paper_2609_16009_b200 as nm
+    kv, rope = 512, 64
+    x, gamma, _ = rows_in(3, kv, rope, 11, std=2.0 ** power)
+    x[1, 5] = 0.0
+    cache = torch.zeros(3, nm.nm_mla_q8_row_bytes(kv, rope), dtype=torch.uint8, device="cuda")
+    nm.nm_mla_cache_write_q8(x.cuda(), gamma.cuda(), None, None, cache, 3, 3, kv, rope, EPS)
+    y, _ = reference(x.double().numpy(), gamma.double().numpy(), None, kv, rope)
+    codes, _, s = records(cache.cpu().numpy(), kv, rope)
+    assert (np.abs(y).max(1) <= 448 * s[:, 0] * (1 + 2.0 ** -20)).all()
+    want = np.clip(y / s, -448, 448)
+    # half a step of e4m3: 2^-4 of the value, 2^-10 below its normal range; fp32 arithmetic before it 2^-20
+    assert np.all(np.abs(codes - want) <= np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10) * (1 + 2.0 ** -15))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("n,kv,rope,stride", [(1, 512, 64, 576), (130, 512, 64, 584), (9, 16, 8, 24), (5, 1024, 256, 1280), (6, 528, 0, 536)])
 def test_read(n, kv, rope, stride):
     import paper_2609_16009_b200 as nm
