@@ -213,7 +213,7 @@ size_t nm_w4_scale_count(int N, int K, int group);        /* 16-bit elements */
 /*
  * Dense weights (B: K x N in NM_ROW_MAJOR or NM_COL_MAJOR, bf16 or fp16 by dtype) to 4 bits, and back.  Per column and group:
  *   scale = round16(max |w| / 7),  code = clamp(round(w / scale), -8, 7) + 8  (8 where scale is 0),  back = round16((code - 8) * scale)
- * round to nearest even throughout; a NaN weight becomes code 0.  Columns and k beyond N and K are stored as zero weights.
+ * N up to 64 * 65535, K up to 2^30.  Round to nearest even throughout; a NaN weight becomes code 0.  Columns and k beyond N and K are stored as zero weights.
  */
 int nm_w4_quantize(const void *B, void *packed, void *scales, int N, int K, int group, nm_dtype dtype, nm_layout layout_B,
                    nm_stream stream);
@@ -271,11 +271,11 @@ int nm_mla_attention_combine(const void *Q, const void *kv_cache, void *o_bf16, 
  *   latent  RMSNorm(x[:kv_lora]; gamma, eps), gamma [kv_lora] bf16; NULL: taken as it is
  *   key     RoPE(x[kv_lora:]) by cos_sin [T][rope] fp32 (rows of nm_rope_table); NULL: taken as it is
  *   then quantised - each value rounded once, from fp32 - and stored as record rows[t] (device, 64-bit) of the cache.  A rows[t] outside
- *   [0, n_cache_rows) writes nothing (padding tokens); rows NULL means row t.  The rows named in one call must differ from
+ *   [0, n_cache_rows) writes nothing (padding tokens); rows NULL means row t.  T is at most 2^30.  The rows named in one call must differ from
  *   each other: what a row named twice holds afterwards is unspecified.  A NaN stays a NaN, an infinite or too large
  *   latent value becomes +-448 s.
  * nm_mla_cache_read_q8: records rows[i] (NULL: i) as bf16 rows out + i * out_stride (elements, a multiple of 8): (latent | key), exact but
- *   for the range of bf16; zeros where rows[i] is outside [0, n_cache_rows).  The same row may be read any number of times.
+ *   for the range of bf16; zeros where rows[i] is outside [0, n_cache_rows).  n is at most 2^30.  The same row may be read any number of times.
  * ckr, gamma, cache and out are 16-byte aligned, cos_sin and rows 8-byte.  Both honour nm_set_programmatic_launch.
  */
 size_t nm_mla_q8_row_bytes(int kv_lora, int rope);
@@ -293,13 +293,14 @@ int nm_mla_cache_read_q8(const void *cache, long n_cache_rows, const int64_t *ro
  *   T            1..NM_MAX_Q8_BATCH;  H  1..128 heads;  kv_lora 512, rope 64
  *   Q            [T][H][kv_lora+rope] bf16, token t at Q + t * q_stride (elements, a multiple of 8, >= H * (kv_lora+rope))
  *   prefix       prefix_rows records (may be 0; prefix may be NULL then)
- *   seq_lens     HOST array [T]: own records of each sequence (0..2^30, the prefix too); cache may be NULL where all are 0
+ *   seq_lens     HOST array [T], read during the call (a captured call keeps the lengths): own records of each sequence
+ *                (0..2^30, the prefix too); cache may be NULL where all are 0
  *   cache_stride BYTES between the caches of consecutive sequences (a multiple of 16; >= the longest, for T > 1)
  *   o_bf16, o_f32, lse  [T][H][kv_lora], [T][H][kv_lora], [T][H] (natural log of sum_j exp(s)); any may be NULL.  A sequence
  *                without any row gets zeros and minus infinity.
  * Nothing behind the rows named here is read into a result, whatever it holds.  A head whose query holds an infinity or a NaN, and a
- * sequence (or all, in the prefix) with a NaN record, gets NaN.  Weights p keep at least eight bits, whatever their size down to 2^-20
- * of the largest; sums are fp32.  Equal calls give equal bits.
+ * sequence (or all, in the prefix) with a NaN record, gets NaN.  A row's weight (p times its scale) keeps at least eight bits,
+ * whatever its size down to 2^-20 of the largest; sums are fp32.  Equal calls give equal bits.
  * Q, prefix, cache, o_f32 and the workspace are 16-byte aligned, o_bf16 8-byte.  Workspace:
  * nm_mla_attention_q8_workspace_bytes, whatever the lengths; nothing in it has to be cleared, and it keeps nothing from one call for the
  * next; calls that overlap on the GPU (two captured graphs among them) need workspaces of their own.

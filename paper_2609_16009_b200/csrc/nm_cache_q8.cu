@@ -16,6 +16,7 @@ namespace nm {
 namespace {
 
 constexpr int kWarpsQ8 = 4;
+constexpr int kMaxCall = 1 << 30;                  // rows of a call: their numbers stay an int in a CTA's last warp too
 
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -184,7 +185,7 @@ size_t nm_mla_q8_row_bytes(int kv_lora, int rope) { return q8_dims_ok(kv_lora, r
 int nm_mla_cache_write_q8(const void *ckr, long ckr_stride, const void *gamma, const float *cos_sin, const int64_t *rows, void *cache,
                           long n_cache_rows, int T, int kv_lora, int rope, float eps, nm_stream stream)
 {
-    if (!ckr || !cache || T < 1 || n_cache_rows < 1 || ckr_stride < (long)kv_lora + rope) return NM_ERR_INVALID_ARG;
+    if (!ckr || !cache || T < 1 || T > kMaxCall || n_cache_rows < 1 || ckr_stride < (long)kv_lora + rope) return NM_ERR_INVALID_ARG;
     if (!q8_dims_ok(kv_lora, rope)) return NM_ERR_UNSUPPORTED;
     if (((uintptr_t)ckr & 15u) || ckr_stride % 8 || ((uintptr_t)cache & 15u) || ((uintptr_t)gamma & 15u) || ((uintptr_t)cos_sin & 7u) || ((uintptr_t)rows & 7u))
         return NM_ERR_ALIGNMENT;
@@ -199,7 +200,7 @@ int nm_mla_cache_write_q8(const void *ckr, long ckr_stride, const void *gamma, c
 int nm_mla_cache_read_q8(const void *cache, long n_cache_rows, const int64_t *rows, void *out, long out_stride, int n, int kv_lora, int rope,
                          nm_stream stream)
 {
-    if (!cache || !out || n < 1 || n_cache_rows < 1 || out_stride < (long)kv_lora + rope) return NM_ERR_INVALID_ARG;
+    if (!cache || !out || n < 1 || n > kMaxCall || n_cache_rows < 1 || out_stride < (long)kv_lora + rope) return NM_ERR_INVALID_ARG;
     if (!q8_dims_ok(kv_lora, rope)) return NM_ERR_UNSUPPORTED;
     if (((uintptr_t)cache & 15u) || ((uintptr_t)out & 15u) || out_stride % 8 || ((uintptr_t)rows & 7u)) return NM_ERR_ALIGNMENT;
     const cudaError_t e = launch_rows(cache_read_q8_kernel, n, (cudaStream_t)stream, static_cast<const unsigned char *>(cache), n_cache_rows, rows,

@@ -232,7 +232,7 @@ int check_pack(const void *B, const void *packed, const void *scales, int N, int
     if (!B || !packed || !scales || N < 1 || K < 1) return NM_ERR_INVALID_ARG;
     if (!w4_dtype_ok(dtype) || !w4_group_ok(group) || (layout != NM_ROW_MAJOR && layout != NM_COL_MAJOR)) return NM_ERR_UNSUPPORTED;
     if (((uintptr_t)B & 1u) || ((uintptr_t)packed & 15u) || ((uintptr_t)scales & 3u)) return NM_ERR_ALIGNMENT;
-    if (((long)N + kCols - 1) / kCols > 65535) return NM_ERR_UNSUPPORTED;
+    if (((long)N + kCols - 1) / kCols > 65535 || K > (1 << 30)) return NM_ERR_UNSUPPORTED;       // the grid; k past the end of a tile stays an int
     return NM_OK;
 }
 

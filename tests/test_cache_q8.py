@@ -197,14 +197,14 @@ def test_refusals():
     def read(cache=256, n_rows=8, rows=512, out=1024, stride=576, n=2, kv=512, rope=64):
         return lib.nm_mla_cache_read_q8(vp(cache), n_rows, vp(rows), vp(out), stride, n, kv, rope, None)
 
-    for bad in (dict(x=None), dict(cache=None), dict(T=0), dict(n=0), dict(stride=575)):
+    for bad in (dict(x=None), dict(cache=None), dict(T=0), dict(T=(1 << 30) + 1), dict(n=0), dict(stride=575)):
         assert write(**bad) == -1, bad
     for bad in (dict(kv=8, rope=64), dict(kv=520, stride=584), dict(kv=1040, stride=4096), dict(rope=12), dict(rope=-8), dict(rope=264, stride=4096)):
         assert write(**bad) == -2, bad
         assert nm.nm_mla_q8_row_bytes(bad.get("kv", 512), bad.get("rope", 64)) == 0
     for bad in (dict(x=264), dict(stride=580), dict(cache=4104), dict(gamma=520), dict(cs=1028), dict(rows=2052)):
         assert write(**bad) == -3, bad
-    for bad in (dict(cache=None), dict(out=None), dict(n=0), dict(n_rows=0), dict(stride=575)):
+    for bad in (dict(cache=None), dict(out=None), dict(n=0), dict(n=(1 << 30) + 1), dict(n_rows=0), dict(stride=575)):
         assert read(**bad) == -1, bad
     for bad in (dict(kv=500), dict(rope=4)):
         assert read(**bad) == -2, bad

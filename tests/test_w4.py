@@ -281,6 +281,8 @@ def test_refusals():
         assert fn(vp(256), vp(512), vp(1024), 16, 64, 64, 0, ROW, None) == -2
         assert fn(vp(256), vp(512), vp(1024), 16, 64, 100, BF16, ROW, None) == -2
         assert fn(vp(256), vp(512), vp(1024), 16, 64, 64, BF16, 2, None) == -2
+        assert fn(vp(256), vp(512), vp(1024), 64 * 65535 + 1, 64, 64, BF16, ROW, None) == -2
+        assert fn(vp(256), vp(512), vp(1024), 16, (1 << 30) + 1, 64, BF16, ROW, None) == -2
         assert fn(vp(256), vp(512), vp(1025), 16, 64, 64, BF16, ROW, None) == -3
 
 
