@@ -274,6 +274,107 @@ def test_decode_from_compressed_storage():
         check(Q, SCALE, shared, own, o.double().cpu().numpy(), o32.double().cpu().numpy(), lse.double().cpu().numpy())
 
 
+@pytest.mark.gpu
+def test_rows_beyond_32_bit_offsets():
+    """A prefix of more than 4 GB and sequences as far apart: rows of zeros (weight 1 each) and 24 that matter at the very end."""
+    import paper_2609_16009_b200 as nm
+    n, H = 6_600_000, 16
+    assert n * REC > 2 ** 32
+    g = torch.Generator().manual_seed(41)
+    last = make_records(24, g, spread=0)
+    Q = (torch.randn(2, H, KV + ROPE, generator=g)).to(torch.bfloat16)
+    cache = torch.zeros(n, REC, dtype=torch.uint8, device="cuda")
+    x = torch.randn(24, KV + ROPE, generator=g).to(torch.bfloat16)
+    nm.nm_mla_cache_write_q8(x.cuda(), None, None, torch.arange(n - 24, n, device="cuda"), cache, n, 24, KV, ROPE)
+    back = torch.zeros(24, KV + ROPE, dtype=torch.bfloat16, device="cuda")
+    nm.nm_mla_cache_read_q8(cache, n, torch.arange(n - 24, n, device="cuda"), back, 24, KV, ROPE)
+    # a value to e4m3 and back: 2^-4 of it, 2^-10 of the row's scale (4 / 448 < 2^-6) below the normal range
+    x = x.double()
+    assert ((back.cpu().double() - x).abs() <= x.abs() * 2.0 ** -4 * (1 + 2.0 ** -7) + 2.0 ** -16).all()
+    cache[n - 24:] = last.cuda()
+    rows = rows_of(last)
+    o32, lse = torch.zeros(2, H, KV, device="cuda"), torch.zeros(2, H, device="cuda")
+    ws = torch.empty(nm.nm_mla_attention_q8_workspace_bytes(2, H), dtype=torch.uint8, device="cuda")
+    scale = 0.7                                                    # scores of about 17, e^17 = 24e6
+    for prefix, lens in ((n, [0, 0]), (0, [0, 24])):
+        if prefix:
+            nm.nm_mla_attention_q8(Q.cuda(), cache, n, None, 0, lens, None, o32, lse, H, KV, ROPE, scale, ws)
+        else:                                                      # the second sequence starts 4 GB behind the first
+            nm.nm_mla_attention_q8(Q.cuda(), None, 0, cache, (n - 24) * REC, lens, None, o32, lse, H, KV, ROPE, scale, ws)
+        torch.cuda.synchronize()
+        nm.nm_check_status()
+        for t in range(2):
+            if not prefix and t == 0:
+                assert not o32[0].any() and torch.isneginf(lse[0]).all()
+                continue
+            q = Q[t].double().numpy()
+            s = q @ rows.T * scale
+            zeros = n - 24 if prefix else 0
+            m = np.maximum(s.max(1, keepdims=True), 0)
+            p = np.exp(s - m)
+            total = p.sum(1, keepdims=True) + zeros * np.exp(-m)
+            ref, size = (p / total) @ rows[:, :KV], (p / total) @ np.abs(rows[:, :KV])
+            # as in check; the sum of the zeros' weights is one of 22000 equal terms a thread at most: 2^-10 of them in fp32
+            drop = scale * (np.abs(q[:, :KV]).max(1, keepdims=True) * 2.0 ** -17.8 * np.abs(rows[:, :KV]).sum(1).max()
+                            + (np.abs(q) @ np.abs(rows).T).max(1, keepdims=True) * 64 * 2.0 ** -23) + np.abs(s).max() * 2.0 ** -21
+            tol = size * (2.0 ** -9 + 2.0 ** -11 + 2.0 ** -20 + 2 * drop + 2.0 ** -10) + 2.0 ** -24 * np.abs(rows).max()
+            assert np.all(np.abs(o32[t].double().cpu().numpy() - ref) <= tol)
+            want = (m + np.log(total))[:, 0]
+            assert np.all(np.abs(lse[t].double().cpu().numpy() - want) <= drop[:, 0] + 2.0 ** -10 + 2.0 ** -22 * np.abs(want))
+
+
+@pytest.mark.gpu
+def test_chain_launched_programmatically():
+    """Projection, cache write, attention and output projection behind each other, each starting while the one before it ends: the
+    bits of the plain order, in a graph and step after step."""
+    import paper_2609_16009_b200 as nm
+    g = torch.Generator().manual_seed(43)
+    T, H, d, room, steps = 8, 32, 1024, 8, 6
+    packs = []
+    for N, K in ((KV + ROPE, d), (d, H * KV)):
+        packs.append((torch.randint(0, 256, (nm.nm_w4_packed_bytes(N, K),), dtype=torch.uint8, generator=g).cuda(),
+                      torch.full((nm.nm_w4_scale_count(N, K, 128),), 0.01, dtype=torch.bfloat16, device="cuda")))
+    gamma, prefix = torch.ones(KV, dtype=torch.bfloat16, device="cuda"), make_records(150, g).cuda()
+    Q = torch.randn(steps, T, H, KV + ROPE, generator=g).to(torch.bfloat16).cuda()
+    h0 = torch.randn(T, d, generator=g).to(torch.bfloat16).cuda()
+    h, ckr = torch.zeros_like(h0), torch.zeros(T, KV + ROPE, dtype=torch.bfloat16, device="cuda")
+    o = torch.zeros(T, H, KV, dtype=torch.bfloat16, device="cuda")
+    ws = torch.empty(nm.nm_mla_attention_q8_workspace_bytes(T, H), dtype=torch.uint8, device="cuda")
+    cache = torch.zeros(T * room, REC, dtype=torch.uint8, device="cuda")
+    rows = [torch.arange(T, device="cuda") * room + i for i in range(steps)]
+
+    def run_all():
+        h.copy_(h0)
+        for i in range(steps):                                     # each step's output is the next one's token
+            nm.nm_matmul_w4(h, *packs[0], ckr, T, KV + ROPE, d, 128, nm.BF16)
+            nm.nm_mla_cache_write_q8(ckr, gamma, None, rows[i], cache, T * room, T, KV, ROPE)
+            nm.nm_mla_attention_q8(Q[i], prefix, 150, cache, room * REC, [i + 1] * T, o, None, None, H, KV, ROPE, SCALE, ws)
+            nm.nm_matmul_w4(o, *packs[1], h, T, d, H * KV, 128, nm.BF16)
+
+    run_all()
+    torch.cuda.synchronize()
+    want = (h.clone(), o.clone(), cache.clone())
+    assert want[0].isfinite().all() and want[0].abs().sum() > 0
+    graph = torch.cuda.CUDAGraph()
+    nm.nm_set_programmatic_launch(True)
+    try:
+        for _ in range(3):
+            cache.zero_()
+            run_all()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(want, (h, o, cache)))
+        with torch.cuda.graph(graph):
+            run_all()
+    finally:
+        nm.nm_set_programmatic_launch(False)
+    for _ in range(3):
+        cache.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, (h, o, cache)))
+    nm.nm_check_status()
+
+
 def test_refusals():
     import paper_2609_16009_b200 as nm
     vp, lib = ctypes.c_void_p, nm._lib

@@ -257,6 +257,36 @@ def test_quantise_strange_weights():
     assert unpack_scales(scales.cpu(), 16, 1)[1].item() == float("inf")
 
 
+@pytest.mark.gpu
+def test_weights_beyond_32_bit_offsets():
+    """Weights of 17 GB, 4 GB packed, zeros but for the last sixteen columns: quantised, multiplied and brought back as those alone are."""
+    import paper_2609_16009_b200 as nm
+    N, K, group = 16 * 8193, 65536, 256
+    assert nm.nm_w4_packed_bytes(N, K) > 2 ** 32
+    g = torch.Generator().manual_seed(5)
+    last = torch.randn(16, K, generator=g).to(torch.bfloat16).cuda()
+    B = torch.zeros(N, K, dtype=torch.bfloat16, device="cuda")
+    B[-16:] = last
+    one, many = ((torch.zeros(nm.nm_w4_packed_bytes(n, K), dtype=torch.uint8, device="cuda"),
+                  torch.zeros(nm.nm_w4_scale_count(n, K, group), dtype=torch.bfloat16, device="cuda")) for n in (16, N))
+    nm.nm_w4_quantize(last, *one, 16, K, group, BF16, COL)
+    nm.nm_w4_quantize(B, *many, N, K, group, BF16, COL)
+    assert torch.equal(many[0][-one[0].numel():], one[0]) and (many[0][:-one[0].numel()] == 0x88).all()
+    assert torch.equal(many[1].view(K // group, -1)[:, -16:].reshape(-1), one[1])
+    A = torch.randn(2, K, generator=g).to(torch.bfloat16).cuda()
+    C, c = torch.full((2, N), 7.0, device="cuda"), torch.zeros(2, 16, device="cuda")
+    nm.nm_matmul_w4(A, *many, C, 2, N, K, group, BF16_F32OUT)
+    nm.nm_matmul_w4(A, *one, c, 2, 16, K, group, BF16_F32OUT)
+    assert (C[:, :-16].abs() <= 0).all()
+    # both are sums of K terms in fp32, split differently: 2^-23 a step and eight-block runs, of the size of the terms (code and 8 apart: 23 / 8)
+    back = torch.zeros(16, K, dtype=torch.bfloat16, device="cuda")
+    nm.nm_w4_dequantize(*one, back, 16, K, group, BF16, COL)
+    size = A.double().abs() @ back.double().abs().T + A.double().abs().sum(1, keepdim=True) * back.double().abs().max()
+    assert ((C[:, -16:].double() - c.double()).abs() <= 2 * 160 * 2.0 ** -23 * 3 * size).all() and c.abs().sum() > 0
+    nm.nm_w4_dequantize(*many, B, N, K, group, BF16, COL)
+    assert torch.equal(B[-16:], back) and not B[:-16].any()
+
+
 def test_refusals():
     """Bad arguments are refused before anything is enqueued: no device is needed."""
     import paper_2609_16009_b200 as nm
