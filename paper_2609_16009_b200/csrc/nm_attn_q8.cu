@@ -570,14 +570,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
     }
 }
 
-// ---- the merge: one CTA per head of a sequence, four columns a thread, four threads for every fourth part -----------------------
-constexpr int kMergeGroups = 4, kMergeThreads = kMergeGroups * 128;
-__global__ void __launch_bounds__(kMergeThreads) q8_merge_kernel(const __grid_constant__ MergeArgs a)
+// ---- the merge: one CTA per head of a sequence, four columns a thread, kGroups threads that take the parts in turn --------------------
+template <int kGroups>
+__global__ void __launch_bounds__(kGroups * 128) q8_merge_kernel(const __grid_constant__ MergeArgs a)
 {
+    constexpr int kMergeThreads = kGroups * 128;
     __shared__ float s_w[2 * kPairs + 2], s_l[2 * kPairs + 2];
     __shared__ int s_row[2 * kPairs + 2];
     __shared__ float s_red[kMergeThreads / 32];
-    __shared__ float4 s_acc[kMergeGroups - 1][128];
+    __shared__ float4 s_acc[kGroups > 1 ? kGroups - 1 : 1][128];
     pdl_launch_dependents();
     pdl_wait_prior_grids();
     const int t = blockIdx.x / a.H, h = blockIdx.x - t * a.H, tid = threadIdx.x, group = tid >> 7, x = tid & 127;
@@ -599,18 +600,20 @@ __global__ void __launch_bounds__(kMergeThreads) q8_merge_kernel(const __grid_co
     for (int w = 0; w < kMergeThreads / 32; ++w) mx = fmaxf(mx, s_red[w]);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-    for (int i = group; i < n; i += kMergeGroups) {
+    for (int i = group; i < n; i += kGroups) {
         const float w = ex2(s_w[i] - mx);
         const float4 v = *reinterpret_cast<const float4 *>(a.O + (long)s_row[i] * kKv + 4 * x);
         acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y); acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
     }
-    if (group > 0) s_acc[group - 1][x] = acc;
-    __syncthreads();
-    if (group > 0) return;
+    if constexpr (kGroups > 1) {
+        if (group > 0) s_acc[group - 1][x] = acc;
+        __syncthreads();
+        if (group > 0) return;
 #pragma unroll
-    for (int g = 0; g < kMergeGroups - 1; ++g) {
-        const float4 v = s_acc[g][x];
-        acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+        for (int g = 0; g < kGroups - 1; ++g) {
+            const float4 v = s_acc[g][x];
+            acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+        }
     }
     float total = 0.f;                                             // (every thread adds the same sums in the same order)
     for (int i = 0; i < n; ++i) total = fmaf(ex2(s_w[i] - mx), s_l[i], total);
@@ -798,7 +801,10 @@ int nm_mla_attention_q8(const void *Q, long q_stride, const void *prefix, long p
         if (e == cudaSuccess) e = launch_after(attn_q8_kernel, 2 * pairs, kThreads, kSmemBytes, s, pa);
         if (e != cudaSuccess) return record_cuda_error(e, "quantised attention launch");
     }
-    const cudaError_t e = launch_after(q8_merge_kernel, (unsigned)total_q, kMergeThreads, 0, s, ma);
+    // Four threads a part's column while their CTAs, four to an SM, need no more than two waves (8 x 128 heads, 4096 rows each: 32.7 us
+    // against 35.4, 1 x 128, 16384: 26.8 against 30.6); one beyond (16 x 128, ragged 4096: 49 us against 53; 64 x 128, 1000: 62 against 78).
+    const cudaError_t e = total_q <= 8 * kSMs ? launch_after(q8_merge_kernel<4>, (unsigned)total_q, 512, 0, s, ma)
+                                              : launch_after(q8_merge_kernel<1>, (unsigned)total_q, 128, 0, s, ma);
     return e == cudaSuccess ? NM_OK : record_cuda_error(e, "quantised attention merge launch");
 }
 
