@@ -4,7 +4,7 @@
 // One warp per row: the whole row lives in the warp's registers (16 values a lane at kv_lora = 512), its sum of squares (fp64, so that
 // a code next to a tie falls where the definition puts it) and its largest value are warp reductions, and nothing is read or
 // written twice.  Bound: 1152 bytes in and 656 out per row (reversed when read back), in runs of 16 bytes a lane.  Measured, 131072
-// rows of 512 + 64 in random order: written in 82 us with norm and rotation (41 for the bytes; conversions and the fp64 sum take 68 % of
+// rows of 512 + 64 in random order: written in 79 us with norm and rotation (41 for the bytes; conversions and the fp64 sum take 68 % of
 // the issue slots), read back in 45 (36 for the bytes); 16 rows are written in 2.8 us.
 #include <cuda_fp8.h>
 
@@ -29,7 +29,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 template <int kVecs>
 __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uint16_t *__restrict__ ckr, long stride, const uint16_t *__restrict__ gamma,
                                                                        const float *__restrict__ cos_sin, const int64_t *__restrict__ rows,
-                                                                       unsigned char *__restrict__ cache, long n_cache_rows, int T, int kv, int rope, float eps)
+                                                                       unsigned char *__restrict__ cache, long n_cache_rows, int T, int kv, int rope, double inv_kv,
+                                                                       float eps)
 {
     const int t = blockIdx.x * kWarpsQ8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     pdl_launch_dependents();
@@ -39,6 +40,18 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
     if (row < 0 || row >= n_cache_rows) return;                    // a padding token, or no such row: written nowhere
     const uint16_t *x = ckr + (long)t * stride;
     const int vecs = kv / 8;
+    // all that the row needs is asked for at once; the key part's first 64 values (all there are, mostly) among it
+    uint4 weight[kVecs] = {};
+    if (gamma) {
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+            if (lane + 32 * i < vecs) weight[i] = __ldg(reinterpret_cast<const uint4 *>(gamma + 8 * (lane + 32 * i)));
+    }
+    auto key_at = [&](int p) { return *reinterpret_cast<const uint32_t *>(x + kv + 2 * p); };
+    auto angle_at = [&](int p) { return cos_sin ? *reinterpret_cast<const float2 *>(cos_sin + (long)t * rope + 2 * p) : make_float2(1.f, 0.f); };
+    const bool has_key = lane < rope / 2;
+    const uint32_t key0 = has_key ? key_at(lane) : 0u;
+    const float2 angle0 = has_key ? angle_at(lane) : make_float2(1.f, 0.f);
     float y[kVecs][8];
     double squares = 0.;
 #pragma unroll
@@ -59,14 +72,16 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
         for (int o = 16; o > 0; o >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, o);
         // The normaliser in 64 bits, and used as two fp32 terms on the exact products x * gamma: y is off by one rounding only.  A code
         // next to a tie of e4m3 falls wrongly by whatever the value is off, and a code is worth 2^-4 of it; the row waits for memory anyway.
-        const double rd = 1. / sqrt(squares / (double)kv + (double)eps);
+        const double mean = squares * inv_kv + (double)eps;
+        double rd;
+        if (mean > 0x1p-100 && mean < 0x1p100) {                   // from fp32's root by one Newton step, 2^-44 off
+            const double r0 = (double)rsqrtf((float)mean);
+            rd = fma(0.5 * r0, fma(-mean * r0, r0, 1.), r0);
+        } else rd = 1. / sqrt(mean);
         const float r = (float)rd, r_low = (float)(rd - (double)r);
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
-            const int v = lane + 32 * i;
-            uint4 u = make_uint4(0u, 0u, 0u, 0u);
-            if (v < vecs) u = __ldg(reinterpret_cast<const uint4 *>(gamma + 8 * v));
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+            const uint32_t w[4] = {weight[i].x, weight[i].y, weight[i].z, weight[i].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float a = y[i][2 * j] * bf_lo(w[j]), b = y[i][2 * j + 1] * bf_hi(w[j]);
@@ -104,10 +119,10 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
         *reinterpret_cast<uint2 *>(rec + 8 * v) = make_uint2(c[0], c[1]);
     }
     for (int p = lane; p < rope / 2; p += 32) {
-        const uint32_t w = *reinterpret_cast<const uint32_t *>(x + kv + 2 * p);
+        const uint32_t w = p == lane ? key0 : key_at(p);
         float a = bf_lo(w), b = bf_hi(w);
         if (cos_sin) {
-            const float2 cs = *reinterpret_cast<const float2 *>(cos_sin + (long)t * rope + 2 * p);
+            const float2 cs = p == lane ? angle0 : angle_at(p);
             const float ra = a * cs.x - b * cs.y, rb = a * cs.y + b * cs.x;
             a = ra; b = rb;
         }
@@ -192,8 +207,8 @@ int nm_mla_cache_write_q8(const void *ckr, long ckr_stride, const void *gamma, c
     cudaStream_t s = (cudaStream_t)stream;
     const uint16_t *x = static_cast<const uint16_t *>(ckr), *gm = static_cast<const uint16_t *>(gamma);
     unsigned char *c = static_cast<unsigned char *>(cache);
-    const cudaError_t e = kv_lora <= 512 ? launch_rows(cache_write_q8_kernel<2>, T, s, x, ckr_stride, gm, cos_sin, rows, c, n_cache_rows, T, kv_lora, rope, eps)
-                                         : launch_rows(cache_write_q8_kernel<4>, T, s, x, ckr_stride, gm, cos_sin, rows, c, n_cache_rows, T, kv_lora, rope, eps);
+    const cudaError_t e = kv_lora <= 512 ? launch_rows(cache_write_q8_kernel<2>, T, s, x, ckr_stride, gm, cos_sin, rows, c, n_cache_rows, T, kv_lora, rope, 1. / kv_lora, eps)
+                                         : launch_rows(cache_write_q8_kernel<4>, T, s, x, ckr_stride, gm, cos_sin, rows, c, n_cache_rows, T, kv_lora, rope, 1. / kv_lora, eps);
     return e == cudaSuccess ? NM_OK : record_cuda_error(e, "quantised cache write launch");
 }
 
