@@ -387,7 +387,9 @@ __global__ void __launch_bounds__(w4_warps(kNT) * 32, kNT == 1 ? 2 : 1) w4_kerne
 
 // How many warps side by side and how many CTAs along k: the least time by a model in microseconds, fitted to sweeps of both on B200
 // (shapes of 0.6 to 18 thousand columns and 1.5 to 16 thousand k).  Per wave of resident CTAs: a fixed start and end, a block of
-// 1024 codes per 12.6 ns and SM (15 for two strips side by side), a block of a token row per 3 (6) ns, and a cluster's exchange.
+// 1024 codes per 12.6 ns and SM (15 for two strips side by side), a block of a token row per 3 (6) ns, and a cluster's exchange of 0.8
+// (3).  (With 0.8 for M > 8 too, 16 x 1536 x 40000 took 31 us instead of 23 and 16 x 7168 x 12288 34 instead of 27; with 1.6 for
+// M <= 8, 4 x 7168 x 1536 10 instead of 7.)
 // `resident`: clusters of each size that run at once (their CTAs need SMs of one GPC, so not every size fills the machine).
 struct W4Plan { int wn, cl; };
 W4Plan plan_w4(int M, int units, int kb, const int (&resident)[9])
@@ -402,7 +404,7 @@ W4Plan plan_w4(int M, int units, int kb, const int (&resident)[9])
             const int tiles = ceil_div(units, wn), blocks = ceil_div(kb, cl), run = ceil_div(blocks, warps / wn);
             const int waves = ceil_div(tiles, resident[cl]), on_sm = wide || (long)tiles * cl <= kSMs ? 1 : 2;
             const double stream = on_sm * warps * run * (wide ? 2 * 0.015 : 0.0126), tokens = on_sm * M * blocks * (wide ? 0.006 : 0.003);
-            const double cost = waves * ((wide ? 2.0 : 1.5) + stream + tokens + (cl > 1 ? 0.8 : 0.0));
+            const double cost = waves * ((wide ? 2.0 : 1.5) + stream + tokens + (cl > 1 ? (wide ? 3.0 : 0.8) : 0.0));
             if (cost < least) { least = cost; best = W4Plan{wn, cl}; }
         }
     return best;
