@@ -4,7 +4,7 @@
 // One warp per row: the whole row lives in the warp's registers (16 values a lane at kv_lora = 512), its sum of squares (fp64, so that
 // a code next to a tie falls where the definition puts it) and its largest value are warp reductions, and nothing is read or
 // written twice.  Bound: 1152 bytes in and 656 out per row (reversed when read back), in runs of 16 bytes a lane.  Measured, 131072
-// rows of 512 + 64 in random order: written in 76 us with norm and rotation (41 for the bytes; conversions and the fp64 sum take 68 % of
+// rows of 512 + 64 in random order: written in 76 us with norm and rotation (41 for the bytes; conversions and the fp64 sum take 71 % of
 // the issue slots), read back in 45 (36 for the bytes); 16 rows are written in 2.4 us.
 // Four rows a CTA; eight take 83 us for the first, two 69 to read back.
 #include <cuda_fp8.h>
