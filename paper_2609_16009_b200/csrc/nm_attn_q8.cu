@@ -75,6 +75,10 @@ struct PassArgs {
     int total_q;
     short first[kPairs + 1];                       // items of each pair of CTAs
     Item items[kMaxItems];
+#ifdef NM_BOUNDS_CHECK
+    int pause_where, pause_warp;                   // see nm_debug_set_attention_q8_pause
+    unsigned pause_ns;
+#endif
 };
 struct MergeArgs {
     const float *ml, *O;
@@ -209,6 +213,21 @@ __device__ __forceinline__ void warp_wait(uint32_t bar, uint32_t par, int lane, 
     tc_fence_after();
 }
 
+// Debug build only: one warp of every CTA is held up at a named place, so that a test can show that the order of what the warps tell each
+// other does not hang on their pace.  Bounded by the clock.
+constexpr int kPauseAfterMaxima = 1;               // a softmax warp, behind the barrier of a tile, before it reads its rows' maxima
+constexpr int kPausePlaces = 1;
+#ifdef NM_BOUNDS_CHECK
+__device__ __noinline__ void pause_here(unsigned ns)
+{
+    const uint64_t t0 = global_timer_ns();
+    while (global_timer_ns() - t0 < ns) __nanosleep(100);
+}
+#define NM_PAUSE(where) do { if (a.pause_where == (where) && a.pause_warp == warp) pause_here(a.pause_ns); } while (0)
+#else
+#define NM_PAUSE(where) do {} while (0)
+#endif
+
 __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_constant__ PassArgs a)
 {
     extern __shared__ unsigned char smem_raw[];
@@ -222,7 +241,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
                    bar_s = bar_qt + 8, bar_p = bar_s + 16, bar_pv = bar_p + 16,
                    bar_free = bar_pv + 8;
     __shared__ uint32_t s_tmem;
-    __shared__ float s_pair[2][kM];                                // what the two threads of a row tell each other
+    // What the two threads of a row tell each other, in turn for the tiles: a thread may be a whole tile ahead of the other one's read of
+    // what it told last (the next tile's scores wait for nobody's softmax), and not two - the barrier of the next tile is in between.
+    __shared__ float s_pair[2][2][kM];
     __shared__ int s_abort;
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31, half = blockIdx.x & 1;
     const int pair = blockIdx.x >> 1, item0 = a.first[pair], item1 = a.first[pair + 1];
@@ -456,11 +477,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
                 for (int i = 0; i < 16; i += 2) { mx = fmaxf(mx, __uint_as_float(raw[c][i])); mx1 = fmaxf(mx1, __uint_as_float(raw[c][i + 1])); }
             // One barrier a tile.  Before it: this tile's scores are in registers (P may overwrite them), its maxima are told, and the
             // table of the tile after next is written - into a buffer whose last readers passed the barrier before this one.
-            s_pair[set][r] = fmaxf(mx, mx1);
+            s_pair[t & 1][set][r] = fmaxf(mx, mx1);
             if (entry < kR) s_table[kR * ((t + 2) % kTables) + entry] = row_entry(s_next);
             named_barrier_sync(1, kSoftmax);
+            NM_PAUSE(kPauseAfterMaxima);
             s_next = row_scale(t + 3);
-            mx = fmaxf(s_pair[0][r], s_pair[1][r]);
+            mx = fmaxf(s_pair[t & 1][0][r], s_pair[t & 1][1][r]);
             const bool grow = t == 0 || mx > m + kLazy;
             if (t > 0 && __any_sync(0xffffffffu, grow)) {
                 // the previous tile's P * V has to be through before O is touched; each of the row's threads takes half of the columns
@@ -527,10 +549,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
         // ---- out: the warp's 32 rows and its set's 128 columns, 64 at a time through its own corner of the queries' place (the last
         //      scores are through), so that the stores run along the rows ----------------------------------------------------------------------
         named_barrier_sync(1, kSoftmax);
-        s_pair[set][r] = l + l1;
+        s_pair[0][set][r] = l + l1;                                // (the next item's maxima come behind its first barrier, which every reader meets)
         named_barrier_sync(1, kSoftmax);
         if (half == 0 && set == 0 && r < it.n_q)
-            *reinterpret_cast<float2 *>(a.ml + 2 * (long)(it.out_row + r)) = make_float2(m, s_pair[0][r] + s_pair[1][r]);
+            *reinterpret_cast<float2 *>(a.ml + 2 * (long)(it.out_row + r)) = make_float2(m, s_pair[0][0][r] + s_pair[0][1][r]);
         float4 *corner = reinterpret_cast<float4 *>(smem + (4 * set + quad) * 8192);        // [32 rows][16 float4], the index XOR-ed with row & 15
         for (int c0 = 128 * set; c0 < 128 * set + 128; c0 += 64) {
             uint32_t o[2][32];
@@ -630,6 +652,10 @@ __global__ void __launch_bounds__(kGroups * 128) q8_merge_kernel(const __grid_co
     if (a.lse && tid == 0) a.lse[blockIdx.x] = n > 0 ? (mx - kHeadroom + log2f(total)) * 0.6931471805599453f : -INFINITY;
 }
 
+#ifdef NM_BOUNDS_CHECK
+std::atomic<unsigned long long> g_q8_pause{0};     // place | warp | nanoseconds, from the top
+#endif
+
 // ---- host ------------------------------------------------------------------------------------------------------------------
 struct Layout { size_t q_rows, mult, ml, O, total; };
 Layout layout_of(int T, int H, long part_rows)
@@ -717,6 +743,18 @@ size_t nm_mla_attention_q8_workspace_bytes(int T, int H)
     return layout_of(T, H, (long)kMaxItems * std::min(kM, T * H)).total;
 }
 
+int nm_debug_set_attention_q8_pause(int where, int warp, unsigned ns)
+{
+#ifdef NM_BOUNDS_CHECK
+    if (where < 0 || where > kPausePlaces || warp < 0 || warp >= kThreads / 32 || ns > 2000000000u) return NM_ERR_INVALID_ARG;
+    g_q8_pause.store(((unsigned long long)where << 40) | ((unsigned long long)warp << 32) | ns, std::memory_order_relaxed);
+    return NM_OK;
+#else
+    (void)where; (void)warp; (void)ns;
+    return NM_ERR_UNSUPPORTED;
+#endif
+}
+
 int nm_mla_attention_q8(const void *Q, long q_stride, const void *prefix, long prefix_rows, const void *cache, long cache_stride, const int *seq_lens,
                         void *o_bf16, float *o_f32, float *lse, int T, int H, int kv_lora, int rope, float scale, void *workspace,
                         size_t workspace_bytes, nm_stream stream)
@@ -785,6 +823,10 @@ int nm_mla_attention_q8(const void *Q, long q_stride, const void *prefix, long p
     pa.first[pairs] = (short)items;
     if (items) {
         pa.status = device_status_ptr();
+#ifdef NM_BOUNDS_CHECK
+        const unsigned long long pause = g_q8_pause.load(std::memory_order_relaxed);
+        pa.pause_ns = (unsigned)pause; pa.pause_warp = (int)(pause >> 32) & 0xff; pa.pause_where = (int)(pause >> 40);
+#endif
         if (!encode_bytes_map(&pa.q, pa.q_rows, total_q, kQRow, kM)) return record_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
         // The maps cover exactly the rows attended: what lies behind them reads as zeros (and has no weight), whatever it holds.
         for (int i = 0; i <= T; ++i) {
