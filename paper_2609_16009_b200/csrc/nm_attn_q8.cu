@@ -216,7 +216,9 @@ __device__ __forceinline__ void warp_wait(uint32_t bar, uint32_t par, int lane, 
 // Debug build only: one warp of every CTA is held up at a named place, so that a test can show that the order of what the warps tell each
 // other does not hang on their pace.  Bounded by the clock.
 constexpr int kPauseAfterMaxima = 1;               // a softmax warp, behind the barrier of a tile, before it reads its rows' maxima
-constexpr int kPausePlaces = 1;
+constexpr int kPauseAfterWeights = 2;              // a softmax warp that has handed in the weights of an item's last tile
+constexpr int kPauseBeforeProduct = 3;             // the issuing warp, with all weights of a tile in and its P * V not issued
+constexpr int kPausePlaces = 3;
 #ifdef NM_BOUNDS_CHECK
 __device__ __noinline__ void pause_here(unsigned ns)
 {
@@ -239,7 +241,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + kQBytes + kSlots * kSlotBytes + kTableBytes);
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * kSlots, bar_q = bar_empty + 8 * kSlots, bar_qt = bar_q + 8,
                    bar_s = bar_qt + 8, bar_p = bar_s + 16, bar_pv = bar_p + 16,
-                   bar_free = bar_pv + 8;
+                   bar_free = bar_pv + 16;
     __shared__ uint32_t s_tmem;
     // What the two threads of a row tell each other, in turn for the tiles: a thread may be a whole tile ahead of the other one's read of
     // what it told last (the next tile's scores wait for nobody's softmax), and not two - the barrier of the next tile is in between.
@@ -252,8 +254,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
         for (int i = 0; i < kSlots; ++i) { mbar_init(bar_full + 8 * i, 1); mbar_init(bar_empty + 8 * i, 1); }
         mbar_init(bar_q, 1);
         mbar_init(bar_qt, 128);
-        for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_p + 8 * i, kSoftmax / 32); }
-        mbar_init(bar_pv, 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_p + 8 * i, kSoftmax / 32); mbar_init(bar_pv + 8 * i, 1); }
         mbar_init(bar_free, kSoftmax / 32);
         mbar_init_fence();
     }
@@ -263,6 +264,13 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
     tc_fence_after();
     const uint32_t tmem = s_tmem;
     pdl_launch_dependents();
+
+    // Barriers of tile g: scores bar_s, weights bar_p and P * V bar_pv, each the one of g's parity in its phase g / 2.  A wait is by one bit of the
+    // phase, so it may meet two states only: the phase before through, or its own.  The one after its own is out of reach of all of them -
+    // scores g + 2 are issued behind the wait for the weights of g, and P * V of g + 2 behind the waiting warp's own arrival for g + 2 - and
+    // the one before is through: scores g seen say so of P * V g - 2, which was issued ahead of them.  (With one bar_pv for all tiles a
+    // warp that has handed in its last weights might find two P * V outstanding, one or none: three states, and the wait for the last but one
+    // takes both through for neither.)
 
     // A tile's five blocks in ring order: the other half's two latent blocks, the key part, this half's two latent blocks (the last
     // ones to be given back: they are also V).  x: byte offset in the record.
@@ -374,6 +382,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
             for (int t = 0; t < ntiles; ++t, ++gp) {
                 if (t + 1 < ntiles) scores();
                 wait(bar_p + 8 * (gp & 1), (gp >> 1) & 1);
+                NM_PAUSE(kPauseBeforeProduct);
                 tc_fence_after();
                 const uint32_t p = tm + kColS + kR * (gp & 1);
                 const int v_next = v_slot + 1 == kSlots ? 0 : v_slot + 1;
@@ -388,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
                                 mma_f8_ts(tm + kColO + 128 * v, p + 32 * kk + 8 * term, (v ? b1 : b0) + 256 * kk, idesc_o, t > 0 || (kk | term) != 0);
                         mma_commit(bar_empty + 8 * (v ? v_next : v_slot));
                     }
-                    mma_commit(bar_pv);
+                    mma_commit(bar_pv + 8 * (gp & 1));
                 }
                 __syncwarp();
                 v_slot += 5;
@@ -486,7 +495,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
             const bool grow = t == 0 || mx > m + kLazy;
             if (t > 0 && __any_sync(0xffffffffu, grow)) {
                 // the previous tile's P * V has to be through before O is touched; each of the row's threads takes half of the columns
-                warp_wait(bar_pv, (g - 1) & 1, lane, &s_abort, a.status);
+                warp_wait(bar_pv + 8 * ((g - 1) & 1), ((g - 1) >> 1) & 1, lane, &s_abort, a.status);
                 const float f = grow ? ex2(m - mx) : 1.f;
 #pragma unroll 1
                 for (int c = 128 * set; c < 128 * set + 128; c += 64) {
@@ -542,10 +551,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_p + 8 * (g & 1));
         }
-        // (both of the last two: the scores of the last tile say that the P * V before these is through, not that the last but one is,
-        // and a wait by parity alone would take an older phase for the last)
-        if (ntiles > 1) warp_wait(bar_pv, g & 1, lane, &s_abort, a.status);
-        warp_wait(bar_pv, (g - 1) & 1, lane, &s_abort, a.status);
+        // both of the last two: the scores of the last tile say that P * V of the last but two is through
+        NM_PAUSE(kPauseAfterWeights);
+        if (ntiles > 1) warp_wait(bar_pv + 8 * (g & 1), ((g - 2) >> 1) & 1, lane, &s_abort, a.status);
+        warp_wait(bar_pv + 8 * ((g - 1) & 1), ((g - 1) >> 1) & 1, lane, &s_abort, a.status);
         // ---- out: the warp's 32 rows and its set's 128 columns, 64 at a time through its own corner of the queries' place (the last
         //      scores are through), so that the stores run along the rows ----------------------------------------------------------------------
         named_barrier_sync(1, kSoftmax);

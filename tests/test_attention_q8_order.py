@@ -39,7 +39,7 @@ def programs(items, rescale, pair_buffers):
     return [issue, *rows]
 
 
-def faults(items, rescale=(True, True), pair_buffers=2, pv_barriers=1):
+def faults(items, rescale=(True, True), pair_buffers=2, pv_barriers=2):
     """Every fault that some interleaving reaches."""
     prog = programs(items, rescale, pair_buffers)
     bars = {"q": 1, "p": 2, "s": 2, "pv": pv_barriers}
@@ -106,9 +106,21 @@ def test_model_sees_the_maximum_of_the_next_tile():
     assert "another tile's" in faults([2], pair_buffers=1)
 
 
+@pytest.mark.parametrize("rescale", RESCALE)
+@pytest.mark.parametrize("items", ITEMS)
+def test_model_every_wait_ends_and_none_too_early(items, rescale):
+    assert not faults(items, rescale)
+
+
+@pytest.mark.parametrize("rescale", RESCALE)
+def test_model_sees_a_wait_that_comes_too_late(rescale):
+    """With one barrier for the P * V of all tiles a thread that finds the last two through waits for a third."""
+    assert faults([2, 1], rescale, pv_barriers=1) == {"stuck"}
+
+
 # ---- the debug build, a warp held up ---------------------------------------------------------------------------------------
 
-PAUSES = {"maxima": 1}
+PAUSES = {"maxima": 1, "weights": 2, "product": 3}
 
 
 def _declare(lib):
@@ -179,6 +191,17 @@ def test_a_thread_late_to_read_the_maxima_changes_nothing(libs, batch, warp):
         got = paused(check, "maxima", warp, ns, lambda: batch.call(check))
         assert check.nm_check_status(None) == 0
         assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("where,warp", [("weights", 2), ("weights", 5), ("weights", 8), ("product", 1)])
+def test_both_last_products_through_or_neither(libs, batch, where, warp):
+    """A softmax warp held up until the last two P * V are through finds them so; an issuing warp held up ahead of each finds nobody gone on."""
+    normal, check = libs
+    want = batch.call(normal)
+    got = paused(check, where, warp, 20_000, lambda: batch.call(check))
+    assert check.nm_check_status(None) == 0, "a wait ran out"
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
 def test_the_pause_belongs_to_the_debug_build():
