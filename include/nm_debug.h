@@ -85,7 +85,8 @@ int nm_debug_bounds_checked(void);
 int nm_debug_bounds_selftest(void *buf, size_t bytes, unsigned *out_loaded, nm_stream stream);
 /* Debug build only (else NM_ERR_UNSUPPORTED): nm_mla_attention_q8 holds up warp `warp` (0 copies, 1 matrix unit, 2..9 softmax) of every CTA for
  * `ns` nanoseconds (at most 2e9) each time it comes to the place `where`: 0 nowhere, 1 a softmax warp between a tile's barrier and its read of
- * the row maxima, 2 a softmax warp with an item's last weights handed in, 3 the matrix unit's warp before a tile's P * V.  A result that changes with it was held together by the warps' pace. */
+ * the row maxima, 2 a softmax warp with an item's last weights handed in, 3 the matrix unit's warp before a tile's P * V, 4 the
+ * copying thread before a copy; not once a wait of the CTA has expired, which a pause of more than a second brings about.  A result that changes with it was held together by the warps' pace. */
 int nm_debug_set_attention_q8_pause(int where, int warp, unsigned ns);
 /* Measurement aid: a kernel that only reads `bytes` bytes of device memory once (16-byte streaming loads, the
  * products' own load instruction, ctas_per_sm x SM-count CTAs of 256 threads) - the read-only bandwidth this GPU

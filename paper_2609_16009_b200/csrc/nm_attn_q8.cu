@@ -190,18 +190,18 @@ __device__ __forceinline__ void mma_key_ss(uint32_t d, uint32_t a, uint32_t b, u
 
 // The bounded wait of the issuing warp: no function call, and every decision is the warp's vote, so that its control flow stays uniform
 // to the compiler and the operands of the MMAs around it stay in uniform registers.
-__device__ __forceinline__ void wait_uniform(uint32_t bar, uint32_t par, volatile int *abort_flag, unsigned *status)
+__device__ __forceinline__ bool wait_uniform(uint32_t bar, uint32_t par, volatile int *abort_flag, unsigned *status)
 {
-    if (__all_sync(0xffffffffu, mbar_try_wait(bar, par))) return;
+    if (__all_sync(0xffffffffu, mbar_try_wait(bar, par))) return true;
     const uint64_t t0 = global_timer_ns();
 #pragma unroll 1
     for (;;) {
-        if (__all_sync(0xffffffffu, mbar_try_wait(bar, par))) return;
-        if (__any_sync(0xffffffffu, *abort_flag != 0)) return;
+        if (__all_sync(0xffffffffu, mbar_try_wait(bar, par))) return true;
+        if (__any_sync(0xffffffffu, *abort_flag != 0)) return false;
         if (__any_sync(0xffffffffu, global_timer_ns() - t0 > kWaitLimitNs)) {
             *abort_flag = 1;
             if (status) atomicOr(status, kStatusWaitExpired);
-            return;
+            return false;
         }
     }
 }
@@ -213,19 +213,31 @@ __device__ __forceinline__ void warp_wait(uint32_t bar, uint32_t par, int lane, 
     tc_fence_after();
 }
 
+// How often a slot of the ring has been filled after so many blocks.
+__host__ __device__ constexpr int times_armed(int blocks, int slot) { return (blocks + kSlots - 1 - slot) / kSlots; }
+static_assert(times_armed(0, 0) == 0 && times_armed(1, 0) == 1 && times_armed(1, 1) == 0 && times_armed(kSlots, kSlots - 1) == 1 && times_armed(kSlots + 1, 0) == 2 &&
+              times_armed(kSlots + 1, 1) == 1, "the ring's slots in turn");
+constexpr uint64_t kDrainLimitNs = 100000000ull;
+__device__ __noinline__ void drain(uint32_t bar, uint32_t par)
+{
+    const uint64_t t0 = global_timer_ns();
+    while (!mbar_try_wait(bar, par) && global_timer_ns() - t0 < kDrainLimitNs) {}
+}
+
 // Debug build only: one warp of every CTA is held up at a named place, so that a test can show that the order of what the warps tell each
 // other does not hang on their pace.  Bounded by the clock.
 constexpr int kPauseAfterMaxima = 1;               // a softmax warp, behind the barrier of a tile, before it reads its rows' maxima
 constexpr int kPauseAfterWeights = 2;              // a softmax warp that has handed in the weights of an item's last tile
 constexpr int kPauseBeforeProduct = 3;             // the issuing warp, with all weights of a tile in and its P * V not issued
-constexpr int kPausePlaces = 3;
+constexpr int kPauseBeforeCopy = 4;                // the copying thread, a slot free and its copy not begun
+constexpr int kPausePlaces = 4;
 #ifdef NM_BOUNDS_CHECK
 __device__ __noinline__ void pause_here(unsigned ns)
 {
     const uint64_t t0 = global_timer_ns();
     while (global_timer_ns() - t0 < ns) __nanosleep(100);
 }
-#define NM_PAUSE(where) do { if (a.pause_where == (where) && a.pause_warp == warp) pause_here(a.pause_ns); } while (0)
+#define NM_PAUSE(where) do { if (a.pause_where == (where) && a.pause_warp == warp && !*static_cast<volatile int *>(&s_abort)) pause_here(a.pause_ns); } while (0)
 #else
 #define NM_PAUSE(where) do {} while (0)
 #endif
@@ -241,7 +253,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
     uint64_t *bars = reinterpret_cast<uint64_t *>(smem + kQBytes + kSlots * kSlotBytes + kTableBytes);
     const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + 8 * kSlots, bar_q = bar_empty + 8 * kSlots, bar_qt = bar_q + 8,
                    bar_s = bar_qt + 8, bar_p = bar_s + 16, bar_pv = bar_p + 16,
-                   bar_free = bar_pv + 16;
+                   bar_free = bar_pv + 16, bar_done = bar_free + 8;
     __shared__ uint32_t s_tmem;
     // What the two threads of a row tell each other, in turn for the tiles: a thread may be a whole tile ahead of the other one's read of
     // what it told last (the next tile's scores wait for nobody's softmax), and not two - the barrier of the next tile is in between.
@@ -256,6 +268,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
         mbar_init(bar_qt, 128);
         for (int i = 0; i < 2; ++i) { mbar_init(bar_s + 8 * i, 1); mbar_init(bar_p + 8 * i, kSoftmax / 32); mbar_init(bar_pv + 8 * i, 1); }
         mbar_init(bar_free, kSoftmax / 32);
+        mbar_init(bar_done, 1);
         mbar_init_fence();
     }
     if (warp == 1) tmem_alloc(&s_tmem, 512);
@@ -277,6 +290,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
     const int other = 2 * (half ^ 1), mine = 2 * half;
     auto block_x = [&](int j) { return j < 2 ? 128 * (other + j) : (j == 2 ? kKv : 128 * (mine + j - 3)); };
 
+    // Copies of blocks and of queries begun by thread 0
+    int blocks = 0, queries = 0;
+
     // The CTA takes its items one after another; the ring runs on from one to the next, so an item's records are on their way while the
     // one before it is being finished.
     if (warp == 0) {
@@ -287,7 +303,9 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
             bool ok = true;
             auto load_queries = [&](int i) {                       // lo 0-3, hi of this half, key part
                 if (i > item0 && !mbar_try_wait(bar_free, (i - item0 - 1) & 1)) ok = mbar_wait(bar_free, (i - item0 - 1) & 1, &s_abort, a.status);
+                if (*static_cast<volatile int *>(&s_abort)) ok = false;        // (the item before was given up, not finished)
                 if (!ok) return;
+                ++queries;
                 mbar_arrive_expect_tx(bar_q, kQBytes);
                 for (int b = 0; b < 7; ++b)
                     tma_load_2d(q_addr + b * kQBlock, &a.q, b < 4 ? kKv + 128 * b : (b < 6 ? 128 * (mine + b - 4) : 2 * kKv), a.items[i].q_row, bar_q, keep);
@@ -307,6 +325,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
                         if (!ok) break;
                     }
                     if (!mbar_try_wait(bar_empty + 8 * slot, par) && !mbar_wait(bar_empty + 8 * slot, par, &s_abort, a.status)) { ok = false; break; }
+                    NM_PAUSE(kPauseBeforeCopy);
+                    ++blocks;
                     mbar_arrive_expect_tx(bar_full + 8 * slot, kSlotBytes);
                     tma_load_2d(ring + slot * kSlotBytes, map_k, block_x(x), row, bar_full + 8 * slot, keep);
                     if (++slot == kSlots) { slot = 0; par ^= 1; }
@@ -325,13 +345,16 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
         constexpr uint32_t idesc_s = instr_desc_f8(kM, kR, 0, false), idesc_key = instr_desc(kM, kR, false, false), idesc_o = instr_desc_f8(kM, 128, 1, true);
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0), sm = __shfl_sync(0xffffffffu, base, 0);
         const bool leader = elect_one();
+        bool alive = true;
         const uint32_t q_low = desc_low(sm, 16), q_other = q_low + other * (kQBlock >> 4), q_mine = q_low + mine * (kQBlock >> 4);
         // A block is waited for before the MMAs of the one before it are issued: the pipe queues only a few, and a wait between them
         // would let it run dry.
-        // (An expired wait changes nothing here: the walk goes on, every operand in its place whatever it holds, so that the control
-        // flow stays uniform; the status word disowns the result.)
+        // (After an expired wait the walk goes on, every operand in its place whatever it holds, so that the control flow stays uniform; the status
+        // word disowns the result.  Only no slot is given back any more: one that is refilled has been waited for.  Of the ways to see to
+        // that this one costs nothing; with `leader` taken away 16 x 128 heads behind 32768 rows took 247 us instead of 214, with the abort
+        // flag looked at ahead of every copy 3 % more.)
         auto wait = [&](uint32_t bar, uint32_t par) {
-            wait_uniform(bar, par, &s_abort, a.status);
+            alive = wait_uniform(bar, par, &s_abort, a.status) && alive;
         };
         int wait_slot = 0, wait_par = 0, slot = 0, v_slot = 3;     // the ring's block waited for next, issued next, and the next tile's first V block
         int gs = 0, gp = 0;                                        // tiles of all items so far: scores issued, P * V issued
@@ -370,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
                                 mma_f8_ss(d, lo + 2 * kk, k + 2 * kk, idesc_s, true);
                             }
                         }
-                        if (j < 3) mma_commit(bar_empty + 8 * slot);
+                        if (j < 3 && alive) mma_commit(bar_empty + 8 * slot);
                         if (j == 4) mma_commit(bar_s + 8 * (gs & 1));
                     }
                     __syncwarp();
@@ -395,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
 #pragma unroll
                             for (int term = 0; term < 3; ++term)
                                 mma_f8_ts(tm + kColO + 128 * v, p + 32 * kk + 8 * term, (v ? b1 : b0) + 256 * kk, idesc_o, t > 0 || (kk | term) != 0);
-                        mma_commit(bar_empty + 8 * (v ? v_next : v_slot));
+                        if (alive) mma_commit(bar_empty + 8 * (v ? v_next : v_slot));
                     }
                     mma_commit(bar_pv + 8 * (gp & 1));
                 }
@@ -591,10 +614,22 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
     }
     tc_fence_before();
     __syncthreads();
-    if (s_abort && tid == 0) {
-        // a wait expired: give copies already issued a bounded chance to land before the CTA exits
-        for (int i = 0; i < (1 << 16) && !mbar_try_wait(bar_full, 0); ++i) {}
-        for (int i = 0; i < (1 << 16) && !mbar_try_wait(bar_q, 0); ++i) {}
+    if (s_abort) {
+        // A wait expired: what is still under way, copies into this CTA's shared memory and products on its TMEM, gets a bounded chance to end
+        // before either is given back.  Of a barrier armed n times phase n - 2 is through: it is armed again only behind what waited for that.
+        if (tid == 0) {
+            for (int i = 0; i < kSlots; ++i) {
+                const int armed = times_armed(blocks, i);
+                if (armed > 0) drain(bar_full + 8 * i, (armed - 1) & 1);
+            }
+            if (queries > 0) drain(bar_q, (queries - 1) & 1);
+        }
+        if (warp == 1) {
+            if (elect_one()) mma_commit(bar_done);                 // (the lane that issued: the same one is elected every time)
+            drain(bar_done, 0);
+        }
+        tc_fence_before();
+        __syncthreads();
     }
     if (warp == 1) {
         tc_fence_after();

@@ -6,6 +6,7 @@ model is told how many buffers and barriers there are, so that the forms that de
 
 On the GPU: the debug build holds one warp up at a named place, many times longer than a tile takes; the bits have to be those of the normal build."""
 import ctypes as C
+import time
 
 import pytest
 import torch
@@ -120,7 +121,7 @@ def test_model_sees_a_wait_that_comes_too_late(rescale):
 
 # ---- the debug build, a warp held up ---------------------------------------------------------------------------------------
 
-PAUSES = {"maxima": 1, "weights": 2, "product": 3}
+PAUSES = {"maxima": 1, "weights": 2, "product": 3, "copy": 4}
 
 
 def _declare(lib):
@@ -201,6 +202,25 @@ def test_both_last_products_through_or_neither(libs, batch, where, warp):
     want = batch.call(normal)
     got = paused(check, where, warp, 20_000, lambda: batch.call(check))
     assert check.nm_check_status(None) == 0, "a wait ran out"
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("where,warp", [("maxima", 7), ("copy", 0), ("product", 1)])
+def test_an_expired_wait_ends_in_order(libs, batch, where, warp):
+    """A warp held up for longer than the others wait: they give up, what is under way ends, the kernel returns.  The call is disowned once, and the
+    next one is right."""
+    normal, check = libs
+    want = batch.call(normal)
+    paused(check, where, warp, 0, lambda: batch.call(check))
+    assert check.nm_check_status(None) == 0
+    t0 = time.monotonic()
+    paused(check, where, warp, 1_300_000_000, lambda: batch.call(check))
+    print("took %.3f s" % (time.monotonic() - t0))
+    assert 1.3 <= time.monotonic() - t0 < 10
+    assert check.nm_check_status(None) == -6 and check.nm_check_status(None) == 0
+    got = batch.call(check)
+    assert check.nm_check_status(None) == 0
     assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
