@@ -192,8 +192,8 @@ int nm_matmul_static(const void *A, const void *B, void *C, int M, int N, int K,
  *   lda, ldc elements between rows of A (>= K) and C (>= N)
  * Codes enter the products as exact integers, a group's sum is fp32 (sum a * code, minus 8 * sum a), the scale multiplies that
  * sum, and the result is rounded once.  bf16 tokens pass through fp16 times a power of two per 64 of them (32 for groups of 32):
- * exact down to 2^-29 of the largest of these, and to 2^-40 of it below.  A row of A that holds an infinity, a NaN or a bf16 of
- * 2^119 and more gives NaN in the whole row of C; other rows are not touched by it.  A row of A that starts on 16 bytes (A 16-byte
+ * exact down to 2^-28 of the largest of these, and to 2^-39 of it below.  A row of A that holds an infinity or a NaN gives NaN in
+ * the whole row of C; other rows are not touched by it.  A row of A that starts on 16 bytes (A 16-byte
  * aligned, lda and K multiples of 8) is read in 16-byte loads, any other element by element.  No workspace: k-splits meet in the shared memory of a cluster, in a fixed order, so equal calls give
  * equal bits and concurrent calls share nothing.  Honours nm_set_programmatic_launch
  * (codes and scales are then read ahead of the wait: not behind an nm_w4_quantize that is still running).

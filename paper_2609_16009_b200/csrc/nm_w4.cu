@@ -15,8 +15,9 @@
 //            the tokens are copied to shared memory and is what the group's accumulator starts from.  All of it is fp32; the
 //            error is that of adding terms of size 15 |a| instead of 8 |a|.
 //   tokens   fp16 as they are; bf16 ones times a power of two that puts the largest of the 64 (32) tokens that share a sum into
-//            fp16's last binade, 2^15: bf16's eight bits fit fp16's eleven, exactly down to 2^-29 of that largest value and to
-//            2^-40 of it absolutely below.  The inverse multiplies the sum together with the scale.
+//            fp16's last two binades, 2^14 to 2^16: bf16's eight bits fit fp16's eleven, exactly down to 2^-28 of that largest value and to
+//            2^-39 of it absolutely below.  The inverse is a square, one root of which multiplies the sum and one the scale: neither product
+//            leaves fp32 unless the result does, whatever the tokens' size.
 //   scale    multiplies the fp32 sum of its group; nothing is rounded before the output.
 //   split    a CTA is eight warps, wn of them side by side over units (a unit: one strip, or two for M > 8), 8 / wn along k; up
 //            to eight CTAs of a cluster split k further.  Two to four CTAs share an SM, so that one fills its tokens while another
@@ -106,7 +107,7 @@ __device__ __forceinline__ void ld_weights_if(uint4 &v, const void *p, bool ok)
 // 128, so that the eight 16-byte reads of a quarter warp (two rows, 64 bytes each) hit 32 different banks.  One pass: the eight
 // (four) lanes that hold the tokens of a sum find their largest and their sum by shuffles.  Per sum and eight rows goes to
 // s_start what lane (g, t) needs for tokens 2 t and 2 t + 1: where the accumulators start, -8 sum a in units of 2^-24, for row g
-// and 16 times that for row g + 8; and to s_inv the powers of two taken out of the tokens and the codes.  Every CTA begins at a place of its own
+// and 16 times that for row g + 8; and to s_inv the roots of the powers of two taken out of the tokens and the codes.  Every CTA begins at a place of its own
 // (`turn`, a multiple of 8): all of them read the same few rows, and in step they would queue for the same lines of L2.
 template <typename T, bool kG32>
 __device__ __forceinline__ void stage_tokens(unsigned char *s, float *s_start, float *s_inv, const W4Args &a, int k0, int n, int turn)
@@ -136,17 +137,17 @@ __device__ __forceinline__ void stage_tokens(unsigned char *s, float *s_start, f
             top = __vmaxu2(top, __shfl_xor_sync(mates, top, 1));
             top = __vmaxu2(top, __shfl_xor_sync(mates, top, 2));
             if constexpr (!kG32) top = __vmaxu2(top, __shfl_xor_sync(mates, top, 4));
-            // exponent e of the largest, at least -112; up = 2^(15 - e) and inv = 2^(24 - 15 + e), both inside fp32's range
-            const int e = max((int)(max(top >> 16, top & 0xffffu) >> 7) - 127, -112);
-            const float up = __uint_as_float((uint32_t)(127 + 15 - min(e, 119)) << 23);
-            inv = e >= 119 ? __uint_as_float(0x7fc00000u)          // (an infinity or NaN among them, or 2^119: the sum is NaN)
-                           : __uint_as_float((uint32_t)(127 + 9 + e) << 23);
+            // exponent e of the largest, at least -112, or one more to make it odd; up = 2^(15 - e), inv^2 = 2^(24 - 15 + e)
+            const int e = max((int)(max(top >> 16, top & 0xffffu) >> 7) - 127, -112) | 1;
+            const float up = __uint_as_float((uint32_t)(127 + 15 - min(e, 127)) << 23);
+            inv = e > 127 ? __uint_as_float(0x7fc00000u)           // (an infinity or a NaN among them: the sum is NaN)
+                          : __uint_as_float((uint32_t)(127 + (9 + e) / 2) << 23);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float x = __uint_as_float(w[j] << 16) * up, y = __uint_as_float(w[j] & 0xffff0000u) * up;
                 const __half2 h = __floats2half2_rn(x, y);
                 w[j] = *reinterpret_cast<const uint32_t *>(&h);
-                sum += x + y;                                      // (what fp16 drops of them is below 2^-40 of the largest)
+                sum += x + y;                                      // (what fp16 drops of them is below 2^-39 of the largest)
             }
         } else {
 #pragma unroll
@@ -213,7 +214,7 @@ __global__ void __launch_bounds__(w4_warps(kNT) * 32, kNT == 1 ? 2 : 1) w4_kerne
     extern __shared__ __align__(16) unsigned char s_raw[];
     unsigned char *s_tok = s_raw;
     float *s_start = reinterpret_cast<float *>(s_tok + a.M * a.pitch);     // [block (half)][eight tokens][t][4]: where the sums start
-    float *s_inv = s_start + a.chunk * kS * kNT * 16;                      // [block (half)][eight tokens][8]: the tokens' powers of two
+    float *s_inv = s_start + a.chunk * kS * kNT * 16;                      // [block (half)][eight tokens][8]: roots of the tokens' powers of two
     uint32_t *s_scale = reinterpret_cast<uint32_t *>(s_raw + a.tok_bytes); // [warp of the row][block (half)][side][8 pairs]
     float *s_red = reinterpret_cast<float *>(s_raw + a.tok_bytes + a.scale_bytes);
     const int tid = threadIdx.x, lane = tid & 31, g = lane >> 2, t = lane & 3;
@@ -291,8 +292,8 @@ __global__ void __launch_bounds__(w4_warps(kNT) * 32, kNT == 1 ? 2 : 1) w4_kerne
                         for (int n = 0; n < kNT; ++n) {
                             float2 inv = make_float2(1.f, 1.f);
                             if constexpr (kBf16) inv = *reinterpret_cast<const float2 *>(iv + ((j * kS + hs) * kNT + n) * 8);
-                            acc[r][n][0] = fmaf(f.x, sum[n][0] * inv.x, acc[r][n][0]); acc[r][n][1] = fmaf(f.x, sum[n][1] * inv.y, acc[r][n][1]);
-                            acc[r][n][2] = fmaf(f.y, sum[n][2] * inv.x, acc[r][n][2]); acc[r][n][3] = fmaf(f.y, sum[n][3] * inv.y, acc[r][n][3]);
+                            acc[r][n][0] = fmaf(f.x * inv.x, sum[n][0] * inv.x, acc[r][n][0]); acc[r][n][1] = fmaf(f.x * inv.y, sum[n][1] * inv.y, acc[r][n][1]);
+                            acc[r][n][2] = fmaf(f.y * inv.x, sum[n][2] * inv.x, acc[r][n][2]); acc[r][n][3] = fmaf(f.y * inv.y, sum[n][3] * inv.y, acc[r][n][3]);
                         }
                     }
                 }
