@@ -214,7 +214,9 @@ size_t nm_w4_scale_count(int N, int K, int group);        /* 16-bit elements */
 /*
  * Dense weights (B: K x N in NM_ROW_MAJOR or NM_COL_MAJOR, bf16 or fp16 by dtype) to 4 bits, and back.  Per column and group:
  *   scale = round16(max |w| / 7),  code = clamp(round(w / scale), -8, 7) + 8  (8 where scale is 0),  back = round16((code - 8) * scale)
- * N up to 64 * 65535, K up to 2^30.  Round to nearest even throughout; a NaN weight becomes code 0.  Columns and k beyond N and K are stored as zero weights.
+ * N up to 64 * 65535, K up to 2^30.  Round to nearest even throughout.  A NaN weight becomes code 0 (8 where scale is 0).
+ * An infinite weight makes its group's scale infinite and becomes code 15 or 0 by its sign, so it reads back as itself; the group's finite
+ * weights become code 8 and read back as NaN.  Columns and k beyond N and K are stored as zero weights.
  */
 int nm_w4_quantize(const void *B, void *packed, void *scales, int N, int K, int group, nm_dtype dtype, nm_layout layout_B,
                    nm_stream stream);

@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const uint16_t *_
                     }
                 } else {
 #pragma unroll
-                    for (int x = 0; x < 8; ++x) v[x] = sc > 0.f ? __fdiv_rn(v[x], sc) : 0.f;
+                    for (int x = 0; x < 8; ++x) v[x] = sc > 0.f ? (isinf(v[x]) ? v[x] : __fdiv_rn(v[x], sc)) : 0.f;      // (infinities keep their sign)
                 }
 #pragma unroll
                 for (int x = 0; x < 8; ++x) {                      // k = r0 + 4 (j & 1) + 2 (b & 1) + (b >> 1)
