@@ -78,7 +78,16 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
         if (mean > 0x1p-100 && mean < 0x1p100) {                   // from fp32's root by one Newton step, 2^-44 off
             const double r0 = (double)rsqrtf((float)mean);
             rd = fma(0.5 * r0, fma(-mean * r0, r0, 1.), r0);
-        } else rd = 1. / sqrt(mean);
+        } else {
+            // A row at an end of the range is brought to its middle by a power of two, or x * gamma, or the normaliser itself, leaves fp32
+            // though y does not.
+            const float shift = mean > 1. ? 0x1p-64f : 0x1p64f;
+#pragma unroll
+            for (int i = 0; i < kVecs; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y[i][j] *= shift;
+            rd = 1. / (sqrt(mean) * (double)shift);
+        }
         const float r = (float)rd, r_low = (float)(rd - (double)r);
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {

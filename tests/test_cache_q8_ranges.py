@@ -1,0 +1,31 @@
+"""Rows of the quantised cache whose values stand at the ends of bf16's range."""
+import numpy as np
+import pytest
+import torch
+
+from test_cache_q8 import records, rows_in
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("kv", [512, 1024])
+@pytest.mark.parametrize("power,eps", [(125, 1e-6), (51, 1e-6), (49, 0.0), (-49, 0.0), (-51, 0.0), (-126, 0.0), (-130, 0.0), (-130, 1e-30)])
+def test_write_normalises_rows_at_the_ends_of_the_range(power, eps, kv):
+    """The normalised row is ordinary; nothing on the way to it leaves fp32."""
+    import paper_2609_16009_b200 as nm
+    rope = 64
+    x, gamma, _ = rows_in(3, kv, rope, 11, std=2.0 ** power)
+    x[1, 5] = 0.0
+    if power == 125:
+        x[2, 7] = torch.finfo(torch.bfloat16).max
+    assert x.isfinite().all() and (x[:, :kv] != 0).sum() > 2 * kv
+    gamma = gamma * 3
+    cache = torch.zeros(3, nm.nm_mla_q8_row_bytes(kv, rope), dtype=torch.uint8, device="cuda")
+    nm.nm_mla_cache_write_q8(x.cuda(), gamma.cuda(), None, None, cache, 3, 3, kv, rope, eps)
+    v = x[:, :kv].double().numpy()
+    y = v / np.sqrt((v ** 2).mean(1, keepdims=True) + np.float64(np.float32(eps))) * gamma.double().numpy()
+    codes, _, s = records(cache.cpu().numpy(), kv, rope)
+    top = np.abs(y).max(1)
+    assert (top <= 448 * s[:, 0] * (1 + 2.0 ** -20)).all() and ((top >= 224 * s[:, 0] * (1 - 2.0 ** -20)) | (s[:, 0] == 2.0 ** -32)).all()
+    want = np.clip(y / s, -448, 448)
+    # half a step of e4m3: 2^-4 of the value, 2^-10 below its normal range; fp32 arithmetic before it 2^-20
+    assert np.all(np.abs(codes - want) <= np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10) * (1 + 2.0 ** -15))
