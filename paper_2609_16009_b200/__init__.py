@@ -145,8 +145,11 @@ def _ptr(t) -> int | None:
 
 
 def _stream(stream) -> int:
-    if stream is None:                             # the raw handle of torch's current stream, without building a Stream object
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    if stream is None:
+        # The handle of torch's current stream.  Where torch offers it raw that saves building a Stream object, 3 us a call; the name is not
+        # public, so nothing depends on it.  current_device initialises CUDA, and refuses a forked process, as current_stream does.
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
