@@ -72,7 +72,8 @@ int nm_debug_set_attention_wide(int tile_rows, int max_runs, int cluster);
 int nm_debug_set_step_kv_beside_attention(int enable);
 /* The debug build.  `python paper_2609_16009_b200/build.py --check` compiles the same sources with -DNM_BOUNDS_CHECK into
  * libnm_check.so: every hand-indexed global access of the narrow-product kernels (the CUDA-core row / column / scalar
- * kernels, the split-K gather, the token loads and the C / partial stores of the TMA ring and tensor-core kernels) is
+ * kernels, the split-K gather, the token loads and the C / partial stores of the TMA ring and tensor-core kernels) and of the
+ * kernels on compressed storage (4-bit product, packing, quantised cache and the attention over it) is
  * checked against the extent of the operand it belongs to; an access outside raises a bit in the device status word
  * (nm_check_status returns NM_ERR_BOUNDS) and is skipped - loads yield zero, stores do nothing, nothing faults.  The paper
  * has no counterpart; it stands in for a memory checker on machines where none can be run.

@@ -12,6 +12,15 @@ namespace nm {
 // it; nm_check_status() reads and clears it.  Kernels receive its address as an argument.
 constexpr unsigned kStatusWaitExpired = 1u;
 unsigned *device_status_ptr();        // host: address of the status word on the current device (nullptr on error)
+// The same for kernels whose only use for it is the debug build's checks.
+inline unsigned *bounds_status_ptr()
+{
+#ifdef NM_BOUNDS_CHECK
+    return device_status_ptr();
+#else
+    return nullptr;
+#endif
+}
 
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 

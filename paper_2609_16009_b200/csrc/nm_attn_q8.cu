@@ -78,6 +78,7 @@ struct PassArgs {
 #ifdef NM_BOUNDS_CHECK
     int pause_where, pause_warp;                   // see nm_debug_set_attention_q8_pause
     unsigned pause_ns;
+    Span in_records[1 + kMaxT], in_q, in_mult, in_ml, in_O;       // extents of the operands
 #endif
 };
 struct MergeArgs {
@@ -87,6 +88,10 @@ struct MergeArgs {
     int H, tile_rows;                              // query rows of a prefix item
     int prefix_row[kMaxT], own_row[kMaxT];         // first partial row of each query tile of the prefix, of each sequence
     short prefix_n[kMaxT], own_n[kMaxT];           // and their parts
+    unsigned *status;                              // of the debug build's checks, as the rest
+#ifdef NM_BOUNDS_CHECK
+    Span in_ml, in_O, in_bf16, in_f32, in_lse;
+#endif
 };
 
 __device__ __forceinline__ float ex2(float x)
@@ -98,16 +103,19 @@ __device__ __forceinline__ float ex2(float x)
 
 // ---- queries ---------------------------------------------------------------------------------------------------------
 __global__ void __launch_bounds__(128) q8_prepare_kernel(const uint16_t *__restrict__ Q, long q_stride, int T, int H, unsigned char *__restrict__ q_rows,
-                                                         float *__restrict__ q_mult, float scale_log2)
+                                                         float *__restrict__ q_mult, float scale_log2, unsigned *status)
 {
+    const Span in_q = make_span(Q, 2 * ((T - 1) * (size_t)q_stride + H * (kKv + kRope))), in_rows = make_span(q_rows, (size_t)T * H * kQRow),
+               in_mult = make_span(q_mult, 4 * (size_t)T * H);
+    (void)in_q; (void)in_rows; (void)in_mult; (void)status;        // (the debug build's)
     pdl_launch_dependents();
     const int row = blockIdx.x * 4 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (row >= T * H) return;
     const int t = row / H, h = row - t * H;
     const uint16_t *q = Q + t * q_stride + (long)h * (kKv + kRope);
-    const uint4 a = *reinterpret_cast<const uint4 *>(q + 16 * lane), b = *reinterpret_cast<const uint4 *>(q + 16 * lane + 8);
+    const uint4 a = NM_LD(reinterpret_cast<const uint4 *>(q + 16 * lane), in_q, status), b = NM_LD(reinterpret_cast<const uint4 *>(q + 16 * lane + 8), in_q, status);
     const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    const uint32_t key = *reinterpret_cast<const uint32_t *>(q + kKv + 2 * lane);
+    const uint32_t key = NM_LD(reinterpret_cast<const uint32_t *>(q + kKv + 2 * lane), in_q, status);
     uint32_t top = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) top = __vmaxu2(top, w[j] & 0x7fff7fffu);
@@ -141,13 +149,13 @@ __global__ void __launch_bounds__(128) q8_prepare_kernel(const uint16_t *__restr
             lo[j] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(x[2 * p] - f.x, x[2 * p + 1] - f.y), __NV_SATFINITE, __NV_E4M3) << (16 * p);
         }
     }
-    *reinterpret_cast<uint4 *>(out + 16 * lane) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-    *reinterpret_cast<uint4 *>(out + kKv + 16 * lane) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    NM_ST(reinterpret_cast<uint4 *>(out + 16 * lane), make_uint4(hi[0], hi[1], hi[2], hi[3]), in_rows, status);
+    NM_ST(reinterpret_cast<uint4 *>(out + kKv + 16 * lane), make_uint4(lo[0], lo[1], lo[2], lo[3]), in_rows, status);
     const float k0 = __uint_as_float(key << 16) * inv, k1 = __uint_as_float(key & 0xffff0000u) * inv;
-    *reinterpret_cast<uint32_t *>(out + 2 * kKv + 4 * lane) =
-        (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(k0)) | ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(k1)) << 16);
+    const uint32_t k01 = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(k0)) | ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(k1)) << 16);
+    NM_ST(reinterpret_cast<uint32_t *>(out + 2 * kKv + 4 * lane), k01, in_rows, status);
     // an infinity or a NaN in a head makes its scores NaN (and nobody else's)
-    if (lane == 0) q_mult[row] = odd ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(127 + e) << 23) * scale_log2;
+    if (lane == 0) NM_ST(&q_mult[row], odd ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)(127 + e) << 23) * scale_log2, in_mult, status);
 }
 
 // ---- the pass ----------------------------------------------------------------------------------------------------------
@@ -226,11 +234,13 @@ __device__ __noinline__ void drain(uint32_t bar, uint32_t par)
 
 // Debug build only: one warp of every CTA is held up at a named place, so that a test can show that the order of what the warps tell each
 // other does not hang on their pace.  Bounded by the clock.
-constexpr int kPauseAfterMaxima = 1;               // a softmax warp, behind the barrier of a tile, before it reads its rows' maxima
-constexpr int kPauseAfterWeights = 2;              // a softmax warp that has handed in the weights of an item's last tile
-constexpr int kPauseBeforeProduct = 3;             // the issuing warp, with all weights of a tile in and its P * V not issued
-constexpr int kPauseBeforeCopy = 4;                // the copying thread, a slot free and its copy not begun
-constexpr int kPausePlaces = 4;
+enum Pause {
+    kPauseAfterMaxima = 1,                         // a softmax warp, behind the barrier of a tile, before it reads its rows' maxima
+    kPauseAfterWeights,                            // a softmax warp that has handed in the weights of an item's last tile
+    kPauseBeforeProduct,                           // the issuing warp, with all weights of a tile in and its P * V not issued
+    kPauseBeforeCopy,                              // the copying thread, a slot free and its copy not begun
+    kPausePlaces = kPauseBeforeCopy
+};
 #ifdef NM_BOUNDS_CHECK
 __device__ __noinline__ void pause_here(unsigned ns)
 {
@@ -443,7 +453,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
         };
         auto row_scale = [&](int t) {
             const int row = row0 + t * kR + entry;
-            return entry < kR && row < row1 ? __ldg(reinterpret_cast<const float *>(records + (long)row * kRec + kKv + 2 * kRope)) : 0.f;
+            const float *s = reinterpret_cast<const float *>(records + (long)row * kRec + kKv + 2 * kRope);
+            return entry < kR && row < row1 && NM_INSIDE(s, 4, a.in_records[it.source], a.status) ? __ldg(s) : 0.f;
         };
         const float s0 = row_scale(0), s1 = row_scale(1);
         float s_next = row_scale(2);
@@ -457,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
                 uint32_t v[16];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const uint4 u = q_row < a.total_q ? src[4 * i + j] : make_uint4(0u, 0u, 0u, 0u);
+                    const uint4 u = q_row < a.total_q ? NM_LD(&src[4 * i + j], a.in_q, a.status) : make_uint4(0u, 0u, 0u, 0u);
                     v[4 * j] = u.x; v[4 * j + 1] = u.y; v[4 * j + 2] = u.z; v[4 * j + 3] = u.w;
                 }
                 tmem_st16(lanes + kColQ + 16 * i, v);
@@ -466,7 +477,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
             tc_fence_before();
             mbar_arrive(bar_qt);
         }
-        const float mult = r < it.n_q ? a.q_mult[it.q_row + r] : 0.f;
+        const float mult = r < it.n_q ? NM_LD(&a.q_mult[it.q_row + r], a.in_mult, a.status) : 0.f;
         if (entry < kR) { s_table[entry] = row_entry(s0); s_table[kR + entry] = row_entry(s1); }
         named_barrier_sync(1, kSoftmax);
         float m = -INFINITY, l = 0.f, l1 = 0.f;
@@ -584,7 +595,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
         s_pair[0][set][r] = l + l1;                                // (the next item's maxima come behind its first barrier, which every reader meets)
         named_barrier_sync(1, kSoftmax);
         if (half == 0 && set == 0 && r < it.n_q)
-            *reinterpret_cast<float2 *>(a.ml + 2 * (long)(it.out_row + r)) = make_float2(m, s_pair[0][0][r] + s_pair[0][1][r]);
+            NM_ST(reinterpret_cast<float2 *>(a.ml + 2 * (long)(it.out_row + r)), make_float2(m, s_pair[0][0][r] + s_pair[0][1][r]), a.in_ml, a.status);
         float4 *corner = reinterpret_cast<float4 *>(smem + (4 * set + quad) * 8192);        // [32 rows][16 float4], the index XOR-ed with row & 15
         for (int c0 = 128 * set; c0 < 128 * set + 128; c0 += 64) {
             uint32_t o[2][32];
@@ -602,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
             for (int i = lane; i < 32 * 16; i += 32) {
                 const int rr = i >> 4, f = i & 15, q = quad * 32 + rr;
                 if (q < it.n_q)
-                    *reinterpret_cast<float4 *>(a.O + (long)(it.out_row + q) * kKv + 256 * half + c0 + 4 * f) = corner[rr * 16 + (f ^ (rr & 15))];
+                    NM_ST(reinterpret_cast<float4 *>(a.O + (long)(it.out_row + q) * kKv + 256 * half + c0 + 4 * f), corner[rr * 16 + (f ^ (rr & 15))], a.in_O, a.status);
             }
         }
         // the next item's queries may come: into the place just used, and (from this warp's threads) into TMEM
@@ -654,7 +665,7 @@ __global__ void __launch_bounds__(kGroups * 128) q8_merge_kernel(const __grid_co
     for (int i = tid; i < n; i += kMergeThreads) {
         // prefix: item (tile of query rows, part); own: item (sequence, part)
         const int row = i < n_prefix ? a.prefix_row[q_tile] + i * a.tile_rows + blockIdx.x % kM : a.own_row[t] + (i - n_prefix) * a.H + h;
-        const float2 ml = *reinterpret_cast<const float2 *>(a.ml + 2 * (long)row);
+        const float2 ml = NM_LD(reinterpret_cast<const float2 *>(a.ml + 2 * (long)row), a.in_ml, a.status);
         s_row[i] = row;
         s_w[i] = ml.x; s_l[i] = ml.y;
         mx = fmaxf(mx, ml.x);
@@ -669,7 +680,7 @@ __global__ void __launch_bounds__(kGroups * 128) q8_merge_kernel(const __grid_co
 #pragma unroll 4
     for (int i = group; i < n; i += kGroups) {
         const float w = ex2(s_w[i] - mx);
-        const float4 v = *reinterpret_cast<const float4 *>(a.O + (long)s_row[i] * kKv + 4 * x);
+        const float4 v = NM_LD(reinterpret_cast<const float4 *>(a.O + (long)s_row[i] * kKv + 4 * x), a.in_O, a.status);
         acc.x = fmaf(w, v.x, acc.x); acc.y = fmaf(w, v.y, acc.y); acc.z = fmaf(w, v.z, acc.z); acc.w = fmaf(w, v.w, acc.w);
     }
     if constexpr (kGroups > 1) {
@@ -687,13 +698,13 @@ __global__ void __launch_bounds__(kGroups * 128) q8_merge_kernel(const __grid_co
     const float inv = n > 0 ? 1.f / total : 0.f;                   // no rows: zeros, and minus infinity below
     const long at = (long)blockIdx.x * kKv + 4 * x;
     acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
-    if (a.o_f32) *reinterpret_cast<float4 *>(a.o_f32 + at) = acc;
+    if (a.o_f32) NM_ST(reinterpret_cast<float4 *>(a.o_f32 + at), acc, a.in_f32, a.status);
     if (a.o_bf16) {
         const uint32_t lo = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(acc.x)) | ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(acc.y)) << 16);
         const uint32_t hi = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(acc.z)) | ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(acc.w)) << 16);
-        *reinterpret_cast<uint2 *>(a.o_bf16 + at) = make_uint2(lo, hi);
+        NM_ST(reinterpret_cast<uint2 *>(a.o_bf16 + at), make_uint2(lo, hi), a.in_bf16, a.status);
     }
-    if (a.lse && tid == 0) a.lse[blockIdx.x] = n > 0 ? (mx - kHeadroom + log2f(total)) * 0.6931471805599453f : -INFINITY;
+    if (a.lse && tid == 0) NM_ST(&a.lse[blockIdx.x], n > 0 ? (mx - kHeadroom + log2f(total)) * 0.6931471805599453f : -INFINITY, a.in_lse, a.status);
 }
 
 #ifdef NM_BOUNDS_CHECK
@@ -865,9 +876,18 @@ int nm_mla_attention_q8(const void *Q, long q_stride, const void *prefix, long p
         out_row += w.out_rows;
     });
     pa.first[pairs] = (short)items;
+    ma.status = bounds_status_ptr();
+#ifdef NM_BOUNDS_CHECK
+    ma.in_ml = make_span(pa.ml, 8 * (size_t)out_row); ma.in_O = make_span(pa.O, 4 * (size_t)out_row * kKv);
+    ma.in_bf16 = make_span(o_bf16, 2 * (size_t)total_q * kKv); ma.in_f32 = make_span(o_f32, 4 * (size_t)total_q * kKv); ma.in_lse = make_span(lse, 4 * (size_t)total_q);
+#endif
     if (items) {
         pa.status = device_status_ptr();
 #ifdef NM_BOUNDS_CHECK
+        for (int i = 0; i <= T; ++i)
+            pa.in_records[i] = i == 0 ? make_span(prefix, (size_t)prefix_rows * kRec) : make_span(static_cast<const unsigned char *>(cache) + (long)(i - 1) * cache_stride, (size_t)seq_lens[i - 1] * kRec);
+        pa.in_q = make_span(pa.q_rows, (size_t)total_q * kQRow); pa.in_mult = make_span(pa.q_mult, 4 * (size_t)total_q);
+        pa.in_ml = ma.in_ml; pa.in_O = ma.in_O;
         const unsigned long long pause = g_q8_pause.load(std::memory_order_relaxed);
         pa.pause_ns = (unsigned)pause; pa.pause_warp = (int)(pause >> 32) & 0xff; pa.pause_where = (int)(pause >> 40);
 #endif
@@ -883,7 +903,7 @@ int nm_mla_attention_q8(const void *Q, long q_stride, const void *prefix, long p
         cudaError_t e = ensure_dynamic_smem(attn_q8_kernel, kSmemBytes, configured);
         if (e != cudaSuccess) return record_cuda_error(e, "quantised attention kernel attribute");
         q8_prepare_kernel<<<ceil_div(total_q, 4), 128, 0, s>>>(static_cast<const uint16_t *>(Q), q_stride, T, H, ws + lay.q_rows,
-                                                              reinterpret_cast<float *>(ws + lay.mult), scale * 1.4426950408889634f);
+                                                              reinterpret_cast<float *>(ws + lay.mult), scale * 1.4426950408889634f, bounds_status_ptr());
         e = cudaGetLastError();
         if (e == cudaSuccess) e = launch_after(attn_q8_kernel, 2 * pairs, kThreads, kSmemBytes, s, pa);
         if (e != cudaSuccess) return record_cuda_error(e, "quantised attention launch");

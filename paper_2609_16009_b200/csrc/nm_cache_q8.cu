@@ -31,13 +31,16 @@ template <int kVecs>
 __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uint16_t *__restrict__ ckr, long stride, const uint16_t *__restrict__ gamma,
                                                                        const float *__restrict__ cos_sin, const int64_t *__restrict__ rows,
                                                                        unsigned char *__restrict__ cache, long n_cache_rows, int T, int kv, int rope, double inv_kv,
-                                                                       float eps)
+                                                                       float eps, unsigned *status)
 {
+    const Span in_rows = make_span(ckr, 2 * ((T - 1) * (size_t)stride + kv + rope)), in_cache = make_span(cache, (size_t)n_cache_rows * q8_row_bytes(kv, rope)),
+               in_gamma = make_span(gamma, 2 * (size_t)kv), in_angles = make_span(cos_sin, 4 * (size_t)T * rope);
+    (void)in_rows; (void)in_cache; (void)in_gamma; (void)in_angles; (void)status;      // (the debug build's)
     const int t = blockIdx.x * kWarpsQ8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     pdl_launch_dependents();
     if (t >= T) return;
     pdl_wait_prior_grids();
-    const int64_t row = rows ? rows[t] : t;
+    const int64_t row = rows ? NM_LD(&rows[t], make_span(rows, 8 * (size_t)T), status) : t;
     if (row < 0 || row >= n_cache_rows) return;                    // a padding token, or no such row: written nowhere
     const uint16_t *x = ckr + (long)t * stride;
     const int vecs = kv / 8;
@@ -46,10 +49,10 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
     if (gamma) {
 #pragma unroll
         for (int i = 0; i < kVecs; ++i)
-            if (lane + 32 * i < vecs) weight[i] = __ldg(reinterpret_cast<const uint4 *>(gamma + 8 * (lane + 32 * i)));
+            if (lane + 32 * i < vecs) weight[i] = NM_LDG16(reinterpret_cast<const uint4 *>(gamma + 8 * (lane + 32 * i)), in_gamma, status);
     }
-    auto key_at = [&](int p) { return *reinterpret_cast<const uint32_t *>(x + kv + 2 * p); };
-    auto angle_at = [&](int p) { return cos_sin ? *reinterpret_cast<const float2 *>(cos_sin + (long)t * rope + 2 * p) : make_float2(1.f, 0.f); };
+    auto key_at = [&](int p) { return NM_LD(reinterpret_cast<const uint32_t *>(x + kv + 2 * p), in_rows, status); };
+    auto angle_at = [&](int p) { return cos_sin ? NM_LD(reinterpret_cast<const float2 *>(cos_sin + (long)t * rope + 2 * p), in_angles, status) : make_float2(1.f, 0.f); };
     const bool has_key = lane < rope / 2;
     const uint32_t key0 = has_key ? key_at(lane) : 0u;
     const float2 angle0 = has_key ? angle_at(lane) : make_float2(1.f, 0.f);
@@ -59,7 +62,7 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
     for (int i = 0; i < kVecs; ++i) {
         const int v = lane + 32 * i;
         uint4 u = make_uint4(0u, 0u, 0u, 0u);
-        if (v < vecs) u = *reinterpret_cast<const uint4 *>(x + 8 * v);
+        if (v < vecs) u = NM_LD(reinterpret_cast<const uint4 *>(x + 8 * v), in_rows, status);
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) { y[i][2 * j] = bf_lo(w[j]); y[i][2 * j + 1] = bf_hi(w[j]); }
@@ -126,7 +129,7 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
             const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(y[i][4 * j + 2] * inv, y[i][4 * j + 3] * inv), __NV_SATFINITE, __NV_E4M3);
             c[j] = lo | (hi << 16);
         }
-        *reinterpret_cast<uint2 *>(rec + 8 * v) = make_uint2(c[0], c[1]);
+        NM_ST(reinterpret_cast<uint2 *>(rec + 8 * v), make_uint2(c[0], c[1]), in_cache, status);
     }
     for (int p = lane; p < rope / 2; p += 32) {
         const uint32_t w = p == lane ? key0 : key_at(p);
@@ -136,27 +139,29 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
             const float ra = a * cs.x - b * cs.y, rb = a * cs.y + b * cs.x;
             a = ra; b = rb;
         }
-        *reinterpret_cast<uint32_t *>(rec + kv + 4 * p) = pack_bf16(a * inv, b * inv);
+        NM_ST(reinterpret_cast<uint32_t *>(rec + kv + 4 * p), pack_bf16(a * inv, b * inv), in_cache, status);
     }
-    if (lane == 0) *reinterpret_cast<float4 *>(rec + kv + 2 * rope) = make_float4(s, 0.f, 0.f, 0.f);
+    if (lane == 0) NM_ST(reinterpret_cast<float4 *>(rec + kv + 2 * rope), make_float4(s, 0.f, 0.f, 0.f), in_cache, status);
 }
 
 __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_read_q8_kernel(const unsigned char *__restrict__ cache, long n_cache_rows, const int64_t *__restrict__ rows,
-                                                                      uint16_t *__restrict__ out, long stride, int n, int kv, int rope)
+                                                                      uint16_t *__restrict__ out, long stride, int n, int kv, int rope, unsigned *status)
 {
+    const Span in_out = make_span(out, 2 * ((n - 1) * (size_t)stride + kv + rope)), in_cache = make_span(cache, (size_t)n_cache_rows * q8_row_bytes(kv, rope));
+    (void)in_out; (void)in_cache; (void)status;                    // (the debug build's)
     const int i = blockIdx.x * kWarpsQ8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     pdl_launch_dependents();
     if (i >= n) return;
     pdl_wait_prior_grids();
-    const int64_t row = rows ? rows[i] : i;
+    const int64_t row = rows ? NM_LD(&rows[i], make_span(rows, 8 * (size_t)n), status) : i;
     uint16_t *o = out + (long)i * stride;
     const bool there = row >= 0 && row < n_cache_rows;             // no such row: zeros
     const unsigned char *rec = cache + (there ? row : 0) * (long)q8_row_bytes(kv, rope);
-    const float s = there ? *reinterpret_cast<const float *>(rec + kv + 2 * rope) : 0.f;
+    const float s = there ? NM_LD(reinterpret_cast<const float *>(rec + kv + 2 * rope), in_cache, status) : 0.f;
     for (int v = lane; v < kv / 16; v += 32) {
         uint4 r[2] = {};
         if (there) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(rec + 16 * v);
+            const uint4 u = NM_LD(reinterpret_cast<const uint4 *>(rec + 16 * v), in_cache, status);
             const uint32_t w[4] = {u.x, u.y, u.z, u.w};
             uint32_t b[8];
 #pragma unroll
@@ -167,17 +172,17 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_read_q8_kernel(const unsi
             }
             r[0] = make_uint4(b[0], b[1], b[2], b[3]); r[1] = make_uint4(b[4], b[5], b[6], b[7]);
         }
-        *reinterpret_cast<uint4 *>(o + 16 * v) = r[0];
-        *reinterpret_cast<uint4 *>(o + 16 * v + 8) = r[1];
+        NM_ST(reinterpret_cast<uint4 *>(o + 16 * v), r[0], in_out, status);
+        NM_ST(reinterpret_cast<uint4 *>(o + 16 * v + 8), r[1], in_out, status);
     }
     for (int v = lane; v < rope / 8; v += 32) {
         uint4 r = make_uint4(0u, 0u, 0u, 0u);
         if (there) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(rec + kv + 16 * v);
+            const uint4 u = NM_LD(reinterpret_cast<const uint4 *>(rec + kv + 16 * v), in_cache, status);
             r = make_uint4(pack_bf16(bf_lo(u.x) * s, bf_hi(u.x) * s), pack_bf16(bf_lo(u.y) * s, bf_hi(u.y) * s),
                            pack_bf16(bf_lo(u.z) * s, bf_hi(u.z) * s), pack_bf16(bf_lo(u.w) * s, bf_hi(u.w) * s));
         }
-        *reinterpret_cast<uint4 *>(o + kv + 8 * v) = r;
+        NM_ST(reinterpret_cast<uint4 *>(o + kv + 8 * v), r, in_out, status);
     }
 }
 
@@ -217,8 +222,8 @@ int nm_mla_cache_write_q8(const void *ckr, long ckr_stride, const void *gamma, c
     cudaStream_t s = (cudaStream_t)stream;
     const uint16_t *x = static_cast<const uint16_t *>(ckr), *gm = static_cast<const uint16_t *>(gamma);
     unsigned char *c = static_cast<unsigned char *>(cache);
-    const cudaError_t e = kv_lora <= 512 ? launch_rows(cache_write_q8_kernel<2>, T, s, x, ckr_stride, gm, cos_sin, rows, c, n_cache_rows, T, kv_lora, rope, 1. / kv_lora, eps)
-                                         : launch_rows(cache_write_q8_kernel<4>, T, s, x, ckr_stride, gm, cos_sin, rows, c, n_cache_rows, T, kv_lora, rope, 1. / kv_lora, eps);
+    const cudaError_t e = kv_lora <= 512 ? launch_rows(cache_write_q8_kernel<2>, T, s, x, ckr_stride, gm, cos_sin, rows, c, n_cache_rows, T, kv_lora, rope, 1. / kv_lora, eps, bounds_status_ptr())
+                                         : launch_rows(cache_write_q8_kernel<4>, T, s, x, ckr_stride, gm, cos_sin, rows, c, n_cache_rows, T, kv_lora, rope, 1. / kv_lora, eps, bounds_status_ptr());
     return e == cudaSuccess ? NM_OK : record_cuda_error(e, "quantised cache write launch");
 }
 
@@ -229,7 +234,7 @@ int nm_mla_cache_read_q8(const void *cache, long n_cache_rows, const int64_t *ro
     if (!q8_dims_ok(kv_lora, rope)) return NM_ERR_UNSUPPORTED;
     if (((uintptr_t)cache & 15u) || ((uintptr_t)out & 15u) || out_stride % 8 || ((uintptr_t)rows & 7u)) return NM_ERR_ALIGNMENT;
     const cudaError_t e = launch_rows(cache_read_q8_kernel, n, (cudaStream_t)stream, static_cast<const unsigned char *>(cache), n_cache_rows, rows,
-                                      static_cast<uint16_t *>(out), out_stride, n, kv_lora, rope);
+                                      static_cast<uint16_t *>(out), out_stride, n, kv_lora, rope, bounds_status_ptr());
     return e == cudaSuccess ? NM_OK : record_cuda_error(e, "quantised cache read launch");
 }
 

@@ -95,7 +95,7 @@ __device__ __forceinline__ uint4 ld_stream16(const void *p) {
 }
 
 // ---- debug build (-DNM_BOUNDS_CHECK, libnm_check.so) -----------------------------------------------------------
-// Every hand-indexed global access of the narrow-product kernels names the operand it belongs to; the debug build
+// Every hand-indexed global access of the narrow-product kernels and of the kernels on compressed storage names the operand it belongs to; the debug build
 // checks the address against that operand's extent first.  An access outside it raises kStatusOutOfBounds in the
 // device status word (nm_check_status then returns NM_ERR_BOUNDS) and is SKIPPED - a load yields zeros, a store does
 // nothing - so nothing faults and nothing traps.  (The tiled TMA copies need no such build: the copy engine clips them
@@ -123,12 +123,14 @@ template <typename T> __device__ __forceinline__ T nm_checked_load(const T *p, S
 #define NM_LD(p, span, st) ::nm::nm_checked_load((p), (span), (st))
 #define NM_LD_CG(p, span, st) (::nm::nm_inside((p), sizeof(float), (span), (st)) ? ::nm::ld_cg(p) : 0.f)
 #define NM_ST(p, v, span, st) do { if (::nm::nm_inside((p), sizeof(*(p)), (span), (st))) *(p) = (v); } while (0)
+#define NM_INSIDE(p, bytes, span, st) ::nm::nm_inside((p), (bytes), (span), (st))
 #else
 #define NM_LD_STREAM16(p, span, st) ::nm::ld_stream16(p)
 #define NM_LDG16(p, span, st) __ldg(p)
 #define NM_LD(p, span, st) (*(p))
 #define NM_LD_CG(p, span, st) ::nm::ld_cg(p)
 #define NM_ST(p, v, span, st) (*(p) = (v))
+#define NM_INSIDE(p, bytes, span, st) true         // for accesses by other instructions: they happen where this holds
 #endif
 
 // Load that bypasses L1 (data written by other SMs in the same launch).

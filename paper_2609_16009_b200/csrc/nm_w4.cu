@@ -66,7 +66,13 @@ struct W4Args {
     int tok_bytes;                                 // of the tokens, the starts of the sums and the powers of two
     int scale_bytes;
     int vec;                                       // token rows start on 16 bytes
+    unsigned *status;                              // of the debug build's checks
 };
+// extents of the operands, for the same
+[[maybe_unused]] __device__ __forceinline__ Span span_of_tokens(const W4Args &a) { return make_span(a.A, 2 * ((a.M - 1) * (size_t)a.lda + a.K)); }
+[[maybe_unused]] __device__ __forceinline__ Span span_of_codes(const W4Args &a) { return make_span(a.packed, (size_t)a.nb * a.kb * kW4BlockBytes); }
+[[maybe_unused]] __device__ __forceinline__ Span span_of_scales(const W4Args &a) { return make_span(a.scales, (size_t)a.groups * a.nb * kW4Cols * 2); }
+template <typename TO> [[maybe_unused]] __device__ __forceinline__ Span span_of_result(const W4Args &a) { return make_span(a.C, sizeof(TO) * ((a.M - 1) * (size_t)a.ldc + a.N)); }
 
 // eight codes of a word -> the four registers of the weight operand
 __device__ __forceinline__ void unpack_codes(uint32_t w, uint32_t (&r)[4])
@@ -122,12 +128,14 @@ __device__ __forceinline__ void stage_tokens(unsigned char *s, float *s_start, f
         w[0] = w[1] = w[2] = w[3] = 0u;
         if (a.vec) {
             if (k < a.K) {
-                const uint4 x = __ldg(reinterpret_cast<const uint4 *>(src));
+                const uint4 x = NM_LDG16(reinterpret_cast<const uint4 *>(src), span_of_tokens(a), a.status);
                 w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = (k + 2 * j < a.K ? (uint32_t)src[2 * j] : 0u) | ((k + 2 * j + 1 < a.K ? (uint32_t)src[2 * j + 1] : 0u) << 16);
+            for (int j = 0; j < 4; ++j)
+                w[j] = (k + 2 * j < a.K ? (uint32_t)NM_LD(src + 2 * j, span_of_tokens(a), a.status) : 0u) |
+                       ((k + 2 * j + 1 < a.K ? (uint32_t)NM_LD(src + 2 * j + 1, span_of_tokens(a), a.status) : 0u) << 16);
         }
     };
     auto finish = [&](int c, int m, uint32_t (&w)[4]) {
@@ -239,7 +247,10 @@ __global__ void __launch_bounds__(w4_warps(kNT) * 32, kNT == 1 ? 2 : 1) w4_kerne
 #pragma unroll
         for (int i = 0; i < kDepth; ++i)
 #pragma unroll
-            for (int r = 0; r < kSide; ++r) ld_weights_if(w[i][r], next + r * side_step + i * 32, b0 + i < b1);
+            for (int r = 0; r < kSide; ++r) {
+                const uint4 *p = next + r * side_step + i * 32;
+                ld_weights_if(w[i][r], p, b0 + i < b1 && NM_INSIDE(p, 16, span_of_codes(a), a.status));
+            }
         next += kDepth * 32;
         if (c0 > cta0) __syncthreads();                            // the chunk before has been read
         // the scales of the warp's own blocks - a block has its own entry even where it shares a scale, so that it is found without arithmetic
@@ -247,7 +258,8 @@ __global__ void __launch_bounds__(w4_warps(kNT) * 32, kNT == 1 ? 2 : 1) w4_kerne
         for (int j = b0 * (kS * kSide) + (lane >> 3); j < b1 * (kS * kSide); j += 4) {
             const int side = both ? j & 1 : 0, half = kG32 ? (j / kSide) & 1 : 0, blk = c0 + j / (kS * kSide);
             const int grp = kG32 ? min(2 * blk + half, a.groups - 1) : blk >> a.group_shift;
-            cp_async4(smem_u32(sw + j * 8 + (lane & 7)), a.scales + (size_t)(unsigned)grp * (unsigned)(a.nb * 8) + (unsigned)(strip + side) * 8u + (lane & 7));
+            const uint32_t *p = a.scales + (size_t)(unsigned)grp * (unsigned)(a.nb * 8) + (unsigned)(strip + side) * 8u + (lane & 7);
+            if (NM_INSIDE(p, 4, span_of_scales(a), a.status)) cp_async4(smem_u32(sw + j * 8 + (lane & 7)), p);
         }
         if (c0 == cta0) pdl_wait_prior_grids();                    // weights may come early, tokens not
         stage_tokens<T, kG32>(s_tok, s_start, s_inv, a, c0 * kW4Rows, R * kW4Rows, (int)((long)R * tile / gridDim.x) * 8);
@@ -311,7 +323,7 @@ __global__ void __launch_bounds__(w4_warps(kNT) * 32, kNT == 1 ? 2 : 1) w4_kerne
             for (int i = 0; i < kDepth; ++i) {
                 multiply(w[i], i);
 #pragma unroll
-                for (int r = 0; r < kSide; ++r) w[i][r] = ld_stream16(next + r * side_step + i * 32);
+                for (int r = 0; r < kSide; ++r) w[i][r] = NM_LD_STREAM16(next + r * side_step + i * 32, span_of_codes(a), a.status);
             }
             turn();
         }
@@ -320,7 +332,10 @@ __global__ void __launch_bounds__(w4_warps(kNT) * 32, kNT == 1 ? 2 : 1) w4_kerne
             for (int i = 0; i < kDepth; ++i) {
                 if (i < left) multiply(w[i], i);
 #pragma unroll
-                for (int r = 0; r < kSide; ++r) ld_weights_if(w[i][r], next + r * side_step + i * 32, kDepth + i < left);
+                for (int r = 0; r < kSide; ++r) {
+                    const uint4 *p = next + r * side_step + i * 32;
+                    ld_weights_if(w[i][r], p, kDepth + i < left && NM_INSIDE(p, 16, span_of_codes(a), a.status));
+                }
             }
             turn();
         }
@@ -382,7 +397,7 @@ __global__ void __launch_bounds__(w4_warps(kNT) * 32, kNT == 1 ? 2 : 1) w4_kerne
     const long n0 = (long)tile * cols;
     for (int i = tid; i < a.M * cols; i += kThreads) {
         const int m = i >> cols_log2, c = i & (cols - 1);
-        if (n0 + c < a.N) C[(long)m * a.ldc + n0 + c] = round_out<TO>(s_red[i]);
+        if (n0 + c < a.N) NM_ST(&C[(long)m * a.ldc + n0 + c], round_out<TO>(s_red[i]), span_of_result<TO>(a), a.status);
     }
 }
 
@@ -518,6 +533,7 @@ int nm_matmul_w4(const void *A, const void *packed, const void *scales, void *C,
     a.groups = (int)(((long)K + group - 1) / group);
     // 16-byte token loads want 16-byte aligned rows and a K that no such load straddles
     a.vec = !((uintptr_t)A & 15u) && lda % 8 == 0 && K % 8 == 0;
+    a.status = bounds_status_ptr();
     const bool pdl = programmatic_launch_enabled(), g32 = group < kW4Rows;
     cudaStream_t s = (cudaStream_t)stream;
     const cudaError_t e = dtype == NM_F16            ? dispatch_w4<f16_t, f16_t>(a, g32, s, pdl)

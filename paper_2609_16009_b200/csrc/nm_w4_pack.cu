@@ -10,6 +10,7 @@
 // some ten per weight: a division each and conversions to integers and back took 145 us.
 #include <type_traits>
 
+#include "nm_async.cuh"
 #include "nm_w4.cuh"
 
 namespace nm {
@@ -56,9 +57,14 @@ template <bool kColMajor, int kRows> struct Tile {
     __device__ __forceinline__ uint16_t &at(int r, int c) { return v[kColMajor ? c * kPitch + r : r * kPitch + c]; }
 };
 
+// Extents of the operands, for the debug build's checks.
+[[maybe_unused]] __device__ __forceinline__ Span span_of_weights(const void *B, int N, int K) { return make_span(B, 2 * (size_t)N * K); }
+[[maybe_unused]] __device__ __forceinline__ Span span_of_codes(const void *packed, int nb, int kb) { return make_span(packed, (size_t)nb * kb * kW4BlockBytes); }
+[[maybe_unused]] __device__ __forceinline__ Span span_of_scales(const void *scales, int nb, int K, int group) { return make_span(scales, 2 * (size_t)((K + group - 1) / group) * nb * kW4Cols); }
+
 // vec: every run of eight elements along the contiguous dimension starts on 16 bytes and ends inside the matrix
 template <bool kColMajor, int kRows>
-__device__ __forceinline__ void load_tile(Tile<kColMajor, kRows> &s, const uint16_t *__restrict__ B, int n0, int k0, int N, int K, bool vec)
+__device__ __forceinline__ void load_tile(Tile<kColMajor, kRows> &s, const uint16_t *__restrict__ B, int n0, int k0, int N, int K, bool vec, unsigned *status)
 {
     constexpr int kInner = kColMajor ? kRows : kCols;
     if (vec) {
@@ -67,7 +73,7 @@ __device__ __forceinline__ void load_tile(Tile<kColMajor, kRows> &s, const uint1
             const int in = (i % (kInner / 8)) * 8, out = i / (kInner / 8), c = kColMajor ? out : in, r = kColMajor ? in : out;
             const int n = n0 + c, k = k0 + r;
             uint4 u = make_uint4(0u, 0u, 0u, 0u);
-            if (n < N && k < K) u = ld_stream16(B + (kColMajor ? (long)n * K + k : (long)k * N + n));
+            if (n < N && k < K) u = NM_LD_STREAM16(B + (kColMajor ? (long)n * K + k : (long)k * N + n), span_of_weights(B, N, K), status);
             uint32_t *d = reinterpret_cast<uint32_t *>(&s.at(r, c));
             if constexpr (kColMajor) *reinterpret_cast<uint4 *>(d) = u;
             else { d[0] = u.x; d[1] = u.y; d[2] = u.z; d[3] = u.w; }
@@ -76,12 +82,12 @@ __device__ __forceinline__ void load_tile(Tile<kColMajor, kRows> &s, const uint1
         for (int i = threadIdx.x; i < kCols * kRows; i += kThreads) {
             const int in = i % kInner, out = i / kInner, c = kColMajor ? out : in, r = kColMajor ? in : out;
             const int n = n0 + c, k = k0 + r;
-            s.at(r, c) = (n < N && k < K) ? B[kColMajor ? (long)n * K + k : (long)k * N + n] : (uint16_t)0;
+            s.at(r, c) = (n < N && k < K) ? NM_LD(&B[kColMajor ? (long)n * K + k : (long)k * N + n], span_of_weights(B, N, K), status) : (uint16_t)0;
         }
     }
 }
 template <bool kColMajor, int kRows>
-__device__ __forceinline__ void store_tile(Tile<kColMajor, kRows> &s, uint16_t *__restrict__ B, int n0, int k0, int N, int K, bool vec)
+__device__ __forceinline__ void store_tile(Tile<kColMajor, kRows> &s, uint16_t *__restrict__ B, int n0, int k0, int N, int K, bool vec, unsigned *status)
 {
     constexpr int kInner = kColMajor ? kRows : kCols;
     if (vec) {
@@ -93,25 +99,25 @@ __device__ __forceinline__ void store_tile(Tile<kColMajor, kRows> &s, uint16_t *
             uint4 u;
             if constexpr (kColMajor) u = *reinterpret_cast<const uint4 *>(d);
             else u = make_uint4(d[0], d[1], d[2], d[3]);
-            *reinterpret_cast<uint4 *>(B + (kColMajor ? (long)n * K + k : (long)k * N + n)) = u;
+            NM_ST(reinterpret_cast<uint4 *>(B + (kColMajor ? (long)n * K + k : (long)k * N + n)), u, span_of_weights(B, N, K), status);
         }
     } else {
         for (int i = threadIdx.x; i < kCols * kRows; i += kThreads) {
             const int in = i % kInner, out = i / kInner, c = kColMajor ? out : in, r = kColMajor ? in : out;
             const int n = n0 + c, k = k0 + r;
-            if (n < N && k < K) B[kColMajor ? (long)n * K + k : (long)k * N + n] = s.at(r, c);
+            if (n < N && k < K) NM_ST(&B[kColMajor ? (long)n * K + k : (long)k * N + n], s.at(r, c), span_of_weights(B, N, K), status);
         }
     }
 }
 
 template <typename T, bool kColMajor, int kRows>
 __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const uint16_t *__restrict__ B, uint4 *__restrict__ packed, uint16_t *__restrict__ scales, int N,
-                                                               int K, int nb, int kb, int group, int vec)
+                                                               int K, int nb, int kb, int group, int vec, unsigned *status)
 {
     __shared__ __align__(16) Tile<kColMajor, kRows> s_w;
     __shared__ float s_max[kRows / 32][kCols + 1];                 // per 32 k: the largest, then the rounded scale of its group
     const int tid = threadIdx.x, n0 = blockIdx.y * kCols, k0 = blockIdx.x * kRows;
-    load_tile<kColMajor, kRows>(s_w, B, n0, k0, N, K, vec != 0);
+    load_tile<kColMajor, kRows>(s_w, B, n0, k0, N, K, vec != 0, status);
     __syncthreads();
     for (int i = tid; i < (kColMajor ? kCols : kCols / 2) * (kRows / 32); i += kThreads) {
         // (pairs of columns along the lanes where columns are contiguous, 32-k pieces of a column otherwise)
@@ -142,7 +148,7 @@ __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const uint16_t *_
         for (int j = 0; j < per; ++j) s_max[q * per + j][c] = Elem<T>::widen(r);       // this thread alone reads and writes the group's entries
         const int n = n0 + c, strip = n / kW4Cols;
         if (strip < nb && k0 + q * group < K)
-            scales[((long)(k0 / group + q) * nb + strip) * kW4Cols + 2 * (n % 8) + (n % kW4Cols) / 8] = r.bits;
+            NM_ST(&scales[((long)(k0 / group + q) * nb + strip) * kW4Cols + 2 * (n % 8) + (n % kW4Cols) / 8], r.bits, span_of_scales(scales, nb, K, group), status);
     }
     __syncthreads();
     for (int i = tid; i < (kCols / kW4Cols) * (kRows / kW4Rows) * 32; i += kThreads) {
@@ -186,13 +192,13 @@ __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const uint16_t *_
                 }
             }
         }
-        packed[((long)strip * kb + kblk) * 32 + lane] = make_uint4(w[0], w[1], w[2], w[3]);
+        NM_ST(&packed[((long)strip * kb + kblk) * 32 + lane], make_uint4(w[0], w[1], w[2], w[3]), span_of_codes(packed, nb, kb), status);
     }
 }
 
 template <typename T, bool kColMajor, int kRows>
 __global__ void __launch_bounds__(kThreads) w4_dequantize_kernel(const uint4 *__restrict__ packed, const uint16_t *__restrict__ scales, uint16_t *__restrict__ B,
-                                                                 int N, int K, int nb, int kb, int group, int vec)
+                                                                 int N, int K, int nb, int kb, int group, int vec, unsigned *status)
 {
     __shared__ __align__(16) Tile<kColMajor, kRows> s_w;
     const int tid = threadIdx.x, n0 = blockIdx.y * kCols, k0 = blockIdx.x * kRows;
@@ -200,12 +206,13 @@ __global__ void __launch_bounds__(kThreads) w4_dequantize_kernel(const uint4 *__
         const int lane = i % 32, blk = (i / 32) % (kRows / kW4Rows), st = i / (32 * (kRows / kW4Rows)), g = lane >> 2, t = lane & 3;
         const int strip = n0 / kW4Cols + st, kblk = k0 / kW4Rows + blk;
         if (strip >= nb || kblk >= kb) continue;
-        const uint4 v = ld_stream16(packed + ((long)strip * kb + kblk) * 32 + lane);
+        const uint4 v = NM_LD_STREAM16(packed + ((long)strip * kb + kblk) * 32 + lane, span_of_codes(packed, nb, kb), status);
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int r0 = blk * kW4Rows + 32 * h + 8 * t, k32 = k0 + r0 / 32 * 32;        // the codes of 32 k share their group
-            const uint32_t pair = *reinterpret_cast<const uint32_t *>(scales + ((long)(k32 < K ? k32 / group : 0) * nb + strip) * kW4Cols + 2 * g);
+            const uint32_t pair = NM_LD(reinterpret_cast<const uint32_t *>(scales + ((long)(k32 < K ? k32 / group : 0) * nb + strip) * kW4Cols + 2 * g),
+                                        span_of_scales(scales, nb, K, group), status);
 #pragma unroll
             for (int hi = 0; hi < 2; ++hi) {
                 const uint32_t sc = __byte_perm(pair, 0u, hi ? 0x3232 : 0x1010);
@@ -221,7 +228,7 @@ __global__ void __launch_bounds__(kThreads) w4_dequantize_kernel(const uint4 *__
         }
     }
     __syncthreads();
-    store_tile<kColMajor, kRows>(s_w, B, n0, k0, N, K, vec != 0);
+    store_tile<kColMajor, kRows>(s_w, B, n0, k0, N, K, vec != 0, status);
 }
 
 // whether the contiguous dimension runs in whole, aligned 16-byte vectors
@@ -264,7 +271,7 @@ int nm_w4_quantize(const void *B, void *packed, void *scales, int N, int K, int 
     const int nb = (int)(((long)N + kW4Cols - 1) / kW4Cols), kb = (int)(((long)K + kW4Rows - 1) / kW4Rows);
     auto go = [&](auto rows, auto kern) {
         const dim3 grid((unsigned)(((long)K + rows - 1) / rows), (unsigned)(((long)N + kCols - 1) / kCols));
-        kern<<<grid, kThreads, 0, (cudaStream_t)stream>>>(static_cast<const uint16_t *>(B), static_cast<uint4 *>(packed), static_cast<uint16_t *>(scales), N, K, nb, kb, group, (int)pack_vec(B, N, K, layout_B));
+        kern<<<grid, kThreads, 0, (cudaStream_t)stream>>>(static_cast<const uint16_t *>(B), static_cast<uint4 *>(packed), static_cast<uint16_t *>(scales), N, K, nb, kb, group, (int)pack_vec(B, N, K, layout_B), bounds_status_ptr());
     };
     auto by_rows = [&](auto t, auto col) {
         using T = decltype(t);
@@ -285,7 +292,7 @@ int nm_w4_dequantize(const void *packed, const void *scales, void *B, int N, int
     const int nb = (int)(((long)N + kW4Cols - 1) / kW4Cols), kb = (int)(((long)K + kW4Rows - 1) / kW4Rows);
     auto go = [&](auto rows, auto kern) {
         const dim3 grid((unsigned)(((long)K + rows - 1) / rows), (unsigned)(((long)N + kCols - 1) / kCols));
-        kern<<<grid, kThreads, 0, (cudaStream_t)stream>>>(static_cast<const uint4 *>(packed), static_cast<const uint16_t *>(scales), static_cast<uint16_t *>(B), N, K, nb, kb, group, (int)pack_vec(B, N, K, layout_B));
+        kern<<<grid, kThreads, 0, (cudaStream_t)stream>>>(static_cast<const uint4 *>(packed), static_cast<const uint16_t *>(scales), static_cast<uint16_t *>(B), N, K, nb, kb, group, (int)pack_vec(B, N, K, layout_B), bounds_status_ptr());
     };
     auto by_rows = [&](auto t, auto col) {
         using T = decltype(t);
