@@ -20,8 +20,8 @@
 // TMEM; nine 12 KB slots of [96 rows x 128 bytes] for the records.  96 rows a tile: two score buffers of 96 columns fit TMEM beside O
 // and Q, so the scores of the next tile run while this one's exponentials do.  The MMAs of a tile by themselves take 3040 clocks
 // (1890 for the scores, bound by shared memory's 128 bytes a clock, 1150 for P * V).
-//   walk     One CTA per SM.  The tiles of all units are cut into even shares for the 74 pairs of CTAs, and a CTA walks over its one to
-//            three items; the ring runs on across them.
+//   walk     One CTA per SM.  The tiles of all units are cut into even shares for the 74 pairs of CTAs, and a CTA walks over the items of its
+//            share - one mostly, nine short sequences behind a long prefix; the ring runs on across them.
 // Measured: 16 x 128 heads, 32768 shared rows and about 500 own ones each: 213 us (148 GFLOP of scores and P * V in one pass: 695 TFLOP/s, 42 % of
 // the bf16 rate, at two and three terms); 16 x 128, ragged 4096: 49 us; 1 x 128, 16384: 27 us; 1 x 16, 257: 13 us.  (In
 // runs of many milliseconds the power cap, 1000 W, takes the clock from 1965 to 1695 MHz: 238 us for the first.)  A tile takes 4300 clocks:

@@ -143,11 +143,11 @@ def libs():
 
 
 class Batch:
-    """A batch whose pairs of CTAs each walk over items of several tiles, the maxima moving from tile to tile."""
+    """A batch whose pairs of CTAs walk over several items, the maxima moving from tile to tile."""
 
     def __init__(self, T=40, H=128, prefix=0, rows=300, seed=5, std=6.0):
         import paper_2609_16009_b200 as nm
-        Q, pre, own = case(T, H, prefix, [rows - 7 * (t % 9) for t in range(T)], seed, std)
+        Q, pre, own = case(T, H, prefix, [rows - (7 * (t % 9) if prefix == 0 else 0) for t in range(T)], seed, std)
         self.lens = (C.c_int * T)(*[len(o) for o in own])
         cache = torch.zeros(T, rows, REC, dtype=torch.uint8)
         for t, o in enumerate(own):
@@ -169,9 +169,10 @@ class Batch:
         return o, lse
 
 
-@pytest.fixture(scope="module")
-def batch():
-    return Batch()
+@pytest.fixture(scope="module", params=["short", "long"])
+def batch(request):
+    """Items of one and two tiles; items of 9 and 17, and six of 2, on a pair of CTAs."""
+    return Batch() if request.param == "short" else Batch(T=16, prefix=12000, rows=150)
 
 
 def paused(lib, where, warp, ns, fn):
