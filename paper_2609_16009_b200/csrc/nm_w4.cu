@@ -215,8 +215,8 @@ __global__ void __launch_bounds__(w4_warps(kNT) * 32, kNT == 1 ? 2 : 1) w4_kerne
     constexpr bool kBf16 = std::is_same<T, bf16_t>::value;
     constexpr int kS = kG32 ? 2 : 1, kSide = kNT;                    // scales of a block; strips of a unit
     constexpr int kWarps = w4_warps(kNT), kThreads = kWarps * 32, kWarpsLog2 = kNT == 1 ? 3 : 4;
-    // blocks of weights on their way, per warp (bf16 in groups of 32, M > 8: 2, as a third one's registers spill, 37.7 us against 35.8 at
-    // 16 x 7168 x 18432)
+    // blocks of weights on their way, per warp (bf16 in groups of 32, M > 8: 2, which spill 32 bytes a thread where three spill 172; 16 x 7168 x
+    // 18432 took 35.8 us against 37.7)
     constexpr int kDepth = kNT == 1 ? 8 : (kG32 && kBf16 ? 2 : 3);
     constexpr int kVals = kSide * kNT * 4;                         // sums a lane holds
     extern __shared__ __align__(16) unsigned char s_raw[];

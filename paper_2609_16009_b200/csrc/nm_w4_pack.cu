@@ -171,9 +171,11 @@ __global__ void __launch_bounds__(kThreads) w4_quantize_kernel(const uint16_t *_
                 else
 #pragma unroll
                     for (int x = 0; x < 8; ++x) v[x] = widen16<T>(s_w.at(r0 + x, c));
-                // w / sc with one reciprocal for eight weights: a product, its exact error, the corrected quotient.  Quotients of two
-                // numbers of a 16-bit type are ties or at least 2^-13 of themselves away from one, and a tie is met exactly, so the
-                // code is that of the rounded quotient.  (At the ends of fp32's range the reciprocal or the error would leave it.)
+                // w / sc with one reciprocal for eight weights: a product, its exact error by a fused multiply-add, the corrected quotient
+                // (Markstein, IBM J. Res. Dev. 34, 1990).  That is within 2^-23 of the quotient, and exact where fp32 holds it.  Quotients of two
+                // numbers of a 16-bit type are ties, which fp32 holds, or at least 2^-15 of themselves away from one (all pairs of fp16
+                // significands; 2^-11.9 for bf16), so the code is that of the rounded quotient.  (At the ends of fp32's range the
+                // reciprocal or the error would leave it.)
                 if (sc > 0x1p-60f && sc < 0x1p60f) {
                     const float inv = 1.f / sc;
 #pragma unroll
