@@ -273,8 +273,8 @@ int nm_mla_attention_combine(const void *Q, const void *kv_cache, void *o_bf16, 
  * nm_mla_cache_write_q8: T rows x = ckr + t * ckr_stride (elements, a multiple of 8), bf16 (latent | key) as W_DKVKR leaves them:
  *   latent  RMSNorm(x[:kv_lora]; gamma, eps), gamma [kv_lora] bf16; NULL: taken as it is
  *   key     RoPE(x[kv_lora:]) by cos_sin [T][rope] fp32 (rows of nm_rope_table); NULL: taken as it is
- *   then quantised - each value rounded once, from fp32 - and stored as record rows[t] (device, 64-bit) of the cache.  A rows[t] outside
- *   [0, n_cache_rows) writes nothing (padding tokens); rows NULL means row t.  T is at most 2^30.  The rows named in one call must differ from
+ *   then quantised - a latent value rounded once, from what it is to 2^-40 of itself, a key value once, from fp32 - and stored as record
+ *   rows[t] (device, 64-bit) of the cache.  A rows[t] outside [0, n_cache_rows) writes nothing (padding tokens); rows NULL means row t.  T is at most 2^30.  The rows named in one call must differ from
  *   each other: what a row named twice holds afterwards is unspecified.  A NaN stays a NaN, an infinite or too large
  *   latent value becomes +-448 s.
  * nm_mla_cache_read_q8: records rows[i] (NULL: i) as bf16 rows out + i * out_stride (elements, a multiple of 8): (latent | key), exact but

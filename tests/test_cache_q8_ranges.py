@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_cache_q8 import records, rows_in
+from test_cache_q8 import records, rounded_to_e4m3, rows_in
 
 
 @pytest.mark.gpu
@@ -29,3 +29,46 @@ def test_write_normalises_rows_at_the_ends_of_the_range(power, eps, kv):
     want = np.clip(y / s, -448, 448)
     # half a step of e4m3: 2^-4 of the value, 2^-10 below its normal range; fp32 arithmetic before it 2^-20
     assert np.all(np.abs(codes - want) <= np.maximum(2.0 ** -4 * np.abs(want), 2.0 ** -10) * (1 + 2.0 ** -15))
+
+
+@pytest.mark.gpu
+def test_codes_next_to_ties():
+    """8 million values: every code is the one of the value in 64 bits, those within fp32's rounding of a tie of e4m3 among them; a value that is not
+    told apart from a tie at 2^-40 of itself may fall either way."""
+    import paper_2609_16009_b200 as nm
+    kv, rope, T = 512, 64, 16000
+    x, gamma, _ = rows_in(T, kv, rope, 5)
+    cache = torch.zeros(T, nm.nm_mla_q8_row_bytes(kv, rope), dtype=torch.uint8, device="cuda")
+    nm.nm_mla_cache_write_q8(x.cuda(), gamma.cuda(), None, None, cache, T, T, kv, rope, 1e-6)
+    codes, _, s = records(cache.cpu().numpy(), kv, rope)
+    v = x[:, :kv].double().numpy()
+    y = v / np.sqrt((v ** 2).mean(1, keepdims=True) + np.float64(np.float32(1e-6))) * gamma.double().numpy()
+    want = rounded_to_e4m3(y / s)
+    off = codes != want
+    near = np.abs(y / s - (codes + want) / 2) <= 2.0 ** -40 * np.abs(want)
+    assert not (off & ~near).any(), f"{(off & ~near).sum()} codes on the wrong side of a tie"
+    # the row's power of two is the least that holds it
+    top = np.abs(y).max(1)
+    assert (top <= 448 * s[:, 0] * (1 + 2.0 ** -40)).all() and (top > 224 * s[:, 0] * (1 - 2.0 ** -40)).all()
+
+
+@pytest.mark.gpu
+def test_a_largest_value_just_above_448():
+    """Rows whose largest normalised value is 448 up to fp32's rounding: the power of two goes by the value itself."""
+    import paper_2609_16009_b200 as nm
+    kv, rope = 16, 0
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn(4096, kv, generator=g).to(torch.bfloat16)
+    gamma = torch.full((kv,), 448.0, dtype=torch.bfloat16)
+    x[:, 0] = 1.0
+    x[:, 1:] = (1 + torch.randint(-2, 3, (4096, kv - 1), generator=g) * 2.0 ** -7).to(torch.bfloat16) * torch.sign(x[:, 1:].float()).to(torch.bfloat16)
+    v = x.double().numpy()
+    for eps in (0.0, 1e-6, 1e-12):
+        cache = torch.zeros(4096, nm.nm_mla_q8_row_bytes(kv, rope), dtype=torch.uint8, device="cuda")
+        nm.nm_mla_cache_write_q8(x.cuda(), gamma.cuda(), None, None, cache, 4096, 4096, kv, rope, eps)
+        codes, _, s = records(cache.cpu().numpy(), kv, rope)
+        y = v / np.sqrt((v ** 2).mean(1, keepdims=True) + np.float64(np.float32(eps))) * 448.0
+        top = np.abs(y).max(1)
+        assert (top <= 448 * s[:, 0] * (1 + 2.0 ** -40)).all() and (top > 224 * s[:, 0] * (1 - 2.0 ** -40)).all()
+        want = rounded_to_e4m3(y / s)
+        assert not ((codes != want) & (np.abs(y / s - (codes + want) / 2) > 2.0 ** -40 * np.abs(want))).any()
