@@ -301,9 +301,10 @@ int nm_mla_cache_read_q8(const void *cache, long n_cache_rows, const int64_t *ro
  *   cache_stride BYTES between the caches of consecutive sequences (a multiple of 16; >= the longest, for T > 1)
  *   o_bf16, o_f32, lse  [T][H][kv_lora], [T][H][kv_lora], [T][H] (natural log of sum_j exp(s)); any may be NULL.  A sequence
  *                without any row gets zeros and minus infinity.
- * Nothing behind the rows named here is read into a result, whatever it holds.  A head whose query holds an infinity or a NaN, and a
+ * Nothing behind the rows named here is read into a result, whatever it holds.  A query's latent elements enter the scores exactly down to
+ * 2^-10 of their head's largest, and to 2^-19 of it below.  A head whose query holds an infinity or a NaN, and a
  * sequence (or all, in the prefix) with a NaN record, gets NaN.  A row's weight (p times its scale) keeps at least eight bits,
- * whatever its size down to 2^-20 of the largest; sums are fp32.  Equal calls give equal bits.
+ * whatever its size down to 2^-20 of the largest; sums are fp32, and o_f32, though not rounded, is no more exact than the weights.  Equal calls give equal bits.
  * Q, prefix, cache, o_f32 and the workspace are 16-byte aligned, o_bf16 8-byte.  Workspace:
  * nm_mla_attention_q8_workspace_bytes, whatever the lengths; nothing in it has to be cleared, and it keeps nothing from one call for the
  * next; calls that overlap on the GPU (two captured graphs among them) need workspaces of their own.

@@ -22,9 +22,9 @@
 // (1890 for the scores, bound by shared memory's 128 bytes a clock, 1150 for P * V).
 //   walk     One CTA per SM.  The tiles of all units are cut into even shares for the 74 pairs of CTAs, and a CTA walks over the items of its
 //            share - one mostly, nine short sequences behind a long prefix; the ring runs on across them.
-// Measured: 16 x 128 heads, 32768 shared rows and about 500 own ones each: 213 us (148 GFLOP of scores and P * V in one pass: 695 TFLOP/s, 42 % of
-// the bf16 rate, at two and three terms); 16 x 128, ragged 4096: 49 us; 1 x 128, 16384: 27 us; 1 x 16, 257: 13 us.  (In
-// runs of many milliseconds the power cap, 1000 W, takes the clock from 1965 to 1695 MHz: 238 us for the first.)  A tile takes 4300 clocks:
+// Measured: 16 x 128 heads, 32768 shared rows and about 500 own ones each: 204 to 220 us (148 GFLOP of scores and P * V in one pass: 700 TFLOP/s, 42 % of
+// the bf16 rate, at two and three terms); 16 x 128, ragged 4096: 49 us; 1 x 128, 16384: 25 us; 1 x 16, 257: 13 us.  (In
+// runs of many milliseconds the power cap, 1000 W, takes the clock from 1965 to 1695 MHz: 251 us for the first.)  A tile takes 4300 clocks:
 // the matrix unit waits neither for copies nor for weights then, but its MMAs run slower beside the softmax warps than alone (3770 with
 // their work taken out).  Made no difference: no copies at all, one polling lane per warp, waits ahead of the MMAs, descriptors as 32-bit
 // words, loops instead of straight-line MMAs, fewer shared-memory reads in the softmax.  Made one: MMAs issued by an elected lane of a walking

@@ -23,8 +23,8 @@
 //            to eight CTAs of a cluster split k further.  Two to four CTAs share an SM, so that one fills its tokens while another
 //            streams.  Partial sums meet in shared memory, then in that of the cluster's first CTA, added in a fixed order:
 //            no workspace, no atomics, the same bits every time, and calls on different streams share nothing.
-// Measured back to back, weights from HBM: M = 1, 16384 x 7168, groups of 64: 16.5 us (62 MB, 3.8 TB/s; loads without the
-// products take 13); 7168 x 576: 4.5 us; 1536 x 24576: 8.6 us; M = 16, 7168 x 18432: 28.7 us.  What bounds it: M <= 8 a start and an end
+// Measured back to back, weights from HBM: M = 1, 16384 x 7168, groups of 64: 16.7 us (62 MB, 3.7 TB/s; loads without the
+// products take 13), M = 8: 22.0; 7168 x 576: 4.5 us; 1536 x 24576: 8.7 us, M = 4: 9.7; M = 16, 7168 x 18432: 28.8 us.  What bounds it: M <= 8 a start and an end
 // of about 5 us around a stream at 5 to 6 TB/s; M > 8 the tokens - made ready once per SM, and read from shared memory
 // by every warp.  Built, measured and left: one CTA per SM whose warps walk evenly over all blocks of its share (20.8 us for the first: its
 // start and end are not hidden by another CTA), rings in shared memory by asynchronous copies (the same stream, more instructions).
