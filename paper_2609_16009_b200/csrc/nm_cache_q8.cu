@@ -3,9 +3,9 @@
 //
 // One warp per row: the whole row lives in the warp's registers (16 values a lane at kv_lora = 512), its sum of squares (fp64, so that
 // a code next to a tie falls where the definition puts it) and its largest value are warp reductions, and nothing is read or
-// written twice (but by the one row in a thousand that has a value on a tie).  Bound: 1152 bytes in and 656 out per row (reversed when read
-// back), in runs of 16 bytes a lane.  Measured, 131072 rows of 512 + 64 in random order: written in 81 us with norm and rotation (41 for the
-// bytes; it is bound by issue: conversions, the fp64 sum, ties), read back in 45 (36 for the bytes); 16 rows are written in 2.7 us.
+// written twice.  Bound: 1152 bytes in and 656 out per row (reversed when read back), in runs of 16 bytes a lane.  Measured, 131072
+// rows of 512 + 64 in random order: written in 78 us with norm and rotation (41 for the bytes; conversions, the fp64 sum and the rounding
+// to odd bind it by issue), read back in 45 (36 for the bytes); 16 rows are written in 2.5 us.
 // Four rows a CTA; eight take 9 % longer for the first, two 69 us to read back.
 #include <cuda_fp8.h>
 
@@ -24,71 +24,6 @@ __device__ __forceinline__ float bf_hi(uint32_t w) { return __uint_as_float(w & 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
     return (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(lo)) | ((uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(hi)) << 16);
-}
-
-// a pair of the key part, rotated and divided by the row's power of two
-__device__ __forceinline__ uint32_t key_pair(uint32_t w, float2 cs, bool rotated, float inv)
-{
-    float a = bf_lo(w), b = bf_hi(w);
-    if (rotated) {
-        const float ra = a * cs.x - b * cs.y, rb = a * cs.y + b * cs.x;
-        a = ra; b = rb;
-    }
-    return pack_bf16(a * inv, b * inv);
-}
-// least e with top <= 448 * 2^e, 448 = 1.75 * 2^8, within the bounds; 0 for a top of 0
-__device__ __forceinline__ int row_exponent(float top)
-{
-    const uint32_t b = __float_as_uint(top);
-    const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u);
-    return top > 0.f ? min(max(e, kQ8LeastExp), kQ8MostExp) : 0;
-}
-__device__ __forceinline__ uint2 codes_of(const float (&y)[8], float inv)
-{
-    uint32_t c[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(y[4 * j] * inv, y[4 * j + 1] * inv), __NV_SATFINITE, __NV_E4M3);
-        const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(y[4 * j + 2] * inv, y[4 * j + 3] * inv), __NV_SATFINITE, __NV_E4M3);
-        c[j] = lo | (hi << 16);
-    }
-    return make_uint2(c[0], c[1]);
-}
-
-// The row once more, for rows with a value that fp32's rounding has put on a tie of e4m3 or on 448 times a power of two (all of these end in 19
-// zeros): such a value goes one step of fp32 to the side that it came from, so that the code, and the row's power of two, see one rounding only.
-// One row in a thousand, and rows that hold a zero; written over by the lanes that wrote it, at the end: as a branch ahead of the codes it costs
-// the other rows 17 % (131072 of them 77 -> 91 us), here the looking for such values does, 6 %.
-__device__ __noinline__ void rewrite_row_off_ties(const uint16_t *x, const uint16_t *gamma, const float *cos_sin, unsigned char *rec, int kv, int rope, float shift, float r,
-                                                  float r_low, Span in_rows, Span in_gamma, Span in_angles, Span in_cache, unsigned *status)
-{
-    const int lane = threadIdx.x & 31;
-    auto value = [&](int k) {
-        const float a = __uint_as_float((uint32_t)NM_LD(&x[k], in_rows, status) << 16) * shift * __uint_as_float((uint32_t)NM_LD(&gamma[k], in_gamma, status) << 16);
-        const float y = fmaf(a, r, a * r_low);
-        const uint32_t bits = __float_as_uint(y);
-        const float rest = fmaf(a, r, -y) + a * r_low;
-        if (bits << 13 || bits << 1 == 0u || !(rest > 0.f || rest < 0.f)) return y;
-        return __uint_as_float((rest > 0.f) == (y > 0.f) ? bits + 1u : bits - 1u);
-    };
-    float top = 0.f;
-    for (int v = lane; v < kv / 8; v += 32)
-        for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(value(8 * v + j)));
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const int e = row_exponent(top);
-    const float inv = __uint_as_float((uint32_t)(127 - e) << 23);
-    for (int v = lane; v < kv / 8; v += 32) {
-        float y[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = value(8 * v + j);
-        NM_ST(reinterpret_cast<uint2 *>(rec + 8 * v), codes_of(y, inv), in_cache, status);
-    }
-    for (int p = lane; p < rope / 2; p += 32) {
-        const uint32_t w = NM_LD(reinterpret_cast<const uint32_t *>(x + kv + 2 * p), in_rows, status);
-        const float2 cs = cos_sin ? NM_LD(reinterpret_cast<const float2 *>(cos_sin + 2 * p), in_angles, status) : make_float2(1.f, 0.f);
-        NM_ST(reinterpret_cast<uint32_t *>(rec + kv + 4 * p), key_pair(w, cs, cos_sin != nullptr, inv), in_cache, status);
-    }
-    if (lane == 0) NM_ST(reinterpret_cast<float4 *>(rec + kv + 2 * rope), make_float4(__uint_as_float((uint32_t)(127 + e) << 23), 0.f, 0.f, 0.f), in_cache, status);
 }
 
 // kVecs: 16-byte vectors of the latent part a lane holds at most (kv_lora <= 256 * kVecs)
@@ -123,8 +58,6 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
     const float2 angle0 = has_key ? angle_at(lane) : make_float2(1.f, 0.f);
     float y[kVecs][8];
     double squares = 0.;
-    float shift = 1.f, r = 0.f, r_low = 0.f;
-    uint32_t zeros = 0u;                                           // bit 19: a value whose last 19 bits are zeros
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
         const int v = lane + 32 * i;
@@ -141,8 +74,8 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
     if (gamma) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, o);
-        // The normaliser in 64 bits, and used as two fp32 terms on the exact products x * gamma: y is off by one rounding only, and by 2^-44 before
-        // it.  A code next to a tie of e4m3 falls wrongly by whatever the value is off, and a code is worth 2^-4 of it.
+        // The normaliser in 64 bits, 2^-44 off at most, and used as two fp32 terms on the exact products x * gamma.  A code next to a tie of e4m3
+        // falls wrongly by whatever the value is off, and a code is worth 2^-4 of it.
         const double mean = squares * inv_kv + (double)eps;
         double rd;
         if (mean > 0x1p-100 && mean < 0x1p100) {                   // from fp32's root by one Newton step, 2^-44 off
@@ -151,23 +84,28 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
         } else {
             // A row at an end of the range is brought to its middle by a power of two, or x * gamma, or the normaliser itself, leaves fp32
             // though y does not.
-            shift = mean > 1. ? 0x1p-64f : 0x1p64f;
+            const float shift = mean > 1. ? 0x1p-64f : 0x1p64f;
 #pragma unroll
             for (int i = 0; i < kVecs; ++i)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) y[i][j] *= shift;
             rd = 1. / (sqrt(mean) * (double)shift);
         }
-        r = (float)rd; r_low = (float)(rd - (double)r);
+        const float r = (float)rd;
+        float r_low = (float)(rd - (double)r);
+        // y is rounded to odd: cut off, and its last bit set, so that what is left of a value beside a tie of e4m3, or beside 448 times a power of
+        // two, stays on its side (rounded to fp32's nearest, 1.5 of 3 million land on a tie and fall wrongly from there).  Where r is an fp32 number
+        // y may BE such a tie; where it has more bits, x * gamma * r has more than 24 too and is none.
+        if (fabsf(r_low) <= 0x1p-40f * r) r_low = 0.f;
+        const uint32_t odd = r_low != 0.f;
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
             const uint32_t w[4] = {weight[i].x, weight[i].y, weight[i].z, weight[i].w};
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float a = y[i][2 * j] * bf_lo(w[j]), b = y[i][2 * j + 1] * bf_hi(w[j]);
-                y[i][2 * j] = fmaf(a, r, a * r_low); y[i][2 * j + 1] = fmaf(b, r, b * r_low);
-                const uint32_t a0 = __float_as_uint(y[i][2 * j]), b0 = __float_as_uint(y[i][2 * j + 1]);
-                zeros |= (a0 ^ (a0 - 1u)) | (b0 ^ (b0 - 1u));
+                y[i][2 * j] = __uint_as_float(__float_as_uint(__fmaf_rz(a, r, a * r_low)) | odd);
+                y[i][2 * j + 1] = __uint_as_float(__float_as_uint(__fmaf_rz(b, r, b * r_low)) | odd);
             }
         }
     }
@@ -178,23 +116,39 @@ __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_write_q8_kernel(const uin
         for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(y[i][j]));      // (a NaN is passed over here and stays a NaN code)
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    const int e = row_exponent(top);
+    // least e with top <= 448 * 2^e, 448 = 1.75 * 2^8
+    int e = 0;
+    if (top > 0x1p-149f) {                                         // (a zero's last bit may be set)
+        const uint32_t b = __float_as_uint(top);
+        e = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u);
+        e = min(max(e, kQ8LeastExp), kQ8MostExp);
+    }
     const float inv = __uint_as_float((uint32_t)(127 - e) << 23), s = __uint_as_float((uint32_t)(127 + e) << 23);
     unsigned char *rec = cache + row * (long)q8_row_bytes(kv, rope);
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
         const int v = lane + 32 * i;
         if (v >= vecs) continue;
-        NM_ST(reinterpret_cast<uint2 *>(rec + 8 * v), codes_of(y[i], inv), in_cache, status);
+        uint32_t c[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(y[i][4 * j] * inv, y[i][4 * j + 1] * inv), __NV_SATFINITE, __NV_E4M3);
+            const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(y[i][4 * j + 2] * inv, y[i][4 * j + 3] * inv), __NV_SATFINITE, __NV_E4M3);
+            c[j] = lo | (hi << 16);
+        }
+        NM_ST(reinterpret_cast<uint2 *>(rec + 8 * v), make_uint2(c[0], c[1]), in_cache, status);
     }
     for (int p = lane; p < rope / 2; p += 32) {
         const uint32_t w = p == lane ? key0 : key_at(p);
-        const float2 cs = !cos_sin || p == lane ? angle0 : angle_at(p);
-        NM_ST(reinterpret_cast<uint32_t *>(rec + kv + 4 * p), key_pair(w, cs, cos_sin != nullptr, inv), in_cache, status);
+        float a = bf_lo(w), b = bf_hi(w);
+        if (cos_sin) {
+            const float2 cs = p == lane ? angle0 : angle_at(p);
+            const float ra = a * cs.x - b * cs.y, rb = a * cs.y + b * cs.x;
+            a = ra; b = rb;
+        }
+        NM_ST(reinterpret_cast<uint32_t *>(rec + kv + 4 * p), pack_bf16(a * inv, b * inv), in_cache, status);
     }
     if (lane == 0) NM_ST(reinterpret_cast<float4 *>(rec + kv + 2 * rope), make_float4(s, 0.f, 0.f, 0.f), in_cache, status);
-    if (__any_sync(0xffffffffu, zeros & 0x80000u) && gamma)
-        rewrite_row_off_ties(x, gamma, cos_sin ? cos_sin + (long)t * rope : nullptr, rec, kv, rope, shift, r, r_low, in_rows, in_gamma, in_angles, in_cache, status);
 }
 
 __global__ void __launch_bounds__(kWarpsQ8 * 32) cache_read_q8_kernel(const unsigned char *__restrict__ cache, long n_cache_rows, const int64_t *__restrict__ rows,

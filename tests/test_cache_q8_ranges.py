@@ -72,3 +72,48 @@ def test_a_largest_value_just_above_448():
         assert (top <= 448 * s[:, 0] * (1 + 2.0 ** -40)).all() and (top > 224 * s[:, 0] * (1 - 2.0 ** -40)).all()
         want = rounded_to_e4m3(y / s)
         assert not ((codes != want) & (np.abs(y / s - (codes + want) / 2) > 2.0 ** -40 * np.abs(want))).any()
+
+
+@pytest.mark.gpu
+def test_values_that_are_ties():
+    """Rows of one magnitude without eps: the normaliser is exact, and values that are ties of e4m3, or 448, are taken for what they are."""
+    import paper_2609_16009_b200 as nm
+    kv, rope = 64, 0
+    ties = torch.tensor([1.0625, 1.1875, 17.0, 34.0, 2.0 ** -10, 3 * 2.0 ** -10, 15 * 2.0 ** -10, 0.0, 448.0, 416.0, 1.0, 240.0, 0.53125, 2.0 ** -6, 232.0, 0.0625])
+    gamma = ties.repeat(4).to(torch.bfloat16)
+    assert torch.equal(gamma.float(), ties.repeat(4))
+    size = torch.tensor([1.0, 2.0 ** 20, 2.0 ** -30, 3.0, 1.5, 2.0 ** 60, 2.0 ** -60, 7.0])
+    x = (size[:, None] * (1 - 2 * (torch.arange(kv) % 3 == 0).float())).to(torch.bfloat16)
+    cache = torch.zeros(8, nm.nm_mla_q8_row_bytes(kv, rope), dtype=torch.uint8, device="cuda")
+    nm.nm_mla_cache_write_q8(x.cuda(), gamma.cuda(), None, None, cache, 8, 8, kv, rope, 0.0)
+    codes, _, s = records(cache.cpu().numpy(), kv, rope)
+    y = torch.sign(x.float()).double().numpy() * gamma.double().numpy()
+    # the normaliser of 1, 2^20 and their like is a power of two; 1 / 3 and its like have no end in binary, and their products are ties to 2^-44 of
+    # themselves only
+    exact = [0, 1, 2, 5, 6]
+    assert (s[exact, 0] == 1).all() and np.isin(s[:, 0], (1, 2)).all()
+    assert np.array_equal(codes[exact], rounded_to_e4m3(y[exact]))
+    assert np.all(np.abs(codes * s - y) <= np.maximum(2.0 ** -4 * np.abs(y), 2.0 ** -10 * s))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("eps", [1e-6, 0.0])
+def test_zeros_in_and_as_rows(eps):
+    """A zero stays one beside other values, and a row of zeros has scale 1."""
+    import paper_2609_16009_b200 as nm
+    kv, rope, T = 272, 8, 5
+    x, gamma, _ = rows_in(T, kv, rope, 8)
+    x[:, 10:30], x[1, :kv] = 0.0, 0.0
+    gamma[40] = 0.0
+    x[2, :kv] = 0.0
+    x[2, 7] = 1.0
+    cache = torch.zeros(T, nm.nm_mla_q8_row_bytes(kv, rope), dtype=torch.uint8, device="cuda")
+    nm.nm_mla_cache_write_q8(x.cuda(), gamma.cuda(), None, None, cache, T, T, kv, rope, eps)
+    codes, _, s = records(cache.cpu().numpy(), kv, rope)
+    keep = [0, 2, 3, 4] + ([1] if eps else [])                     # (without eps a row of zeros is 0 / 0)
+    assert not codes[keep][:, 10:30].any() and not codes[keep][:, 40].any()
+    assert (codes[2] != 0).sum() == 1
+    if eps:
+        assert s[1, 0] == 1 and not codes[1].any()
+    else:
+        assert np.isnan(codes[1]).all()
