@@ -293,7 +293,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_q8_kernel(const __grid_const
     // scores g + 2 are issued behind the wait for the weights of g, and P * V of g + 2 behind the waiting warp's own arrival for g + 2 - and
     // the one before is through: scores g seen say so of P * V g - 2, which was issued ahead of them.  (With one bar_pv for all tiles a
     // warp that has handed in its last weights might find two P * V outstanding, one or none: three states, and the wait for the last but one
-    // takes both through for neither.)
+    // takes both through for neither.)  The barriers of an item - bar_q its queries in place, bar_qt their part in TMEM, bar_free everything of it
+    // read - go through one phase an item, and each is waited for once in it: queries i + 1 are asked for behind bar_free of i, which needs all
+    // weights of i handed in, and those need the scores that the issuing warp gives behind its waits for i.  The ring's pair is the usual one: a slot is
+    // filled behind its release and released behind the wait for its fill.
 
     // A tile's five blocks in ring order: the other half's two latent blocks, the key part, this half's two latent blocks (the last
     // ones to be given back: they are also V).  x: byte offset in the record.
