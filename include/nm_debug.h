@@ -93,6 +93,10 @@ int nm_debug_set_attention_q8_pause(int where, int warp, unsigned ns);
  * products' own load instruction, ctas_per_sm x SM-count CTAs of 256 threads) - the read-only bandwidth this GPU
  * delivers, to set beside the copy bandwidth the roofline uses.  src 16-byte aligned; sink4: 4 writable bytes. */
 int nm_debug_stream_read(const void *src, size_t bytes, void *sink4, int ctas_per_sm, nm_stream stream);
+/* nm_matmul_w4: force the warps of a CTA side by side over the columns (1, 2, 4, 8, 16), the CTAs of a cluster along k (1..8) and the most
+ * blocks of 64 k whose tokens a CTA holds at a time; zeros give each choice back to the planner, and a split that the shape cannot have (more CTAs
+ * than blocks, more warps than a CTA has, sums that do not fit) is left to it too. */
+int nm_debug_set_w4_plan(int warps_across, int ctas_along_k, int piece_blocks);
 /* Report the plan for a problem: out[0..5] = kernel kind (0 row-major vector, 1 column-major
  * vector, 2 scalar), columns per tile, k-splits, k-rows per split, column tiles, CTAs. */
 int nm_debug_get_plan(int M, int N, int K, int H, nm_dtype dtype, nm_layout layout_B, int vec_ok,

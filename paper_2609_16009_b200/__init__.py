@@ -65,6 +65,7 @@ _lib.nm_w4_scale_count.argtypes = [_i, _i, _i]
 _lib.nm_w4_quantize.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _i, _vp]
 _lib.nm_w4_dequantize.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _i, _vp]
 _lib.nm_debug_set_plan.argtypes = [_i, _i]
+_lib.nm_debug_set_w4_plan.argtypes = [_i, _i, _i]
 _lib.nm_debug_set_kernel.argtypes = [_i, _i]
 _lib.nm_set_tensor_core_min_m.argtypes = [_i]
 _lib.nm_set_programmatic_launch.argtypes = [_i]
@@ -245,6 +246,10 @@ def nm_w4_quantize(B, packed, scales, N, K, group, dtype=BF16, layout_B=ROW_MAJO
 
 def nm_w4_dequantize(packed, scales, B_out, N, K, group, dtype=BF16, layout_B=ROW_MAJOR, stream=None) -> None:
     _check(_lib.nm_w4_dequantize(_ptr(packed), _ptr(scales), _ptr(B_out), N, K, group, dtype, layout_B, _stream(stream)), "nm_w4_dequantize")
+
+
+def nm_debug_set_w4_plan(warps_across: int = 0, ctas_along_k: int = 0, piece_blocks: int = 0) -> None:
+    _check(_lib.nm_debug_set_w4_plan(warps_across, ctas_along_k, piece_blocks), "nm_debug_set_w4_plan")
 
 
 def nm_debug_set_plan(tile_n: int = 0, nsplit: int = 0) -> None:

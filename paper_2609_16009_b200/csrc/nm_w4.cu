@@ -408,6 +408,7 @@ __global__ void __launch_bounds__(w4_warps(kNT) * 32, kNT == 1 ? 2 : 1) w4_kerne
 // M <= 8, 4 x 7168 x 1536 10 instead of 7.)
 // `resident`: clusters of each size that run at once (their CTAs need SMs of one GPC, so not every size fills the machine).
 struct W4Plan { int wn, cl; };
+std::atomic<unsigned> g_w4_forced{0};              // nm_debug_set_w4_plan: warps across | CTAs << 8 | blocks of a piece << 16
 W4Plan plan_w4(int M, int units, int kb, const int (&resident)[9])
 {
     const bool wide = M > 8;
@@ -464,7 +465,12 @@ cudaError_t launch_w4(W4Args a, cudaStream_t stream, bool pdl)
     int resident[9];
     e = resident_clusters<kNT>(resident);
     if (e != cudaSuccess) return e;
-    const W4Plan p = plan_w4(a.M, units, a.kb, resident);
+    W4Plan p = plan_w4(a.M, units, a.kb, resident);
+    const unsigned forced = g_w4_forced.load(std::memory_order_relaxed);
+    if (forced) {                                                  // (where the shape and the machine can have it)
+        const W4Plan f{forced & 0xff ? (int)(forced & 0xff) : p.wn, forced >> 8 & 0xff ? (int)(forced >> 8 & 0xff) : p.cl};
+        if (f.wn <= kWarps && f.cl <= a.kb && resident[f.cl] > 0 && w4_sum_bytes(kNT, f.wn, f.cl) <= (kNT == 2 ? 96 : 40) * 1024) p = f;
+    }
     for (a.wn_log2 = 0; (1 << a.wn_log2) < p.wn; ++a.wn_log2) {}
     a.cl = p.cl;
     a.blocks_each = a.kb / a.cl; a.blocks_more = a.kb % a.cl;
@@ -472,6 +478,7 @@ cudaError_t launch_w4(W4Args a, cudaStream_t stream, bool pdl)
     const int scale_block = kS * kSide * 32 * p.wn, run = ceil_div(a.kb, a.cl), sum_bytes = w4_sum_bytes(kNT, p.wn, p.cl);
     const int fit = ((kNT == 1 ? kSmemMost / 2 : kSmemMost) - sum_bytes - a.M * 64) / (a.M * kW4Rows * 2 + kStart + scale_block);
     a.chunk = ceil_div(run, ceil_div(run, fit));
+    if (forced >> 16 && a.chunk > (int)(forced >> 16)) a.chunk = (int)(forced >> 16);
     a.pitch = a.chunk * (kW4Rows * 2) + 64;
     a.tok_bytes = a.M * a.pitch + a.chunk * kStart;
     a.scale_bytes = a.chunk * scale_block;
@@ -512,6 +519,14 @@ using namespace nm;
 
 extern "C" {
 #pragma GCC visibility push(default)
+
+int nm_debug_set_w4_plan(int warps_across, int ctas_along_k, int piece_blocks)
+{
+    if (warps_across < 0 || warps_across > 16 || (warps_across & (warps_across - 1)) || ctas_along_k < 0 || ctas_along_k > 8 || piece_blocks < 0 || piece_blocks > 0xffff)
+        return NM_ERR_INVALID_ARG;
+    g_w4_forced.store((unsigned)warps_across | (unsigned)ctas_along_k << 8 | (unsigned)piece_blocks << 16, std::memory_order_relaxed);
+    return NM_OK;
+}
 
 int nm_matmul_w4(const void *A, const void *packed, const void *scales, void *C, int M, int N, int K, int group, long lda, long ldc,
                  nm_dtype dtype, nm_stream stream)
