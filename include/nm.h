@@ -223,6 +223,72 @@ int nm_w4_quantize(const void *B, void *packed, void *scales, int N, int K, int 
 int nm_w4_dequantize(const void *packed, const void *scales, void *B, int N, int K, int group, nm_dtype dtype,
                      nm_layout layout_B, nm_stream stream);
 
+/* ---- feed-forward half of a decode layer: routing to experts, their products, products with an epilogue -------------- */
+
+/*
+ * Tokens to experts (the paper has no counterpart: it ends with the attention half of a layer).  Per token, over its E logits x:
+ *   s = softmax(x) or sigmoid(x),  key = s + bias
+ *   groups > 1: groups of E / groups experts count as their largest key (group_best 1) or the sum of their two largest (2); the
+ *   keep_groups best stay (ties to the lowest group)
+ *   experts[t][0..top_k): the largest keys that are left, ties to the lowest index, in falling order
+ *   weights[t][j] = s of that expert, divided by the sum of the chosen ones where `renormalise`, times `scale`
+ * Scores, keys and sums are fp64; a weight is rounded once, to fp32.
+ *   logits    [T] rows of E, ld_logits elements apart; NM_F32, NM_BF16 or NM_F16.  bias [E] fp32 or NULL
+ *   E         1..NM_MAX_EXPERTS; groups 1..32, a divisor of E; top_k 1..32, at most keep_groups * E / groups;  T up to 2^24
+ * A NaN logit counts as minus infinity, a NaN key (by the bias) as the least one.  Logits of minus infinity (masked experts) score 0 and are
+ * chosen only where nothing else is left; where the chosen scores sum to 0 the renormalised weights are 0.  Logits of plus infinity share the softmax's
+ * whole weight.  The experts of a token always differ from each other and lie in [0, E).  Honours nm_set_programmatic_launch.
+ */
+#define NM_MAX_EXPERTS 1024
+typedef enum { NM_SCORE_SOFTMAX = 0, NM_SCORE_SIGMOID = 1 } nm_score;
+int nm_moe_route(const void *logits, long ld_logits, const float *bias, int32_t *experts, float *weights, int T, int E, int top_k,
+                 nm_dtype dtype, nm_score score, int groups, int keep_groups, int group_best, int renormalise, float scale,
+                 nm_stream stream);
+
+/* Activations: x; max(x, 0); x / (1 + exp(-x)); x * Phi(x); x / (1 + exp(-2 sqrt(2/pi) (x + 0.044715 x^3))) (the tanh form). */
+typedef enum { NM_ACT_NONE = 0, NM_ACT_RELU = 1, NM_ACT_SILU = 2, NM_ACT_GELU = 3, NM_ACT_GELU_TANH = 4 } nm_act;
+
+/*
+ * A product with its epilogue:
+ *   gated = 0:  C = act(A B + bias) + residual                         B: K x N,  bias [N]
+ *   gated = 1:  C = act(A B_g + bias_g) o (A B_u + bias_u) + residual  B = (B_g | B_u): K x 2N,  bias [2N]
+ *   A         M rows of K, lda elements apart; residual and C: M rows of N, ld_residual and ldc apart
+ *   B         dense, NM_ROW_MAJOR ([K][N or 2N]) or NM_COL_MAJOR ([N or 2N][K])
+ *   dtype     NM_BF16 or NM_F16, of A, B, bias, residual and C alike; NM_ERR_UNSUPPORTED otherwise
+ *   M         1..NM_MAX_FFN_ROWS; N, K any >= 1 (up to 2^30)
+ * bias and residual may be NULL; residual may be C itself (same pitch).  A and B must not overlap C.  Sums are fp32, the epilogue is fp32, the result is rounded once.
+ * Equal calls give equal bits.  A and B whose rows all start on 16 bytes take the tensor-core kernel, any others a
+ * simple one.  Workspace: nm_matmul_act_workspace_bytes, counters cleared once by nm_workspace_init (and again after NM_ERR_TIMEOUT); calls that overlap on
+ * the GPU (two captured graphs among them) need workspaces of their own.  Honours nm_set_programmatic_launch (B is then read ahead of the wait).
+ */
+#define NM_MAX_FFN_ROWS 65536
+size_t nm_matmul_act_workspace_bytes(int M, int N, int K, int gated, nm_dtype dtype);
+int nm_matmul_act(const void *A, long lda, const void *B, const void *bias, const void *residual, long ld_residual, void *C, long ldc, int M,
+                  int N, int K, nm_act act, int gated, nm_dtype dtype, nm_layout layout_B, void *workspace, size_t workspace_bytes,
+                  nm_stream stream);
+
+/*
+ * The products of the chosen experts, and their weighted sum:
+ *   y[t] = residual[t] + sum_j weights[t][j] * h[t][j] W_down[e],  e = experts[t][j] - first_expert
+ *   h[t][j] = act(x[t] W_g[e]) o (x[t] W_u[e])  (gated),  act(x[t] W_u[e])  (not gated)
+ * A choice with e outside [0, E) adds nothing: -1 for padding, or an expert that another GPU holds (the results of all then add up, the residual
+ * being given to one of them).  An expert may stand twice in a token's list; it is then counted twice.
+ *   x, residual, out   T rows of d, ldx / ld_residual / ldo elements apart; out may be x or residual itself (same pitch)
+ *   experts, weights   dense [T][top_k] (nm_moe_route); weights NULL: all 1
+ *   W_up, W_down       dense, expert behind expert.  NM_COL_MAJOR: [E][2 inter][d] (gate rows, then up rows; [E][inter][d] without a gate) and [E][d][inter];
+ *                      NM_ROW_MAJOR: [E][d][2 inter] (gate columns, then up columns) and [E][inter][d]
+ *   dtype              NM_BF16 or NM_F16, of x, the weights, residual and out alike; NM_ERR_UNSUPPORTED otherwise
+ *   T * top_k          up to 2^22; E up to NM_MAX_EXPERTS
+ * Sums and activations are fp32, h is kept to 16 bits or more, the result is rounded once.  The weights of an expert that no token chose
+ * are not read.  Equal calls give equal bits.  Operands whose rows all start on 16 bytes (d and inter multiples of 8) take the tensor-core kernels, any others simple ones.
+ * Workspace: nm_moe_ffn_workspace_bytes; nothing in it has to be cleared and it keeps nothing from one call for the next; calls that
+ * overlap on the GPU (two captured graphs among them) need workspaces of their own.  Honours nm_set_programmatic_launch.
+ */
+size_t nm_moe_ffn_workspace_bytes(int T, int d, int inter, int E, int top_k, nm_dtype dtype);
+int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *weights, const void *W_up, const void *W_down,
+               const void *residual, long ld_residual, void *out, long ldo, int T, int d, int inter, int E, int top_k, int first_expert,
+               nm_act act, int gated, nm_dtype dtype, nm_layout layout, void *workspace, size_t workspace_bytes, nm_stream stream);
+
 /* ---- single-token MLA decode step ------------------------------------------------------------------ */
 
 /*

@@ -18,6 +18,8 @@ LIB_PATH = os.path.join(_PKG, "libnm.so")
 F32, BF16, BF16_F32OUT, F16 = 0, 1, 2, 3
 ROW_MAJOR, COL_MAJOR, FRACTAL_NZ = 0, 1, 2
 MAX_M = 16
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU, ACT_GELU_TANH = 0, 1, 2, 3, 4
 WS_COUNTER_BYTES = 65536
 
 if not os.path.exists(LIB_PATH):
@@ -110,6 +112,13 @@ _lib.nm_mla_cache_read_q8.argtypes = [_vp, _l, _vp, _vp, _l, _i, _i, _i, _vp]
 _lib.nm_mla_attention_q8_workspace_bytes.restype = _sz
 _lib.nm_mla_attention_q8_workspace_bytes.argtypes = [_i, _i]
 _lib.nm_mla_attention_q8.argtypes = [_vp, _l, _vp, _l, _vp, _l, _vp, _vp, _vp, _vp, _i, _i, _i, _i, C.c_float, _vp, _sz, _vp]
+_lib.nm_moe_route.argtypes = [_vp, _l, _vp, _vp, _vp] + [_i] * 9 + [C.c_float, _vp]
+_lib.nm_matmul_act_workspace_bytes.restype = _sz
+_lib.nm_matmul_act_workspace_bytes.argtypes = [_i] * 5
+_lib.nm_matmul_act.argtypes = [_vp, _l, _vp, _vp, _vp, _l, _vp, _l] + [_i] * 7 + [_vp, _sz, _vp]
+_lib.nm_moe_ffn_workspace_bytes.restype = _sz
+_lib.nm_moe_ffn_workspace_bytes.argtypes = [_i] * 6
+_lib.nm_moe_ffn.argtypes = [_vp, _l, _vp, _vp, _vp, _vp, _vp, _l, _vp, _l] + [_i] * 10 + [_vp, _sz, _vp]
 _lib.nm_mla_workspace_bytes.restype = _sz
 _lib.nm_mla_workspace_bytes.argtypes = [C.POINTER(MlaParams)]
 _lib.nm_mla_decode_step.argtypes = [C.POINTER(MlaParams), _vp, _vp]
@@ -349,6 +358,39 @@ def nm_mla_attention_q8(Q, prefix, prefix_rows, cache, cache_stride, seq_lens, o
     _check(_lib.nm_mla_attention_q8(_ptr(Q), H * (kv_lora + rope) if q_stride is None else q_stride, _ptr(prefix), prefix_rows, _ptr(cache), cache_stride,
                                     (_i * T)(*seq_lens), _ptr(o_bf16), _ptr(o_f32), _ptr(lse), T, H, kv_lora, rope, scale, _ptr(workspace),
                                     workspace.numel() * workspace.element_size(), _stream(stream)), "nm_mla_attention_q8")
+
+
+# ---- feed-forward half of a decode layer ---------------------------------------------------------------------
+
+def nm_moe_route(logits, bias, experts, weights, T, E, top_k, dtype, score=SCORE_SOFTMAX, groups=1, keep_groups=1, group_best=1, renormalise=True, scale=1.0,
+                 ld_logits=None, stream=None) -> None:
+    """bias (fp32) may be None; experts int32 and weights fp32, dense [T][top_k]; ld_logits defaults to dense rows."""
+    _check(_lib.nm_moe_route(_ptr(logits), E if ld_logits is None else ld_logits, _ptr(bias), _ptr(experts), _ptr(weights), T, E, top_k, dtype, score, groups,
+                             keep_groups, group_best, int(renormalise), scale, _stream(stream)), "nm_moe_route")
+
+
+def nm_matmul_act_workspace_bytes(M, N, K, gated=False, dtype=BF16) -> int:
+    return int(_lib.nm_matmul_act_workspace_bytes(M, N, K, int(gated), dtype))
+
+
+def nm_matmul_act(A, B, C_out, M, N, K, act, dtype, layout_B, workspace, gated=False, bias=None, residual=None, lda=None, ldc=None, ld_residual=None,
+                  stream=None) -> None:
+    """N: columns of C; B has 2 N where gated.  lda, ldc and ld_residual default to dense rows."""
+    _check(_lib.nm_matmul_act(_ptr(A), K if lda is None else lda, _ptr(B), _ptr(bias), _ptr(residual), N if ld_residual is None else ld_residual, _ptr(C_out),
+                              N if ldc is None else ldc, M, N, K, act, int(gated), dtype, layout_B, _ptr(workspace),
+                              0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "nm_matmul_act")
+
+
+def nm_moe_ffn_workspace_bytes(T, d, inter, E, top_k, dtype=BF16) -> int:
+    return int(_lib.nm_moe_ffn_workspace_bytes(T, d, inter, E, top_k, dtype))
+
+
+def nm_moe_ffn(x, experts, weights, W_up, W_down, out, T, d, inter, E, top_k, act, dtype, layout, workspace, gated=True, residual=None, first_expert=0, ldx=None,
+               ldo=None, ld_residual=None, stream=None) -> None:
+    """weights and residual may be None; ldx, ldo and ld_residual default to dense rows."""
+    _check(_lib.nm_moe_ffn(_ptr(x), d if ldx is None else ldx, _ptr(experts), _ptr(weights), _ptr(W_up), _ptr(W_down), _ptr(residual),
+                           d if ld_residual is None else ld_residual, _ptr(out), d if ldo is None else ldo, T, d, inter, E, top_k, first_expert, act, int(gated),
+                           dtype, layout, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "nm_moe_ffn")
 
 
 def mla_params(dims: dict, seq_len: int, tensors: dict, rms_eps=1e-6, softmax_scale=None, layout_dense=ROW_MAJOR,

@@ -1,0 +1,277 @@
+// Feed-forward half of a decode layer: the products of the chosen experts (nm_moe_ffn) and a product with bias, activation, gate and
+// residual in its epilogue (nm_matmul_act).
+//
+//     y[t] = residual[t] + sum_j w[t, j] * h[t, j] Wdown[e],   h[t, j] = act(x[t] Wgate[e]) o (x[t] Wup[e]),   e = experts[t, j] - first
+//
+// What bounds them: the weights of every expert that some token chose, read once from HBM.
+//
+// In this file: the kernels around the products (the weighted sum of a token's experts) and the products for operands that tensor maps cannot
+// address (rows that do not start on 16 bytes): one warp a row and 32 outputs, fp32 sums.
+#include <algorithm>
+
+#include "nm_ffn.cuh"
+
+namespace nm {
+
+namespace {
+
+constexpr int kMaxPairs = 1 << 22;
+
+// ---- products of operands of any alignment -----------------------------------------------------------------------------------
+// A block of four warps computes 32 outputs of one row.  Column-major weights: a warp per output in turn, lanes along k.  Row-major: a lane
+// per output, the warps along k, their sums joined in shared memory.  What is read is read element by element; there is nothing to reuse but
+// the row itself, which stays in L1.
+constexpr int kSimpleN = 32, kSimpleThreads = 128;
+
+struct SimpleArgs {
+    const void *x; long ldx; bool x_f32;       // token rows, 16-bit or fp32
+    const int32_t *experts; int first, E, top_k;  // NULL: one set of weights, rows as they are
+    bool x_by_pair;                             // row p of the operand belongs to pair p (else to token p / top_k)
+    const uint16_t *W; long w_expert; bool col, gated, f16;
+    const uint16_t *bias, *residual; long ld_residual;
+    void *out; long ldo; bool out_f32;
+    long rows;
+    int N, K, act;
+    Span in_x, in_W, in_bias, in_residual, in_out, in_experts;
+    unsigned *status;
+};
+
+__global__ void __launch_bounds__(kSimpleThreads) simple_product_kernel(const SimpleArgs a)
+{
+    __shared__ float s_part[2][4][kSimpleN];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int ntiles = ceil_div(a.N, kSimpleN);
+    const long total = a.rows * ntiles;
+    pdl_launch_dependents();
+    pdl_wait_prior_grids();
+    for (long item = blockIdx.x; item < total; item += gridDim.x) {
+        const long r = item / ntiles;
+        const int n0 = (int)(item % ntiles) * kSimpleN;
+        long e = 0, xr = r;
+        if (a.experts) {
+            e = (long)NM_LD(a.experts + r, a.in_experts, a.status) - a.first;
+            if (e < 0 || e >= a.E) continue;                     // the same for the whole block
+            xr = a.x_by_pair ? r : r / a.top_k;
+        }
+        const uint16_t *W = a.W + e * a.w_expert;
+        const int parts = a.gated ? 2 : 1;
+        const long wide = (long)a.N * parts;
+        auto token = [&](int k) {
+            return a.x_f32 ? NM_LD(static_cast<const float *>(a.x) + xr * a.ldx + k, a.in_x, a.status)
+                           : widen16(NM_LD(static_cast<const uint16_t *>(a.x) + xr * a.ldx + k, a.in_x, a.status), a.f16);
+        };
+        __syncthreads();                                          // the sums of the item before have been read
+        if (a.col) {
+            for (int i = warp; i < kSimpleN * parts; i += 4) {
+                const int n = n0 + i % kSimpleN, part = i / kSimpleN;
+                float sum = 0.f;
+                if (n < a.N) {
+                    const uint16_t *w = W + ((long)part * a.N + n) * a.K;
+                    for (int k = lane; k < a.K; k += 32) sum = fmaf(token(k), widen16(NM_LD(w + k, a.in_W, a.status), a.f16), sum);
+                }
+#pragma unroll
+                for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                if (lane == 0) s_part[part][0][i % kSimpleN] = sum;
+            }
+        } else {
+            const int n = n0 + lane;
+            for (int part = 0; part < parts; ++part) {
+                float sum = 0.f;
+                if (n < a.N)
+                    for (int k = warp; k < a.K; k += 4) sum = fmaf(token(k), widen16(NM_LD(W + k * wide + (long)part * a.N + n, a.in_W, a.status), a.f16), sum);
+                s_part[part][warp][lane] = sum;
+            }
+        }
+        __syncthreads();
+        const int n = n0 + lane;
+        if (warp == 0 && n < a.N) {
+            float z[2] = {0.f, 0.f};
+            for (int part = 0; part < parts; ++part) {
+                z[part] = s_part[part][0][lane];
+                if (!a.col) z[part] = (z[part] + s_part[part][1][lane]) + (s_part[part][2][lane] + s_part[part][3][lane]);
+                if (a.bias) z[part] += widen16(NM_LD(a.bias + (long)part * a.N + n, a.in_bias, a.status), a.f16);
+            }
+            float v = activate(a.act, z[0]);
+            if (a.gated) v *= z[1];
+            if (a.residual) v += widen16(NM_LD(a.residual + r * a.ld_residual + n, a.in_residual, a.status), a.f16);
+            if (a.out_f32) NM_ST(static_cast<float *>(a.out) + r * a.ldo + n, v, a.in_out, a.status);
+            else NM_ST(static_cast<uint16_t *>(a.out) + r * a.ldo + n, round16(v, a.f16), a.in_out, a.status);
+        }
+    }
+}
+
+// ---- the weighted sum of a token's experts -----------------------------------------------------------------------------------
+struct CombineArgs {
+    const float *y;                             // [rows][d]
+    const int *place;                           // pair -> row of y; NULL: the pair itself
+    const int32_t *experts; int first, E, top_k;
+    const float *weights;                       // NULL: all one
+    const uint16_t *residual; long ld_residual;
+    uint16_t *out; long ldo;
+    int T, d;
+    bool f16;
+    Span in_y, in_place, in_experts, in_weights, in_residual, in_out;
+    unsigned *status;
+};
+
+// One thread a value, the choices in their order: fp32 sum, one rounding.
+__global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a)
+{
+    pdl_launch_dependents();
+    pdl_wait_prior_grids();
+    const long total = (long)a.T * a.d;
+    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long)gridDim.x * 256) {
+        const long t = i / a.d;
+        const int n = (int)(i % a.d);
+        float sum = 0.f;
+        for (int j = 0; j < a.top_k; ++j) {
+            const long p = t * a.top_k + j;
+            const long e = (long)NM_LD(a.experts + p, a.in_experts, a.status) - a.first;
+            if (e < 0 || e >= a.E) continue;
+            const long row = a.place ? NM_LD(a.place + p, a.in_place, a.status) : p;
+            const float w = a.weights ? NM_LD(a.weights + p, a.in_weights, a.status) : 1.f;
+            sum = fmaf(w, NM_LD(a.y + row * a.d + n, a.in_y, a.status), sum);
+        }
+        if (a.residual) sum += widen16(NM_LD(a.residual + t * a.ld_residual + n, a.in_residual, a.status), a.f16);
+        NM_ST(a.out + t * a.ldo + n, round16(sum, a.f16), a.in_out, a.status);
+    }
+}
+
+template <typename... P, typename... Args>
+cudaError_t launch(void (*kern)(P...), long grid, unsigned threads, bool programmatic, cudaStream_t s, const Args &...args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)std::min<long>(grid, 1 << 20));
+    cfg.blockDim = dim3(threads);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = programmatic ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kern, args...);
+}
+
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+bool ffn_dtype_ok(nm_dtype t) { return t == NM_BF16 || t == NM_F16; }
+bool ffn_layout_ok(nm_layout l) { return l == NM_ROW_MAJOR || l == NM_COL_MAJOR; }
+bool act_ok(nm_act act) { return act >= NM_ACT_NONE && act <= NM_ACT_GELU_TANH; }
+
+struct MoeLayout { size_t h, y, total; };
+MoeLayout moe_layout(long pairs, int d, int inter)
+{
+    MoeLayout l;
+    size_t at = NM_WS_COUNTER_BYTES;
+    l.h = at; at += align256((size_t)pairs * inter * 4);
+    l.y = at; at += align256((size_t)pairs * d * 4);
+    l.total = at;
+    return l;
+}
+
+}  // namespace
+
+}  // namespace nm
+
+using namespace nm;
+
+extern "C" {
+#pragma GCC visibility push(default)
+
+size_t nm_matmul_act_workspace_bytes(int M, int N, int K, int gated, nm_dtype dtype)
+{
+    if (M < 1 || N < 1 || K < 1 || !ffn_dtype_ok(dtype)) return 0;
+    (void)gated;
+    return NM_WS_COUNTER_BYTES;
+}
+
+int nm_matmul_act(const void *A, long lda, const void *B, const void *bias, const void *residual, long ld_residual, void *C, long ldc, int M,
+                  int N, int K, nm_act act, int gated, nm_dtype dtype, nm_layout layout_B, void *workspace, size_t workspace_bytes,
+                  nm_stream stream)
+{
+    if (!A || !B || !C || M < 1 || M > NM_MAX_FFN_ROWS || N < 1 || N > (1 << 30) || K < 1 || K > (1 << 30) || lda < K || ldc < N || (residual && ld_residual < N)) return NM_ERR_INVALID_ARG;
+    if (!ffn_dtype_ok(dtype) || !ffn_layout_ok(layout_B) || !act_ok(act)) return NM_ERR_UNSUPPORTED;
+    if (((uintptr_t)A & 1u) || ((uintptr_t)B & 1u) || ((uintptr_t)C & 1u) || ((uintptr_t)bias & 1u) || ((uintptr_t)residual & 1u)) return NM_ERR_ALIGNMENT;
+    if (!workspace || workspace_bytes < nm_matmul_act_workspace_bytes(M, N, K, gated, dtype)) return NM_ERR_WORKSPACE;
+    if ((uintptr_t)workspace & 15u) return NM_ERR_ALIGNMENT;
+    const int parts = gated ? 2 : 1;
+    SimpleArgs a{};
+    a.x = A; a.ldx = lda;
+    a.W = static_cast<const uint16_t *>(B); a.col = layout_B == NM_COL_MAJOR; a.gated = gated != 0; a.f16 = dtype == NM_F16;
+    a.bias = static_cast<const uint16_t *>(bias); a.residual = static_cast<const uint16_t *>(residual); a.ld_residual = ld_residual;
+    a.out = C; a.ldo = ldc;
+    a.rows = M; a.N = N; a.K = K; a.act = act;
+    a.in_x = make_span(A, 2 * ((size_t)(M - 1) * lda + K));
+    a.in_W = make_span(B, 2 * (size_t)parts * N * K);
+    a.in_bias = make_span(bias, bias ? 2 * (size_t)parts * N : 0);
+    a.in_residual = make_span(residual, residual ? 2 * ((size_t)(M - 1) * ld_residual + N) : 0);
+    a.in_out = make_span(C, 2 * ((size_t)(M - 1) * ldc + N));
+    a.status = bounds_status_ptr();
+    const cudaError_t e = launch(simple_product_kernel, (long)M * ceil_div(N, kSimpleN), kSimpleThreads, programmatic_launch_enabled(), (cudaStream_t)stream, a);
+    return e == cudaSuccess ? NM_OK : record_cuda_error(e, "product with epilogue launch");
+}
+
+size_t nm_moe_ffn_workspace_bytes(int T, int d, int inter, int E, int top_k, nm_dtype dtype)
+{
+    if (T < 1 || d < 1 || inter < 1 || E < 1 || top_k < 1 || (long)T * top_k > kMaxPairs || !ffn_dtype_ok(dtype)) return 0;
+    return moe_layout((long)T * top_k, d, inter).total;
+}
+
+int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *weights, const void *W_up, const void *W_down,
+               const void *residual, long ld_residual, void *out, long ldo, int T, int d, int inter, int E, int top_k, int first_expert,
+               nm_act act, int gated, nm_dtype dtype, nm_layout layout, void *workspace, size_t workspace_bytes, nm_stream stream)
+{
+    if (!x || !experts || !W_up || !W_down || !out || T < 1 || d < 1 || d > (1 << 24) || inter < 1 || inter > (1 << 24) || E < 1 || top_k < 1 ||
+        first_expert < 0 || ldx < d || ldo < d || (residual && ld_residual < d))
+        return NM_ERR_INVALID_ARG;
+    if (!ffn_dtype_ok(dtype) || !ffn_layout_ok(layout) || !act_ok(act) || E > NM_MAX_EXPERTS || (long)T * top_k > kMaxPairs) return NM_ERR_UNSUPPORTED;
+    if (((uintptr_t)x & 1u) || ((uintptr_t)W_up & 1u) || ((uintptr_t)W_down & 1u) || ((uintptr_t)residual & 1u) || ((uintptr_t)out & 1u) ||
+        ((uintptr_t)experts & 3u) || ((uintptr_t)weights & 3u))
+        return NM_ERR_ALIGNMENT;
+    if (!workspace || workspace_bytes < nm_moe_ffn_workspace_bytes(T, d, inter, E, top_k, dtype)) return NM_ERR_WORKSPACE;
+    if ((uintptr_t)workspace & 15u) return NM_ERR_ALIGNMENT;
+    cudaStream_t s = (cudaStream_t)stream;
+    const long pairs = (long)T * top_k;
+    const MoeLayout lay = moe_layout(pairs, d, inter);
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+    float *h = reinterpret_cast<float *>(ws + lay.h), *y = reinterpret_cast<float *>(ws + lay.y);
+    const int parts = gated ? 2 : 1;
+
+    SimpleArgs a{};
+    a.x = x; a.ldx = ldx;
+    a.experts = experts; a.first = first_expert; a.E = E; a.top_k = top_k;
+    a.W = static_cast<const uint16_t *>(W_up); a.w_expert = (long)parts * inter * d; a.col = layout == NM_COL_MAJOR; a.gated = gated != 0; a.f16 = dtype == NM_F16;
+    a.out = h; a.ldo = inter; a.out_f32 = true;
+    a.rows = pairs; a.N = inter; a.K = d; a.act = act;
+    a.in_x = make_span(x, 2 * ((size_t)(T - 1) * ldx + d));
+    a.in_W = make_span(W_up, 2 * (size_t)E * a.w_expert);
+    a.in_experts = make_span(experts, 4 * (size_t)pairs);
+    a.in_out = make_span(h, 4 * (size_t)pairs * inter);
+    a.status = bounds_status_ptr();
+    cudaError_t e = launch(simple_product_kernel, pairs * ceil_div(inter, kSimpleN), kSimpleThreads, programmatic_launch_enabled(), s, a);
+
+    SimpleArgs b = a;
+    b.x = h; b.ldx = inter; b.x_f32 = true; b.x_by_pair = true;
+    b.W = static_cast<const uint16_t *>(W_down); b.w_expert = (long)inter * d; b.gated = false;
+    b.out = y; b.ldo = d;
+    b.N = d; b.K = inter; b.act = NM_ACT_NONE;
+    b.in_x = a.in_out;
+    b.in_W = make_span(W_down, 2 * (size_t)E * b.w_expert);
+    b.in_out = make_span(y, 4 * (size_t)pairs * d);
+    if (e == cudaSuccess) e = launch(simple_product_kernel, pairs * ceil_div(d, kSimpleN), kSimpleThreads, true, s, b);
+
+    CombineArgs c{};
+    c.y = y; c.experts = experts; c.first = first_expert; c.E = E; c.top_k = top_k; c.weights = weights;
+    c.residual = static_cast<const uint16_t *>(residual); c.ld_residual = ld_residual;
+    c.out = static_cast<uint16_t *>(out); c.ldo = ldo; c.T = T; c.d = d; c.f16 = a.f16;
+    c.in_y = b.in_out; c.in_experts = a.in_experts;
+    c.in_weights = make_span(weights, weights ? 4 * (size_t)pairs : 0);
+    c.in_residual = make_span(residual, residual ? 2 * ((size_t)(T - 1) * ld_residual + d) : 0);
+    c.in_out = make_span(out, 2 * ((size_t)(T - 1) * ldo + d));
+    c.status = a.status;
+    if (e == cudaSuccess) e = launch(combine_kernel, ((long)T * d + 255) / 256, 256, true, s, c);
+    return e == cudaSuccess ? NM_OK : record_cuda_error(e, "experts' products launch");
+}
+
+#pragma GCC visibility pop
+}  // extern "C"
