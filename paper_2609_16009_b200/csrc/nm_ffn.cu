@@ -137,6 +137,111 @@ __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a)
     }
 }
 
+// ---- rows by expert ------------------------------------------------------------------------------------------------------------
+// A CTA an expert: all count how many pairs each expert has (shared-memory counters), so each knows where its own rows begin, and then puts its
+// pairs there in their order.  Nothing is passed between CTAs and the order is always the same.
+constexpr int kPlanThreads = 512;
+struct PlanArgs {
+    const int32_t *experts; int first, E;
+    int pairs, R;
+    RowTile *tiles; int *n_tiles; int *order; int *place;
+    unsigned *counters;                         // cleared for the products that follow
+    Span in_experts, in_tiles, in_order, in_place;
+    unsigned *status;
+};
+
+__device__ __forceinline__ int block_sum(int v, int *s_warp)     // the same for all threads
+{
+    v = __reduce_add_sync(0xffffffffu, v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = v;
+    __syncthreads();
+    int sum = 0;
+#pragma unroll
+    for (int i = 0; i < kPlanThreads / 32; ++i) sum += s_warp[i];
+    return sum;
+}
+
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a)
+{
+    __shared__ int s_count[NM_MAX_EXPERTS], s_warp[kPlanThreads / 32], s_before[2][kPlanThreads / 32];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, mine = blockIdx.x;
+    for (int i = tid; i < a.E; i += kPlanThreads) s_count[i] = 0;
+    pdl_launch_dependents();
+    pdl_wait_prior_grids();
+    __syncthreads();
+    auto expert_of = [&](int p) {
+        const long e = (long)NM_LD(a.experts + p, a.in_experts, a.status) - a.first;
+        return e >= 0 && e < a.E ? (int)e : -1;
+    };
+    for (int p = tid; p < a.pairs; p += kPlanThreads) {
+        const int e = expert_of(p);
+        if (e >= 0) atomicAdd(&s_count[e], 1);
+    }
+    __syncthreads();
+    int rows = 0, tiles = 0;
+    for (int i = tid; i < mine; i += kPlanThreads) { rows += s_count[i]; tiles += ceil_div(s_count[i], a.R); }
+    const int row0 = block_sum(rows, s_warp), tile0 = block_sum(tiles, s_warp);
+    const int count = s_count[mine], own = ceil_div(count, a.R);
+    if (mine == a.E - 1 && tid == 0) *a.n_tiles = tile0 + own;
+    if (mine == 0 && tid < kSMs) a.counters[tid] = 0u;
+    for (int i = tid; i < own; i += kPlanThreads) NM_ST(a.tiles + tile0 + i, (RowTile{mine, row0 + i * a.R, min(a.R, count - i * a.R), 0}), a.in_tiles, a.status);
+    if (count == 0) return;
+    int at = row0;
+    for (int p0 = 0, buf = 0; p0 < a.pairs; p0 += kPlanThreads, buf ^= 1) {
+        const int p = p0 + tid;
+        const bool here = p < a.pairs && expert_of(p) == mine;
+        const unsigned votes = __ballot_sync(0xffffffffu, here);
+        if (lane == 0) s_before[buf][warp] = __popc(votes);
+        __syncthreads();
+        int before = 0, all = 0;
+#pragma unroll
+        for (int i = 0; i < kPlanThreads / 32; ++i) { const int n = s_before[buf][i]; before += i < warp ? n : 0; all += n; }
+        if (here) {
+            const int row = at + before + __popc(votes & ((1u << lane) - 1u));
+            NM_ST(a.order + row, p, a.in_order, a.status);
+            NM_ST(a.place + p, row, a.in_place, a.status);
+        }
+        at += all;
+    }
+}
+
+// ---- fp16: hidden values beyond the type's range ---------------------------------------------------------------------------------
+// act(g) * u may leave fp16 at either end, so a row is scaled by a power of two that brings its largest value to 2^14 .. 2^15, and the product's
+// row is scaled back (fp32, exact).  Two terms: 22 bits, down to 2^-40 of the row's largest.
+__global__ void __launch_bounds__(256) hidden_terms_kernel(const float *h, uint16_t *terms, float *row_scale, int rows, int n, unsigned *status, Span in_h, Span in_terms, Span in_scale)
+{
+    __shared__ float s_max[8];
+    pdl_launch_dependents();
+    pdl_wait_prior_grids();
+    for (int r = blockIdx.x; r < rows; r += gridDim.x) {
+        const float *x = h + (size_t)r * n;
+        float m = 0.f;
+        for (int i = threadIdx.x; i < n; i += 256) {
+            const float v = fabsf(NM_LD(x + i, in_h, status));
+            if (v < INFINITY) m = fmaxf(m, v);
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        __syncthreads();
+        if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = fmaxf(m, s_max[i]);
+        int e = 0;
+        if (m > 0.f) { frexpf(m, &e); e = max(e - 15, -100); }   // (not below 2^-100: the factor back has to be a normal number)
+        for (int i = threadIdx.x; i < n; i += 256) {
+            const float v = scalbnf(NM_LD(x + i, in_h, status), -e);
+            const __half hi = __float2half_rn(v);
+            const float rest = v - __half2float(hi);
+            uint16_t *to = terms + (size_t)r * n + i;
+            NM_ST(to, __half_as_ushort(hi), in_terms, status);
+            NM_ST(to + (size_t)rows * n, fabsf(v) < INFINITY ? __half_as_ushort(__float2half_rn(rest)) : (uint16_t)0, in_terms, status);
+        }
+        if (threadIdx.x == 0) NM_ST(row_scale + r, scalbnf(1.f, e), in_scale, status);
+    }
+}
+
 template <typename... P, typename... Args>
 cudaError_t launch(void (*kern)(P...), long grid, unsigned threads, bool programmatic, cudaStream_t s, const Args &...args)
 {
@@ -158,13 +263,26 @@ bool ffn_dtype_ok(nm_dtype t) { return t == NM_BF16 || t == NM_F16; }
 bool ffn_layout_ok(nm_layout l) { return l == NM_ROW_MAJOR || l == NM_COL_MAJOR; }
 bool act_ok(nm_act act) { return act >= NM_ACT_NONE && act <= NM_ACT_GELU_TANH; }
 
-struct MoeLayout { size_t h, y, total; };
-MoeLayout moe_layout(long pairs, int d, int inter)
+// Whether tensor maps can address rows of `pitch` 16-bit elements at p: both on 16 bytes.
+bool rows_on_16(const void *p, long pitch) { return !((uintptr_t)p & 15u) && pitch % 8 == 0; }
+
+struct MoeLayout { size_t tiles, n_tiles, order, place, partial, h, terms, scale, y, total; };
+MoeLayout moe_layout(long pairs, int T, int d, int inter, int E, bool f16)
 {
-    MoeLayout l;
-    size_t at = NM_WS_COUNTER_BYTES;
-    l.h = at; at += align256((size_t)pairs * inter * 4);
-    l.y = at; at += align256((size_t)pairs * d * 4);
+    const int R = stream_tile_rows((double)pairs / E, (int)std::min<long>(pairs, 128));
+    (void)T;
+    MoeLayout l{};
+    size_t at = 1024;                                             // counters
+    l.n_tiles = at; at += 256;
+    l.tiles = at; at += align256((E + pairs / 16) * sizeof(RowTile));
+    l.order = at; at += align256(4 * (size_t)pairs);
+    l.place = at; at += align256(4 * (size_t)pairs);
+    l.scale = at; at += align256(4 * (size_t)pairs);
+    l.partial = at; at += align256(stream_partial_bytes(R, 2));
+    l.h = at; at += align256(4 * (size_t)pairs * inter);
+    l.terms = f16 ? at : l.h;
+    if (f16) at += align256(4 * (size_t)pairs * inter);
+    l.y = at; at += align256(4 * (size_t)pairs * d);
     l.total = at;
     return l;
 }
@@ -181,8 +299,9 @@ extern "C" {
 size_t nm_matmul_act_workspace_bytes(int M, int N, int K, int gated, nm_dtype dtype)
 {
     if (M < 1 || N < 1 || K < 1 || !ffn_dtype_ok(dtype)) return 0;
-    (void)gated;
-    return NM_WS_COUNTER_BYTES;
+    (void)N; (void)K;
+    const int R = stream_tile_rows(M, M);
+    return NM_WS_COUNTER_BYTES + stream_partial_bytes(R, stream_slabs(R, gated != 0));
 }
 
 int nm_matmul_act(const void *A, long lda, const void *B, const void *bias, const void *residual, long ld_residual, void *C, long ldc, int M,
@@ -195,6 +314,23 @@ int nm_matmul_act(const void *A, long lda, const void *B, const void *bias, cons
     if (!workspace || workspace_bytes < nm_matmul_act_workspace_bytes(M, N, K, gated, dtype)) return NM_ERR_WORKSPACE;
     if ((uintptr_t)workspace & 15u) return NM_ERR_ALIGNMENT;
     const int parts = gated ? 2 : 1;
+    cudaStream_t s = (cudaStream_t)stream;
+    const bool col = layout_B == NM_COL_MAJOR, programmatic = programmatic_launch_enabled();
+    if (rows_on_16(A, lda) && rows_on_16(B, col ? K : N)) {
+        ProductArgs p{};
+        p.rows = M; p.N = N; p.K = K; p.R = stream_tile_rows(M, M); p.terms = 1;
+        p.col = col; p.f16 = dtype == NM_F16; p.early_weights = p.programmatic = programmatic;
+        p.act = act;
+        p.W = B; p.w_expert = (long)parts * N * K; p.E = 1;
+        p.x = A; p.ldx = lda; p.x_rows = M; p.x_term = (long)M * lda;
+        p.bias = bias; p.residual = residual; p.ld_residual = ld_residual;
+        p.out = C; p.ldo = ldc;
+        p.counters = static_cast<unsigned *>(workspace);
+        p.partial = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + NM_WS_COUNTER_BYTES);
+        const char *what = "";
+        const cudaError_t e = launch_product(kOutAct, gated != 0, p, s, &what);
+        return e == cudaSuccess ? NM_OK : record_cuda_error(e, what);
+    }
     SimpleArgs a{};
     a.x = A; a.ldx = lda;
     a.W = static_cast<const uint16_t *>(B); a.col = layout_B == NM_COL_MAJOR; a.gated = gated != 0; a.f16 = dtype == NM_F16;
@@ -207,14 +343,14 @@ int nm_matmul_act(const void *A, long lda, const void *B, const void *bias, cons
     a.in_residual = make_span(residual, residual ? 2 * ((size_t)(M - 1) * ld_residual + N) : 0);
     a.in_out = make_span(C, 2 * ((size_t)(M - 1) * ldc + N));
     a.status = bounds_status_ptr();
-    const cudaError_t e = launch(simple_product_kernel, (long)M * ceil_div(N, kSimpleN), kSimpleThreads, programmatic_launch_enabled(), (cudaStream_t)stream, a);
+    const cudaError_t e = launch(simple_product_kernel, (long)M * ceil_div(N, kSimpleN), kSimpleThreads, programmatic, s, a);
     return e == cudaSuccess ? NM_OK : record_cuda_error(e, "product with epilogue launch");
 }
 
 size_t nm_moe_ffn_workspace_bytes(int T, int d, int inter, int E, int top_k, nm_dtype dtype)
 {
     if (T < 1 || d < 1 || inter < 1 || E < 1 || top_k < 1 || (long)T * top_k > kMaxPairs || !ffn_dtype_ok(dtype)) return 0;
-    return moe_layout((long)T * top_k, d, inter).total;
+    return moe_layout((long)T * top_k, T, d, inter, E, dtype == NM_F16).total;
 }
 
 int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *weights, const void *W_up, const void *W_down,
@@ -232,45 +368,89 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
     if ((uintptr_t)workspace & 15u) return NM_ERR_ALIGNMENT;
     cudaStream_t s = (cudaStream_t)stream;
     const long pairs = (long)T * top_k;
-    const MoeLayout lay = moe_layout(pairs, d, inter);
+    const bool col = layout == NM_COL_MAJOR, f16 = dtype == NM_F16, programmatic = programmatic_launch_enabled();
+    const MoeLayout lay = moe_layout(pairs, T, d, inter, E, f16);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     float *h = reinterpret_cast<float *>(ws + lay.h), *y = reinterpret_cast<float *>(ws + lay.y);
+    const int *place = nullptr;
     const int parts = gated ? 2 : 1;
+    const Span in_experts = make_span(experts, 4 * (size_t)pairs);
+    unsigned *const status = bounds_status_ptr();
+    const char *what = "experts' products launch";
+    cudaError_t e;
+    if (rows_on_16(x, ldx) && rows_on_16(W_up, col ? d : inter) && rows_on_16(W_down, col ? inter : d) && inter % 8 == 0) {
+        PlanArgs pl{};
+        pl.experts = experts; pl.first = first_expert; pl.E = E; pl.pairs = (int)pairs;
+        pl.R = stream_tile_rows((double)pairs / E, (int)std::min<long>(pairs, 128));
+        pl.tiles = reinterpret_cast<RowTile *>(ws + lay.tiles); pl.n_tiles = reinterpret_cast<int *>(ws + lay.n_tiles);
+        pl.order = reinterpret_cast<int *>(ws + lay.order); pl.place = reinterpret_cast<int *>(ws + lay.place);
+        pl.counters = reinterpret_cast<unsigned *>(ws);
+        pl.in_experts = in_experts; pl.in_tiles = make_span(pl.tiles, sizeof(RowTile) * (E + (size_t)pairs / pl.R));
+        pl.in_order = make_span(pl.order, 4 * (size_t)pairs); pl.in_place = make_span(pl.place, 4 * (size_t)pairs);
+        pl.status = status;
+        place = pl.place;
+        e = launch(plan_kernel, E, kPlanThreads, programmatic, s, pl);
 
-    SimpleArgs a{};
-    a.x = x; a.ldx = ldx;
-    a.experts = experts; a.first = first_expert; a.E = E; a.top_k = top_k;
-    a.W = static_cast<const uint16_t *>(W_up); a.w_expert = (long)parts * inter * d; a.col = layout == NM_COL_MAJOR; a.gated = gated != 0; a.f16 = dtype == NM_F16;
-    a.out = h; a.ldo = inter; a.out_f32 = true;
-    a.rows = pairs; a.N = inter; a.K = d; a.act = act;
-    a.in_x = make_span(x, 2 * ((size_t)(T - 1) * ldx + d));
-    a.in_W = make_span(W_up, 2 * (size_t)E * a.w_expert);
-    a.in_experts = make_span(experts, 4 * (size_t)pairs);
-    a.in_out = make_span(h, 4 * (size_t)pairs * inter);
-    a.status = bounds_status_ptr();
-    cudaError_t e = launch(simple_product_kernel, pairs * ceil_div(inter, kSimpleN), kSimpleThreads, programmatic_launch_enabled(), s, a);
+        ProductArgs p{};
+        p.rows = (int)pairs; p.N = inter; p.K = d; p.R = pl.R; p.terms = 1;
+        p.col = col; p.f16 = f16; p.gather = p.planned = p.programmatic = true;
+        p.act = act;
+        p.plan = RowPlan{pl.tiles, pl.n_tiles, pl.order, pl.place, top_k};
+        p.W = W_up; p.w_expert = (long)parts * inter * d; p.E = E;
+        p.x = x; p.ldx = ldx; p.x_rows = T;
+        p.out = h; p.ldo = inter;
+        p.counters = pl.counters; p.partial = reinterpret_cast<float *>(ws + lay.partial);
+        if (e == cudaSuccess) e = launch_product(kOutHidden, gated != 0, p, s, &what);
 
-    SimpleArgs b = a;
-    b.x = h; b.ldx = inter; b.x_f32 = true; b.x_by_pair = true;
-    b.W = static_cast<const uint16_t *>(W_down); b.w_expert = (long)inter * d; b.gated = false;
-    b.out = y; b.ldo = d;
-    b.N = d; b.K = inter; b.act = NM_ACT_NONE;
-    b.in_x = a.in_out;
-    b.in_W = make_span(W_down, 2 * (size_t)E * b.w_expert);
-    b.in_out = make_span(y, 4 * (size_t)pairs * d);
-    if (e == cudaSuccess) e = launch(simple_product_kernel, pairs * ceil_div(d, kSimpleN), kSimpleThreads, true, s, b);
+        float *row_scale = reinterpret_cast<float *>(ws + lay.scale);
+        uint16_t *terms = reinterpret_cast<uint16_t *>(ws + lay.terms);
+        if (e == cudaSuccess && f16)
+            e = launch(hidden_terms_kernel, pairs, 256, true, s, static_cast<const float *>(h), terms, row_scale, (int)pairs, inter, status, make_span(h, 4 * (size_t)pairs * inter),
+                       make_span(terms, 4 * (size_t)pairs * inter), make_span(row_scale, 4 * (size_t)pairs));
+
+        ProductArgs q = p;
+        q.N = d; q.K = inter; q.terms = 2; q.gather = false; q.early_weights = true; q.act = NM_ACT_NONE;
+        q.W = W_down; q.w_expert = (long)inter * d;
+        q.x = terms; q.ldx = inter; q.x_rows = pairs; q.x_term = pairs * inter;
+        q.row_scale = f16 ? row_scale : nullptr;
+        q.out = y; q.ldo = d;
+        if (e == cudaSuccess) e = launch_product(kOutDown, false, q, s, &what);
+    } else {
+        SimpleArgs a{};
+        a.x = x; a.ldx = ldx;
+        a.experts = experts; a.first = first_expert; a.E = E; a.top_k = top_k;
+        a.W = static_cast<const uint16_t *>(W_up); a.w_expert = (long)parts * inter * d; a.col = col; a.gated = gated != 0; a.f16 = f16;
+        a.out = h; a.ldo = inter; a.out_f32 = true;
+        a.rows = pairs; a.N = inter; a.K = d; a.act = act;
+        a.in_x = make_span(x, 2 * ((size_t)(T - 1) * ldx + d));
+        a.in_W = make_span(W_up, 2 * (size_t)E * a.w_expert);
+        a.in_experts = in_experts;
+        a.in_out = make_span(h, 4 * (size_t)pairs * inter);
+        a.status = status;
+        e = launch(simple_product_kernel, pairs * ceil_div(inter, kSimpleN), kSimpleThreads, programmatic, s, a);
+
+        SimpleArgs b = a;
+        b.x = h; b.ldx = inter; b.x_f32 = true; b.x_by_pair = true;
+        b.W = static_cast<const uint16_t *>(W_down); b.w_expert = (long)inter * d; b.gated = false;
+        b.out = y; b.ldo = d;
+        b.N = d; b.K = inter; b.act = NM_ACT_NONE;
+        b.in_x = a.in_out;
+        b.in_W = make_span(W_down, 2 * (size_t)E * b.w_expert);
+        b.in_out = make_span(y, 4 * (size_t)pairs * d);
+        if (e == cudaSuccess) e = launch(simple_product_kernel, pairs * ceil_div(d, kSimpleN), kSimpleThreads, true, s, b);
+    }
 
     CombineArgs c{};
-    c.y = y; c.experts = experts; c.first = first_expert; c.E = E; c.top_k = top_k; c.weights = weights;
+    c.y = y; c.place = place; c.experts = experts; c.first = first_expert; c.E = E; c.top_k = top_k; c.weights = weights;
     c.residual = static_cast<const uint16_t *>(residual); c.ld_residual = ld_residual;
-    c.out = static_cast<uint16_t *>(out); c.ldo = ldo; c.T = T; c.d = d; c.f16 = a.f16;
-    c.in_y = b.in_out; c.in_experts = a.in_experts;
+    c.out = static_cast<uint16_t *>(out); c.ldo = ldo; c.T = T; c.d = d; c.f16 = f16;
+    c.in_y = make_span(y, 4 * (size_t)pairs * d); c.in_experts = in_experts; c.in_place = make_span(place, place ? 4 * (size_t)pairs : 0);
     c.in_weights = make_span(weights, weights ? 4 * (size_t)pairs : 0);
     c.in_residual = make_span(residual, residual ? 2 * ((size_t)(T - 1) * ld_residual + d) : 0);
     c.in_out = make_span(out, 2 * ((size_t)(T - 1) * ldo + d));
-    c.status = a.status;
+    c.status = status;
     if (e == cudaSuccess) e = launch(combine_kernel, ((long)T * d + 255) / 256, 256, true, s, c);
-    return e == cudaSuccess ? NM_OK : record_cuda_error(e, "experts' products launch");
+    return e == cudaSuccess ? NM_OK : record_cuda_error(e, what);
 }
 
 #pragma GCC visibility pop
