@@ -114,26 +114,78 @@ struct CombineArgs {
     unsigned *status;
 };
 
-// One thread a value, the choices in their order: fp32 sum, one rounding.
+// A block takes kV * 256 columns of one token: the token's rows and weights once, then the choices in their order, eight rows of y asked for at a
+// time; fp32 sum, one rounding.  kV = 4: 16-byte loads (d, pitches and pointers allow them); kV = 1: any.
+constexpr int kCombineChoices = 64;             // choices whose rows a block keeps at a time
+template <int kV>
 __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a)
 {
+    __shared__ int s_row[kCombineChoices];
+    __shared__ float s_weight[kCombineChoices];
     pdl_launch_dependents();
+    const int chunks = ceil_div(a.d, 256 * kV);
+    const long total = (long)a.T * chunks;
     pdl_wait_prior_grids();
-    const long total = (long)a.T * a.d;
-    for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < total; i += (long)gridDim.x * 256) {
-        const long t = i / a.d;
-        const int n = (int)(i % a.d);
-        float sum = 0.f;
-        for (int j = 0; j < a.top_k; ++j) {
-            const long p = t * a.top_k + j;
-            const long e = (long)NM_LD(a.experts + p, a.in_experts, a.status) - a.first;
-            if (e < 0 || e >= a.E) continue;
-            const long row = a.place ? NM_LD(a.place + p, a.in_place, a.status) : p;
-            const float w = a.weights ? NM_LD(a.weights + p, a.in_weights, a.status) : 1.f;
-            sum = fmaf(w, NM_LD(a.y + row * a.d + n, a.in_y, a.status), sum);
+    for (long item = blockIdx.x; item < total; item += gridDim.x) {
+        const long t = item / chunks;
+        const int n = ((int)(item % chunks) * 256 + (int)threadIdx.x) * kV;
+        float sum[kV], skip[kV];
+#pragma unroll
+        for (int i = 0; i < kV; ++i) { sum[i] = 0.f; skip[i] = 0.f; }
+        if (a.residual && n < a.d) {
+            const uint16_t *r = a.residual + t * a.ld_residual + n;
+            if constexpr (kV == 4) {
+                const uint2 v = NM_LD(reinterpret_cast<const uint2 *>(r), a.in_residual, a.status);
+                skip[0] = widen16((uint16_t)v.x, a.f16); skip[1] = widen16((uint16_t)(v.x >> 16), a.f16);
+                skip[2] = widen16((uint16_t)v.y, a.f16); skip[3] = widen16((uint16_t)(v.y >> 16), a.f16);
+            } else {
+                skip[0] = widen16(NM_LD(r, a.in_residual, a.status), a.f16);
+            }
         }
-        if (a.residual) sum += widen16(NM_LD(a.residual + t * a.ld_residual + n, a.in_residual, a.status), a.f16);
-        NM_ST(a.out + t * a.ldo + n, round16(sum, a.f16), a.in_out, a.status);
+        for (int j0 = 0; j0 < a.top_k; j0 += kCombineChoices) {
+            const int here = min(kCombineChoices, a.top_k - j0);
+            __syncthreads();
+            if ((int)threadIdx.x < here) {
+                const long p = t * a.top_k + j0 + threadIdx.x;
+                const long e = (long)NM_LD(a.experts + p, a.in_experts, a.status) - a.first;
+                const bool held = e >= 0 && e < a.E;
+                s_row[threadIdx.x] = !held ? -1 : a.place ? NM_LD(a.place + p, a.in_place, a.status) : (int)p;
+                s_weight[threadIdx.x] = held && a.weights ? NM_LD(a.weights + p, a.in_weights, a.status) : 1.f;
+            }
+            __syncthreads();
+            if (n < a.d)
+                for (int j = 0; j < here; j += 8) {
+                    float v[8][kV];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const int row = j + q < here ? s_row[j + q] : -1;
+                        const float *y = a.y + (long)row * a.d + n;
+                        if constexpr (kV == 4) {
+                            float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
+                            if (row >= 0) f = NM_LD(reinterpret_cast<const float4 *>(y), a.in_y, a.status);
+                            v[q][0] = f.x; v[q][1] = f.y; v[q][2] = f.z; v[q][3] = f.w;
+                        } else {
+                            v[q][0] = row >= 0 ? NM_LD(y, a.in_y, a.status) : 0.f;
+                        }
+                    }
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (j + q < here && s_row[j + q] >= 0)
+#pragma unroll
+                            for (int i = 0; i < kV; ++i) sum[i] = fmaf(s_weight[j + q], v[q][i], sum[i]);
+                }
+        }
+        if (n < a.d) {
+            uint16_t *o = a.out + t * a.ldo + n;
+            if constexpr (kV == 4) {
+                uint32_t w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[i] = round16(sum[i] + skip[i], a.f16);
+                NM_ST(reinterpret_cast<uint2 *>(o), make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16), a.in_out, a.status);
+            } else {
+                NM_ST(o, round16(sum[0] + skip[0], a.f16), a.in_out, a.status);
+            }
+        }
     }
 }
 
@@ -449,7 +501,8 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
     c.in_residual = make_span(residual, residual ? 2 * ((size_t)(T - 1) * ld_residual + d) : 0);
     c.in_out = make_span(out, 2 * ((size_t)(T - 1) * ldo + d));
     c.status = status;
-    if (e == cudaSuccess) e = launch(combine_kernel, ((long)T * d + 255) / 256, 256, true, s, c);
+    const bool wide = d % 4 == 0 && ldo % 4 == 0 && !((uintptr_t)out & 7u) && (!residual || (ld_residual % 4 == 0 && !((uintptr_t)residual & 7u)));
+    if (e == cudaSuccess) e = wide ? launch(combine_kernel<4>, (long)T * ceil_div(d, 1024), 256, true, s, c) : launch(combine_kernel<1>, (long)T * ceil_div(d, 256), 256, true, s, c);
     return e == cudaSuccess ? NM_OK : record_cuda_error(e, what);
 }
 

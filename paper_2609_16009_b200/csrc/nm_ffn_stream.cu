@@ -102,12 +102,17 @@ __device__ __forceinline__ void finish(const StreamArgs &a, int r, int count, in
     if constexpr (kMode == kOutAct) {
         const float b0 = a.bias ? widen16(NM_LD(a.bias + n, a.in_bias, a.status), a.f16) : 0.f;
         const float b1 = kGated && a.bias ? widen16(NM_LD(a.bias + a.N + n, a.in_bias, a.status), a.f16) : 0.f;
+        // All of the residual before the first store: it may be the output itself, so no load would be moved ahead of a store.
+        float more[kW];
+#pragma unroll
+        for (int i = 0; i < kW; ++i)
+            more[i] = a.residual && i < count ? widen16(NM_LD(a.residual + (long)(r + i) * a.ld_residual + n, a.in_residual, a.status), a.f16) : 0.f;
 #pragma unroll
         for (int i = 0; i < kW; ++i) {
             if (i < count) {
                 float v = activate(a.act, a.bias ? z[i] + b0 : z[i]);
                 if constexpr (kGated) v *= a.bias ? z2[i] + b1 : z2[i];
-                if (a.residual) v += widen16(NM_LD(a.residual + (long)(r + i) * a.ld_residual + n, a.in_residual, a.status), a.f16);
+                if (a.residual) v += more[i];
                 NM_ST(static_cast<uint16_t *>(a.out) + (long)(r + i) * a.ldo + n, round16(v, a.f16), a.in_out, a.status);
             }
         }
@@ -139,6 +144,50 @@ __device__ __forceinline__ void finish(const StreamArgs &a, int r, int count, in
                 NM_ST(static_cast<float *>(a.out) + (long)(r + i) * a.ldo + n, z[i] * s, a.in_out, a.status);
             }
         }
+    }
+}
+
+// Partial sums lie in groups of four rows, [group][slab][128 outputs][4 rows]: a thread moves 16 bytes at a time.  Adds up the pieces of an item
+// (CTAs first .. last) for kGroups groups from row j on, in the order of k, and finishes them; kAhead pieces are asked for at once.
+template <int kMode, bool kGated, int kSlabs, int kGroups, int kAhead>
+__device__ __forceinline__ void join(const StreamArgs &a, const Item &t, int j, int first, int last, int n_lane)
+{
+    float z[kSlabs][4 * kGroups];
+#pragma unroll
+    for (int sl = 0; sl < kSlabs; ++sl)
+#pragma unroll
+        for (int i = 0; i < 4 * kGroups; ++i) z[sl][i] = 0.f;
+    const size_t piece = (size_t)a.R * (kSlabs * kSlab) / 4;
+    for (int p0 = first; p0 <= last; p0 += kAhead) {
+        float4 v[kAhead][kGroups][kSlabs];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            const int p = p0 + q;
+            const float4 *from = reinterpret_cast<const float4 *>(a.partial) + (size_t)(2 * p + (p == first ? 1 : 0)) * piece + (size_t)(j / 4) * (kSlabs * kSlab) + n_lane;
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                for (int sl = 0; sl < kSlabs; ++sl) {
+                    const bool there = p <= last && j + 4 * g < t.rows;
+                    const float4 *at = from + (g * kSlabs + sl) * kSlab;
+                    v[q][g][sl] = there && NM_INSIDE(at, 16, a.in_partial, a.status) ? __ldcg(at) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+        }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                for (int sl = 0; sl < kSlabs; ++sl) {
+                    z[sl][4 * g] += v[q][g][sl].x; z[sl][4 * g + 1] += v[q][g][sl].y; z[sl][4 * g + 2] += v[q][g][sl].z; z[sl][4 * g + 3] += v[q][g][sl].w;
+                }
+    }
+    const int count = min(4 * kGroups, t.rows - j);
+    if constexpr (kGated) {
+        finish<kMode, true>(a, t.row0 + j, count, t.n0 + n_lane, z[0], z[kSlabs - 1]);
+    } else {
+#pragma unroll
+        for (int sl = 0; sl < kSlabs; ++sl) finish<kMode, false>(a, t.row0 + j, count, t.n0 + sl * kSlab + n_lane, z[sl], z[sl]);
     }
 }
 
@@ -336,11 +385,12 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
+                    for (int i = 0; i < 16; i += 4)
                         if (i < count)
 #pragma unroll
                             for (int sl = 0; sl < kSlabs; ++sl)
-                                NM_ST(mine + (size_t)(j + i) * (kSlabs * kSlab) + sl * kSlab + n_lane, z[sl][i], a.in_partial, a.status);
+                                NM_ST(reinterpret_cast<float4 *>(mine) + ((j + i) / 4 * kSlabs + sl) * kSlab + n_lane,
+                                      make_float4(z[sl][i], z[sl][i + 1], z[sl][i + 2], z[sl][i + 3]), a.in_partial, a.status);
                 }
             }
             tc_fence_before();
@@ -363,29 +413,9 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             named_barrier_sync(1, 128);
             if (!s_last) continue;
             __threadfence();
-            for (int j = 0; j < t.rows; j += 4) {
-                float z[kSlabs][4];
-#pragma unroll
-                for (int sl = 0; sl < kSlabs; ++sl)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) z[sl][i] = 0.f;
-#pragma unroll 2
-                for (int p = first; p <= last; ++p) {
-                    const float *from = a.partial + (size_t)(2 * p + (p == first ? 1 : 0)) * a.R * (kSlabs * kSlab) + (size_t)j * (kSlabs * kSlab) + n_lane;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (j + i < t.rows)
-#pragma unroll
-                            for (int sl = 0; sl < kSlabs; ++sl) z[sl][i] += NM_LD_CG(from + i * (kSlabs * kSlab) + sl * kSlab, a.in_partial, a.status);
-                }
-                const int count = min(4, t.rows - j);
-                if constexpr (kGated) {
-                    finish<kMode, true>(a, t.row0 + j, count, t.n0 + n_lane, z[0], z[kSlabs - 1]);
-                } else {
-#pragma unroll
-                    for (int sl = 0; sl < kSlabs; ++sl) finish<kMode, false>(a, t.row0 + j, count, t.n0 + sl * kSlab + n_lane, z[sl], z[sl]);
-                }
-            }
+            // Few rows: many pieces on their way at once; more rows: more of each piece.
+            if (t.rows <= 4) join<kMode, kGated, kSlabs, 1, 8>(a, t, 0, first, last, n_lane);
+            else for (int j = 0; j < t.rows; j += 16) join<kMode, kGated, kSlabs, 4, 2>(a, t, j, first, last, n_lane);
         }
     }
 
