@@ -255,7 +255,7 @@ typedef enum { NM_ACT_NONE = 0, NM_ACT_RELU = 1, NM_ACT_SILU = 2, NM_ACT_GELU = 
  *   A         M rows of K, lda elements apart; residual and C: M rows of N, ld_residual and ldc apart
  *   B         dense, NM_ROW_MAJOR ([K][N or 2N]) or NM_COL_MAJOR ([N or 2N][K])
  *   dtype     NM_BF16 or NM_F16, of A, B, bias, residual and C alike; NM_ERR_UNSUPPORTED otherwise
- *   M         1..NM_MAX_FFN_ROWS; N, K any >= 1 (up to 2^30)
+ *   M         1..NM_MAX_FFN_ROWS; N, K any >= 1 (up to 2^20)
  * bias and residual may be NULL; residual may be C itself (same pitch).  A and B must not overlap C.  Sums are fp32, the epilogue is fp32, the result is rounded once.
  * Equal calls give equal bits.  A and B whose rows all start on 16 bytes take the tensor-core kernel, any others a
  * simple one.  Workspace: nm_matmul_act_workspace_bytes, counters cleared once by nm_workspace_init (and again after NM_ERR_TIMEOUT); calls that overlap on
@@ -278,7 +278,7 @@ int nm_matmul_act(const void *A, long lda, const void *B, const void *bias, cons
  *   W_up, W_down       dense, expert behind expert.  NM_COL_MAJOR: [E][2 inter][d] (gate rows, then up rows; [E][inter][d] without a gate) and [E][d][inter];
  *                      NM_ROW_MAJOR: [E][d][2 inter] (gate columns, then up columns) and [E][inter][d]
  *   dtype              NM_BF16 or NM_F16, of x, the weights, residual and out alike; NM_ERR_UNSUPPORTED otherwise
- *   T * top_k          up to 2^22; E up to NM_MAX_EXPERTS
+ *   T * top_k          up to 2^22; d and inter up to 2^20; E up to NM_MAX_EXPERTS
  * Sums and activations are fp32, h is kept to 16 bits or more, the result is rounded once.  The weights of an expert that no token chose
  * are not read.  Equal calls give equal bits.  Operands whose rows all start on 16 bytes (d and inter multiples of 8) take the tensor-core kernels, any others simple ones.
  * Workspace: nm_moe_ffn_workspace_bytes; nothing in it has to be cleared and it keeps nothing from one call for the next; calls that

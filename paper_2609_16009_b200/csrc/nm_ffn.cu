@@ -15,7 +15,7 @@ namespace nm {
 
 namespace {
 
-constexpr int kMaxPairs = 1 << 22;
+constexpr int kMaxPairs = 1 << 22, kMaxDim = 1 << 20;  // (items and chunks are then counted in 32 bits)
 
 // ---- products of operands of any alignment -----------------------------------------------------------------------------------
 // A block of four warps computes 32 outputs of one row.  Column-major weights: a warp per output in turn, lanes along k.  Row-major: a lane
@@ -91,7 +91,9 @@ __global__ void __launch_bounds__(kSimpleThreads) simple_product_kernel(const Si
                 if (!a.col) z[part] = (z[part] + s_part[part][1][lane]) + (s_part[part][2][lane] + s_part[part][3][lane]);
                 if (a.bias) z[part] += widen16(NM_LD(a.bias + (long)part * a.N + n, a.in_bias, a.status), a.f16);
             }
-            float v = activate(a.act, z[0]);
+            float one[1] = {z[0]};
+            activate(a.act, one);
+            float v = one[0];
             if (a.gated) v *= z[1];
             if (a.residual) v += widen16(NM_LD(a.residual + r * a.ld_residual + n, a.in_residual, a.status), a.f16);
             if (a.out_f32) NM_ST(static_cast<float *>(a.out) + r * a.ldo + n, v, a.in_out, a.status);
@@ -196,7 +198,10 @@ constexpr int kPlanThreads = 512;
 struct PlanArgs {
     const int32_t *experts; int first, E;
     int pairs, R;
-    RowTile *tiles; int *n_tiles; int *order; int *place;
+    RowTile *tiles; int *order; int *place;
+    int *n_rows;                                // rows there are in all
+    Schedule *schedules;                        // of the two products
+    CutModel model[2];
     unsigned *counters;                         // cleared for the products that follow
     Span in_experts, in_tiles, in_order, in_place;
     unsigned *status;
@@ -235,8 +240,19 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a)
     for (int i = tid; i < mine; i += kPlanThreads) { rows += s_count[i]; tiles += ceil_div(s_count[i], a.R); }
     const int row0 = block_sum(rows, s_warp), tile0 = block_sum(tiles, s_warp);
     const int count = s_count[mine], own = ceil_div(count, a.R);
-    if (mine == a.E - 1 && tid == 0) *a.n_tiles = tile0 + own;
-    if (mine == 0 && tid < kSMs) a.counters[tid] = 0u;
+    if (mine == a.E - 1) {
+        if (tid == 0) *a.n_rows = row0 + count;
+        if (warp < 2) {                                           // a warp a product: a lane for each number of parts
+            const CutModel &m = a.model[warp];
+            const int items = (tile0 + own) * m.column_tiles, rest = items - whole_items(items), parts = lane + 1;
+            const bool may = parts == 1 || (parts <= m.kb && (long)rest * parts <= m.most_chunks);
+            const float cost = may ? cut_cost(rest, m.kb, parts, m.sums_steps, m.latency_steps) : INFINITY;
+            const unsigned least = __reduce_min_sync(0xffffffffu, __float_as_uint(cost));       // (costs are not negative: their bits order as they do)
+            const int best = __ffs((int)__ballot_sync(0xffffffffu, __float_as_uint(cost) == least));
+            if (lane == 0) a.schedules[warp] = schedule_of(items, m.kb, best);
+        }
+    }
+    if (mine == 0) for (int i = tid; i < kCounterWords; i += kPlanThreads) a.counters[i] = 0u;
     for (int i = tid; i < own; i += kPlanThreads) NM_ST(a.tiles + tile0 + i, (RowTile{mine, row0 + i * a.R, min(a.R, count - i * a.R), 0}), a.in_tiles, a.status);
     if (count == 0) return;
     int at = row0;
@@ -255,6 +271,21 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a)
             NM_ST(a.place + p, row, a.in_place, a.status);
         }
         at += all;
+    }
+}
+
+// ---- rows in the order of their experts ------------------------------------------------------------------------------------------
+// For tiles of many rows (see nm_ffn_stream.cu): a block a row, 16 bytes a thread.
+__global__ void __launch_bounds__(256) sort_rows_kernel(const uint16_t *x, long ldx, const int *order, int top_k, const int *n_rows, int d, uint16_t *to, unsigned *status, Span in_x,
+                                                        Span in_order, Span in_to)
+{
+    pdl_launch_dependents();
+    pdl_wait_prior_grids();
+    const int rows = *n_rows;
+    for (int r = blockIdx.x; r < rows; r += gridDim.x) {
+        const uint16_t *from = x + (long)(NM_LD(order + r, in_order, status) / top_k) * ldx;
+        for (int i = 8 * threadIdx.x; i < d; i += 2048)
+            NM_ST(reinterpret_cast<uint4 *>(to + (size_t)r * d + i), NM_LD(reinterpret_cast<const uint4 *>(from + i), in_x, status), in_to, status);
     }
 }
 
@@ -318,19 +349,19 @@ bool act_ok(nm_act act) { return act >= NM_ACT_NONE && act <= NM_ACT_GELU_TANH; 
 // Whether tensor maps can address rows of `pitch` 16-bit elements at p: both on 16 bytes.
 bool rows_on_16(const void *p, long pitch) { return !((uintptr_t)p & 15u) && pitch % 8 == 0; }
 
-struct MoeLayout { size_t tiles, n_tiles, order, place, partial, h, terms, scale, y, total; };
-MoeLayout moe_layout(long pairs, int T, int d, int inter, int E, bool f16)
+struct MoeLayout { size_t tiles, n_rows, schedules, order, place, partial, h, terms, scale, y, total; };
+MoeLayout moe_layout(long pairs, int d, int inter, int E, bool f16)
 {
     const int R = stream_tile_rows((double)pairs / E, (int)std::min<long>(pairs, 128));
-    (void)T;
     MoeLayout l{};
-    size_t at = 1024;                                             // counters
-    l.n_tiles = at; at += 256;
+    size_t at = align256(kCounterWords * sizeof(unsigned));
+    l.n_rows = at; at += 256;
+    l.schedules = at; at += 256;
     l.tiles = at; at += align256((E + pairs / 16) * sizeof(RowTile));
     l.order = at; at += align256(4 * (size_t)pairs);
     l.place = at; at += align256(4 * (size_t)pairs);
     l.scale = at; at += align256(4 * (size_t)pairs);
-    l.partial = at; at += align256(stream_partial_bytes(R, 2));
+    l.partial = at; at += align256(std::max(stream_partial_bytes(R, inter, true), std::max(stream_partial_bytes(R, inter, false), stream_partial_bytes(R, d, false))));
     l.h = at; at += align256(4 * (size_t)pairs * inter);
     l.terms = f16 ? at : l.h;
     if (f16) at += align256(4 * (size_t)pairs * inter);
@@ -351,16 +382,14 @@ extern "C" {
 size_t nm_matmul_act_workspace_bytes(int M, int N, int K, int gated, nm_dtype dtype)
 {
     if (M < 1 || N < 1 || K < 1 || !ffn_dtype_ok(dtype)) return 0;
-    (void)N; (void)K;
-    const int R = stream_tile_rows(M, M);
-    return NM_WS_COUNTER_BYTES + stream_partial_bytes(R, stream_slabs(R, gated != 0));
+    return NM_WS_COUNTER_BYTES + stream_partial_bytes(stream_tile_rows(M, M), N, gated != 0);
 }
 
 int nm_matmul_act(const void *A, long lda, const void *B, const void *bias, const void *residual, long ld_residual, void *C, long ldc, int M,
                   int N, int K, nm_act act, int gated, nm_dtype dtype, nm_layout layout_B, void *workspace, size_t workspace_bytes,
                   nm_stream stream)
 {
-    if (!A || !B || !C || M < 1 || M > NM_MAX_FFN_ROWS || N < 1 || N > (1 << 30) || K < 1 || K > (1 << 30) || lda < K || ldc < N || (residual && ld_residual < N)) return NM_ERR_INVALID_ARG;
+    if (!A || !B || !C || M < 1 || M > NM_MAX_FFN_ROWS || N < 1 || N > kMaxDim || K < 1 || K > kMaxDim || lda < K || ldc < N || (residual && ld_residual < N)) return NM_ERR_INVALID_ARG;
     if (!ffn_dtype_ok(dtype) || !ffn_layout_ok(layout_B) || !act_ok(act)) return NM_ERR_UNSUPPORTED;
     if (((uintptr_t)A & 1u) || ((uintptr_t)B & 1u) || ((uintptr_t)C & 1u) || ((uintptr_t)bias & 1u) || ((uintptr_t)residual & 1u)) return NM_ERR_ALIGNMENT;
     if (!workspace || workspace_bytes < nm_matmul_act_workspace_bytes(M, N, K, gated, dtype)) return NM_ERR_WORKSPACE;
@@ -402,14 +431,14 @@ int nm_matmul_act(const void *A, long lda, const void *B, const void *bias, cons
 size_t nm_moe_ffn_workspace_bytes(int T, int d, int inter, int E, int top_k, nm_dtype dtype)
 {
     if (T < 1 || d < 1 || inter < 1 || E < 1 || top_k < 1 || (long)T * top_k > kMaxPairs || !ffn_dtype_ok(dtype)) return 0;
-    return moe_layout((long)T * top_k, T, d, inter, E, dtype == NM_F16).total;
+    return moe_layout((long)T * top_k, d, inter, E, dtype == NM_F16).total;
 }
 
 int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *weights, const void *W_up, const void *W_down,
                const void *residual, long ld_residual, void *out, long ldo, int T, int d, int inter, int E, int top_k, int first_expert,
                nm_act act, int gated, nm_dtype dtype, nm_layout layout, void *workspace, size_t workspace_bytes, nm_stream stream)
 {
-    if (!x || !experts || !W_up || !W_down || !out || T < 1 || d < 1 || d > (1 << 24) || inter < 1 || inter > (1 << 24) || E < 1 || top_k < 1 ||
+    if (!x || !experts || !W_up || !W_down || !out || T < 1 || d < 1 || d > kMaxDim || inter < 1 || inter > kMaxDim || E < 1 || top_k < 1 ||
         first_expert < 0 || ldx < d || ldo < d || (residual && ld_residual < d))
         return NM_ERR_INVALID_ARG;
     if (!ffn_dtype_ok(dtype) || !ffn_layout_ok(layout) || !act_ok(act) || E > NM_MAX_EXPERTS || (long)T * top_k > kMaxPairs) return NM_ERR_UNSUPPORTED;
@@ -421,7 +450,7 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
     cudaStream_t s = (cudaStream_t)stream;
     const long pairs = (long)T * top_k;
     const bool col = layout == NM_COL_MAJOR, f16 = dtype == NM_F16, programmatic = programmatic_launch_enabled();
-    const MoeLayout lay = moe_layout(pairs, T, d, inter, E, f16);
+    const MoeLayout lay = moe_layout(pairs, d, inter, E, f16);
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     float *h = reinterpret_cast<float *>(ws + lay.h), *y = reinterpret_cast<float *>(ws + lay.y);
     const int *place = nullptr;
@@ -434,7 +463,10 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
         PlanArgs pl{};
         pl.experts = experts; pl.first = first_expert; pl.E = E; pl.pairs = (int)pairs;
         pl.R = stream_tile_rows((double)pairs / E, (int)std::min<long>(pairs, 128));
-        pl.tiles = reinterpret_cast<RowTile *>(ws + lay.tiles); pl.n_tiles = reinterpret_cast<int *>(ws + lay.n_tiles);
+        pl.tiles = reinterpret_cast<RowTile *>(ws + lay.tiles); pl.n_rows = reinterpret_cast<int *>(ws + lay.n_rows);
+        pl.schedules = reinterpret_cast<Schedule *>(ws + lay.schedules);
+        pl.model[0] = stream_cut_model(pl.R, inter, d, gated != 0, 1);
+        pl.model[1] = stream_cut_model(pl.R, d, inter, false, 2);
         pl.order = reinterpret_cast<int *>(ws + lay.order); pl.place = reinterpret_cast<int *>(ws + lay.place);
         pl.counters = reinterpret_cast<unsigned *>(ws);
         pl.in_experts = in_experts; pl.in_tiles = make_span(pl.tiles, sizeof(RowTile) * (E + (size_t)pairs / pl.R));
@@ -445,13 +477,22 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
 
         ProductArgs p{};
         p.rows = (int)pairs; p.N = inter; p.K = d; p.R = pl.R; p.terms = 1;
-        p.col = col; p.f16 = f16; p.gather = p.planned = p.programmatic = true;
+        p.col = col; p.f16 = f16; p.planned = p.programmatic = true;
         p.act = act;
-        p.plan = RowPlan{pl.tiles, pl.n_tiles, pl.order, pl.place, top_k};
+        p.plan = RowPlan{pl.tiles, pl.schedules, pl.order, top_k};
         p.W = W_up; p.w_expert = (long)parts * inter * d; p.E = E;
-        p.x = x; p.ldx = ldx; p.x_rows = T;
+        p.gather = pl.R <= 32;
+        if (p.gather) {
+            p.x = x; p.ldx = ldx; p.x_rows = T;
+        } else {                                                  // the sorted rows lie where y will be
+            uint16_t *sorted = reinterpret_cast<uint16_t *>(y);
+            if (e == cudaSuccess)
+                e = launch(sort_rows_kernel, pairs, 256, true, s, static_cast<const uint16_t *>(x), ldx, static_cast<const int *>(pl.order), top_k, static_cast<const int *>(pl.n_rows), d,
+                           sorted, status, make_span(x, 2 * ((size_t)(T - 1) * ldx + d)), pl.in_order, make_span(sorted, 2 * (size_t)pairs * d));
+            p.x = sorted; p.ldx = d; p.x_rows = pairs; p.x_term = pairs * d;
+        }
         p.out = h; p.ldo = inter;
-        p.counters = pl.counters; p.partial = reinterpret_cast<float *>(ws + lay.partial);
+        p.counters = pl.counters; p.ticket = kTicketUp; p.partial = reinterpret_cast<float *>(ws + lay.partial);
         if (e == cudaSuccess) e = launch_product(kOutHidden, gated != 0, p, s, &what);
 
         float *row_scale = reinterpret_cast<float *>(ws + lay.scale);
@@ -462,6 +503,7 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
 
         ProductArgs q = p;
         q.N = d; q.K = inter; q.terms = 2; q.gather = false; q.early_weights = true; q.act = NM_ACT_NONE;
+        q.plan.schedule = pl.schedules + 1; q.ticket = kTicketDown;
         q.W = W_down; q.w_expert = (long)inter * d;
         q.x = terms; q.ldx = inter; q.x_rows = pairs; q.x_term = pairs * inter;
         q.row_scale = f16 ? row_scale : nullptr;

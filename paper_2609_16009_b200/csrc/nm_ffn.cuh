@@ -6,14 +6,29 @@
 namespace nm {
 
 // ---- activations, fp32 -------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ float activate(int act, float x)
+// Of n values at once: one branch.  __expf is within 2 + |1.2 x| steps of exp(x) and the quotient within 2, which the 16 or 17 bits that are kept do not see;
+// a denominator beyond 2^126 makes the quotient 0, as near as fp32 gets.
+template <int n>
+__device__ __forceinline__ void activate(int act, float (&v)[n])
 {
     switch (act) {
-    case NM_ACT_RELU: return x < 0.f ? 0.f : x;                                        // a NaN stays one
-    case NM_ACT_SILU: return x / (1.f + expf(-x));
-    case NM_ACT_GELU: return 0.5f * x * erfcf(-0.70710678f * x);                        // erfc: no cancellation for negative x
-    case NM_ACT_GELU_TANH: return x / (1.f + expf(-1.59576912f * (x + 0.044715f * x * x * x)));   // 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z))
-    default: return x;
+    case NM_ACT_RELU:
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = v[i] < 0.f ? 0.f : v[i];                       // a NaN stays one
+        break;
+    case NM_ACT_SILU:
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = __fdividef(v[i], 1.f + __expf(-v[i]));
+        break;
+    case NM_ACT_GELU:
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = 0.5f * v[i] * erfcf(-0.70710678f * v[i]);       // erfc: no cancellation for negative values
+        break;
+    case NM_ACT_GELU_TANH:                                                              // 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z))
+#pragma unroll
+        for (int i = 0; i < n; ++i) v[i] = __fdividef(v[i], 1.f + __expf(-1.59576912f * (v[i] + 0.044715f * v[i] * v[i] * v[i])));
+        break;
+    default: break;
     }
 }
 
@@ -24,13 +39,39 @@ __device__ __forceinline__ uint16_t round16(float v, bool f16) { return f16 ? __
 // Rows of the experts.  Pair p = (token p / top_k, choice p % top_k) belongs to expert experts[p] - first where that is one of the E held
 // here.  `order` lists the pairs by expert, each expert's in rising order; `place` is its inverse; a tile is up to R of one expert's rows.
 struct RowTile { int expert, row0, rows, unused; };
+
+// How the items of a product (a row tile x a column tile, kb steps of 64 k each) are dealt out: the first `whole` as they are, each of the others in
+// `parts` chunks of kc steps (the last one shorter).  Chunk c < whole is item c; behind them part (c - whole) % parts of item whole + (c - whole) / parts.
+struct Schedule { int whole, parts, kc, chunks; };
+
 struct RowPlan {
     const RowTile *tiles;
-    const int *n_tiles;
+    const Schedule *schedule;          // of this product
     const int *order;                  // [sorted row] -> pair
-    const int *place;                  // [pair] -> sorted row
     int top_k;
 };
+
+// Words of the counter area: a ticket for each product of a call (the chunks dealt out beyond one for each CTA), CTAs that are done, and the chunks there
+// are of an item that is cut.
+constexpr int kTicketUp = 0, kTicketDown = 1, kDone = 2, kItemCounters = 32, kMaxCut = 2 * kSMs, kCounterWords = kItemCounters + kMaxCut;
+
+// The cut with the least modelled time.  In steps of one CTA working alone (~70 GB/s of weights): with all CTAs working a step takes kBusy times as
+// long (HBM, measured 6.5 TB/s, against 148 * 70 GB/s); a chunk's sums go to the workspace and back; and joining costs `latency` steps once.
+// All items but the last one to two rounds stay whole: sums in the workspace cost as much as the rows do, and only the end has to be even.
+constexpr float kBusy = 1.6f;
+__host__ __device__ inline float cut_cost(int rest, int kb, int parts, float sums_steps, float latency_steps)
+{
+    const int kc = (kb + parts - 1) / parts, p = (kb + kc - 1) / kc, rounds = (rest * p + kSMs - 1) / kSMs;
+    const float hbm = (float)rest * kb * kBusy / kSMs, sm = (float)rounds * kc, each = p > 1 ? sums_steps * rounds + latency_steps : 0.f;
+    return (hbm > sm ? hbm : sm) + each;
+}
+struct CutModel { int kb, column_tiles, most_chunks; float sums_steps, latency_steps; };
+__host__ __device__ inline int whole_items(int items) { return items >= 2 * kSMs ? (items / kSMs - 1) * kSMs : 0; }
+__host__ __device__ inline Schedule schedule_of(int items, int kb, int parts)
+{
+    const int whole = whole_items(items), kc = (kb + parts - 1) / parts, p = (kb + kc - 1) / kc;
+    return p > 1 ? Schedule{whole, p, kc, whole + (items - whole) * p} : Schedule{items, 1, kb, items};
+}
 
 // One product of the streaming kernel (nm_ffn_stream.cu): rows of a token operand against weights of their expert.
 enum { kOutAct = 0, kOutHidden = 1, kOutDown = 2 };
@@ -53,12 +94,14 @@ struct ProductArgs {
     const void *bias, *residual; long ld_residual;
     void *out; long ldo;               // kOutAct: 16-bit C; kOutHidden: 16-bit terms [2][rows][ldo] (bf16) or fp32 [rows][ldo] (fp16); kOutDown: fp32 [rows][ldo]
     const float *row_scale;            // kOutDown: factor of each row, or NULL
-    float *partial; unsigned *counters;
+    float *partial; unsigned *counters; int ticket;
 };
-size_t stream_partial_bytes(int R, int slabs);
-// The widest row tile for `rows` rows a group on average (at most `most`), and the 128-wide slabs of weights an item has.
+// The widest row tile for `rows` rows a group on average (at most `most`), the 128-wide slabs of weights that an item of N outputs has, and the workspace for
+// sums of chunks.
 int stream_tile_rows(double average, int most);
-int stream_slabs(int R, bool gated);
+int stream_slabs(int N, bool gated);
+size_t stream_partial_bytes(int R, int N, bool gated);
+CutModel stream_cut_model(int R, int N, int K, bool gated, int terms);
 cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStream_t s, const char **what);
 
 }  // namespace nm

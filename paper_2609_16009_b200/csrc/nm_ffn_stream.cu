@@ -7,13 +7,16 @@
 //
 //   item   one row tile (up to R rows of one expert) x one column tile (kSlabs slabs of 128 outputs; where gated, one slab each of gate and up,
 //          so that a thread ends up with both values of an output), kb steps of 64 k
-//   share  steps [c U / C, (c + 1) U / C) of the U = items * kb steps go to CTA c of C.  An item that is cut is finished by whoever of its CTAs
-//          arrives last (a counter; nobody waits): every CTA leaves its fp32 sums in the workspace, the last adds them in the order of k.
-//          So sums do not depend on who came last, and equal calls give equal bits.
-//   warps  0: copies (all lanes: up to 32 row groups a step); 1: MMAs; 2-5: the epilogue, from the other one of two accumulators
+//   chunk  an item, or for the last round or two one of `parts` runs of its steps; the cuts are a rule on sizes (schedule_of), the CTAs take chunks as they
+//          get done: with equal shares the fastest SMs were done after 652 us where the slowest took 870.  A chunk's fp32 sums wait in the workspace for
+//          the last of its item (a counter; nobody waits), which adds them in the order of k.  So results do not depend on who took what or came last.
+//   warps  0: copies, and the next chunk; 1: MMAs; from 2: the epilogue, from the other one of two accumulators.  Four to sixteen warps by the rows of a
+//          tile: what an output costs is latency (tensor memory, exp, residual; 128 rows of 1536 x 24576 took 96 us with four warps, 48 with sixteen),
+//          and a launch of more warps costs a short call 1.5 us
 //
-// Token rows are copied as they lie in groups of eight, or gathered by token four at a time (tile::gather4) where the rows of an expert are
-// scattered.  The number of accumulator columns is that of the rows there are, rounded up to 16; what the columns beyond hold is not read.
+// Token rows are copied as they lie, or gathered by token four at a time (tile::gather4) where the rows of an expert are scattered and few: a
+// request takes the copy engine ~40 ns whatever its size, so more than eight a step would be what bounds the kernel, and rows are sorted first.
+// The number of accumulator columns is that of the rows there are, rounded up to 16; what the columns beyond hold is not read.
 // A hidden value is the sum of two 16-bit terms (bf16: 16 bits and more, fp16: 22), both multiplied into the same accumulator: the MMAs are far
 // from being the bound, and the second term keeps the rounding of the hidden values out of the result.
 #include <algorithm>
@@ -25,7 +28,8 @@ namespace nm {
 
 namespace {
 
-constexpr int kThreads = 192;
+constexpr int kMaxThreads = 64 + 32 * 16;
+constexpr int kQueue = 4;                       // chunks that the copies may be ahead of the epilogue
 constexpr int kKT = 64;                        // k of a stage
 constexpr int kSlab = 128;                     // outputs of a slab (the MMA's M)
 constexpr int kSlabBytes = kSlab * kKT * 2;
@@ -33,10 +37,9 @@ constexpr int kMaxStages = 12;
 constexpr int kRingBytes = 216 * 1024;
 
 struct StreamArgs {
-    long units, items;                          // where the plan is on the host
+    Schedule schedule;                          // where the rows are known on the host
     int kb, column_tiles, tile_n;               // steps of an item, column tiles of a row tile, outputs of one
-    int n_second;                               // where the second slab's rows (columns) start within its map: +128, or +0 in a map of its own
-    int rows, N, R, terms, nstage, stage_bytes;
+    int rows, N, R, box_rows, terms, nstage, stage_bytes;
     unsigned tmem_columns;
     bool col, f16, gather, planned, early_weights, programmatic;
     int act;
@@ -44,7 +47,7 @@ struct StreamArgs {
     const uint16_t *bias, *residual; long ld_residual;
     void *out; long ldo; long out_term;
     const float *row_scale;
-    float *partial; unsigned *counters;
+    float *partial; unsigned *counters; int ticket;
     Span in_bias, in_residual, in_out, in_scale, in_partial, in_tiles, in_order;
     unsigned *status;
 };
@@ -65,27 +68,20 @@ __device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap *map
         ::"r"(dst), "l"(map), "r"(x), "r"(row[0]), "r"(row[1]), "r"(row[2]), "r"(row[3]), "r"(bar), "l"(policy) : "memory");
 }
 
-// A CTA's share of the steps, item by item.
-struct Walk {
-    long unit, end;
-    int kb;
-    long item; int k0, k1;
-    __device__ bool next()
-    {
-        if (unit >= end) return false;
-        item = unit / kb;
-        k0 = (int)(unit - item * kb);
-        k1 = (int)min((long)kb, k0 + (end - unit));
-        unit += k1 - k0;
-        return true;
-    }
-};
+// A chunk: steps [k0, k1) of an item; where that is not all of it, the place of its sums and of the item's first chunk's, and the item's counter.
+struct Chunk { int item, k0, k1, slot, first_slot, cut; };
+__device__ __forceinline__ Chunk chunk_of(const Schedule &s, int kb, int id)
+{
+    if (id < s.whole) return Chunk{id, 0, kb, 0, 0, -1};
+    const int at = id - s.whole, cut = at / s.parts, part = at - cut * s.parts, k0 = part * s.kc;
+    return Chunk{s.whole + cut, k0, min(kb, k0 + s.kc), at, cut * s.parts, cut};
+}
 
 // One item: its rows and outputs.
 struct Item { int expert, row0, rows, n0; };
-__device__ __forceinline__ Item item_of(const StreamArgs &a, long item)
+__device__ __forceinline__ Item item_of(const StreamArgs &a, int item)
 {
-    const int tile = (int)(item / a.column_tiles), n0 = (int)(item % a.column_tiles) * a.tile_n;
+    const int tile = item / a.column_tiles, n0 = (item - tile * a.column_tiles) * a.tile_n;
     if (a.planned) {
         const RowTile t = NM_LD(a.plan.tiles + tile, a.in_tiles, a.status);
         return Item{t.expert, t.row0, t.rows, n0};
@@ -95,32 +91,38 @@ __device__ __forceinline__ Item item_of(const StreamArgs &a, long item)
 }
 
 // What becomes of finished outputs: z[i] is output n of row r + i, i < count; z2 the same of the up part.
-template <int kMode, bool kGated, int kW>
-__device__ __forceinline__ void finish(const StreamArgs &a, int r, int count, int n, const float (&z)[kW], const float (&z2)[kW])
+template <int kMode, bool kGated>
+__device__ __forceinline__ void finish(const StreamArgs &a, int r, int count, int n, float (&z)[4], float (&z2)[4])
 {
     if (n >= a.N) return;
     if constexpr (kMode == kOutAct) {
-        const float b0 = a.bias ? widen16(NM_LD(a.bias + n, a.in_bias, a.status), a.f16) : 0.f;
-        const float b1 = kGated && a.bias ? widen16(NM_LD(a.bias + a.N + n, a.in_bias, a.status), a.f16) : 0.f;
         // All of the residual before the first store: it may be the output itself, so no load would be moved ahead of a store.
-        float more[kW];
+        float more[4];
 #pragma unroll
-        for (int i = 0; i < kW; ++i)
+        for (int i = 0; i < 4; ++i)
             more[i] = a.residual && i < count ? widen16(NM_LD(a.residual + (long)(r + i) * a.ld_residual + n, a.in_residual, a.status), a.f16) : 0.f;
+        if (a.bias) {
+            const float b0 = widen16(NM_LD(a.bias + n, a.in_bias, a.status), a.f16);
+            const float b1 = kGated ? widen16(NM_LD(a.bias + a.N + n, a.in_bias, a.status), a.f16) : 0.f;
 #pragma unroll
-        for (int i = 0; i < kW; ++i) {
+            for (int i = 0; i < 4; ++i) { z[i] += b0; if constexpr (kGated) z2[i] += b1; }
+        }
+        activate(a.act, z);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
             if (i < count) {
-                float v = activate(a.act, a.bias ? z[i] + b0 : z[i]);
-                if constexpr (kGated) v *= a.bias ? z2[i] + b1 : z2[i];
+                float v = z[i];
+                if constexpr (kGated) v *= z2[i];
                 if (a.residual) v += more[i];
                 NM_ST(static_cast<uint16_t *>(a.out) + (long)(r + i) * a.ldo + n, round16(v, a.f16), a.in_out, a.status);
             }
         }
     } else if constexpr (kMode == kOutHidden) {
+        activate(a.act, z);
 #pragma unroll
-        for (int i = 0; i < kW; ++i) {
+        for (int i = 0; i < 4; ++i) {
             if (i < count) {
-                float v = activate(a.act, z[i]);
+                float v = z[i];
                 if constexpr (kGated) v *= z2[i];
                 if (a.f16) {
                     NM_ST(static_cast<float *>(a.out) + (long)(r + i) * a.ldo + n, v, a.in_out, a.status);
@@ -138,7 +140,7 @@ __device__ __forceinline__ void finish(const StreamArgs &a, int r, int count, in
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < kW; ++i) {
+        for (int i = 0; i < 4; ++i) {
             if (i < count) {
                 const float s = a.row_scale ? NM_LD(a.row_scale + r + i, a.in_scale, a.status) : 1.f;
                 NM_ST(static_cast<float *>(a.out) + (long)(r + i) * a.ldo + n, z[i] * s, a.in_out, a.status);
@@ -147,70 +149,71 @@ __device__ __forceinline__ void finish(const StreamArgs &a, int r, int count, in
     }
 }
 
-// Partial sums lie in groups of four rows, [group][slab][128 outputs][4 rows]: a thread moves 16 bytes at a time.  Adds up the pieces of an item
-// (CTAs first .. last) for kGroups groups from row j on, in the order of k, and finishes them; kAhead pieces are asked for at once.
-template <int kMode, bool kGated, int kSlabs, int kGroups, int kAhead>
-__device__ __forceinline__ void join(const StreamArgs &a, const Item &t, int j, int first, int last, int n_lane)
+// The outputs of four rows from row j of the item on, of all slabs.
+template <int kMode, bool kGated, int kSlabs>
+__device__ __forceinline__ void finish_all(const StreamArgs &a, const Item &t, int j, int n_lane, float (&z)[kSlabs][4])
 {
-    float z[kSlabs][4 * kGroups];
-#pragma unroll
-    for (int sl = 0; sl < kSlabs; ++sl)
-#pragma unroll
-        for (int i = 0; i < 4 * kGroups; ++i) z[sl][i] = 0.f;
-    const size_t piece = (size_t)a.R * (kSlabs * kSlab) / 4;
-    for (int p0 = first; p0 <= last; p0 += kAhead) {
-        float4 v[kAhead][kGroups][kSlabs];
-#pragma unroll
-        for (int q = 0; q < kAhead; ++q) {
-            const int p = p0 + q;
-            const float4 *from = reinterpret_cast<const float4 *>(a.partial) + (size_t)(2 * p + (p == first ? 1 : 0)) * piece + (size_t)(j / 4) * (kSlabs * kSlab) + n_lane;
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g)
-#pragma unroll
-                for (int sl = 0; sl < kSlabs; ++sl) {
-                    const bool there = p <= last && j + 4 * g < t.rows;
-                    const float4 *at = from + (g * kSlabs + sl) * kSlab;
-                    v[q][g][sl] = there && NM_INSIDE(at, 16, a.in_partial, a.status) ? __ldcg(at) : make_float4(0.f, 0.f, 0.f, 0.f);
-                }
-        }
-#pragma unroll
-        for (int q = 0; q < kAhead; ++q)
-#pragma unroll
-            for (int g = 0; g < kGroups; ++g)
-#pragma unroll
-                for (int sl = 0; sl < kSlabs; ++sl) {
-                    z[sl][4 * g] += v[q][g][sl].x; z[sl][4 * g + 1] += v[q][g][sl].y; z[sl][4 * g + 2] += v[q][g][sl].z; z[sl][4 * g + 3] += v[q][g][sl].w;
-                }
-    }
-    const int count = min(4 * kGroups, t.rows - j);
+    const int count = min(4, t.rows - j);
     if constexpr (kGated) {
-        finish<kMode, true>(a, t.row0 + j, count, t.n0 + n_lane, z[0], z[kSlabs - 1]);
+        finish<kMode, true>(a, t.row0 + j, count, t.n0 + n_lane, z[0], z[1]);
     } else {
 #pragma unroll
         for (int sl = 0; sl < kSlabs; ++sl) finish<kMode, false>(a, t.row0 + j, count, t.n0 + sl * kSlab + n_lane, z[sl], z[sl]);
     }
 }
 
+// Sums of a chunk lie in groups of four rows, [group][slab][128 outputs][4 rows]: a thread moves 16 bytes at a time.  Adds up the `parts` chunks of an
+// item from slot `first` on for the group from row j on, in the order of k; several chunks are asked for at once.
+template <int kSlabs>
+__device__ __forceinline__ void join(const StreamArgs &a, int j, int first, int parts, int n_lane, float (&z)[kSlabs][4])
+{
+    constexpr int kAhead = kSlabs == 2 ? 4 : 6;
+#pragma unroll
+    for (int sl = 0; sl < kSlabs; ++sl)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[sl][i] = 0.f;
+    const size_t piece = (size_t)a.R * (kSlabs * kSlab) / 4;
+    const float4 *from = reinterpret_cast<const float4 *>(a.partial) + first * piece + (size_t)(j / 4) * (kSlabs * kSlab) + n_lane;
+    for (int p0 = 0; p0 < parts; p0 += kAhead) {
+        float4 v[kAhead][kSlabs];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+            if (p0 + q < parts)
+#pragma unroll
+                for (int sl = 0; sl < kSlabs; ++sl) {
+                    const float4 *at = from + (p0 + q) * piece + sl * kSlab;
+                    v[q][sl] = NM_INSIDE(at, 16, a.in_partial, a.status) ? __ldcg(at) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+            if (p0 + q < parts)
+#pragma unroll
+                for (int sl = 0; sl < kSlabs; ++sl) { z[sl][0] += v[q][sl].x; z[sl][1] += v[q][sl].y; z[sl][2] += v[q][sl].z; z[sl][3] += v[q][sl].w; }
+    }
+}
+
 template <int kMode, bool kGated, int kSlabs>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kMaxThreads, 1)
 stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1, const __grid_constant__ CUtensorMap map_x, const StreamArgs a)
 {
     static_assert(!kGated || kSlabs == 2, "gate and up are a slab each");
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-    __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 5];
+    __shared__ __align__(8) uint64_t s_bars[2 * kMaxStages + 2 * kQueue + 5];
     __shared__ uint32_t s_tmem;
-    __shared__ int s_abort;
+    __shared__ int s_abort, s_queue[kQueue], s_next[2];
     __shared__ unsigned s_last;
-    const uint32_t full0 = smem_u32(s_bars), empty0 = full0 + 8 * kMaxStages, acc_full0 = empty0 + 8 * kMaxStages, acc_empty0 = acc_full0 + 16, drained = acc_empty0 + 16;
+    const uint32_t full0 = smem_u32(s_bars), empty0 = full0 + 8 * kMaxStages, queued0 = empty0 + 8 * kMaxStages, taken0 = queued0 + 8 * kQueue,
+                   acc_full0 = taken0 + 8 * kQueue, acc_empty0 = acc_full0 + 16, drained = acc_empty0 + 16;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int NS = a.nstage;
+    const int NS = a.nstage, finishers = (int)blockDim.x - 64;
 
-    if (tid == 0) {
-        s_abort = 0;
-        for (int i = 0; i < NS; ++i) { mbar_init(full0 + 8 * i, 1); mbar_init(empty0 + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(acc_full0 + 8 * i, 1); mbar_init(acc_empty0 + 8 * i, 4); }
-        mbar_init(drained, 1);
+    if (warp == 0) {
+        if (lane == 0) { tma_prefetch_descriptor(&map_w0); tma_prefetch_descriptor(&map_w1); tma_prefetch_descriptor(&map_x); s_abort = 0; }
+        if (lane < NS) { mbar_init(full0 + 8 * lane, 1); mbar_init(empty0 + 8 * lane, 1); }
+        if (lane < kQueue) { mbar_init(queued0 + 8 * lane, 1); mbar_init(taken0 + 8 * lane, 2); }      // (taken by the MMA warp and the epilogue)
+        if (lane < 2) { mbar_init(acc_full0 + 8 * lane, 1); mbar_init(acc_empty0 + 8 * lane, (uint32_t)finishers / 32); }
+        if (lane == 2) mbar_init(drained, 1);
         mbar_init_fence();
     }
     if (warp == 1) tmem_alloc(&s_tmem, a.tmem_columns);
@@ -223,18 +226,13 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
     // be waited for.  Without early_weights everything is behind the wait.
     if (!a.early_weights) pdl_wait_prior_grids();
     if (a.programmatic) pdl_launch_dependents();
-    long units = a.units;
-    if (a.planned) {
-        units = (long)*a.plan.n_tiles * a.column_tiles * a.kb;
-    }
-    const long C = min((long)gridDim.x, units), c = blockIdx.x;   // no more CTAs than steps: then none between the first and the last of an item is without a share
-    Walk all{0, 0, a.kb, 0, 0, 0};
-    if (c < C) { all.unit = c * units / C; all.end = (c + 1) * units / C; }
+    const Schedule sched = a.planned ? *a.plan.schedule : a.schedule;
+    const int first_id = blockIdx.x;
+    const bool more_than_one = sched.chunks > (int)gridDim.x;
     int filled = 0;                                            // stages filled so far (warp 0)
 
     if (warp == 0) {
         const uint64_t stream = l2_policy_evict_first(), keep = l2_policy_evict_last();
-        if (lane == 0) { tma_prefetch_descriptor(&map_w0); tma_prefetch_descriptor(&map_w1); tma_prefetch_descriptor(&map_x); }
         auto weights = [&](const Item &t, int k, int s) {      // one lane
             const uint32_t dst = base + (uint32_t)s * a.stage_bytes, bar = full0 + 8 * s;
 #pragma unroll
@@ -249,8 +247,10 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                 }
             }
         };
-        // bytes of a step's token rows: groups of four gathered rows, or of eight rows as they lie, for each term
-        auto token_bytes = [&](const Item &t) { return a.gather ? (uint32_t)ceil_div(t.rows, 4) * 512u : (uint32_t)ceil_div(t.rows, 8) * 1024u * a.terms; };
+        // bytes of a step's token rows: groups of four gathered rows, or boxes of rows as they lie, for each term
+        auto token_bytes = [&](const Item &t) {
+            return a.gather ? (uint32_t)ceil_div(t.rows, 4) * 512u : (uint32_t)(ceil_div(t.rows, a.box_rows) * a.box_rows * a.terms) * 128u;
+        };
         auto rows_of = [&](const Item &t, int (&ids)[4]) {     // lane i: the token rows of group i
             if (!a.gather) return;
 #pragma unroll
@@ -264,37 +264,38 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             if (a.gather) {
                 if (4 * lane < t.rows) tma_gather4(dst + lane * 512, &map_x, k * kKT, ids, bar, keep);
             } else {
-                const int group = lane & 15, term = lane >> 4;
-                if (8 * group < t.rows && term < a.terms)
-                    tma_load_3d(dst + (uint32_t)term * a.R * 128 + group * 1024, &map_x, k * kKT, t.row0 + 8 * group, term, bar, keep);
+                const int row = (lane & 7) * a.box_rows, term = lane >> 3;
+                if (row < t.rows && term < a.terms) tma_load_3d(dst + (uint32_t)(term * a.R + row) * 128, &map_x, k * kKT, t.row0 + row, term, bar, keep);
             }
         };
         // The first fills: weights before the wait, tokens behind it.
         int head = 0;
         if (a.early_weights) {
-            Walk w = all;
-            while (head < NS && w.next()) {
-                const Item t = item_of(a, w.item);
-                for (int k = w.k0; k < w.k1 && head < NS; ++k, ++head) {
-                    if (lane == 0) {
-                        mbar_arrive_expect_tx(full0 + 8 * head, kSlabs * kSlabBytes + token_bytes(t));
-                        weights(t, k, head);
+            if (first_id < sched.chunks) {
+                const Chunk c = chunk_of(sched, a.kb, first_id);
+                const Item t = item_of(a, c.item);
+                head = min(NS, c.k1 - c.k0);
+                if (lane == 0)
+                    for (int i = 0; i < head; ++i) {
+                        mbar_arrive_expect_tx(full0 + 8 * i, kSlabs * kSlabBytes + token_bytes(t));
+                        weights(t, c.k0 + i, i);
                     }
-                }
+                filled = head;
             }
-            filled = head;
             pdl_wait_prior_grids();
         }
         __syncwarp();
-        Walk w = all;
-        int s = 0, n = 0;
-        uint32_t ph = 1;                                        // a fresh barrier passes a wait for the phase before its first
+        int s = 0, n = 0, queue = 0;
+        uint32_t ph = 1, queue_ph = 1;                          // a fresh barrier passes a wait for the phase before its first
         bool ok = true;
-        while (ok && w.next()) {
-            const Item t = item_of(a, w.item);
+        for (int id = first_id; ok && id < sched.chunks;) {
+            int next = sched.chunks;                            // asked for now, needed when this chunk has been copied
+            if (more_than_one && lane == 0) next = (int)gridDim.x + (int)atomicAdd(a.counters + a.ticket, 1u);
+            const Chunk c = chunk_of(sched, a.kb, id);
+            const Item t = item_of(a, c.item);
             int ids[4] = {0, 0, 0, 0};
             rows_of(t, ids);
-            for (int k = w.k0; k < w.k1; ++k, ++n) {
+            for (int k = c.k0; k < c.k1; ++k, ++n) {
                 if (n >= head) {
                     if (lane == 0) {
                         ok = mbar_try_wait(empty0 + 8 * s, ph) || mbar_wait(empty0 + 8 * s, ph, &s_abort, a.status);
@@ -310,25 +311,41 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                 tokens(t, ids, k, s);
                 if (++s == NS) { s = 0; ph ^= 1; }
             }
+            id = sched.chunks;
+            if (ok && more_than_one) {
+                id = __shfl_sync(0xffffffffu, next, 0);
+                if (lane == 0) {
+                    ok = mbar_try_wait(taken0 + 8 * queue, queue_ph) || mbar_wait(taken0 + 8 * queue, queue_ph, &s_abort, a.status);
+                    if (ok) { s_queue[queue] = id; mbar_arrive(queued0 + 8 * queue); }
+                }
+                ok = __shfl_sync(0xffffffffu, ok, 0);
+                if (++queue == kQueue) { queue = 0; queue_ph ^= 1; }
+            }
+        }
+        // Every CTA has its last ticket: whoever is last to say so clears them for the next call.
+        if (more_than_one && !a.planned && lane == 0 && atomicAdd(a.counters + kDone, 1u) == gridDim.x - 1) {
+            a.counters[a.ticket] = 0u;
+            a.counters[kDone] = 0u;
         }
     } else if (warp == 1) {
         // The whole warp walks, one elected lane issues: descriptors are then uniform values.
         const bool leader = elect_one();
-        Walk w = all;
-        int s = 0, acc = 0;
-        uint32_t ph = 0, acc_ph = 1;
+        int s = 0, acc = 0, queue = 0;
+        uint32_t ph = 0, acc_ph = 1, queue_ph = 0;
         bool ok = true;
-        while (ok && w.next()) {
-            const Item t = item_of(a, w.item);
+        for (int id = first_id; id < sched.chunks;) {
+            const Chunk c = chunk_of(sched, a.kb, id);
+            const Item t = item_of(a, c.item);
             const int columns = max(16, (t.rows + 15) & ~15);
             const uint32_t idesc = a.f16 ? instr_desc_f16(kSlab, columns, !a.col, false) : instr_desc(kSlab, columns, !a.col, false);
             ok = mbar_try_wait(acc_empty0 + 8 * acc, acc_ph) || mbar_wait(acc_empty0 + 8 * acc, acc_ph, &s_abort, a.status);
-            if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+            if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
             const uint32_t d = tmem + (uint32_t)acc * kSlabs * a.R;
-            for (int k = w.k0; k < w.k1; ++k) {
+            for (int k = c.k0; k < c.k1; ++k) {
                 ok = mbar_try_wait(full0 + 8 * s, ph) || mbar_wait(full0 + 8 * s, ph, &s_abort, a.status);
-                if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
+                ok = __all_sync(0xffffffffu, ok);
+                if (!ok) break;
                 tc_fence_after();
                 const uint32_t sw = base + (uint32_t)s * a.stage_bytes, sx = sw + kSlabs * kSlabBytes;
                 if (leader) {
@@ -338,7 +355,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                         for (int sl = 0; sl < kSlabs; ++sl) {
                             const uint32_t swl = sw + sl * kSlabBytes;
                             const uint64_t wd = a.col ? smem_desc(swl + kk * 32, 16, 1024) : smem_desc(swl + kk * 2048, kSlabBytes / 2, 1024);
-                            mma_ss(d + sl * a.R, wd, smem_desc(sx + kk * 32, 16, 1024), idesc, k != w.k0 || kk != 0);
+                            mma_ss(d + sl * a.R, wd, smem_desc(sx + kk * 32, 16, 1024), idesc, k != c.k0 || kk != 0);
                             if (a.terms == 2) mma_ss(d + sl * a.R, wd, smem_desc(sx + a.R * 128 + kk * 32, 16, 1024), idesc, true);
                         }
                     mma_commit(empty0 + 8 * s);
@@ -349,48 +366,45 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             if (leader) mma_commit(acc_full0 + 8 * acc);
             if (acc) acc_ph ^= 1;
             acc ^= 1;
+            id = sched.chunks;
+            if (more_than_one) {
+                ok = mbar_try_wait(queued0 + 8 * queue, queue_ph) || mbar_wait(queued0 + 8 * queue, queue_ph, &s_abort, a.status);
+                if (!__all_sync(0xffffffffu, ok)) break;
+                id = *static_cast<volatile int *>(s_queue + queue);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(taken0 + 8 * queue);
+                if (++queue == kQueue) { queue = 0; queue_ph ^= 1; }
+            }
         }
     } else {
-        const int quad = warp & 3, n_lane = quad * 32 + lane, thread = tid - 64;
+        const int quad = warp & 3, turn = (warp - 2) >> 2, step = finishers / 32, n_lane = quad * 32 + lane, thread = tid - 64;
         if (a.early_weights) pdl_wait_prior_grids();            // nothing is written, and nothing of earlier kernels read, before they are done
-        Walk w = all;
-        int acc = 0;
-        uint32_t ph = 0;
-        while (w.next()) {
-            const Item t = item_of(a, w.item);
+        int acc = 0, queue = 0, round = 0;
+        uint32_t ph = 0, queue_ph = 0;
+        for (int id = first_id; id < sched.chunks; round ^= 1) {
+            const Chunk c = chunk_of(sched, a.kb, id);
+            const Item t = item_of(a, c.item);
             mbar_wait(acc_full0 + 8 * acc, ph, &s_abort, a.status);   // (where it ran out the walk goes on, over values that the status disowns: the
-                                                                    // barriers below are for all four warps)
+                                                                    // barriers below are for all of the warps)
             tc_fence_after();
             const uint32_t d = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)acc * kSlabs * a.R;
-            const bool whole = w.k0 == 0 && w.k1 == a.kb;
-            float *mine = a.partial + (size_t)(2 * c + (w.k0 == 0 ? 1 : 0)) * a.R * (kSlabs * kSlab);
-            for (int j = 0; j < t.rows; j += 16) {
-                uint32_t bits[kSlabs][16];
-                float z[kSlabs][16];
+            float4 *mine = reinterpret_cast<float4 *>(a.partial) + (size_t)c.slot * a.R * (kSlabs * kSlab / 4);
+            for (int j = 4 * turn; j < t.rows; j += step) {
+                uint32_t bits[kSlabs][4];
+                float z[kSlabs][4];
 #pragma unroll
-                for (int sl = 0; sl < kSlabs; ++sl) tmem_ld16(d + sl * a.R + j, bits[sl]);
+                for (int sl = 0; sl < kSlabs; ++sl) tmem_ld4(d + sl * a.R + j, bits[sl]);
                 tmem_wait_ld();
 #pragma unroll
                 for (int sl = 0; sl < kSlabs; ++sl)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) z[sl][i] = __uint_as_float(bits[sl][i]);
-                const int count = min(16, t.rows - j);
-                if (whole) {
-                    if constexpr (kGated) {
-                        finish<kMode, true>(a, t.row0 + j, count, t.n0 + n_lane, z[0], z[kSlabs - 1]);
-                    } else {
-#pragma unroll
-                        for (int sl = 0; sl < kSlabs; ++sl)
-                            finish<kMode, false>(a, t.row0 + j, count, t.n0 + sl * kSlab + n_lane, z[sl], z[sl]);
-                    }
+                    for (int i = 0; i < 4; ++i) z[sl][i] = __uint_as_float(bits[sl][i]);
+                if (c.cut < 0) {
+                    finish_all<kMode, kGated, kSlabs>(a, t, j, n_lane, z);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < 16; i += 4)
-                        if (i < count)
-#pragma unroll
-                            for (int sl = 0; sl < kSlabs; ++sl)
-                                NM_ST(reinterpret_cast<float4 *>(mine) + ((j + i) / 4 * kSlabs + sl) * kSlab + n_lane,
-                                      make_float4(z[sl][i], z[sl][i + 1], z[sl][i + 2], z[sl][i + 3]), a.in_partial, a.status);
+                    for (int sl = 0; sl < kSlabs; ++sl)
+                        NM_ST(mine + (j / 4 * kSlabs + sl) * kSlab + n_lane, make_float4(z[sl][0], z[sl][1], z[sl][2], z[sl][3]), a.in_partial, a.status);
                 }
             }
             tc_fence_before();
@@ -398,24 +412,34 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             if (lane == 0) mbar_arrive(acc_empty0 + 8 * acc);
             if (acc) ph ^= 1;
             acc ^= 1;
-            if (whole) continue;
 
-            // The CTAs that share the item: those of its first and last step, and all between.
-            const long u0 = w.item * a.kb, u1 = u0 + a.kb - 1;
-            const int first = (int)(((u0 + 1) * C - 1) / units), last = (int)(((u1 + 1) * C - 1) / units);
-            __threadfence();
-            named_barrier_sync(1, 128);
-            if (thread == 0) {
-                const unsigned there = atomicAdd(a.counters + first, 1u);
-                s_last = there == (unsigned)(last - first);
-                if (s_last) a.counters[first] = 0u;             // ready for the next call
+            if (c.cut >= 0) {
+                __threadfence();
+                named_barrier_sync(1, finishers);
+                if (thread == 0) {
+                    s_last = atomicAdd(a.counters + kItemCounters + c.cut, 1u) == (unsigned)(sched.parts - 1);
+                    if (s_last) a.counters[kItemCounters + c.cut] = 0u;             // ready for the next product
+                }
+                named_barrier_sync(1, finishers);
+                if (s_last) {
+                    __threadfence();
+                    for (int j = 4 * turn; j < t.rows; j += step) {
+                        float z[kSlabs][4];
+                        join<kSlabs>(a, j, c.first_slot, sched.parts, n_lane, z);
+                        finish_all<kMode, kGated, kSlabs>(a, t, j, n_lane, z);
+                    }
+                }
             }
-            named_barrier_sync(1, 128);
-            if (!s_last) continue;
-            __threadfence();
-            // Few rows: many pieces on their way at once; more rows: more of each piece.
-            if (t.rows <= 4) join<kMode, kGated, kSlabs, 1, 8>(a, t, 0, first, last, n_lane);
-            else for (int j = 0; j < t.rows; j += 16) join<kMode, kGated, kSlabs, 4, 2>(a, t, j, first, last, n_lane);
+            if (!more_than_one) break;
+            // One thread takes the next chunk for all, so that they agree where a wait runs out.
+            if (thread == 0) {
+                const bool ok = mbar_wait(queued0 + 8 * queue, queue_ph, &s_abort, a.status);
+                s_next[round] = ok ? *static_cast<volatile int *>(s_queue + queue) : sched.chunks;
+                mbar_arrive(taken0 + 8 * queue);
+            }
+            if (++queue == kQueue) { queue = 0; queue_ph ^= 1; }
+            named_barrier_sync(1, finishers);
+            id = *static_cast<volatile int *>(s_next + round);
         }
     }
 
@@ -459,7 +483,8 @@ cudaError_t launch_stream(const CUtensorMap &w0, const CUtensorMap &w1, const CU
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
-    cfg.blockDim = dim3(kThreads);
+    // four rows at a time for each warp of a quarter: one to four of them
+    cfg.blockDim = dim3(64 + 128 * (a.R <= 16 ? 1 : a.R == 32 ? 2 : 4));
     cfg.dynamicSmemBytes = (size_t)a.nstage * a.stage_bytes + 1024;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
@@ -472,8 +497,6 @@ cudaError_t launch_stream(const CUtensorMap &w0, const CUtensorMap &w1, const CU
 
 }  // namespace
 
-size_t stream_partial_bytes(int R, int slabs) { return (size_t)2 * kSMs * R * slabs * kSlab * sizeof(float); }
-
 int stream_tile_rows(double average, int most)
 {
     for (int R = 16; R < 128; R *= 2)
@@ -481,18 +504,43 @@ int stream_tile_rows(double average, int most)
     return 128;
 }
 
-int stream_slabs(int R, bool gated) { return gated || R == 128 ? 2 : 1; }
+// Two slabs halve how often the token rows are read (and the MMAs that share them come in pairs); of a narrow matrix too much of the last tile would be empty.
+int stream_slabs(int N, bool gated) { return gated || N >= 2048 ? 2 : 1; }
+
+// Sums of chunks: as many as 64 MB hold, and no more than 1024.
+static int most_chunks(int R, int N, bool gated) { return (int)std::min<size_t>(1024, ((size_t)64 << 20) / ((size_t)R * stream_slabs(N, gated) * kSlab * sizeof(float))); }
+size_t stream_partial_bytes(int R, int N, bool gated) { return (size_t)most_chunks(R, N, gated) * R * stream_slabs(N, gated) * kSlab * sizeof(float); }
+
+CutModel stream_cut_model(int R, int N, int K, bool gated, int terms)
+{
+    const int slabs = stream_slabs(N, gated);
+    const float step_bytes = (float)(slabs * kSlabBytes + terms * R * 128 / 2), step_us = step_bytes / 70e3f;      // (half of the rows there may be)
+    CutModel m;
+    m.kb = ceil_div(K, kKT);
+    m.column_tiles = ceil_div(N, gated ? kSlab : slabs * kSlab);
+    m.most_chunks = most_chunks(R, N, gated);
+    m.sums_steps = (float)(R / 2) * slabs * kSlab * 8 / step_bytes;
+    m.latency_steps = 2.5f / step_us;
+    return m;
+}
 
 cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStream_t s, const char **what)
 {
     StreamArgs a{};
-    const int slabs = stream_slabs(p.R, gated);
-    a.kb = ceil_div(p.K, kKT);
+    const int slabs = stream_slabs(p.N, gated);
+    const CutModel m = stream_cut_model(p.R, p.N, p.K, gated, p.terms);
+    a.kb = m.kb;
     a.tile_n = gated ? kSlab : slabs * kSlab;
-    a.column_tiles = ceil_div(p.N, a.tile_n);
+    a.column_tiles = m.column_tiles;
+    a.box_rows = std::min(32, p.R / 2);
     a.rows = p.rows; a.N = p.N; a.R = p.R; a.terms = p.terms;
-    a.items = p.planned ? 0 : (long)ceil_div(p.rows, p.R) * a.column_tiles;
-    a.units = a.items * a.kb;
+    if (!p.planned) {
+        const int items = ceil_div(p.rows, p.R) * a.column_tiles, rest = items - whole_items(items);
+        int best = 1;
+        for (int parts = 2; parts <= std::min(a.kb, kSMs) && rest * parts <= m.most_chunks; ++parts)
+            if (cut_cost(rest, a.kb, parts, m.sums_steps, m.latency_steps) < cut_cost(rest, a.kb, best, m.sums_steps, m.latency_steps)) best = parts;
+        a.schedule = schedule_of(items, a.kb, best);
+    }
     a.stage_bytes = slabs * kSlabBytes + p.terms * p.R * 128;
     a.nstage = std::min(kMaxStages, kRingBytes / a.stage_bytes);
     a.tmem_columns = std::max(32, 2 * slabs * p.R);
@@ -500,13 +548,13 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     a.act = p.act; a.plan = p.plan;
     a.bias = static_cast<const uint16_t *>(p.bias); a.residual = static_cast<const uint16_t *>(p.residual); a.ld_residual = p.ld_residual;
     a.out = p.out; a.ldo = p.ldo; a.out_term = (long)p.rows * p.ldo; a.row_scale = p.row_scale;
-    a.partial = p.partial; a.counters = p.counters;
+    a.partial = p.partial; a.counters = p.counters; a.ticket = p.ticket;
     const int parts = gated ? 2 : 1;
     a.in_bias = make_span(p.bias, p.bias ? 2 * (size_t)parts * p.N : 0);
     a.in_residual = make_span(p.residual, p.residual ? 2 * ((size_t)(p.rows - 1) * p.ld_residual + p.N) : 0);
     a.in_out = make_span(p.out, mode == kOutAct ? 2 * ((size_t)(p.rows - 1) * p.ldo + p.N) : 4 * (size_t)p.rows * p.ldo);
     a.in_scale = make_span(p.row_scale, p.row_scale ? 4 * (size_t)p.rows : 0);
-    a.in_partial = make_span(p.partial, stream_partial_bytes(p.R, slabs));
+    a.in_partial = make_span(p.partial, stream_partial_bytes(p.R, p.N, gated));
     a.in_tiles = make_span(p.plan.tiles, sizeof(RowTile) * ((size_t)p.E + p.rows / p.R));
     a.in_order = make_span(p.plan.order, 4 * (size_t)p.rows);
     a.status = device_status_ptr();
@@ -532,13 +580,13 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
         ok = ok && encode_map(&x, p.x, p.f16, 2, dims, strides, box);
     } else {
         const cuuint64_t dims[3] = {(cuuint64_t)p.K, (cuuint64_t)p.x_rows, (cuuint64_t)p.terms}, strides[2] = {(cuuint64_t)p.ldx * 2, (cuuint64_t)p.x_term * 2};
-        const cuuint32_t box[3] = {kKT, 8, 1};
+        const cuuint32_t box[3] = {kKT, (cuuint32_t)a.box_rows, 1};
         ok = ok && encode_map(&x, p.x, p.f16, 3, dims, strides, box);
     }
     if (!ok) { *what = "cuTensorMapEncodeTiled"; return cudaErrorInvalidValue; }
     if (!a.status) { *what = "device status word"; return cudaErrorInvalidValue; }
     *what = "streamed product launch";
-    const long ctas = p.planned ? kSMs : std::min<long>(kSMs, a.units);
+    const long ctas = p.planned ? kSMs : std::min(kSMs, a.schedule.chunks);
     if (!gated) w[1] = w[0];
     switch (mode) {
     case kOutAct:
