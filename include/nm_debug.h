@@ -19,6 +19,9 @@ extern "C" {
 /* Override the tiling heuristic: columns per CTA tile of the row-major kernel and number of
  * k-splits; 0 restores the heuristic.  Values are clamped to what the workspace bound covers. */
 int nm_debug_set_plan(int tile_n, int nsplit);
+/* Feed-forward products (nm_matmul_act, nm_moe_ffn): the chunks that an item of the last rounds is cut into, or as near to it as the workspace and the inner
+ * dimension allow; 0 gives it back to the model.  Results of equal cuts have equal bits. */
+int nm_debug_set_ffn_cut(int parts);
 /* Force the kernel family for row-major bf16 weights (-1 heuristic; 0 plain-load kernel; 3 TMA-ring
  * CUDA-core kernel; 4 swap-AB tensor-core kernel) and the ring depth in stages (0 heuristic). */
 int nm_debug_set_kernel(int kind, int stages);

@@ -67,6 +67,7 @@ _lib.nm_w4_scale_count.argtypes = [_i, _i, _i]
 _lib.nm_w4_quantize.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _i, _vp]
 _lib.nm_w4_dequantize.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _i, _vp]
 _lib.nm_debug_set_plan.argtypes = [_i, _i]
+_lib.nm_debug_set_ffn_cut.argtypes = [_i]
 _lib.nm_debug_set_w4_plan.argtypes = [_i, _i, _i]
 _lib.nm_debug_set_kernel.argtypes = [_i, _i]
 _lib.nm_set_tensor_core_min_m.argtypes = [_i]
@@ -259,6 +260,10 @@ def nm_w4_dequantize(packed, scales, B_out, N, K, group, dtype=BF16, layout_B=RO
 
 def nm_debug_set_w4_plan(warps_across: int = 0, ctas_along_k: int = 0, piece_blocks: int = 0) -> None:
     _check(_lib.nm_debug_set_w4_plan(warps_across, ctas_along_k, piece_blocks), "nm_debug_set_w4_plan")
+
+
+def nm_debug_set_ffn_cut(parts: int = 0) -> None:
+    _check(_lib.nm_debug_set_ffn_cut(int(parts)), "nm_debug_set_ffn_cut")
 
 
 def nm_debug_set_plan(tile_n: int = 0, nsplit: int = 0) -> None:

@@ -197,7 +197,7 @@ __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a)
 constexpr int kPlanThreads = 512;
 struct PlanArgs {
     const int32_t *experts; int first, E;
-    int pairs, R;
+    int pairs, R, top_k;
     RowTile *tiles; int *order; int *place;
     int *n_rows;                                // rows there are in all
     Schedule *schedules;                        // of the two products
@@ -246,7 +246,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a)
             const CutModel &m = a.model[warp];
             const int items = (tile0 + own) * m.column_tiles, rest = items - whole_items(items), parts = lane + 1;
             const bool may = parts == 1 || (parts <= m.kb && (long)rest * parts <= m.most_chunks);
-            const float cost = may ? cut_cost(rest, m.kb, parts, m.sums_steps, m.latency_steps) : INFINITY;
+            const float cost = may ? cut_cost(m, rest, parts) : INFINITY;
             const unsigned least = __reduce_min_sync(0xffffffffu, __float_as_uint(cost));       // (costs are not negative: their bits order as they do)
             const int best = __ffs((int)__ballot_sync(0xffffffffu, __float_as_uint(cost) == least));
             if (lane == 0) a.schedules[warp] = schedule_of(items, m.kb, best);
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a)
         for (int i = 0; i < kPlanThreads / 32; ++i) { const int n = s_before[buf][i]; before += i < warp ? n : 0; all += n; }
         if (here) {
             const int row = at + before + __popc(votes & ((1u << lane) - 1u));
-            NM_ST(a.order + row, p, a.in_order, a.status);
+            NM_ST(a.order + row, p / a.top_k, a.in_order, a.status);
             NM_ST(a.place + p, row, a.in_place, a.status);
         }
         at += all;
@@ -276,14 +276,14 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a)
 
 // ---- rows in the order of their experts ------------------------------------------------------------------------------------------
 // For tiles of many rows (see nm_ffn_stream.cu): a block a row, 16 bytes a thread.
-__global__ void __launch_bounds__(256) sort_rows_kernel(const uint16_t *x, long ldx, const int *order, int top_k, const int *n_rows, int d, uint16_t *to, unsigned *status, Span in_x,
+__global__ void __launch_bounds__(256) sort_rows_kernel(const uint16_t *x, long ldx, const int *order, const int *n_rows, int d, uint16_t *to, unsigned *status, Span in_x,
                                                         Span in_order, Span in_to)
 {
     pdl_launch_dependents();
     pdl_wait_prior_grids();
     const int rows = *n_rows;
     for (int r = blockIdx.x; r < rows; r += gridDim.x) {
-        const uint16_t *from = x + (long)(NM_LD(order + r, in_order, status) / top_k) * ldx;
+        const uint16_t *from = x + (long)NM_LD(order + r, in_order, status) * ldx;
         for (int i = 8 * threadIdx.x; i < d; i += 2048)
             NM_ST(reinterpret_cast<uint4 *>(to + (size_t)r * d + i), NM_LD(reinterpret_cast<const uint4 *>(from + i), in_x, status), in_to, status);
     }
@@ -461,7 +461,7 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
     cudaError_t e;
     if (rows_on_16(x, ldx) && rows_on_16(W_up, col ? d : inter) && rows_on_16(W_down, col ? inter : d) && inter % 8 == 0) {
         PlanArgs pl{};
-        pl.experts = experts; pl.first = first_expert; pl.E = E; pl.pairs = (int)pairs;
+        pl.experts = experts; pl.first = first_expert; pl.E = E; pl.pairs = (int)pairs; pl.top_k = top_k;
         pl.R = stream_tile_rows((double)pairs / E, (int)std::min<long>(pairs, 128));
         pl.tiles = reinterpret_cast<RowTile *>(ws + lay.tiles); pl.n_rows = reinterpret_cast<int *>(ws + lay.n_rows);
         pl.schedules = reinterpret_cast<Schedule *>(ws + lay.schedules);
@@ -479,15 +479,15 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
         p.rows = (int)pairs; p.N = inter; p.K = d; p.R = pl.R; p.terms = 1;
         p.col = col; p.f16 = f16; p.planned = p.programmatic = true;
         p.act = act;
-        p.plan = RowPlan{pl.tiles, pl.schedules, pl.order, top_k};
+        p.plan = RowPlan{pl.tiles, pl.schedules, pl.order};
         p.W = W_up; p.w_expert = (long)parts * inter * d; p.E = E;
-        p.gather = pl.R <= 32;
+        p.gather = pl.R <= 16;
         if (p.gather) {
             p.x = x; p.ldx = ldx; p.x_rows = T;
         } else {                                                  // the sorted rows lie where y will be
             uint16_t *sorted = reinterpret_cast<uint16_t *>(y);
             if (e == cudaSuccess)
-                e = launch(sort_rows_kernel, pairs, 256, true, s, static_cast<const uint16_t *>(x), ldx, static_cast<const int *>(pl.order), top_k, static_cast<const int *>(pl.n_rows), d,
+                e = launch(sort_rows_kernel, pairs, 256, true, s, static_cast<const uint16_t *>(x), ldx, static_cast<const int *>(pl.order), static_cast<const int *>(pl.n_rows), d,
                            sorted, status, make_span(x, 2 * ((size_t)(T - 1) * ldx + d)), pl.in_order, make_span(sorted, 2 * (size_t)pairs * d));
             p.x = sorted; p.ldx = d; p.x_rows = pairs; p.x_term = pairs * d;
         }

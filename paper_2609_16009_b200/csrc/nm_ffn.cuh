@@ -37,7 +37,8 @@ __device__ __forceinline__ float widen16(uint16_t v, bool f16) { return f16 ? __
 __device__ __forceinline__ uint16_t round16(float v, bool f16) { return f16 ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 
 // Rows of the experts.  Pair p = (token p / top_k, choice p % top_k) belongs to expert experts[p] - first where that is one of the E held
-// here.  `order` lists the pairs by expert, each expert's in rising order; `place` is its inverse; a tile is up to R of one expert's rows.
+// here.  Rows are the pairs sorted by expert, each expert's in rising order: `order` has their tokens, `place` the row of each pair; a tile is up to R of one
+// expert's rows.
 struct RowTile { int expert, row0, rows, unused; };
 
 // How the items of a product (a row tile x a column tile, kb steps of 64 k each) are dealt out: the first `whole` as they are, each of the others in
@@ -47,8 +48,7 @@ struct Schedule { int whole, parts, kc, chunks; };
 struct RowPlan {
     const RowTile *tiles;
     const Schedule *schedule;          // of this product
-    const int *order;                  // [sorted row] -> pair
-    int top_k;
+    const int *order;                  // [sorted row] -> token
 };
 
 // Words of the counter area: a ticket for each product of a call (the chunks dealt out beyond one for each CTA), CTAs that are done, and the chunks there
@@ -59,13 +59,14 @@ constexpr int kTicketUp = 0, kTicketDown = 1, kDone = 2, kItemCounters = 32, kMa
 // long (HBM, measured 6.5 TB/s, against 148 * 70 GB/s); a chunk's sums go to the workspace and back; and joining costs `latency` steps once.
 // All items but the last one to two rounds stay whole: sums in the workspace cost as much as the rows do, and only the end has to be even.
 constexpr float kBusy = 1.6f;
-__host__ __device__ inline float cut_cost(int rest, int kb, int parts, float sums_steps, float latency_steps)
+struct CutModel { int kb, column_tiles, most_chunks, forced; float sums_steps, latency_steps; };
+__host__ __device__ inline float cut_cost(const CutModel &m, int rest, int parts)
 {
-    const int kc = (kb + parts - 1) / parts, p = (kb + kc - 1) / kc, rounds = (rest * p + kSMs - 1) / kSMs;
-    const float hbm = (float)rest * kb * kBusy / kSMs, sm = (float)rounds * kc, each = p > 1 ? sums_steps * rounds + latency_steps : 0.f;
+    if (m.forced) return parts <= m.forced ? (float)(m.forced - parts) : 1e9f;        // the nearest that may be
+    const int kc = (m.kb + parts - 1) / parts, p = (m.kb + kc - 1) / kc, rounds = (rest * p + kSMs - 1) / kSMs;
+    const float hbm = (float)rest * m.kb * kBusy / kSMs, sm = (float)rounds * kc, each = p > 1 ? m.sums_steps * rounds + m.latency_steps : 0.f;
     return (hbm > sm ? hbm : sm) + each;
 }
-struct CutModel { int kb, column_tiles, most_chunks; float sums_steps, latency_steps; };
 __host__ __device__ inline int whole_items(int items) { return items >= 2 * kSMs ? (items / kSMs - 1) * kSMs : 0; }
 __host__ __device__ inline Schedule schedule_of(int items, int kb, int parts)
 {

@@ -14,12 +14,16 @@
 //          tile: what an output costs is latency (tensor memory, exp, residual; 128 rows of 1536 x 24576 took 96 us with four warps, 48 with sixteen),
 //          and a launch of more warps costs a short call 1.5 us
 //
-// Token rows are copied as they lie, or gathered by token four at a time (tile::gather4) where the rows of an expert are scattered and few: a
-// request takes the copy engine ~40 ns whatever its size, so more than eight a step would be what bounds the kernel, and rows are sorted first.
-// The number of accumulator columns is that of the rows there are, rounded up to 16; what the columns beyond hold is not read.
-// A hidden value is the sum of two 16-bit terms (bf16: 16 bits and more, fp16: 22), both multiplied into the same accumulator: the MMAs are far
-// from being the bound, and the second term keeps the rounding of the hidden values out of the result.
+// A step's token rows are ONE copy: of the four box heights there are a tensor map of, the least that holds the tile's rows.  A request costs the copy
+// engine and the thread that makes it 40 to 60 ns whatever its size, and requests made by several lanes at once take their turns (two boxes of 8 rows by two lanes: 0.2 us
+// a step, as much as 16 KB of weights).  Scattered rows are gathered by token where they are few (tile::gather4, four rows a request), and sorted first where not.
+// The number of accumulator columns is that of the rows there are, rounded up; what the columns beyond hold is not read.
+//
+// A hidden value is the sum of two 16-bit terms (bf16: 16 bits and more, fp16: 22), which keeps its rounding out of the result.  A row's terms are two rows of
+// the token operand: up to 64 rows one MMA takes both, in columns of their own that the epilogue adds (an MMA of 16 columns takes as long as one of 32); beyond, an
+// MMA each into the same columns.
 #include <algorithm>
+#include <type_traits>
 
 #include "nm_ffn.cuh"
 #include "nm_tcgen05.cuh"
@@ -36,12 +40,16 @@ constexpr int kSlabBytes = kSlab * kKT * 2;
 constexpr int kMaxStages = 12;
 constexpr int kRingBytes = 216 * 1024;
 
+std::atomic<int> g_forced_parts{0};             // nm_debug_set_ffn_cut
+
 struct StreamArgs {
     Schedule schedule;                          // where the rows are known on the host
     int kb, column_tiles, tile_n;               // steps of an item, column tiles of a row tile, outputs of one
-    int rows, N, R, box_rows, terms, nstage, stage_bytes;
+    int rows, N, R, box_rows, terms, nstage, stage_bytes;   // box_rows: the least of the box heights, the others its multiples
+    int acc_columns;                            // of a slab: R, twice that where the terms have columns of their own
+    bool apart;
     unsigned tmem_columns;
-    bool col, f16, gather, planned, early_weights, programmatic;
+    bool f16, gather, planned, early_weights, programmatic;
     int act;
     RowPlan plan;
     const uint16_t *bias, *residual; long ld_residual;
@@ -60,13 +68,16 @@ __device__ __forceinline__ bool elect_one()
 }
 
 // Four rows of a 2-D tensor, 64 k each, to consecutive 128-byte rows of shared memory.
-__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap *map, int x, const int (&row)[4], uint32_t bar, uint64_t policy)
+__device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap *map, int x, int r0, int r1, int r2, int r3, uint32_t bar, uint64_t policy)
 {
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cta.global.tile::gather4.mbarrier::complete_tx::bytes.L2::cache_hint"
         " [%0], [%1, {%2, %3, %4, %5, %6}], [%7], %8;"
-        ::"r"(dst), "l"(map), "r"(x), "r"(row[0]), "r"(row[1]), "r"(row[2]), "r"(row[3]), "r"(bar), "l"(policy) : "memory");
+        ::"r"(dst), "l"(map), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar), "l"(policy) : "memory");
 }
+
+// Token rows: boxes of 1, 2, 3 and 4 times box_rows rows (the first alone for gathered rows).
+struct TokenMaps { CUtensorMap of[4]; };
 
 // A chunk: steps [k0, k1) of an item; where that is not all of it, the place of its sums and of the item's first chunk's, and the item's counter.
 struct Chunk { int item, k0, k1, slot, first_slot, cut; };
@@ -192,9 +203,9 @@ __device__ __forceinline__ void join(const StreamArgs &a, int j, int first, int 
     }
 }
 
-template <int kMode, bool kGated, int kSlabs>
+template <int kMode, bool kGated, int kSlabs, bool kCol>
 __global__ void __launch_bounds__(kMaxThreads, 1)
-stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1, const __grid_constant__ CUtensorMap map_x, const StreamArgs a)
+stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1, const __grid_constant__ TokenMaps maps_x, const StreamArgs a)
 {
     static_assert(!kGated || kSlabs == 2, "gate and up are a slab each");
     extern __shared__ unsigned char smem_raw[];
@@ -209,7 +220,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
     const int NS = a.nstage, finishers = (int)blockDim.x - 64;
 
     if (warp == 0) {
-        if (lane == 0) { tma_prefetch_descriptor(&map_w0); tma_prefetch_descriptor(&map_w1); tma_prefetch_descriptor(&map_x); s_abort = 0; }
+        if (lane == 0) { tma_prefetch_descriptor(&map_w0); if (kGated) tma_prefetch_descriptor(&map_w1); tma_prefetch_descriptor(&maps_x.of[0]); s_abort = 0; }
         if (lane < NS) { mbar_init(full0 + 8 * lane, 1); mbar_init(empty0 + 8 * lane, 1); }
         if (lane < kQueue) { mbar_init(queued0 + 8 * lane, 1); mbar_init(taken0 + 8 * lane, 2); }      // (taken by the MMA warp and the epilogue)
         if (lane < 2) { mbar_init(acc_full0 + 8 * lane, 1); mbar_init(acc_empty0 + 8 * lane, (uint32_t)finishers / 32); }
@@ -232,100 +243,90 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
     int filled = 0;                                            // stages filled so far (warp 0)
 
     if (warp == 0) {
-        const uint64_t stream = l2_policy_evict_first(), keep = l2_policy_evict_last();
-        auto weights = [&](const Item &t, int k, int s) {      // one lane
-            const uint32_t dst = base + (uint32_t)s * a.stage_bytes, bar = full0 + 8 * s;
+        if (lane == 0) {
+            const uint64_t stream = l2_policy_evict_first(), keep = l2_policy_evict_last();
+            auto weights = [&](const Item &t, int k, int s) {
+                const uint32_t dst = base + (uint32_t)s * a.stage_bytes, bar = full0 + 8 * s;
 #pragma unroll
-            for (int sl = 0; sl < kSlabs; ++sl) {
-                const CUtensorMap *m = kGated && sl ? &map_w1 : &map_w0;
-                const int n = t.n0 + (kGated ? 0 : sl * kSlab);
-                if (a.col) {
-                    tma_load_3d(dst + sl * kSlabBytes, m, k * kKT, n, t.expert, bar, stream);
-                } else {
-                    tma_load_3d(dst + sl * kSlabBytes, m, n, k * kKT, t.expert, bar, stream);
-                    tma_load_3d(dst + sl * kSlabBytes + kSlabBytes / 2, m, n + 64, k * kKT, t.expert, bar, stream);
+                for (int sl = 0; sl < kSlabs; ++sl) {
+                    const CUtensorMap *m = kGated && sl ? &map_w1 : &map_w0;
+                    const int n = t.n0 + (kGated ? 0 : sl * kSlab);
+                    if constexpr (kCol) {
+                        tma_load_3d(dst + sl * kSlabBytes, m, k * kKT, n, t.expert, bar, stream);
+                    } else {
+                        tma_load_3d(dst + sl * kSlabBytes, m, n, k * kKT, t.expert, bar, stream);
+                        tma_load_3d(dst + sl * kSlabBytes + kSlabBytes / 2, m, n + 64, k * kKT, t.expert, bar, stream);
+                    }
                 }
-            }
-        };
-        // bytes of a step's token rows: groups of four gathered rows, or boxes of rows as they lie, for each term
-        auto token_bytes = [&](const Item &t) {
-            return a.gather ? (uint32_t)ceil_div(t.rows, 4) * 512u : (uint32_t)(ceil_div(t.rows, a.box_rows) * a.box_rows * a.terms) * 128u;
-        };
-        auto rows_of = [&](const Item &t, int (&ids)[4]) {     // lane i: the token rows of group i
-            if (!a.gather) return;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = 4 * lane + i;
-                ids[i] = r < t.rows ? NM_LD(a.plan.order + t.row0 + r, a.in_order, a.status) / a.plan.top_k : 0;
-            }
-        };
-        auto tokens = [&](const Item &t, const int (&ids)[4], int k, int s) {
-            const uint32_t dst = base + (uint32_t)s * a.stage_bytes + kSlabs * kSlabBytes, bar = full0 + 8 * s;
-            if (a.gather) {
-                if (4 * lane < t.rows) tma_gather4(dst + lane * 512, &map_x, k * kKT, ids, bar, keep);
-            } else {
-                const int row = (lane & 7) * a.box_rows, term = lane >> 3;
-                if (row < t.rows && term < a.terms) tma_load_3d(dst + (uint32_t)(term * a.R + row) * 128, &map_x, k * kKT, t.row0 + row, term, bar, keep);
-            }
-        };
-        // The first fills: weights before the wait, tokens behind it.
-        int head = 0;
-        if (a.early_weights) {
-            if (first_id < sched.chunks) {
-                const Chunk c = chunk_of(sched, a.kb, first_id);
-                const Item t = item_of(a, c.item);
-                head = min(NS, c.k1 - c.k0);
-                if (lane == 0)
+            };
+            // bytes of a step
+            auto step_bytes = [&](const Item &t) {
+                return kSlabs * kSlabBytes + (a.gather ? (uint32_t)ceil_div(t.rows, 4) * 512u : (uint32_t)(ceil_div(t.rows, a.box_rows) * a.box_rows * a.terms) * 128u);
+            };
+            // The first fills: weights before the wait, tokens behind it.
+            int head = 0;
+            if (a.early_weights) {
+                if (first_id < sched.chunks) {
+                    const Chunk c = chunk_of(sched, a.kb, first_id);
+                    const Item t = item_of(a, c.item);
+                    head = min(NS, c.k1 - c.k0);
                     for (int i = 0; i < head; ++i) {
-                        mbar_arrive_expect_tx(full0 + 8 * i, kSlabs * kSlabBytes + token_bytes(t));
+                        mbar_arrive_expect_tx(full0 + 8 * i, step_bytes(t));
                         weights(t, c.k0 + i, i);
                     }
-                filled = head;
-            }
-            pdl_wait_prior_grids();
-        }
-        __syncwarp();
-        int s = 0, n = 0, queue = 0;
-        uint32_t ph = 1, queue_ph = 1;                          // a fresh barrier passes a wait for the phase before its first
-        bool ok = true;
-        for (int id = first_id; ok && id < sched.chunks;) {
-            int next = sched.chunks;                            // asked for now, needed when this chunk has been copied
-            if (more_than_one && lane == 0) next = (int)gridDim.x + (int)atomicAdd(a.counters + a.ticket, 1u);
-            const Chunk c = chunk_of(sched, a.kb, id);
-            const Item t = item_of(a, c.item);
-            int ids[4] = {0, 0, 0, 0};
-            rows_of(t, ids);
-            for (int k = c.k0; k < c.k1; ++k, ++n) {
-                if (n >= head) {
-                    if (lane == 0) {
-                        ok = mbar_try_wait(empty0 + 8 * s, ph) || mbar_wait(empty0 + 8 * s, ph, &s_abort, a.status);
-                        if (ok) {
-                            mbar_arrive_expect_tx(full0 + 8 * s, kSlabs * kSlabBytes + token_bytes(t));
-                            weights(t, k, s);
-                            filled = n + 1;
-                        }
-                    }
-                    ok = __shfl_sync(0xffffffffu, ok, 0);
-                    if (!ok) break;
+                    filled = head;
                 }
-                tokens(t, ids, k, s);
-                if (++s == NS) { s = 0; ph ^= 1; }
+                pdl_wait_prior_grids();
             }
-            id = sched.chunks;
-            if (ok && more_than_one) {
-                id = __shfl_sync(0xffffffffu, next, 0);
-                if (lane == 0) {
+            int s = 0, n = 0, queue = 0;
+            uint32_t ph = 1, queue_ph = 1;                      // a fresh barrier passes a wait for the phase before its first
+            bool ok = true;
+            for (int id = first_id; ok && id < sched.chunks;) {
+                int next = sched.chunks;                        // asked for now, needed when this chunk has been copied
+                if (more_than_one) next = (int)gridDim.x + (int)atomicAdd(a.counters + a.ticket, 1u);
+                const Chunk c = chunk_of(sched, a.kb, id);
+                const Item t = item_of(a, c.item);
+                const uint32_t bytes = step_bytes(t);
+                const int boxes = ceil_div(t.rows, a.box_rows);
+                const CUtensorMap *map_x = a.gather ? &maps_x.of[0] : &maps_x.of[boxes - 1];
+                const uint32_t term_bytes = (uint32_t)((a.apart ? boxes * a.box_rows : a.R) * 128);
+                int ids[16];
+                if (a.gather) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) ids[i] = i < t.rows ? NM_LD(a.plan.order + t.row0 + i, a.in_order, a.status) : 0;
+                }
+                for (int k = c.k0; k < c.k1; ++k, ++n) {
+                    if (n >= head) {
+                        ok = mbar_try_wait(empty0 + 8 * s, ph) || mbar_wait(empty0 + 8 * s, ph, &s_abort, a.status);
+                        if (!ok) break;
+                        mbar_arrive_expect_tx(full0 + 8 * s, bytes);
+                        weights(t, k, s);
+                        filled = n + 1;
+                    }
+                    const uint32_t dst = base + (uint32_t)s * a.stage_bytes + kSlabs * kSlabBytes, bar = full0 + 8 * s;
+                    if (a.gather) {
+#pragma unroll
+                        for (int g = 0; g < 4; ++g)
+                            if (4 * g < t.rows) tma_gather4(dst + g * 512, map_x, k * kKT, ids[4 * g], ids[4 * g + 1], ids[4 * g + 2], ids[4 * g + 3], bar, keep);
+                    } else {
+                        tma_load_3d(dst, map_x, k * kKT, t.row0, 0, bar, keep);
+                        if (a.terms == 2) tma_load_3d(dst + term_bytes, map_x, k * kKT, t.row0, 1, bar, keep);
+                    }
+                    if (++s == NS) { s = 0; ph ^= 1; }
+                }
+                id = sched.chunks;
+                if (ok && more_than_one) {
+                    id = next;
                     ok = mbar_try_wait(taken0 + 8 * queue, queue_ph) || mbar_wait(taken0 + 8 * queue, queue_ph, &s_abort, a.status);
                     if (ok) { s_queue[queue] = id; mbar_arrive(queued0 + 8 * queue); }
+                    if (++queue == kQueue) { queue = 0; queue_ph ^= 1; }
                 }
-                ok = __shfl_sync(0xffffffffu, ok, 0);
-                if (++queue == kQueue) { queue = 0; queue_ph ^= 1; }
             }
-        }
-        // Every CTA has its last ticket: whoever is last to say so clears them for the next call.
-        if (more_than_one && !a.planned && lane == 0 && atomicAdd(a.counters + kDone, 1u) == gridDim.x - 1) {
-            a.counters[a.ticket] = 0u;
-            a.counters[kDone] = 0u;
+            // Every CTA has its last ticket: whoever is last to say so clears them for the next call.
+            if (more_than_one && !a.planned && atomicAdd(a.counters + kDone, 1u) == gridDim.x - 1) {
+                a.counters[a.ticket] = 0u;
+                a.counters[kDone] = 0u;
+            }
         }
     } else if (warp == 1) {
         // The whole warp walks, one elected lane issues: descriptors are then uniform values.
@@ -336,27 +337,29 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
         for (int id = first_id; id < sched.chunks;) {
             const Chunk c = chunk_of(sched, a.kb, id);
             const Item t = item_of(a, c.item);
-            const int columns = max(16, (t.rows + 15) & ~15);
-            const uint32_t idesc = a.f16 ? instr_desc_f16(kSlab, columns, !a.col, false) : instr_desc(kSlab, columns, !a.col, false);
+            const int columns = a.apart ? 2 * ceil_div(t.rows, a.box_rows) * a.box_rows : (t.rows + 15) & ~15;
+            const uint32_t idesc = a.f16 ? instr_desc_f16(kSlab, columns, !kCol, false) : instr_desc(kSlab, columns, !kCol, false);
+            const bool twice = a.terms == 2 && !a.apart;
             ok = mbar_try_wait(acc_empty0 + 8 * acc, acc_ph) || mbar_wait(acc_empty0 + 8 * acc, acc_ph, &s_abort, a.status);
             if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
-            const uint32_t d = tmem + (uint32_t)acc * kSlabs * a.R;
+            const uint32_t d = tmem + (uint32_t)acc * kSlabs * a.acc_columns;
             for (int k = c.k0; k < c.k1; ++k) {
                 ok = mbar_try_wait(full0 + 8 * s, ph) || mbar_wait(full0 + 8 * s, ph, &s_abort, a.status);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t sw = base + (uint32_t)s * a.stage_bytes, sx = sw + kSlabs * kSlabBytes;
+                // descriptors count 16 bytes: 16 k further are 32 bytes of a row of k, 2048 of rows of outputs
+                const uint64_t w0 = kCol ? smem_desc(sw, 16, 1024) : smem_desc(sw, kSlabBytes / 2, 1024), x0 = smem_desc(sx, 16, 1024);
                 if (leader) {
 #pragma unroll
                     for (int kk = 0; kk < kKT / 16; ++kk)
 #pragma unroll
                         for (int sl = 0; sl < kSlabs; ++sl) {
-                            const uint32_t swl = sw + sl * kSlabBytes;
-                            const uint64_t wd = a.col ? smem_desc(swl + kk * 32, 16, 1024) : smem_desc(swl + kk * 2048, kSlabBytes / 2, 1024);
-                            mma_ss(d + sl * a.R, wd, smem_desc(sx + kk * 32, 16, 1024), idesc, k != c.k0 || kk != 0);
-                            if (a.terms == 2) mma_ss(d + sl * a.R, wd, smem_desc(sx + a.R * 128 + kk * 32, 16, 1024), idesc, true);
+                            const uint64_t wd = w0 + kk * (kCol ? 2 : 128) + sl * (kSlabBytes >> 4);
+                            mma_ss(d + sl * a.acc_columns, wd, x0 + kk * 2, idesc, k != c.k0 || kk != 0);
+                            if (twice) mma_ss(d + sl * a.acc_columns, wd, x0 + kk * 2 + a.R * 8, idesc, true);
                         }
                     mma_commit(empty0 + 8 * s);
                 }
@@ -387,18 +390,28 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             mbar_wait(acc_full0 + 8 * acc, ph, &s_abort, a.status);   // (where it ran out the walk goes on, over values that the status disowns: the
                                                                     // barriers below are for all of the warps)
             tc_fence_after();
-            const uint32_t d = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)acc * kSlabs * a.R;
+            const uint32_t d = tmem + ((uint32_t)(quad * 32) << 16) + (uint32_t)acc * kSlabs * a.acc_columns;
+            const int second = ceil_div(t.rows, a.box_rows) * a.box_rows;     // (where the terms are apart: the other one's first column)
             float4 *mine = reinterpret_cast<float4 *>(a.partial) + (size_t)c.slot * a.R * (kSlabs * kSlab / 4);
             for (int j = 4 * turn; j < t.rows; j += step) {
                 uint32_t bits[kSlabs][4];
                 float z[kSlabs][4];
 #pragma unroll
-                for (int sl = 0; sl < kSlabs; ++sl) tmem_ld4(d + sl * a.R + j, bits[sl]);
+                for (int sl = 0; sl < kSlabs; ++sl) tmem_ld4(d + sl * a.acc_columns + j, bits[sl]);
                 tmem_wait_ld();
 #pragma unroll
                 for (int sl = 0; sl < kSlabs; ++sl)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) z[sl][i] = __uint_as_float(bits[sl][i]);
+                if (kMode == kOutDown && a.apart) {
+#pragma unroll
+                    for (int sl = 0; sl < kSlabs; ++sl) tmem_ld4(d + sl * a.acc_columns + second + j, bits[sl]);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int sl = 0; sl < kSlabs; ++sl)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) z[sl][i] += __uint_as_float(bits[sl][i]);
+                }
                 if (c.cut < 0) {
                     finish_all<kMode, kGated, kSlabs>(a, t, j, n_lane, z);
                 } else {
@@ -474,11 +487,11 @@ bool encode_map(CUtensorMap *map, const void *p, bool f16, int rank, const cuuin
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int kMode, bool kGated, int kSlabs>
-cudaError_t launch_stream(const CUtensorMap &w0, const CUtensorMap &w1, const CUtensorMap &x, const StreamArgs &a, long ctas, cudaStream_t s)
+template <int kMode, bool kGated, int kSlabs, bool kCol>
+cudaError_t launch_stream(const CUtensorMap &w0, const CUtensorMap &w1, const TokenMaps &x, const StreamArgs &a, long ctas, cudaStream_t s)
 {
     static std::atomic<unsigned long long> configured{0};
-    auto kern = stream_kernel<kMode, kGated, kSlabs>;
+    auto kern = stream_kernel<kMode, kGated, kSlabs, kCol>;
     cudaError_t e = ensure_dynamic_smem(kern, kRingBytes + 1024, configured);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
@@ -521,6 +534,7 @@ CutModel stream_cut_model(int R, int N, int K, bool gated, int terms)
     m.most_chunks = most_chunks(R, N, gated);
     m.sums_steps = (float)(R / 2) * slabs * kSlab * 8 / step_bytes;
     m.latency_steps = 2.5f / step_us;
+    m.forced = g_forced_parts.load(std::memory_order_relaxed);
     return m;
 }
 
@@ -532,19 +546,21 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     a.kb = m.kb;
     a.tile_n = gated ? kSlab : slabs * kSlab;
     a.column_tiles = m.column_tiles;
-    a.box_rows = std::min(32, p.R / 2);
+    a.box_rows = std::max(8, p.R / 4);
     a.rows = p.rows; a.N = p.N; a.R = p.R; a.terms = p.terms;
     if (!p.planned) {
         const int items = ceil_div(p.rows, p.R) * a.column_tiles, rest = items - whole_items(items);
         int best = 1;
         for (int parts = 2; parts <= std::min(a.kb, kSMs) && rest * parts <= m.most_chunks; ++parts)
-            if (cut_cost(rest, a.kb, parts, m.sums_steps, m.latency_steps) < cut_cost(rest, a.kb, best, m.sums_steps, m.latency_steps)) best = parts;
+            if (cut_cost(m, rest, parts) < cut_cost(m, rest, best)) best = parts;
         a.schedule = schedule_of(items, a.kb, best);
     }
     a.stage_bytes = slabs * kSlabBytes + p.terms * p.R * 128;
     a.nstage = std::min(kMaxStages, kRingBytes / a.stage_bytes);
-    a.tmem_columns = std::max(32, 2 * slabs * p.R);
-    a.col = p.col; a.f16 = p.f16; a.gather = p.gather; a.planned = p.planned; a.early_weights = p.early_weights; a.programmatic = p.programmatic;
+    a.apart = p.terms == 2 && p.R <= 64;
+    a.acc_columns = a.apart ? 2 * p.R : p.R;
+    a.tmem_columns = std::max(32, 2 * slabs * a.acc_columns);
+    a.f16 = p.f16; a.gather = p.gather; a.planned = p.planned; a.early_weights = p.early_weights; a.programmatic = p.programmatic;
     a.act = p.act; a.plan = p.plan;
     a.bias = static_cast<const uint16_t *>(p.bias); a.residual = static_cast<const uint16_t *>(p.residual); a.ld_residual = p.ld_residual;
     a.out = p.out; a.ldo = p.ldo; a.out_term = (long)p.rows * p.ldo; a.row_scale = p.row_scale;
@@ -559,7 +575,8 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     a.in_order = make_span(p.plan.order, 4 * (size_t)p.rows);
     a.status = device_status_ptr();
 
-    CUtensorMap w[2], x;
+    CUtensorMap w[2];
+    TokenMaps x;
     const uint16_t *W = static_cast<const uint16_t *>(p.W);
     bool ok = true;
     for (int part = 0; part < parts; ++part) {
@@ -577,27 +594,47 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     if (p.gather) {
         const cuuint64_t dims[2] = {(cuuint64_t)p.K, (cuuint64_t)p.x_rows}, strides[1] = {(cuuint64_t)p.ldx * 2};
         const cuuint32_t box[2] = {kKT, 1};
-        ok = ok && encode_map(&x, p.x, p.f16, 2, dims, strides, box);
+        ok = ok && encode_map(&x.of[0], p.x, p.f16, 2, dims, strides, box);
     } else {
         const cuuint64_t dims[3] = {(cuuint64_t)p.K, (cuuint64_t)p.x_rows, (cuuint64_t)p.terms}, strides[2] = {(cuuint64_t)p.ldx * 2, (cuuint64_t)p.x_term * 2};
-        const cuuint32_t box[3] = {kKT, (cuuint32_t)a.box_rows, 1};
-        ok = ok && encode_map(&x, p.x, p.f16, 3, dims, strides, box);
+        for (int i = 0; (i + 1) * a.box_rows <= p.R; ++i) {
+            const cuuint32_t box[3] = {kKT, (cuuint32_t)((i + 1) * a.box_rows), 1};
+            ok = ok && encode_map(&x.of[i], p.x, p.f16, 3, dims, strides, box);
+        }
     }
     if (!ok) { *what = "cuTensorMapEncodeTiled"; return cudaErrorInvalidValue; }
     if (!a.status) { *what = "device status word"; return cudaErrorInvalidValue; }
     *what = "streamed product launch";
     const long ctas = p.planned ? kSMs : std::min(kSMs, a.schedule.chunks);
     if (!gated) w[1] = w[0];
+    auto launch = [&](auto mode_, auto gated_, auto slabs_) {
+        constexpr int kM = decltype(mode_)::value, kS = decltype(slabs_)::value;
+        constexpr bool kG = decltype(gated_)::value;
+        return p.col ? launch_stream<kM, kG, kS, true>(w[0], w[1], x, a, ctas, s) : launch_stream<kM, kG, kS, false>(w[0], w[1], x, a, ctas, s);
+    };
+    auto of_mode = [&](auto mode_) {
+        if constexpr (decltype(mode_)::value != kOutDown)
+            if (gated) return launch(mode_, std::true_type{}, std::integral_constant<int, 2>{});
+        return slabs == 2 ? launch(mode_, std::false_type{}, std::integral_constant<int, 2>{}) : launch(mode_, std::false_type{}, std::integral_constant<int, 1>{});
+    };
     switch (mode) {
-    case kOutAct:
-        return gated ? launch_stream<kOutAct, true, 2>(w[0], w[1], x, a, ctas, s)
-                     : slabs == 2 ? launch_stream<kOutAct, false, 2>(w[0], w[1], x, a, ctas, s) : launch_stream<kOutAct, false, 1>(w[0], w[1], x, a, ctas, s);
-    case kOutHidden:
-        return gated ? launch_stream<kOutHidden, true, 2>(w[0], w[1], x, a, ctas, s)
-                     : slabs == 2 ? launch_stream<kOutHidden, false, 2>(w[0], w[1], x, a, ctas, s) : launch_stream<kOutHidden, false, 1>(w[0], w[1], x, a, ctas, s);
-    default:
-        return slabs == 2 ? launch_stream<kOutDown, false, 2>(w[0], w[1], x, a, ctas, s) : launch_stream<kOutDown, false, 1>(w[0], w[1], x, a, ctas, s);
+    case kOutAct: return of_mode(std::integral_constant<int, kOutAct>{});
+    case kOutHidden: return of_mode(std::integral_constant<int, kOutHidden>{});
+    default: return of_mode(std::integral_constant<int, kOutDown>{});
     }
 }
 
 }  // namespace nm
+
+extern "C" {
+#pragma GCC visibility push(default)
+
+int nm_debug_set_ffn_cut(int parts)
+{
+    if (parts < 0) return NM_ERR_INVALID_ARG;
+    nm::g_forced_parts.store(parts, std::memory_order_relaxed);
+    return NM_OK;
+}
+
+#pragma GCC visibility pop
+}  // extern "C"
