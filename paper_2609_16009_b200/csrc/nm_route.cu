@@ -5,11 +5,14 @@
 //     groups of E / G experts count as their best key (or the sum of their two best); the `keep` best groups stay
 //     the k largest keys among them, ties to the lowest index, in falling order;  weight = s [/ sum of the chosen s] * scale
 //
-// One warp a token, expert 32 i + lane in register i of a lane.  Which expert is chosen is a matter of comparisons, so scores and keys are
-// fp64: two keys that differ are told apart whatever the order their sums were taken in, and 64-bit arithmetic is a small part of what
-// bounds the kernel (latency for few tokens).  A key becomes an unsigned word that orders as
-// the key does, and a round of the selection is a maximum over a lane's own keys followed by three warp reductions of 32 bits: high half,
-// low half, index.
+// One warp a token, expert 32 i + lane in register i of a lane.  Which expert is chosen is a matter of comparisons, and what it says is decided in 64 bits:
+//   - keys in fp32 come first.  Without a bias that is the logit itself, which orders as the score does (while the score in 64 bits tells neighbouring logits
+//     apart); with one it is the score in fp32 plus the bias, off by no more than a bound that goes with it.
+//   - where two keys whose order matters (neighbours among the chosen, the last chosen and the best that is left, the last group kept and the best that is
+//     not) are nearer than that, the token is done again with fp64 keys.  Equal logits without a bias are equal keys, and no doubt.
+// A key becomes an unsigned word that orders as it does; a round of the selection is a maximum over a lane's own keys and two warp reductions (three in
+// 64 bits: high half, low half, index).  The chosen scores, and the sum of all where the weights are not renormalised, are always fp64.
+// Bound by issue: 8192 tokens over 320 experts, all in fp64, took 52 us.
 #include "nm_async.cuh"
 
 namespace nm {
@@ -36,6 +39,14 @@ template <typename T> struct Logit;
 template <> struct Logit<float> { __device__ static float get(const float *p, const RouteArgs &a) { return NM_LD(p, a.in_logits, a.status); } };
 template <> struct Logit<bf16_t> { __device__ static float get(const bf16_t *p, const RouteArgs &a) { return Elem<bf16_t>::widen(NM_LD(p, a.in_logits, a.status)); } };
 template <> struct Logit<f16_t> { __device__ static float get(const f16_t *p, const RouteArgs &a) { return Elem<f16_t>::widen(NM_LD(p, a.in_logits, a.status)); } };
+
+// A NaN logit counts as minus infinity.
+template <typename TL>
+__device__ __forceinline__ float logit_of(const TL *row, int e, const RouteArgs &a)
+{
+    const float x = Logit<TL>::get(row + e, a);
+    return x == x ? x : -INFINITY;
+}
 
 // Unsigned order of fp64 keys; a NaN counts as minus infinity, -0 as 0.  0 is below every key: what may not be chosen (any more).
 __device__ __forceinline__ unsigned long long ordered(double key)
@@ -69,73 +80,69 @@ __device__ __forceinline__ int warp_best(unsigned long long v, int index)
     return (int)__reduce_min_sync(kAll, top && (unsigned)v == lo ? (unsigned)index : kAll);
 }
 
-template <typename TL, int kPer>
-__global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs a)
+// Where the groups' best keys lie: the lanes of a group of lanes share a group of experts, `take(v)` of them merged by `merge`.
+struct GroupLanes { int each, group, sub; };                     // lanes a group (a power of two), this lane's group and place
+__device__ __forceinline__ GroupLanes group_lanes(int groups, int lane)
 {
-    extern __shared__ double s_keys[];                          // [warp][E], where there are groups
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const long t = (long)blockIdx.x * kRouteWarps + warp;
-    pdl_launch_dependents();
-    pdl_wait_prior_grids();
-    if (t >= a.T) return;
-    const TL *row = static_cast<const TL *>(a.logits) + t * a.ld;
-    auto logit = [&](int e) {
-        const float x = Logit<TL>::get(row + e, a);
-        return x == x ? x : -INFINITY;                          // a NaN logit counts as minus infinity
-    };
-    float x[kPer];
-    float m = -INFINITY;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int e = 32 * i + lane;
-        x[i] = e < a.E ? logit(e) : -INFINITY;
-        m = fmaxf(m, x[i]);
+    const int each = 1 << (31 - __clz(32 / groups));
+    return GroupLanes{each, lane / each, lane & (each - 1)};
+}
+
+// The two largest of a group's keys, over the lanes that share it.
+template <typename K>
+__device__ __forceinline__ void best_two(const K *keys, const RouteArgs &a, const GroupLanes &g, K lowest, K &first, K &second)
+{
+    first = lowest; second = lowest;
+    if (g.group < a.groups)
+        for (int j = g.sub; j < a.group_size; j += g.each) {
+            const K v = keys[g.group * a.group_size + j];
+            if (v > first) { second = first; first = v; }
+            else if (v > second) second = v;
+        }
+    for (int o = 1; o < g.each; o <<= 1) {
+        const K f = __shfl_xor_sync(kAll, first, o), s = __shfl_xor_sync(kAll, second, o);
+        second = f > first ? (first > s ? first : s) : (second > f ? second : f);
+        first = f > first ? f : first;
     }
+}
+
+// The chosen experts with fp64 keys: lane j returns the j-th.  `m` is the largest logit.
+template <typename TL, int kPer>
+__device__ __noinline__ int choose64(const RouteArgs &a, const TL *row, float m, double *mine, int lane)
+{
+    unsigned long long key[kPer];
     double sum = 1.0;
-    double s[kPer];
-    if (a.sigmoid) {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) s[i] = sigmoid64(x[i]);
-    } else {
-#pragma unroll
-        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, o));
+    if (!a.sigmoid) {
         sum = 0.0;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) { s[i] = numerator(x[i], m); sum += s[i]; }
+        for (int i = 0; i < kPer; ++i)
+            if (32 * i + lane < a.E) sum += numerator(logit_of(row, 32 * i + lane, a), m);
         sum = warp_sum(sum);
         if (sum == 0.0) sum = 1.0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) s[i] /= sum;
     }
-    unsigned long long key[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int e = 32 * i + lane;
-        if (e < a.E && a.bias) s[i] += (double)NM_LD(a.bias + e, a.in_bias, a.status);
-        key[i] = e < a.E ? ordered(s[i]) : 0ull;
-    }
-
-    if (a.groups > 1) {
-        double *mine = s_keys + (size_t)warp * a.E;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (32 * i + lane < a.E) mine[32 * i + lane] = s[i] == s[i] ? s[i] : -INFINITY;
-        __syncwarp();
-        unsigned long long of_group = 0ull;                      // lane g: group g
-        if (lane < a.groups) {
-            double first = -INFINITY, second = -INFINITY;
-            for (int j = 0; j < a.group_size; ++j) {
-                const double v = mine[lane * a.group_size + j];
-                if (v > first) { second = first; first = v; }
-                else if (v > second) second = v;
-            }
-            of_group = ordered(a.best == 2 ? first + second : first);
+        key[i] = 0ull;
+        if (e < a.E) {
+            const float x = logit_of(row, e, a);
+            double s = a.sigmoid ? sigmoid64(x) : numerator(x, m) / sum;
+            if (a.bias) s += (double)NM_LD(a.bias + e, a.in_bias, a.status);
+            key[i] = ordered(s);
+            if (a.groups > 1) mine[e] = s == s ? s : -INFINITY;
         }
+    }
+    if (a.groups > 1) {
+        __syncwarp();
+        const GroupLanes g = group_lanes(a.groups, lane);
+        double first, second;
+        best_two<double>(mine, a, g, -INFINITY, first, second);
+        unsigned long long of_group = g.group < a.groups && g.sub == 0 ? ordered(a.best == 2 ? first + second : first) : 0ull;
         unsigned kept = 0u;
         for (int j = 0; j < a.keep; ++j) {
-            const int g = warp_best(of_group, lane);
-            kept |= 1u << g;
-            if (lane == g) of_group = 0ull;
+            const int at = warp_best(of_group, lane);
+            kept |= 1u << (at / g.each);
+            if (lane == at) of_group = 0ull;
         }
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
@@ -143,10 +150,8 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs
             if (e < a.E && !(kept >> (e / a.group_size) & 1u)) key[i] = 0ull;
         }
     }
-
-    int chosen = 0;                                              // lane j: the j-th choice
+    int chosen = 0, at = 0;
     unsigned long long best = 0ull;
-    int at = 0;
     auto local_best = [&] {
         best = key[0]; at = lane;
 #pragma unroll
@@ -164,9 +169,152 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs
             local_best();
         }
     }
+    return chosen;
+}
+
+// fp32 keys as words that order as they do; 0 is below every key.
+__device__ __forceinline__ unsigned ordered32(float key)
+{
+    const unsigned b = __float_as_uint(key + 0.f);                // (-0 as 0)
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float key_of(unsigned word) { return __uint_as_float(word & 0x80000000u ? word & 0x7fffffffu : ~word); }
+
+template <typename TL, int kPer>
+__global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs a)
+{
+    extern __shared__ double s_keys[];                          // [warp][E], where there are groups
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const long t = (long)blockIdx.x * kRouteWarps + warp;
+    pdl_launch_dependents();
+    pdl_wait_prior_grids();
+    if (t >= a.T) return;
+    const TL *row = static_cast<const TL *>(a.logits) + t * a.ld;
+    float x[kPer];
+    float m = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+        const int e = 32 * i + lane;
+        x[i] = e < a.E ? logit_of(row, e, a) : -INFINITY;
+        m = fmaxf(m, x[i]);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(kAll, m, o));
+    double sum = 1.0;
+    if (!a.sigmoid && !a.renormalise) {
+        sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (32 * i + lane < a.E) sum += numerator(x[i], m);
+        sum = warp_sum(sum);
+        if (sum == 0.0) sum = 1.0;
+    }
+
+    // fp32 keys, and how far each may be from its fp64 key at most: `off` + 2^-23 |key|.
+    //   sigmoid: exp within 2 steps (2^-22 of e / (1 + e)^2 <= 1/4), sum and quotient within 2^-23 of s <= 1: below 2^-22; the bias adds half a step of the key
+    //   softmax: exp within 2 steps, the sum of up to 32 + 5 roundings, the quotient: below 2^-18 of s, which is at most the largest one, 1 / sum
+    //   the logit itself: exact, where fp64 scores tell what logits do: equal ones, and ones 2^-30 apart (s' is 3e-4 of that or more while a sigmoid's logits are
+    //   up to 8; below, scores differ in proportion) that are not within reach of an underflow, 600 below 0 or the largest; what is beyond is `dubious`
+    const bool plain = !a.bias && !(a.groups > 1 && a.best == 2);
+    float off = 0.f;
+    bool dubious = !(fabsf(m) < 1e30f);                           // infinities, the lowest values: in fp64
+    unsigned key[kPer];
+    if (plain) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) key[i] = 32 * i + lane < a.E ? ordered32(x[i]) : 0u;
+        if (a.sigmoid) dubious = dubious || m > 8.f;
+    } else {
+        float total = 1.f;
+        if (!a.sigmoid) {
+            total = 0.f;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) { x[i] = 32 * i + lane < a.E ? expf(x[i] - m) : 0.f; total += x[i]; }
+#pragma unroll
+            for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(kAll, total, o);
+        }
+        off = a.sigmoid ? 0x1p-22f : 0x1p-18f / total;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int e = 32 * i + lane;
+            float s = a.sigmoid ? 1.f / (1.f + expf(-x[i])) : x[i] / total;
+            if (a.bias && e < a.E) s += NM_LD(a.bias + e, a.in_bias, a.status);
+            if (e < a.E && !(fabsf(s) < 1e30f)) dubious = true;
+            key[i] = e < a.E ? ordered32(s) : 0u;
+            x[i] = s;
+        }
+        dubious = __any_sync(kAll, dubious);
+    }
+    const float floor = a.sigmoid ? -600.f : m - 600.f;
+    auto near = [&](float above, float below) {
+        return plain ? !(above == below || above - below > 0x1p-30f) || !(above > floor) : !(above - below > 2.f * off + 0x1p-22f * (fabsf(above) + fabsf(below)));
+    };
+
+    if (a.groups > 1) {
+        float *mine = reinterpret_cast<float *>(s_keys + (size_t)warp * a.E);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (32 * i + lane < a.E) mine[32 * i + lane] = x[i];
+        __syncwarp();
+        const GroupLanes g = group_lanes(a.groups, lane);
+        float first, second;
+        best_two<float>(mine, a, g, -INFINITY, first, second);
+        unsigned of_group = g.group < a.groups && g.sub == 0 ? ordered32(a.best == 2 ? first + second : first) : 0u;
+        unsigned kept = 0u, last = 0u;
+        for (int j = 0; j < a.keep; ++j) {
+            last = __reduce_max_sync(kAll, of_group);
+            const int at = __ffs((int)__ballot_sync(kAll, of_group == last)) - 1;
+            kept |= 1u << (at / g.each);
+            if (lane == at) of_group = 0u;
+        }
+        // the best group that is not kept; where equal keys are no doubt, the best that differs
+        const unsigned next = __reduce_max_sync(kAll, plain && of_group == last ? 0u : of_group);
+        // (a sum of two keys: twice the distance, and roundings of what was added; of every group, though two alone matter)
+        if (a.best == 2) dubious = dubious || (g.group < a.groups && !(key_of(last) - key_of(next) > 4.f * off + 0x1p-21f * (fabsf(first) + fabsf(second))));
+        else dubious = dubious || (next != 0u ? near(key_of(last), key_of(next)) : plain && !(key_of(last) > floor));
+        dubious = __any_sync(kAll, dubious);
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            const int e = 32 * i + lane;
+            if (e < a.E && !(kept >> (e / a.group_size) & 1u)) key[i] = 0u;
+        }
+    }
+
+    int chosen = 0, at = 0;                                       // lane j: the j-th choice
+    unsigned best = 0u, before = 0u;
+    auto local_best = [&] {
+        best = key[0]; at = lane;
+#pragma unroll
+        for (int i = 1; i < kPer; ++i)
+            if (key[i] > best) { best = key[i]; at = 32 * i + lane; }
+    };
+    local_best();
+    for (int j = 0; j <= a.k && !dubious; ++j) {                  // (one more round: the best that is left)
+        const unsigned top = __reduce_max_sync(kAll, best);
+        if (j == a.k) {
+            unsigned left = 0u;                                    // the same of the keys that are left
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (!plain || key[i] != before) left = max(left, key[i]);
+            left = __reduce_max_sync(kAll, left);
+            if (left != 0u ? near(key_of(before), key_of(left)) : plain && !(key_of(before) > floor)) dubious = true;
+            break;
+        }
+        if (j > 0 && near(key_of(before), key_of(top))) dubious = true;
+        before = top;
+        const int e = (int)__reduce_min_sync(kAll, best == top ? (unsigned)at : kAll);
+        if (lane == j) chosen = e;
+        if (at == e) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (32 * i + lane == e) key[i] = 0u;
+            local_best();
+        }
+    }
+    if (dubious) chosen = choose64<TL, kPer>(a, row, m, s_keys + (size_t)warp * a.E, lane);
 
     double w = 0.0;
-    if (lane < a.k) w = a.sigmoid ? sigmoid64(logit(chosen)) : numerator(logit(chosen), m) / sum;
+    if (lane < a.k) w = a.sigmoid ? sigmoid64(logit_of(row, chosen, a)) : numerator(logit_of(row, chosen, a), m) / sum;
     if (a.renormalise) {
         const double total = warp_sum(w);
         w = total > 0.0 ? w / total : 0.0;
@@ -199,6 +347,7 @@ cudaError_t launch_by_width(const RouteArgs &a, cudaStream_t s)
     if (a.E <= 64) return launch_route<TL, 2>(a, s);
     if (a.E <= 128) return launch_route<TL, 4>(a, s);
     if (a.E <= 256) return launch_route<TL, 8>(a, s);
+    if (a.E <= 384) return launch_route<TL, 12>(a, s);
     if (a.E <= 512) return launch_route<TL, 16>(a, s);
     return launch_route<TL, 32>(a, s);
 }

@@ -144,6 +144,22 @@ def test_scores_that_fp32_cannot_tell_apart():
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("score", [SOFTMAX, SIGMOID])
+@pytest.mark.parametrize("groups,keep,best", [(1, 1, 1), (8, 3, 1), (8, 3, 2), (16, 5, 2)])
+def test_keys_near_each_other(score, groups, keep, best):
+    """Logits and biases a few steps of fp32 apart, or less than fp64 scores tell apart (ties then), from far below to far above."""
+    g = torch.Generator().manual_seed(8)
+    pick = torch.randint(-3, 4, (160, 64), generator=g).float()
+    base = torch.tensor([0.0, 1e-30, 1e-8, 0.37, -5.0, 7.99, 9.0, 40.0, -40.0, -300.0, -650.0, -720.0, -745.0, 700.0, 1e5, -1e5]).repeat(10)[:, None]
+    x = base + pick * torch.where(base == 0, torch.tensor(1e-32), torch.finfo(torch.float32).eps * base.abs())
+    x[::5, ::7] = float("-inf")
+    for bias in (None, torch.zeros(64), 1e-7 * torch.randint(-2, 3, (64,), generator=g).float(), 1000 + 1e-4 * torch.randint(-2, 3, (64,), generator=g).float(),
+                 0.5 * torch.randn(64, generator=g)):
+        check(x, bias, 6, F32, score, groups, keep, best)
+        check(x + torch.randn(160, 64, generator=g), bias, 6, F32, score, groups, keep, best, renorm=False)
+
+
+@pytest.mark.gpu
 def test_equal_calls_and_programmatic_launch_give_equal_bits():
     import paper_2609_16009_b200 as nm
     x = torch.randn(77, 200, generator=torch.Generator().manual_seed(1))
