@@ -34,6 +34,16 @@ __device__ __forceinline__ void activate(int act, float (&v)[n])
 
 // A value of either 16-bit type, and rounding to it.
 __device__ __forceinline__ float widen16(uint16_t v, bool f16) { return f16 ? __half2float(__ushort_as_half(v)) : __uint_as_float((uint32_t)v << 16); }
+__device__ __forceinline__ float widen16_either(uint32_t v, bool f16)      // without a branch: both, and the one that is meant
+{
+    const float h = __half2float(__ushort_as_half((uint16_t)v)), b = __uint_as_float(v << 16);
+    return f16 ? h : b;
+}
+__device__ __forceinline__ uint16_t round16_either(float v, bool f16)
+{
+    const uint16_t h = __half_as_ushort(__float2half_rn(v)), b = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+    return f16 ? h : b;
+}
 __device__ __forceinline__ uint16_t round16(float v, bool f16) { return f16 ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 
 // Rows of the experts.  Pair p = (token p / top_k, choice p % top_k) belongs to expert experts[p] - first where that is one of the E held

@@ -101,84 +101,107 @@ __device__ __forceinline__ Item item_of(const StreamArgs &a, int item)
     return Item{0, row0, min(a.R, a.rows - row0), n0};
 }
 
-// What becomes of finished outputs: z[i] is output n of row r + i, i < count; z2 the same of the up part.
-template <int kMode, bool kGated>
-__device__ __forceinline__ void finish(const StreamArgs &a, int r, int count, int n, float (&z)[4], float (&z2)[4])
-{
-    if (n >= a.N) return;
-    if constexpr (kMode == kOutAct) {
-        // All of the residual before the first store: it may be the output itself, so no load would be moved ahead of a store.
-        float more[4];
+// What the epilogue reads beside the sums of four rows: their residual (16 bits, as it lies) or their factors.  Asked for a group of rows early, and used
+// (widened) only then; the residual is brought into L2 when a chunk begins.
+template <int kSlabs> struct Side { uint32_t of[kSlabs][4]; };
+__device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
+
+// Four rows of one output of each slab: where they lie and what there is of them.  The pointers walk with the rows.
+template <int kMode, bool kGated, int kSlabs>
+struct Rows {
+    const StreamArgs &a;
+    int n;                                       // output of the first slab; the others 128 further each
+    long out_pitch, side_pitch;                  // in bytes
+    char *out;
+    const char *side;
+    float bias[kSlabs];
+
+    __device__ __forceinline__ Rows(const StreamArgs &args, const Item &t, int j, int n_lane) : a(args), n(t.n0 + n_lane)
+    {
+        const long r = t.row0 + j;
+        const int size = kMode == kOutAct || (kMode == kOutHidden && !a.f16) ? 2 : 4;
+        out_pitch = a.ldo * size;
+        out = static_cast<char *>(a.out) + r * out_pitch + (long)n * size;
+        side_pitch = kMode == kOutAct ? a.ld_residual * 2 : 4;
+        side = kMode == kOutAct ? reinterpret_cast<const char *>(a.residual) + (a.residual ? r * side_pitch + 2l * n : 0)
+                                : reinterpret_cast<const char *>(a.row_scale) + (a.row_scale ? r * side_pitch : 0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            more[i] = a.residual && i < count ? widen16(NM_LD(a.residual + (long)(r + i) * a.ld_residual + n, a.in_residual, a.status), a.f16) : 0.f;
-        if (a.bias) {
-            const float b0 = widen16(NM_LD(a.bias + n, a.in_bias, a.status), a.f16);
-            const float b1 = kGated ? widen16(NM_LD(a.bias + a.N + n, a.in_bias, a.status), a.f16) : 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { z[i] += b0; if constexpr (kGated) z2[i] += b1; }
+        for (int sl = 0; sl < kSlabs; ++sl) {
+            const int at = kGated ? n : n + sl * kSlab;
+            bias[sl] = kMode == kOutAct && a.bias && at < a.N ? widen16(NM_LD(a.bias + (kGated && sl ? a.N : 0) + at, a.in_bias, a.status), a.f16) : 0.f;
         }
-        activate(a.act, z);
+    }
+    __device__ __forceinline__ void advance(int rows) { out += rows * out_pitch; }
+    // of rows `ahead` further; count: the rows there are
+    __device__ __forceinline__ void ask(Side<kSlabs> &s, int ahead, int count) const
+    {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i < count) {
-                float v = z[i];
-                if constexpr (kGated) v *= z2[i];
-                if (a.residual) v += more[i];
-                NM_ST(static_cast<uint16_t *>(a.out) + (long)(r + i) * a.ldo + n, round16(v, a.f16), a.in_out, a.status);
+        for (int sl = 0; sl < (kGated || kMode == kOutDown ? 1 : kSlabs); ++sl)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s.of[sl][i] = kMode == kOutDown ? 0x3f800000u : 0u;
+                if (kMode == kOutHidden || i >= count) continue;
+                const char *p = side + (ahead + i) * side_pitch + 256 * sl;
+                if (kMode == kOutAct && a.residual && n + sl * kSlab < a.N) s.of[sl][i] = NM_LD(reinterpret_cast<const uint16_t *>(p), a.in_residual, a.status);
+                if (kMode == kOutDown && a.row_scale) s.of[sl][i] = NM_LD(reinterpret_cast<const uint32_t *>(p), a.in_scale, a.status);
+            }
+    }
+    // z[sl][i]: the sum of row i for output n of slab sl.
+    template <bool kAll>
+    __device__ __forceinline__ void put(float (&z)[kSlabs][4], const Side<kSlabs> &s, int count) const
+    {
+        if constexpr (kMode != kOutDown) {
+#pragma unroll
+            for (int sl = 0; sl < kSlabs; ++sl)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[sl][i] += bias[sl];
+            activate(a.act, z[0]);
+            if constexpr (!kGated && kSlabs > 1) activate(a.act, z[1]);
+            if constexpr (kGated) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[0][i] *= z[1][i];
             }
         }
-    } else if constexpr (kMode == kOutHidden) {
-        activate(a.act, z);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i < count) {
-                float v = z[i];
-                if constexpr (kGated) v *= z2[i];
-                if (a.f16) {
-                    NM_ST(static_cast<float *>(a.out) + (long)(r + i) * a.ldo + n, v, a.in_out, a.status);
+        for (int sl = 0; sl < (kGated ? 1 : kSlabs); ++sl) {
+            if (n + sl * kSlab >= a.N) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!kAll && i >= count) continue;
+                char *p = out + i * out_pitch;
+                const float v = z[sl][i];
+                if constexpr (kMode == kOutDown) {
+                    NM_ST(reinterpret_cast<float *>(p) + sl * kSlab, v * __uint_as_float(s.of[0][i]), a.in_out, a.status);
+                } else if constexpr (kMode == kOutAct) {
+                    NM_ST(reinterpret_cast<uint16_t *>(p) + sl * kSlab, round16_either(a.residual ? v + widen16_either(s.of[sl][i], a.f16) : v, a.f16), a.in_out, a.status);
+                } else if (a.f16) {
+                    NM_ST(reinterpret_cast<float *>(p) + sl * kSlab, v, a.in_out, a.status);
                 } else {
                     // The upper half of the word and what is left of it, rounded: 2^-17 of the value.  (Cut off, not rounded, so that no finite
                     // value becomes an infinite term; an infinity or a NaN is the first term alone.)
                     const uint32_t hi = __float_as_uint(v) & 0xffff0000u;
                     const float rest = v - __uint_as_float(hi);
                     const bool finite = (hi & 0x7f800000u) != 0x7f800000u;
-                    uint16_t *h = static_cast<uint16_t *>(a.out) + (long)(r + i) * a.ldo + n;
+                    uint16_t *h = reinterpret_cast<uint16_t *>(p) + sl * kSlab;
                     NM_ST(h, (uint16_t)((hi >> 16) | (v != v ? 0x40u : 0u)), a.in_out, a.status);
                     NM_ST(h + a.out_term, finite ? __bfloat16_as_ushort(__float2bfloat16_rn(rest)) : (uint16_t)0, a.in_out, a.status);
                 }
             }
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i < count) {
-                const float s = a.row_scale ? NM_LD(a.row_scale + r + i, a.in_scale, a.status) : 1.f;
-                NM_ST(static_cast<float *>(a.out) + (long)(r + i) * a.ldo + n, z[i] * s, a.in_out, a.status);
-            }
-        }
     }
-}
-
-// The outputs of four rows from row j of the item on, of all slabs.
-template <int kMode, bool kGated, int kSlabs>
-__device__ __forceinline__ void finish_all(const StreamArgs &a, const Item &t, int j, int n_lane, float (&z)[kSlabs][4])
-{
-    const int count = min(4, t.rows - j);
-    if constexpr (kGated) {
-        finish<kMode, true>(a, t.row0 + j, count, t.n0 + n_lane, z[0], z[1]);
-    } else {
-#pragma unroll
-        for (int sl = 0; sl < kSlabs; ++sl) finish<kMode, false>(a, t.row0 + j, count, t.n0 + sl * kSlab + n_lane, z[sl], z[sl]);
+    __device__ __forceinline__ void put(float (&z)[kSlabs][4], const Side<kSlabs> &s, int count) const
+    {
+        if (count >= 4) put<true>(z, s, 4);
+        else put<false>(z, s, count);
     }
-}
+};
 
 // Sums of a chunk lie in groups of four rows, [group][slab][128 outputs][4 rows]: a thread moves 16 bytes at a time.  Adds up the `parts` chunks of an
 // item from slot `first` on for the group from row j on, in the order of k; several chunks are asked for at once.
 template <int kSlabs>
 __device__ __forceinline__ void join(const StreamArgs &a, int j, int first, int parts, int n_lane, float (&z)[kSlabs][4])
 {
-    constexpr int kAhead = kSlabs == 2 ? 4 : 6;
+    constexpr int kAhead = kSlabs == 2 ? 3 : 6;
 #pragma unroll
     for (int sl = 0; sl < kSlabs; ++sl)
 #pragma unroll
@@ -387,6 +410,16 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
         for (int id = first_id; id < sched.chunks; round ^= 1) {
             const Chunk c = chunk_of(sched, a.kb, id);
             const Item t = item_of(a, c.item);
+            Rows<kMode, kGated, kSlabs> rows(a, t, 4 * turn, n_lane);
+            if (kMode == kOutAct && a.residual) {
+                // (a lane a row: this warp's rows are four of every `step`)
+                const int r = 4 * turn + (lane >> 2) * step + (lane & 3), n_warp = t.n0 + quad * 32;
+#pragma unroll
+                for (int sl = 0; sl < (kGated ? 1 : kSlabs); ++sl)
+                    if (r < t.rows && n_warp + sl * kSlab < a.N) prefetch_l2(a.residual + (t.row0 + r) * a.ld_residual + n_warp + sl * kSlab);
+            }
+            Side<kSlabs> side;
+            rows.ask(side, 0, t.rows - 4 * turn);
             mbar_wait(acc_full0 + 8 * acc, ph, &s_abort, a.status);   // (where it ran out the walk goes on, over values that the status disowns: the
                                                                     // barriers below are for all of the warps)
             tc_fence_after();
@@ -413,7 +446,10 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                         for (int i = 0; i < 4; ++i) z[sl][i] += __uint_as_float(bits[sl][i]);
                 }
                 if (c.cut < 0) {
-                    finish_all<kMode, kGated, kSlabs>(a, t, j, n_lane, z);
+                    const Side<kSlabs> now = side;
+                    rows.ask(side, j - 4 * turn + step, t.rows - j - step);
+                    rows.put(z, now, t.rows - j);
+                    rows.advance(step);
                 } else {
 #pragma unroll
                     for (int sl = 0; sl < kSlabs; ++sl)
@@ -439,7 +475,10 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                     for (int j = 4 * turn; j < t.rows; j += step) {
                         float z[kSlabs][4];
                         join<kSlabs>(a, j, c.first_slot, sched.parts, n_lane, z);
-                        finish_all<kMode, kGated, kSlabs>(a, t, j, n_lane, z);
+                        const Side<kSlabs> now = side;
+                        rows.ask(side, j - 4 * turn + step, t.rows - j - step);
+                        rows.put(z, now, t.rows - j);
+                        rows.advance(step);
                     }
                 }
             }

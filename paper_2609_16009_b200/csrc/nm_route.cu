@@ -10,8 +10,8 @@
 //     apart); with one it is the score in fp32 plus the bias, off by no more than a bound that goes with it.
 //   - where two keys whose order matters (neighbours among the chosen, the last chosen and the best that is left, the last group kept and the best that is
 //     not) are nearer than that, the token is done again with fp64 keys.  Equal logits without a bias are equal keys, and no doubt.
-// A key becomes an unsigned word that orders as it does; a round of the selection is a maximum over a lane's own keys and two warp reductions (three in
-// 64 bits: high half, low half, index).  The chosen scores, and the sum of all where the weights are not renormalised, are always fp64.
+// A key becomes an unsigned word that orders as it does; a round of the selection is a warp reduction and a vote (in 64 bits three reductions: high half,
+// low half, index).  The chosen scores, and the sum of all where the weights are not renormalised, are always fp64.
 // Bound by issue: 8192 tokens over 320 experts, all in fp64, took 52 us.
 #include "nm_async.cuh"
 
@@ -30,6 +30,8 @@ struct RouteArgs {
     int32_t *experts;
     float *weights;
     int T, E, k, groups, group_size, keep, best, sigmoid, renormalise;
+    int group_shift;                            // lanes a group: 2^group_shift
+    unsigned group_mul;                         // e / group_size = e * group_mul >> 20, for e < 1024 (a division takes three conversions in the unit that is the bound)
     float scale;
     Span in_logits, in_bias, in_experts, in_weights;
     unsigned *status;
@@ -81,11 +83,10 @@ __device__ __forceinline__ int warp_best(unsigned long long v, int index)
 }
 
 // Where the groups' best keys lie: the lanes of a group of lanes share a group of experts, `take(v)` of them merged by `merge`.
-struct GroupLanes { int each, group, sub; };                     // lanes a group (a power of two), this lane's group and place
-__device__ __forceinline__ GroupLanes group_lanes(int groups, int lane)
+struct GroupLanes { int shift, each, group, sub; };              // lanes a group (a power of two), this lane's group and place
+__device__ __forceinline__ GroupLanes group_lanes(const RouteArgs &a, int lane)
 {
-    const int each = 1 << (31 - __clz(32 / groups));
-    return GroupLanes{each, lane / each, lane & (each - 1)};
+    return GroupLanes{a.group_shift, 1 << a.group_shift, lane >> a.group_shift, lane & ((1 << a.group_shift) - 1)};
 }
 
 // The two largest of a group's keys, over the lanes that share it.
@@ -94,6 +95,7 @@ __device__ __forceinline__ void best_two(const K *keys, const RouteArgs &a, cons
 {
     first = lowest; second = lowest;
     if (g.group < a.groups)
+#pragma unroll 4
         for (int j = g.sub; j < a.group_size; j += g.each) {
             const K v = keys[g.group * a.group_size + j];
             if (v > first) { second = first; first = v; }
@@ -134,20 +136,20 @@ __device__ __noinline__ int choose64(const RouteArgs &a, const TL *row, float m,
     }
     if (a.groups > 1) {
         __syncwarp();
-        const GroupLanes g = group_lanes(a.groups, lane);
+        const GroupLanes g = group_lanes(a, lane);
         double first, second;
         best_two<double>(mine, a, g, -INFINITY, first, second);
         unsigned long long of_group = g.group < a.groups && g.sub == 0 ? ordered(a.best == 2 ? first + second : first) : 0ull;
         unsigned kept = 0u;
         for (int j = 0; j < a.keep; ++j) {
             const int at = warp_best(of_group, lane);
-            kept |= 1u << (at / g.each);
+            kept |= 1u << (at >> g.shift);
             if (lane == at) of_group = 0ull;
         }
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int e = 32 * i + lane;
-            if (e < a.E && !(kept >> (e / a.group_size) & 1u)) key[i] = 0ull;
+            if (e < a.E && !(kept >> ((unsigned)e * a.group_mul >> 20) & 1u)) key[i] = 0ull;
         }
     }
     int chosen = 0, at = 0;
@@ -184,18 +186,20 @@ template <typename TL, int kPer>
 __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs a)
 {
     extern __shared__ double s_keys[];                          // [warp][E], where there are groups
+    __shared__ unsigned s_cand[kRouteWarps][64];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const long t = (long)blockIdx.x * kRouteWarps + warp;
     pdl_launch_dependents();
     pdl_wait_prior_grids();
     if (t >= a.T) return;
     const TL *row = static_cast<const TL *>(a.logits) + t * a.ld;
-    float x[kPer];
+    float x[kPer], bias[kPer];
     float m = -INFINITY;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         const int e = 32 * i + lane;
         x[i] = e < a.E ? logit_of(row, e, a) : -INFINITY;
+        bias[i] = a.bias && e < a.E ? NM_LD(a.bias + e, a.in_bias, a.status) : 0.f;
         m = fmaxf(m, x[i]);
     }
 #pragma unroll
@@ -211,8 +215,10 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs
     }
 
     // fp32 keys, and how far each may be from its fp64 key at most: `off` + 2^-23 |key|.
-    //   sigmoid: exp within 2 steps (2^-22 of e / (1 + e)^2 <= 1/4), sum and quotient within 2^-23 of s <= 1: below 2^-22; the bias adds half a step of the key
-    //   softmax: exp within 2 steps, the sum of up to 32 + 5 roundings, the quotient: below 2^-18 of s, which is at most the largest one, 1 / sum
+    //   sigmoid: exp within 2 + 1.2 |x| steps of itself (s' = s (1 - s) of that: below 2^-23), sum 2^-24 and quotient 2^-22 of s <= 1: below 2^-21; the bias adds
+    //   half a step of the key
+    //   softmax: exp(x - m) within 3 + 1.2 |x - m| steps (times exp(x - m): below 2^-21), a sum of up to 32 + 5 roundings, reciprocal and product: below 2^-18 of the
+    //   largest score, 1 / sum
     //   the logit itself: exact, where fp64 scores tell what logits do: equal ones, and ones 2^-30 apart (s' is 3e-4 of that or more while a sigmoid's logits are
     //   up to 8; below, scores differ in proportion) that are not within reach of an underflow, 600 below 0 or the largest; what is beyond is `dubious`
     const bool plain = !a.bias && !(a.groups > 1 && a.best == 2);
@@ -228,16 +234,17 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs
         if (!a.sigmoid) {
             total = 0.f;
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) { x[i] = 32 * i + lane < a.E ? expf(x[i] - m) : 0.f; total += x[i]; }
+            for (int i = 0; i < kPer; ++i) { x[i] = 32 * i + lane < a.E ? __expf(x[i] - m) : 0.f; total += x[i]; }
 #pragma unroll
             for (int o = 16; o; o >>= 1) total += __shfl_xor_sync(kAll, total, o);
         }
-        off = a.sigmoid ? 0x1p-22f : 0x1p-18f / total;
+        const float share = 1.f / total;
+        off = a.sigmoid ? 0x1p-21f : 0x1p-18f * share;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int e = 32 * i + lane;
-            float s = a.sigmoid ? 1.f / (1.f + expf(-x[i])) : x[i] / total;
-            if (a.bias && e < a.E) s += NM_LD(a.bias + e, a.in_bias, a.status);
+            float s = a.sigmoid ? __fdividef(1.f, 1.f + __expf(-x[i])) : x[i] * share;
+            s += bias[i];
             if (e < a.E && !(fabsf(s) < 1e30f)) dubious = true;
             key[i] = e < a.E ? ordered32(s) : 0u;
             x[i] = s;
@@ -255,7 +262,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs
         for (int i = 0; i < kPer; ++i)
             if (32 * i + lane < a.E) mine[32 * i + lane] = x[i];
         __syncwarp();
-        const GroupLanes g = group_lanes(a.groups, lane);
+        const GroupLanes g = group_lanes(a, lane);
         float first, second;
         best_two<float>(mine, a, g, -INFINITY, first, second);
         unsigned of_group = g.group < a.groups && g.sub == 0 ? ordered32(a.best == 2 ? first + second : first) : 0u;
@@ -263,7 +270,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs
         for (int j = 0; j < a.keep; ++j) {
             last = __reduce_max_sync(kAll, of_group);
             const int at = __ffs((int)__ballot_sync(kAll, of_group == last)) - 1;
-            kept |= 1u << (at / g.each);
+            kept |= 1u << (at >> g.shift);
             if (lane == at) of_group = 0u;
         }
         // the best group that is not kept; where equal keys are no doubt, the best that differs
@@ -276,39 +283,54 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteArgs
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             const int e = 32 * i + lane;
-            if (e < a.E && !(kept >> (e / a.group_size) & 1u)) key[i] = 0u;
+            if (e < a.E && !(kept >> ((unsigned)e * a.group_mul >> 20) & 1u)) key[i] = 0u;
         }
     }
 
-    int chosen = 0, at = 0;                                       // lane j: the j-th choice
-    unsigned best = 0u, before = 0u;
-    auto local_best = [&] {
-        best = key[0]; at = lane;
+    // The k-th largest of the lanes' own largest keys bounds the k-th largest of all from below: what is not below it, rarely more than 2 k keys, goes to a lane
+    // each, in the order of experts.  A round then is a maximum and a vote, and the first of equals is the lowest lane.
+    int chosen = 0;                                               // lane j: the j-th choice
+    if (!dubious) {
+        unsigned v = key[0];
 #pragma unroll
-        for (int i = 1; i < kPer; ++i)
-            if (key[i] > best) { best = key[i]; at = 32 * i + lane; }
-    };
-    local_best();
-    for (int j = 0; j <= a.k && !dubious; ++j) {                  // (one more round: the best that is left)
-        const unsigned top = __reduce_max_sync(kAll, best);
-        if (j == a.k) {
-            unsigned left = 0u;                                    // the same of the keys that are left
-#pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (!plain || key[i] != before) left = max(left, key[i]);
-            left = __reduce_max_sync(kAll, left);
-            if (left != 0u ? near(key_of(before), key_of(left)) : plain && !(key_of(before) > floor)) dubious = true;
-            break;
+        for (int i = 1; i < kPer; ++i) v = max(v, key[i]);
+        unsigned least = 0u;
+        for (int j = 0; j < a.k; ++j) {
+            least = __reduce_max_sync(kAll, v);
+            if (lane == __ffs((int)__ballot_sync(kAll, v == least)) - 1) v = 0u;
         }
-        if (j > 0 && near(key_of(before), key_of(top))) dubious = true;
-        before = top;
-        const int e = (int)__reduce_min_sync(kAll, best == top ? (unsigned)at : kAll);
-        if (lane == j) chosen = e;
-        if (at == e) {
+        least = max(least, 1u);
+        unsigned *cand = s_cand[warp];
+        int count = 0;
+        unsigned under = 0u;                                      // the best key that is no candidate
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (32 * i + lane == e) key[i] = 0u;
-            local_best();
+        for (int i = 0; i < kPer; ++i) {
+            const bool is = key[i] >= least;
+            const unsigned votes = __ballot_sync(kAll, is);
+            const int at = count + __popc(votes & ((1u << lane) - 1u));
+            if (is && at < 32) { cand[at] = key[i]; cand[32 + at] = 32u * i + lane; }
+            if (!is) under = max(under, key[i]);
+            count += __popc(votes);
+        }
+        __syncwarp();
+        if (count > 32) {
+            dubious = true;                                       // (many equal keys)
+        } else {
+            v = lane < count ? cand[lane] : 0u;
+            const int e = lane < count ? (int)cand[32 + lane] : 0;
+            unsigned mine = 0u;
+            for (int j = 0; j < a.k; ++j) {
+                const unsigned top = __reduce_max_sync(kAll, v);
+                const int from = __ffs((int)__ballot_sync(kAll, v == top)) - 1, who = __shfl_sync(kAll, e, from);
+                if (lane == j) { chosen = who; mine = top; }
+                if (lane == from) v = 0u;
+            }
+            // neighbours among the chosen; the last one and the best that is left (where equal keys are no doubt, the best that differs)
+            const unsigned last = __shfl_sync(kAll, mine, a.k - 1), left = __reduce_max_sync(kAll, max(under, plain && v == last ? 0u : v));
+            const unsigned below = __shfl_down_sync(kAll, mine, 1);
+            if (lane < a.k - 1) dubious = near(key_of(mine), key_of(below));
+            if (lane == a.k - 1) dubious = left != 0u ? near(key_of(last), key_of(left)) : plain && !(key_of(last) > floor);
+            dubious = __any_sync(kAll, dubious);
         }
     }
     if (dubious) chosen = choose64<TL, kPer>(a, row, m, s_keys + (size_t)warp * a.E, lane);
@@ -347,6 +369,7 @@ cudaError_t launch_by_width(const RouteArgs &a, cudaStream_t s)
     if (a.E <= 64) return launch_route<TL, 2>(a, s);
     if (a.E <= 128) return launch_route<TL, 4>(a, s);
     if (a.E <= 256) return launch_route<TL, 8>(a, s);
+    if (a.E <= 320) return launch_route<TL, 10>(a, s);
     if (a.E <= 384) return launch_route<TL, 12>(a, s);
     if (a.E <= 512) return launch_route<TL, 16>(a, s);
     return launch_route<TL, 32>(a, s);
@@ -375,6 +398,8 @@ int nm_moe_route(const void *logits, long ld_logits, const float *bias, int32_t 
     RouteArgs a{};
     a.logits = logits; a.ld = ld_logits; a.bias = bias; a.experts = experts; a.weights = weights;
     a.T = T; a.E = E; a.k = top_k; a.groups = keep_groups == groups ? 1 : groups; a.group_size = E / groups; a.keep = keep_groups; a.best = group_best;
+    a.group_mul = ((1u << 20) + a.group_size - 1) / a.group_size;
+    for (a.group_shift = 0; a.groups << (a.group_shift + 1) <= 32; ++a.group_shift) {}
     a.sigmoid = score == NM_SCORE_SIGMOID; a.renormalise = renormalise != 0; a.scale = scale;
     a.in_logits = make_span(logits, size * ((size_t)(T - 1) * ld_logits + E));
     a.in_bias = make_span(bias, bias ? 4 * (size_t)E : 0);
