@@ -465,8 +465,9 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
         pl.R = stream_tile_rows((double)pairs / E, (int)std::min<long>(pairs, 128));
         pl.tiles = reinterpret_cast<RowTile *>(ws + lay.tiles); pl.n_rows = reinterpret_cast<int *>(ws + lay.n_rows);
         pl.schedules = reinterpret_cast<Schedule *>(ws + lay.schedules);
-        pl.model[0] = stream_cut_model(pl.R, inter, d, gated != 0, 1);
-        pl.model[1] = stream_cut_model(pl.R, d, inter, false, 2);
+        const float rows = (float)std::min<double>(pl.R, std::max(1.0, (double)pairs / E));
+        pl.model[0] = stream_cut_model(pl.R, rows, inter, d, gated != 0, 1);
+        pl.model[1] = stream_cut_model(pl.R, rows, d, inter, false, 2);
         pl.order = reinterpret_cast<int *>(ws + lay.order); pl.place = reinterpret_cast<int *>(ws + lay.place);
         pl.counters = reinterpret_cast<unsigned *>(ws);
         pl.in_experts = in_experts; pl.in_tiles = make_span(pl.tiles, sizeof(RowTile) * (E + (size_t)pairs / pl.R));

@@ -34,16 +34,6 @@ __device__ __forceinline__ void activate(int act, float (&v)[n])
 
 // A value of either 16-bit type, and rounding to it.
 __device__ __forceinline__ float widen16(uint16_t v, bool f16) { return f16 ? __half2float(__ushort_as_half(v)) : __uint_as_float((uint32_t)v << 16); }
-__device__ __forceinline__ float widen16_either(uint32_t v, bool f16)      // without a branch: both, and the one that is meant
-{
-    const float h = __half2float(__ushort_as_half((uint16_t)v)), b = __uint_as_float(v << 16);
-    return f16 ? h : b;
-}
-__device__ __forceinline__ uint16_t round16_either(float v, bool f16)
-{
-    const uint16_t h = __half_as_ushort(__float2half_rn(v)), b = __bfloat16_as_ushort(__float2bfloat16_rn(v));
-    return f16 ? h : b;
-}
 __device__ __forceinline__ uint16_t round16(float v, bool f16) { return f16 ? __half_as_ushort(__float2half_rn(v)) : __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 
 // Rows of the experts.  Pair p = (token p / top_k, choice p % top_k) belongs to expert experts[p] - first where that is one of the E held
@@ -65,17 +55,17 @@ struct RowPlan {
 // are of an item that is cut.
 constexpr int kTicketUp = 0, kTicketDown = 1, kDone = 2, kItemCounters = 32, kMaxCut = 2 * kSMs, kCounterWords = kItemCounters + kMaxCut;
 
-// The cut with the least modelled time.  In steps of one CTA working alone (~70 GB/s of weights): with all CTAs working a step takes kBusy times as
-// long (HBM, measured 6.5 TB/s, against 148 * 70 GB/s); a chunk's sums go to the workspace and back; and joining costs `latency` steps once.
+// The cut with the least modelled time: rounds in which all CTAs work take a step in busy_us (HBM: 148 x 32 KB at 6.9 TB/s, 0.70 us), the last one with what is
+// left alone_us at least (a CTA takes in 96 GB/s, measured; 0.25 us a step of 16 KB); at the end a chunk's sums go to the workspace and all of an item's come back to
+// one CTA, sums_us each (35 GB/s, measured), behind 3.5 us for a fence, a counter and the first of them.
 // All items but the last one to two rounds stay whole: sums in the workspace cost as much as the rows do, and only the end has to be even.
-constexpr float kBusy = 1.6f;
-struct CutModel { int kb, column_tiles, most_chunks, forced; float sums_steps, latency_steps; };
+struct CutModel { int kb, column_tiles, most_chunks, forced; float alone_us, busy_us, sums_us; };
 __host__ __device__ inline float cut_cost(const CutModel &m, int rest, int parts)
 {
     if (m.forced) return parts <= m.forced ? (float)(m.forced - parts) : 1e9f;        // the nearest that may be
-    const int kc = (m.kb + parts - 1) / parts, p = (m.kb + kc - 1) / kc, rounds = (rest * p + kSMs - 1) / kSMs;
-    const float hbm = (float)rest * m.kb * kBusy / kSMs, sm = (float)rounds * kc, each = p > 1 ? m.sums_steps * rounds + m.latency_steps : 0.f;
-    return (hbm > sm ? hbm : sm) + each;
+    const int kc = (m.kb + parts - 1) / parts, p = (m.kb + kc - 1) / kc, chunks = rest * p, rounds = chunks / kSMs, left = chunks - rounds * kSMs;
+    const float last = m.busy_us * left / kSMs, step = left ? (last > m.alone_us ? last : m.alone_us) : 0.f;
+    return kc * (rounds * m.busy_us + step) + (p > 1 ? 3.5f + (1 + p) * m.sums_us : 0.f);
 }
 __host__ __device__ inline int whole_items(int items) { return items >= 2 * kSMs ? (items / kSMs - 1) * kSMs : 0; }
 __host__ __device__ inline Schedule schedule_of(int items, int kb, int parts)
@@ -112,7 +102,7 @@ struct ProductArgs {
 int stream_tile_rows(double average, int most);
 int stream_slabs(int N, bool gated);
 size_t stream_partial_bytes(int R, int N, bool gated);
-CutModel stream_cut_model(int R, int N, int K, bool gated, int terms);
+CutModel stream_cut_model(int R, float rows, int N, int K, bool gated, int terms);
 cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStream_t s, const char **what);
 
 }  // namespace nm

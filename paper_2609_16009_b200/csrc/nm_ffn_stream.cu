@@ -10,7 +10,7 @@
 //   chunk  an item, or for the last round or two one of `parts` runs of its steps; the cuts are a rule on sizes (schedule_of), the CTAs take chunks as they
 //          get done: with equal shares the fastest SMs were done after 652 us where the slowest took 870.  A chunk's fp32 sums wait in the workspace for
 //          the last of its item (a counter; nobody waits), which adds them in the order of k.  So results do not depend on who took what or came last.
-//   warps  0: copies, and the next chunk; 1: MMAs; from 2: the epilogue, from the other one of two accumulators.  Four to sixteen warps by the rows of a
+//   warps  0: copies, and the next chunk; 1: MMAs; from 2: the epilogue, from the other one of two accumulators.  Four to twelve warps by the rows of a
 //          tile: what an output costs is latency (tensor memory, exp, residual; 128 rows of 1536 x 24576 took 96 us with four warps, 48 with sixteen),
 //          and a launch of more warps costs a short call 1.5 us
 //
@@ -32,7 +32,7 @@ namespace nm {
 
 namespace {
 
-constexpr int kMaxThreads = 64 + 32 * 16;
+constexpr int kMaxThreads = 64 + 32 * 8;
 constexpr int kQueue = 4;                       // chunks that the copies may be ahead of the epilogue
 constexpr int kKT = 64;                        // k of a stage
 constexpr int kSlab = 128;                     // outputs of a slab (the MMA's M)
@@ -49,7 +49,7 @@ struct StreamArgs {
     int acc_columns;                            // of a slab: R, twice that where the terms have columns of their own
     bool apart;
     unsigned tmem_columns;
-    bool f16, gather, planned, early_weights, programmatic;
+    bool gather, planned, early_weights, programmatic;
     int act;
     RowPlan plan;
     const uint16_t *bias, *residual; long ld_residual;
@@ -106,55 +106,91 @@ __device__ __forceinline__ Item item_of(const StreamArgs &a, int item)
 template <int kSlabs> struct Side { uint32_t of[kSlabs][4]; };
 __device__ __forceinline__ void prefetch_l2(const void *p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
-// Four rows of one output of each slab: where they lie and what there is of them.  The pointers walk with the rows.
-template <int kMode, bool kGated, int kSlabs>
+// Four rows of one output of each slab: where they lie and what there is of them.  The pointers walk with the rows.  (Instructions are what the epilogue
+// costs: 128 rows of 1536 x 24576 took 10 us of 30 at forty an output.)
+template <int kMode, bool kGated, int kSlabs, bool kF16>
 struct Rows {
+    static constexpr bool kWide = kMode == kOutDown || (kMode == kOutHidden && kF16);          // fp32 outputs
+    static constexpr int kOutSlabs = kGated ? 1 : kSlabs;
     const StreamArgs &a;
     int n;                                       // output of the first slab; the others 128 further each
-    long out_pitch, side_pitch;                  // in bytes
-    char *out;
+    long out_step, side_pitch;                   // bytes
+    char *out[4];
     const char *side;
     float bias[kSlabs];
 
-    __device__ __forceinline__ Rows(const StreamArgs &args, const Item &t, int j, int n_lane) : a(args), n(t.n0 + n_lane)
+    __device__ __forceinline__ Rows(const StreamArgs &args, const Item &t, int j, int step, int n_lane) : a(args), n(t.n0 + n_lane)
     {
-        const long r = t.row0 + j;
-        const int size = kMode == kOutAct || (kMode == kOutHidden && !a.f16) ? 2 : 4;
-        out_pitch = a.ldo * size;
-        out = static_cast<char *>(a.out) + r * out_pitch + (long)n * size;
+        const long r = t.row0 + j, pitch = a.ldo * (kWide ? 4 : 2);
+        out_step = step * pitch;
+        out[0] = static_cast<char *>(a.out) + r * pitch + (long)n * (kWide ? 4 : 2);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) out[i] = out[i - 1] + pitch;
         side_pitch = kMode == kOutAct ? a.ld_residual * 2 : 4;
         side = kMode == kOutAct ? reinterpret_cast<const char *>(a.residual) + (a.residual ? r * side_pitch + 2l * n : 0)
                                 : reinterpret_cast<const char *>(a.row_scale) + (a.row_scale ? r * side_pitch : 0);
 #pragma unroll
         for (int sl = 0; sl < kSlabs; ++sl) {
             const int at = kGated ? n : n + sl * kSlab;
-            bias[sl] = kMode == kOutAct && a.bias && at < a.N ? widen16(NM_LD(a.bias + (kGated && sl ? a.N : 0) + at, a.in_bias, a.status), a.f16) : 0.f;
+            bias[sl] = kMode == kOutAct && a.bias && at < a.N ? widen16(NM_LD(a.bias + (kGated && sl ? a.N : 0) + at, a.in_bias, a.status), kF16) : 0.f;
         }
     }
-    __device__ __forceinline__ void advance(int rows) { out += rows * out_pitch; }
     // of rows `ahead` further; count: the rows there are
     __device__ __forceinline__ void ask(Side<kSlabs> &s, int ahead, int count) const
     {
+        constexpr int kSideSlabs = kMode == kOutDown ? 1 : kMode == kOutHidden ? 0 : kOutSlabs;
+        if (kMode == kOutAct ? !a.residual : !a.row_scale) return;
 #pragma unroll
-        for (int sl = 0; sl < (kGated || kMode == kOutDown ? 1 : kSlabs); ++sl)
+        for (int sl = 0; sl < kSideSlabs; ++sl)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                s.of[sl][i] = kMode == kOutDown ? 0x3f800000u : 0u;
-                if (kMode == kOutHidden || i >= count) continue;
                 const char *p = side + (ahead + i) * side_pitch + 256 * sl;
-                if (kMode == kOutAct && a.residual && n + sl * kSlab < a.N) s.of[sl][i] = NM_LD(reinterpret_cast<const uint16_t *>(p), a.in_residual, a.status);
-                if (kMode == kOutDown && a.row_scale) s.of[sl][i] = NM_LD(reinterpret_cast<const uint32_t *>(p), a.in_scale, a.status);
+                s.of[sl][i] = 0u;
+                if (i >= count) continue;
+                if (kMode == kOutAct && n + sl * kSlab < a.N) s.of[sl][i] = NM_LD(reinterpret_cast<const uint16_t *>(p), a.in_residual, a.status);
+                if (kMode == kOutDown) s.of[sl][i] = NM_LD(reinterpret_cast<const uint32_t *>(p), a.in_scale, a.status);
             }
     }
-    // z[sl][i]: the sum of row i for output n of slab sl.
-    template <bool kAll>
-    __device__ __forceinline__ void put(float (&z)[kSlabs][4], const Side<kSlabs> &s, int count) const
+    // z[sl][i]: the sum of row i for output n of slab sl.  kSide: residual or factors are there; kAll: four rows are.
+    template <bool kSide, bool kAll>
+    __device__ __forceinline__ void store(float (&z)[kSlabs][4], const Side<kSlabs> &s, int count) const
+    {
+#pragma unroll
+        for (int sl = 0; sl < kOutSlabs; ++sl) {
+            if (n + sl * kSlab >= a.N) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!kAll && i >= count) continue;
+                float v = z[sl][i];
+                if constexpr (kMode == kOutDown) {
+                    if (kSide) v *= __uint_as_float(s.of[0][i]);
+                    NM_ST(reinterpret_cast<float *>(out[i]) + sl * kSlab, v, a.in_out, a.status);
+                } else if constexpr (kMode == kOutAct) {
+                    if (kSide) v += widen16((uint16_t)s.of[sl][i], kF16);
+                    NM_ST(reinterpret_cast<uint16_t *>(out[i]) + sl * kSlab, round16(v, kF16), a.in_out, a.status);
+                } else if constexpr (kF16) {
+                    NM_ST(reinterpret_cast<float *>(out[i]) + sl * kSlab, v, a.in_out, a.status);
+                } else {
+                    // The upper half of the word and what is left of it, rounded: 2^-17 of the value.  (Cut off, not rounded, so that no finite
+                    // value becomes an infinite term; an infinity or a NaN is the first term alone.)
+                    const uint32_t hi = __float_as_uint(v) & 0xffff0000u;
+                    const float rest = v - __uint_as_float(hi);
+                    const bool finite = (hi & 0x7f800000u) != 0x7f800000u;
+                    uint16_t *h = reinterpret_cast<uint16_t *>(out[i]) + sl * kSlab;
+                    NM_ST(h, (uint16_t)((hi >> 16) | (v != v ? 0x40u : 0u)), a.in_out, a.status);
+                    NM_ST(h + a.out_term, finite ? __bfloat16_as_ushort(__float2bfloat16_rn(rest)) : (uint16_t)0, a.in_out, a.status);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void put(float (&z)[kSlabs][4], const Side<kSlabs> &s, int count)
     {
         if constexpr (kMode != kOutDown) {
+            if (kMode == kOutAct && a.bias)
 #pragma unroll
-            for (int sl = 0; sl < kSlabs; ++sl)
+                for (int sl = 0; sl < kSlabs; ++sl)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) z[sl][i] += bias[sl];
+                    for (int i = 0; i < 4; ++i) z[sl][i] += bias[sl];
             activate(a.act, z[0]);
             if constexpr (!kGated && kSlabs > 1) activate(a.act, z[1]);
             if constexpr (kGated) {
@@ -162,73 +198,72 @@ struct Rows {
                 for (int i = 0; i < 4; ++i) z[0][i] *= z[1][i];
             }
         }
+        const bool with = kMode != kOutHidden && (kMode == kOutAct ? a.residual != nullptr : a.row_scale != nullptr);
+        if (count < 4) { if (with) store<true, false>(z, s, count); else store<false, false>(z, s, count); }
+        else if (with) store<true, true>(z, s, 4);
+        else store<false, true>(z, s, 4);
 #pragma unroll
-        for (int sl = 0; sl < (kGated ? 1 : kSlabs); ++sl) {
-            if (n + sl * kSlab >= a.N) continue;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (!kAll && i >= count) continue;
-                char *p = out + i * out_pitch;
-                const float v = z[sl][i];
-                if constexpr (kMode == kOutDown) {
-                    NM_ST(reinterpret_cast<float *>(p) + sl * kSlab, v * __uint_as_float(s.of[0][i]), a.in_out, a.status);
-                } else if constexpr (kMode == kOutAct) {
-                    NM_ST(reinterpret_cast<uint16_t *>(p) + sl * kSlab, round16_either(a.residual ? v + widen16_either(s.of[sl][i], a.f16) : v, a.f16), a.in_out, a.status);
-                } else if (a.f16) {
-                    NM_ST(reinterpret_cast<float *>(p) + sl * kSlab, v, a.in_out, a.status);
-                } else {
-                    // The upper half of the word and what is left of it, rounded: 2^-17 of the value.  (Cut off, not rounded, so that no finite
-                    // value becomes an infinite term; an infinity or a NaN is the first term alone.)
-                    const uint32_t hi = __float_as_uint(v) & 0xffff0000u;
-                    const float rest = v - __uint_as_float(hi);
-                    const bool finite = (hi & 0x7f800000u) != 0x7f800000u;
-                    uint16_t *h = reinterpret_cast<uint16_t *>(p) + sl * kSlab;
-                    NM_ST(h, (uint16_t)((hi >> 16) | (v != v ? 0x40u : 0u)), a.in_out, a.status);
-                    NM_ST(h + a.out_term, finite ? __bfloat16_as_ushort(__float2bfloat16_rn(rest)) : (uint16_t)0, a.in_out, a.status);
-                }
-            }
-        }
-    }
-    __device__ __forceinline__ void put(float (&z)[kSlabs][4], const Side<kSlabs> &s, int count) const
-    {
-        if (count >= 4) put<true>(z, s, 4);
-        else put<false>(z, s, count);
+        for (int i = 0; i < 4; ++i) out[i] += out_step;
     }
 };
 
-// Sums of a chunk lie in groups of four rows, [group][slab][128 outputs][4 rows]: a thread moves 16 bytes at a time.  Adds up the `parts` chunks of an
-// item from slot `first` on for the group from row j on, in the order of k; several chunks are asked for at once.
-template <int kSlabs>
-__device__ __forceinline__ void join(const StreamArgs &a, int j, int first, int parts, int n_lane, float (&z)[kSlabs][4])
+// How an item's token rows are copied: gathered (their tokens), or one box for each term; and the bytes of a step, weights and all.
+struct TokenCopy { int ids[16], boxes; uint32_t term_bytes, step_bytes; };
+__device__ __forceinline__ TokenCopy token_copy(const StreamArgs &a, const Item &t, int slabs)
 {
-    constexpr int kAhead = kSlabs == 2 ? 3 : 6;
+    TokenCopy x;
+    x.boxes = ceil_div(t.rows, a.box_rows);
+    x.term_bytes = (uint32_t)((a.apart ? x.boxes * a.box_rows : a.R) * 128);
+    x.step_bytes = (uint32_t)slabs * kSlabBytes + (a.gather ? (uint32_t)ceil_div(t.rows, 4) * 512u : (uint32_t)(x.boxes * a.box_rows * a.terms) * 128u);
+    if (a.gather) {
 #pragma unroll
-    for (int sl = 0; sl < kSlabs; ++sl)
+        for (int i = 0; i < 16; ++i) x.ids[i] = i < t.rows ? NM_LD(a.plan.order + t.row0 + i, a.in_order, a.status) : 0;
+    }
+    return x;
+}
+
+// Sums of a chunk lie in groups of four rows, [group][slab][128 outputs][4 rows]: a thread moves 16 bytes at a time.  Adds up the `parts` chunks of an
+// item from slot `first` on for the groups from rows j, j + step .. on, in the order of k; several chunks are asked for at once.
+template <int kSlabs, int kGroups>
+__device__ __forceinline__ void join(const StreamArgs &a, int j, int step, int first, int parts, int n_lane, float (&z)[kGroups][kSlabs][4])
+{
+    constexpr int kAhead = 8 / (kSlabs * kGroups);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) z[sl][i] = 0.f;
+    for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+        for (int sl = 0; sl < kSlabs; ++sl)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[g][sl][i] = 0.f;
     const size_t piece = (size_t)a.R * (kSlabs * kSlab) / 4;
     const float4 *from = reinterpret_cast<const float4 *>(a.partial) + first * piece + (size_t)(j / 4) * (kSlabs * kSlab) + n_lane;
+    const int further = step / 4 * (kSlabs * kSlab);
     for (int p0 = 0; p0 < parts; p0 += kAhead) {
-        float4 v[kAhead][kSlabs];
+        float4 v[kAhead][kGroups][kSlabs];
 #pragma unroll
         for (int q = 0; q < kAhead; ++q)
             if (p0 + q < parts)
 #pragma unroll
-                for (int sl = 0; sl < kSlabs; ++sl) {
-                    const float4 *at = from + (p0 + q) * piece + sl * kSlab;
-                    v[q][sl] = NM_INSIDE(at, 16, a.in_partial, a.status) ? __ldcg(at) : make_float4(0.f, 0.f, 0.f, 0.f);
-                }
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int sl = 0; sl < kSlabs; ++sl) {
+                        const float4 *at = from + (p0 + q) * piece + g * further + sl * kSlab;
+                        v[q][g][sl] = NM_INSIDE(at, 16, a.in_partial, a.status) ? __ldcg(at) : make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
 #pragma unroll
         for (int q = 0; q < kAhead; ++q)
             if (p0 + q < parts)
 #pragma unroll
-                for (int sl = 0; sl < kSlabs; ++sl) { z[sl][0] += v[q][sl].x; z[sl][1] += v[q][sl].y; z[sl][2] += v[q][sl].z; z[sl][3] += v[q][sl].w; }
+                for (int g = 0; g < kGroups; ++g)
+#pragma unroll
+                    for (int sl = 0; sl < kSlabs; ++sl) {
+                        z[g][sl][0] += v[q][g][sl].x; z[g][sl][1] += v[q][g][sl].y; z[g][sl][2] += v[q][g][sl].z; z[g][sl][3] += v[q][g][sl].w;
+                    }
     }
 }
 
-template <int kMode, bool kGated, int kSlabs, bool kCol>
+template <int kMode, bool kGated, int kSlabs, bool kCol, bool kF16>
 __global__ void __launch_bounds__(kMaxThreads, 1)
-stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1, const __grid_constant__ TokenMaps maps_x, const StreamArgs a)
+stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant__ CUtensorMap map_w1, const __grid_constant__ TokenMaps maps_x, const __grid_constant__ StreamArgs a)
 {
     static_assert(!kGated || kSlabs == 2, "gate and up are a slab each");
     extern __shared__ unsigned char smem_raw[];
@@ -249,58 +284,69 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
         if (lane < 2) { mbar_init(acc_full0 + 8 * lane, 1); mbar_init(acc_empty0 + 8 * lane, (uint32_t)finishers / 32); }
         if (lane == 2) mbar_init(drained, 1);
         mbar_init_fence();
+        __syncwarp();
+    }
+    const int first_id = blockIdx.x;
+    int filled = 0, head = 0;                                  // stages filled so far, of them before the others were ready (lane 0 of warp 0)
+    const uint64_t stream = l2_policy_evict_first(), keep = l2_policy_evict_last();
+    auto weights = [&](const Item &t, int k, int s) {
+        const uint32_t dst = base + (uint32_t)s * a.stage_bytes, bar = full0 + 8 * s;
+#pragma unroll
+        for (int sl = 0; sl < kSlabs; ++sl) {
+            const CUtensorMap *m = kGated && sl ? &map_w1 : &map_w0;
+            const int n = t.n0 + (kGated ? 0 : sl * kSlab);
+            if constexpr (kCol) {
+                tma_load_3d(dst + sl * kSlabBytes, m, k * kKT, n, t.expert, bar, stream);
+            } else {
+                tma_load_3d(dst + sl * kSlabBytes, m, n, k * kKT, t.expert, bar, stream);
+                tma_load_3d(dst + sl * kSlabBytes + kSlabBytes / 2, m, n + 64, k * kKT, t.expert, bar, stream);
+            }
+        }
+    };
+    auto tokens = [&](const Item &t, const TokenCopy &x, int k, int s) {
+        const uint32_t dst = base + (uint32_t)s * a.stage_bytes + kSlabs * kSlabBytes, bar = full0 + 8 * s;
+        if (a.gather) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                if (4 * g < t.rows) tma_gather4(dst + g * 512, &maps_x.of[0], k * kKT, x.ids[4 * g], x.ids[4 * g + 1], x.ids[4 * g + 2], x.ids[4 * g + 3], bar, keep);
+        } else {
+            tma_load_3d(dst, &maps_x.of[x.boxes - 1], k * kKT, t.row0, 0, bar, keep);
+            if (a.terms == 2) tma_load_3d(dst + x.term_bytes, &maps_x.of[x.boxes - 1], k * kKT, t.row0, 1, bar, keep);
+        }
+    };
+    auto schedule = [&] { return a.planned ? *a.plan.schedule : a.schedule; };
+    // The plan of a programmatic chain is two kernels back and complete (the kernel before waited for it): only what the kernel before wrote has to
+    // be waited for.  Without early_weights everything is behind the wait.  The copies begin while tensor memory is still being allocated.
+    if (!a.early_weights) pdl_wait_prior_grids();
+    if (a.programmatic) pdl_launch_dependents();
+    if (warp == 0 && lane == 0) {
+        const Schedule sc = schedule();
+        if (first_id < sc.chunks) {
+            const Chunk c = chunk_of(sc, a.kb, first_id);
+            const Item t = item_of(a, c.item);
+            const TokenCopy x = token_copy(a, t, kSlabs);
+            head = min(NS, c.k1 - c.k0);
+            for (int i = 0; i < head; ++i) {
+                mbar_arrive_expect_tx(full0 + 8 * i, x.step_bytes);
+                weights(t, c.k0 + i, i);
+            }
+            if (a.early_weights) pdl_wait_prior_grids();
+            for (int i = 0; i < head; ++i) tokens(t, x, c.k0 + i, i);
+            filled = head;
+        } else if (a.early_weights) {
+            pdl_wait_prior_grids();
+        }
     }
     if (warp == 1) tmem_alloc(&s_tmem, a.tmem_columns);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
-
-    // The plan of a programmatic chain is two kernels back and complete (the kernel before waited for it): only what the kernel before wrote has to
-    // be waited for.  Without early_weights everything is behind the wait.
-    if (!a.early_weights) pdl_wait_prior_grids();
-    if (a.programmatic) pdl_launch_dependents();
-    const Schedule sched = a.planned ? *a.plan.schedule : a.schedule;
-    const int first_id = blockIdx.x;
+    const Schedule sched = schedule();
     const bool more_than_one = sched.chunks > (int)gridDim.x;
-    int filled = 0;                                            // stages filled so far (warp 0)
 
     if (warp == 0) {
         if (lane == 0) {
-            const uint64_t stream = l2_policy_evict_first(), keep = l2_policy_evict_last();
-            auto weights = [&](const Item &t, int k, int s) {
-                const uint32_t dst = base + (uint32_t)s * a.stage_bytes, bar = full0 + 8 * s;
-#pragma unroll
-                for (int sl = 0; sl < kSlabs; ++sl) {
-                    const CUtensorMap *m = kGated && sl ? &map_w1 : &map_w0;
-                    const int n = t.n0 + (kGated ? 0 : sl * kSlab);
-                    if constexpr (kCol) {
-                        tma_load_3d(dst + sl * kSlabBytes, m, k * kKT, n, t.expert, bar, stream);
-                    } else {
-                        tma_load_3d(dst + sl * kSlabBytes, m, n, k * kKT, t.expert, bar, stream);
-                        tma_load_3d(dst + sl * kSlabBytes + kSlabBytes / 2, m, n + 64, k * kKT, t.expert, bar, stream);
-                    }
-                }
-            };
-            // bytes of a step
-            auto step_bytes = [&](const Item &t) {
-                return kSlabs * kSlabBytes + (a.gather ? (uint32_t)ceil_div(t.rows, 4) * 512u : (uint32_t)(ceil_div(t.rows, a.box_rows) * a.box_rows * a.terms) * 128u);
-            };
-            // The first fills: weights before the wait, tokens behind it.
-            int head = 0;
-            if (a.early_weights) {
-                if (first_id < sched.chunks) {
-                    const Chunk c = chunk_of(sched, a.kb, first_id);
-                    const Item t = item_of(a, c.item);
-                    head = min(NS, c.k1 - c.k0);
-                    for (int i = 0; i < head; ++i) {
-                        mbar_arrive_expect_tx(full0 + 8 * i, step_bytes(t));
-                        weights(t, c.k0 + i, i);
-                    }
-                    filled = head;
-                }
-                pdl_wait_prior_grids();
-            }
             int s = 0, n = 0, queue = 0;
             uint32_t ph = 1, queue_ph = 1;                      // a fresh barrier passes a wait for the phase before its first
             bool ok = true;
@@ -309,31 +355,15 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                 if (more_than_one) next = (int)gridDim.x + (int)atomicAdd(a.counters + a.ticket, 1u);
                 const Chunk c = chunk_of(sched, a.kb, id);
                 const Item t = item_of(a, c.item);
-                const uint32_t bytes = step_bytes(t);
-                const int boxes = ceil_div(t.rows, a.box_rows);
-                const CUtensorMap *map_x = a.gather ? &maps_x.of[0] : &maps_x.of[boxes - 1];
-                const uint32_t term_bytes = (uint32_t)((a.apart ? boxes * a.box_rows : a.R) * 128);
-                int ids[16];
-                if (a.gather) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) ids[i] = i < t.rows ? NM_LD(a.plan.order + t.row0 + i, a.in_order, a.status) : 0;
-                }
+                const TokenCopy x = token_copy(a, t, kSlabs);
                 for (int k = c.k0; k < c.k1; ++k, ++n) {
                     if (n >= head) {
                         ok = mbar_try_wait(empty0 + 8 * s, ph) || mbar_wait(empty0 + 8 * s, ph, &s_abort, a.status);
                         if (!ok) break;
-                        mbar_arrive_expect_tx(full0 + 8 * s, bytes);
+                        mbar_arrive_expect_tx(full0 + 8 * s, x.step_bytes);
                         weights(t, k, s);
+                        tokens(t, x, k, s);
                         filled = n + 1;
-                    }
-                    const uint32_t dst = base + (uint32_t)s * a.stage_bytes + kSlabs * kSlabBytes, bar = full0 + 8 * s;
-                    if (a.gather) {
-#pragma unroll
-                        for (int g = 0; g < 4; ++g)
-                            if (4 * g < t.rows) tma_gather4(dst + g * 512, map_x, k * kKT, ids[4 * g], ids[4 * g + 1], ids[4 * g + 2], ids[4 * g + 3], bar, keep);
-                    } else {
-                        tma_load_3d(dst, map_x, k * kKT, t.row0, 0, bar, keep);
-                        if (a.terms == 2) tma_load_3d(dst + term_bytes, map_x, k * kKT, t.row0, 1, bar, keep);
                     }
                     if (++s == NS) { s = 0; ph ^= 1; }
                 }
@@ -361,7 +391,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             const Chunk c = chunk_of(sched, a.kb, id);
             const Item t = item_of(a, c.item);
             const int columns = a.apart ? 2 * ceil_div(t.rows, a.box_rows) * a.box_rows : (t.rows + 15) & ~15;
-            const uint32_t idesc = a.f16 ? instr_desc_f16(kSlab, columns, !kCol, false) : instr_desc(kSlab, columns, !kCol, false);
+            const uint32_t idesc = kF16 ? instr_desc_f16(kSlab, columns, !kCol, false) : instr_desc(kSlab, columns, !kCol, false);
             const bool twice = a.terms == 2 && !a.apart;
             ok = mbar_try_wait(acc_empty0 + 8 * acc, acc_ph) || mbar_wait(acc_empty0 + 8 * acc, acc_ph, &s_abort, a.status);
             if (!__all_sync(0xffffffffu, ok)) break;
@@ -410,7 +440,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
         for (int id = first_id; id < sched.chunks; round ^= 1) {
             const Chunk c = chunk_of(sched, a.kb, id);
             const Item t = item_of(a, c.item);
-            Rows<kMode, kGated, kSlabs> rows(a, t, 4 * turn, n_lane);
+            Rows<kMode, kGated, kSlabs, kF16> rows(a, t, 4 * turn, step, n_lane);
             if (kMode == kOutAct && a.residual) {
                 // (a lane a row: this warp's rows are four of every `step`)
                 const int r = 4 * turn + (lane >> 2) * step + (lane & 3), n_warp = t.n0 + quad * 32;
@@ -449,7 +479,6 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                     const Side<kSlabs> now = side;
                     rows.ask(side, j - 4 * turn + step, t.rows - j - step);
                     rows.put(z, now, t.rows - j);
-                    rows.advance(step);
                 } else {
 #pragma unroll
                     for (int sl = 0; sl < kSlabs; ++sl)
@@ -463,22 +492,31 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             acc ^= 1;
 
             if (c.cut >= 0) {
-                __threadfence();
                 named_barrier_sync(1, finishers);
                 if (thread == 0) {
+                    __threadfence();                             // (all of the CTA's sums: the barrier comes first)
                     s_last = atomicAdd(a.counters + kItemCounters + c.cut, 1u) == (unsigned)(sched.parts - 1);
                     if (s_last) a.counters[kItemCounters + c.cut] = 0u;             // ready for the next product
                 }
                 named_barrier_sync(1, finishers);
                 if (s_last) {
                     __threadfence();
-                    for (int j = 4 * turn; j < t.rows; j += step) {
-                        float z[kSlabs][4];
-                        join<kSlabs>(a, j, c.first_slot, sched.parts, n_lane, z);
+                    auto put_next = [&](float (&z)[kSlabs][4], int j) {
                         const Side<kSlabs> now = side;
                         rows.ask(side, j - 4 * turn + step, t.rows - j - step);
                         rows.put(z, now, t.rows - j);
-                        rows.advance(step);
+                    };
+                    int j = 4 * turn;
+                    for (; j + step < t.rows; j += 2 * step) {
+                        float z[2][kSlabs][4];
+                        join<kSlabs, 2>(a, j, step, c.first_slot, sched.parts, n_lane, z);
+                        put_next(z[0], j);
+                        put_next(z[1], j + step);
+                    }
+                    if (j < t.rows) {
+                        float z[1][kSlabs][4];
+                        join<kSlabs, 1>(a, j, step, c.first_slot, sched.parts, n_lane, z);
+                        put_next(z[0], j);
                     }
                 }
             }
@@ -526,17 +564,17 @@ bool encode_map(CUtensorMap *map, const void *p, bool f16, int rank, const cuuin
                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int kMode, bool kGated, int kSlabs, bool kCol>
+template <int kMode, bool kGated, int kSlabs, bool kCol, bool kF16>
 cudaError_t launch_stream(const CUtensorMap &w0, const CUtensorMap &w1, const TokenMaps &x, const StreamArgs &a, long ctas, cudaStream_t s)
 {
     static std::atomic<unsigned long long> configured{0};
-    auto kern = stream_kernel<kMode, kGated, kSlabs, kCol>;
+    auto kern = stream_kernel<kMode, kGated, kSlabs, kCol, kF16>;
     cudaError_t e = ensure_dynamic_smem(kern, kRingBytes + 1024, configured);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
     // four rows at a time for each warp of a quarter: one to four of them
-    cfg.blockDim = dim3(64 + 128 * (a.R <= 16 ? 1 : a.R == 32 ? 2 : 4));
+    cfg.blockDim = dim3(a.R <= 16 ? kMaxThreads - 128 : kMaxThreads);
     cfg.dynamicSmemBytes = (size_t)a.nstage * a.stage_bytes + 1024;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
@@ -563,16 +601,17 @@ int stream_slabs(int N, bool gated) { return gated || N >= 2048 ? 2 : 1; }
 static int most_chunks(int R, int N, bool gated) { return (int)std::min<size_t>(1024, ((size_t)64 << 20) / ((size_t)R * stream_slabs(N, gated) * kSlab * sizeof(float))); }
 size_t stream_partial_bytes(int R, int N, bool gated) { return (size_t)most_chunks(R, N, gated) * R * stream_slabs(N, gated) * kSlab * sizeof(float); }
 
-CutModel stream_cut_model(int R, int N, int K, bool gated, int terms)
+CutModel stream_cut_model(int R, float rows, int N, int K, bool gated, int terms)
 {
     const int slabs = stream_slabs(N, gated);
-    const float step_bytes = (float)(slabs * kSlabBytes + terms * R * 128 / 2), step_us = step_bytes / 70e3f;      // (half of the rows there may be)
+    const float step_bytes = slabs * kSlabBytes + terms * rows * 128;
     CutModel m;
     m.kb = ceil_div(K, kKT);
     m.column_tiles = ceil_div(N, gated ? kSlab : slabs * kSlab);
     m.most_chunks = most_chunks(R, N, gated);
-    m.sums_steps = (float)(R / 2) * slabs * kSlab * 8 / step_bytes;
-    m.latency_steps = 2.5f / step_us;
+    m.alone_us = std::max(0.245f, step_bytes / 96e3f);
+    m.busy_us = std::max(m.alone_us, kSMs * (float)(slabs * kSlabBytes) / 6.9e6f);
+    m.sums_us = std::max(4.f, rows) * slabs * kSlab * 4 / 35e3f;
     m.forced = g_forced_parts.load(std::memory_order_relaxed);
     return m;
 }
@@ -581,7 +620,7 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
 {
     StreamArgs a{};
     const int slabs = stream_slabs(p.N, gated);
-    const CutModel m = stream_cut_model(p.R, p.N, p.K, gated, p.terms);
+    const CutModel m = stream_cut_model(p.R, (float)std::min(p.rows, p.R), p.N, p.K, gated, p.terms);
     a.kb = m.kb;
     a.tile_n = gated ? kSlab : slabs * kSlab;
     a.column_tiles = m.column_tiles;
@@ -599,7 +638,7 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     a.apart = p.terms == 2 && p.R <= 64;
     a.acc_columns = a.apart ? 2 * p.R : p.R;
     a.tmem_columns = std::max(32, 2 * slabs * a.acc_columns);
-    a.f16 = p.f16; a.gather = p.gather; a.planned = p.planned; a.early_weights = p.early_weights; a.programmatic = p.programmatic;
+    a.gather = p.gather; a.planned = p.planned; a.early_weights = p.early_weights; a.programmatic = p.programmatic;
     a.act = p.act; a.plan = p.plan;
     a.bias = static_cast<const uint16_t *>(p.bias); a.residual = static_cast<const uint16_t *>(p.residual); a.ld_residual = p.ld_residual;
     a.out = p.out; a.ldo = p.ldo; a.out_term = (long)p.rows * p.ldo; a.row_scale = p.row_scale;
@@ -649,7 +688,8 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     auto launch = [&](auto mode_, auto gated_, auto slabs_) {
         constexpr int kM = decltype(mode_)::value, kS = decltype(slabs_)::value;
         constexpr bool kG = decltype(gated_)::value;
-        return p.col ? launch_stream<kM, kG, kS, true>(w[0], w[1], x, a, ctas, s) : launch_stream<kM, kG, kS, false>(w[0], w[1], x, a, ctas, s);
+        if (p.f16) return p.col ? launch_stream<kM, kG, kS, true, true>(w[0], w[1], x, a, ctas, s) : launch_stream<kM, kG, kS, false, true>(w[0], w[1], x, a, ctas, s);
+        return p.col ? launch_stream<kM, kG, kS, true, false>(w[0], w[1], x, a, ctas, s) : launch_stream<kM, kG, kS, false, false>(w[0], w[1], x, a, ctas, s);
     };
     auto of_mode = [&](auto mode_) {
         if constexpr (decltype(mode_)::value != kOutDown)
