@@ -55,17 +55,20 @@ struct RowPlan {
 // are of an item that is cut.
 constexpr int kTicketUp = 0, kTicketDown = 1, kDone = 2, kItemCounters = 32, kMaxCut = 2 * kSMs, kCounterWords = kItemCounters + kMaxCut;
 
-// The cut with the least modelled time: rounds in which all CTAs work take a step in busy_us (HBM: 148 x 32 KB at 6.9 TB/s, 0.70 us), the last one with what is
-// left alone_us at least (a CTA takes in 96 GB/s, measured; 0.25 us a step of 16 KB); at the end a chunk's sums go to the workspace and all of an item's come back to
-// one CTA, sums_us each (35 GB/s, measured), behind 3.5 us for a fence, a counter and the first of them.
+// The cut with the least modelled time.  Rounds in which all CTAs work take a step in busy_us (HBM: 148 x 32 KB at 6.9 TB/s, 0.70 us).  In the last one, with what
+// is left, a CTA takes in 96 GB/s at most (0.25 us a step of 16 KB at least), or its part of HBM's rate; near each other the two add up to more than the
+// larger, taken as a norm (72 CTAs: 0.48 us a step of 32 KB where either bound says 0.35).  The sums of a chunk take a CTA chunk_us - the store, a fence, a counter, each
+// behind the copies' traffic - which has to fit beside the next chunk's copies; and at the end all of an item's come back to one CTA, sums_us each (35 GB/s), behind
+// 2.5 us for the last counter and the first of them.
 // All items but the last one to two rounds stay whole: sums in the workspace cost as much as the rows do, and only the end has to be even.
-struct CutModel { int kb, column_tiles, most_chunks, forced; float alone_us, busy_us, sums_us; };
+struct CutModel { int kb, column_tiles, most_chunks, forced; float alone_us, busy_us, sums_us, chunk_us; };
 __host__ __device__ inline float cut_cost(const CutModel &m, int rest, int parts)
 {
     if (m.forced) return parts <= m.forced ? (float)(m.forced - parts) : 1e9f;        // the nearest that may be
     const int kc = (m.kb + parts - 1) / parts, p = (m.kb + kc - 1) / kc, chunks = rest * p, rounds = chunks / kSMs, left = chunks - rounds * kSMs;
-    const float last = m.busy_us * left / kSMs, step = left ? (last > m.alone_us ? last : m.alone_us) : 0.f;
-    return kc * (rounds * m.busy_us + step) + (p > 1 ? 3.5f + (1 + p) * m.sums_us : 0.f);
+    const float share = m.busy_us * left / kSMs, step = left ? cbrtf(share * share * share + m.alone_us * m.alone_us * m.alone_us) : 0.f;
+    const float body = kc * (rounds * m.busy_us + step), between = m.chunk_us * (rounds - (left ? 0 : 1));
+    return p > 1 ? (body > between ? body : between) + 2.5f + (1 + p) * m.sums_us : body;
 }
 __host__ __device__ inline int whole_items(int items) { return items >= 2 * kSMs ? (items / kSMs - 1) * kSMs : 0; }
 __host__ __device__ inline Schedule schedule_of(int items, int kb, int parts)

@@ -76,6 +76,13 @@ __device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap *map
         ::"r"(dst), "l"(map), "r"(x), "r"(r0), "r"(r1), "r"(r2), "r"(r3), "r"(bar), "l"(policy) : "memory");
 }
 
+__device__ __forceinline__ unsigned ask_ticket(unsigned *counter)
+{
+    unsigned t;
+    asm volatile("atom.global.add.u32 %0, [%1], 1;" : "=r"(t) : "l"(counter) : "memory");
+    return t;
+}
+
 // Token rows: boxes of 1, 2, 3 and 4 times box_rows rows (the first alone for gathered rows).
 struct TokenMaps { CUtensorMap of[4]; };
 
@@ -350,13 +357,24 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             int s = 0, n = 0, queue = 0;
             uint32_t ph = 1, queue_ph = 1;                      // a fresh barrier passes a wait for the phase before its first
             bool ok = true;
+            // The next chunk is asked for eight steps before this one's last copy, and its item read three steps before: in time for neither to be waited for
+            // (a ticket takes 1 to 2 us), and late enough that whoever is done first takes what is left.
+            Item t{}, t_next{};
+            unsigned ticket = 0u;
+            if (first_id < sched.chunks) t = item_of(a, chunk_of(sched, a.kb, first_id).item);
             for (int id = first_id; ok && id < sched.chunks;) {
-                int next = sched.chunks;                        // asked for now, needed when this chunk has been copied
-                if (more_than_one) next = (int)gridDim.x + (int)atomicAdd(a.counters + a.ticket, 1u);
                 const Chunk c = chunk_of(sched, a.kb, id);
-                const Item t = item_of(a, c.item);
                 const TokenCopy x = token_copy(a, t, kSlabs);
+                const int ask_at = max(c.k0, c.k1 - 8), read_at = max(c.k0, c.k1 - 3);
+                id = sched.chunks;
                 for (int k = c.k0; k < c.k1; ++k, ++n) {
+                    if (more_than_one) {
+                        if (k == ask_at) ticket = ask_ticket(a.counters + a.ticket);
+                        if (k == read_at) {
+                            id = (int)(gridDim.x + ticket);
+                            if (id < sched.chunks) t_next = item_of(a, chunk_of(sched, a.kb, id).item);
+                        }
+                    }
                     if (n >= head) {
                         ok = mbar_try_wait(empty0 + 8 * s, ph) || mbar_wait(empty0 + 8 * s, ph, &s_abort, a.status);
                         if (!ok) break;
@@ -367,16 +385,15 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                     }
                     if (++s == NS) { s = 0; ph ^= 1; }
                 }
-                id = sched.chunks;
+                t = t_next;
                 if (ok && more_than_one) {
-                    id = next;
                     ok = mbar_try_wait(taken0 + 8 * queue, queue_ph) || mbar_wait(taken0 + 8 * queue, queue_ph, &s_abort, a.status);
                     if (ok) { s_queue[queue] = id; mbar_arrive(queued0 + 8 * queue); }
                     if (++queue == kQueue) { queue = 0; queue_ph ^= 1; }
                 }
             }
-            // Every CTA has its last ticket: whoever is last to say so clears them for the next call.
-            if (more_than_one && !a.planned && atomicAdd(a.counters + kDone, 1u) == gridDim.x - 1) {
+            // Every CTA has had its last ticket (the value is looked at, so it has come): whoever is last to say so clears them for the next call.
+            if (more_than_one && !a.planned && ticket != 0xffffffffu && atomicAdd(a.counters + kDone, 1u) == gridDim.x - 1) {
                 a.counters[a.ticket] = 0u;
                 a.counters[kDone] = 0u;
             }
@@ -612,6 +629,7 @@ CutModel stream_cut_model(int R, float rows, int N, int K, bool gated, int terms
     m.alone_us = std::max(0.245f, step_bytes / 96e3f);
     m.busy_us = std::max(m.alone_us, kSMs * (float)(slabs * kSlabBytes) / 6.9e6f);
     m.sums_us = std::max(4.f, rows) * slabs * kSlab * 4 / 35e3f;
+    m.chunk_us = 8.f + 0.1f * rows * slabs;
     m.forced = g_forced_parts.load(std::memory_order_relaxed);
     return m;
 }
