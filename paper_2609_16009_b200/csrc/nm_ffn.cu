@@ -193,8 +193,9 @@ __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a)
 
 // ---- rows by expert ------------------------------------------------------------------------------------------------------------
 // A CTA an expert: all count how many pairs each expert has (shared-memory counters), so each knows where its own rows begin, and then puts its
-// pairs there in their order.  Nothing is passed between CTAs and the order is always the same.
-constexpr int kPlanThreads = 512;
+// pairs there in their order: a warp takes a run of pairs, counts its own among them, and writes them behind those of the warps before.  Nothing is passed
+// between CTAs and the order is always the same.  The experts of up to 8192 pairs are read once and kept (16 bits each).
+constexpr int kPlanThreads = 512, kPlanWarps = kPlanThreads / 32, kPlanKept = 8192;
 struct PlanArgs {
     const int32_t *experts; int first, E;
     int pairs, R, top_k;
@@ -207,39 +208,45 @@ struct PlanArgs {
     unsigned *status;
 };
 
-__device__ __forceinline__ int block_sum(int v, int *s_warp)     // the same for all threads
+__device__ __forceinline__ int2 block_sum(int2 v, int2 *s_warp)     // the same for all threads
 {
-    v = __reduce_add_sync(0xffffffffu, v);
-    __syncthreads();
+    v.x = __reduce_add_sync(0xffffffffu, v.x);
+    v.y = __reduce_add_sync(0xffffffffu, v.y);
     if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = v;
     __syncthreads();
-    int sum = 0;
+    int2 sum = make_int2(0, 0);
 #pragma unroll
-    for (int i = 0; i < kPlanThreads / 32; ++i) sum += s_warp[i];
+    for (int i = 0; i < kPlanWarps; ++i) { sum.x += s_warp[i].x; sum.y += s_warp[i].y; }
     return sum;
 }
 
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a)
 {
-    __shared__ int s_count[NM_MAX_EXPERTS], s_warp[kPlanThreads / 32], s_before[2][kPlanThreads / 32];
+    __shared__ int s_count[NM_MAX_EXPERTS], s_before[kPlanWarps];
+    __shared__ int2 s_warp[kPlanWarps];
+    __shared__ uint16_t s_expert[kPlanKept];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, mine = blockIdx.x;
+    const bool kept = a.pairs <= kPlanKept;
     for (int i = tid; i < a.E; i += kPlanThreads) s_count[i] = 0;
     pdl_launch_dependents();
     pdl_wait_prior_grids();
     __syncthreads();
+    constexpr uint16_t kNone = 0xffffu;
     auto expert_of = [&](int p) {
         const long e = (long)NM_LD(a.experts + p, a.in_experts, a.status) - a.first;
-        return e >= 0 && e < a.E ? (int)e : -1;
+        return e >= 0 && e < a.E ? (uint16_t)e : kNone;
     };
+#pragma unroll 4
     for (int p = tid; p < a.pairs; p += kPlanThreads) {
-        const int e = expert_of(p);
-        if (e >= 0) atomicAdd(&s_count[e], 1);
+        const uint16_t e = expert_of(p);
+        if (kept) s_expert[p] = e;
+        if (e != kNone) atomicAdd(&s_count[e], 1);
     }
     __syncthreads();
-    int rows = 0, tiles = 0;
-    for (int i = tid; i < mine; i += kPlanThreads) { rows += s_count[i]; tiles += ceil_div(s_count[i], a.R); }
-    const int row0 = block_sum(rows, s_warp), tile0 = block_sum(tiles, s_warp);
-    const int count = s_count[mine], own = ceil_div(count, a.R);
+    int2 before = make_int2(0, 0);
+    for (int i = tid; i < mine; i += kPlanThreads) { before.x += s_count[i]; before.y += ceil_div(s_count[i], a.R); }
+    before = block_sum(before, s_warp);
+    const int row0 = before.x, tile0 = before.y, count = s_count[mine], own = ceil_div(count, a.R);
     if (mine == a.E - 1) {
         if (tid == 0) *a.n_rows = row0 + count;
         if (warp < 2) {                                           // a warp a product: a lane for each number of parts
@@ -255,22 +262,23 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a)
     if (mine == 0) for (int i = tid; i < kCounterWords; i += kPlanThreads) a.counters[i] = 0u;
     for (int i = tid; i < own; i += kPlanThreads) NM_ST(a.tiles + tile0 + i, (RowTile{mine, row0 + i * a.R, min(a.R, count - i * a.R), 0}), a.in_tiles, a.status);
     if (count == 0) return;
-    int at = row0;
-    for (int p0 = 0, buf = 0; p0 < a.pairs; p0 += kPlanThreads, buf ^= 1) {
-        const int p = p0 + tid;
-        const bool here = p < a.pairs && expert_of(p) == mine;
-        const unsigned votes = __ballot_sync(0xffffffffu, here);
-        if (lane == 0) s_before[buf][warp] = __popc(votes);
-        __syncthreads();
-        int before = 0, all = 0;
-#pragma unroll
-        for (int i = 0; i < kPlanThreads / 32; ++i) { const int n = s_before[buf][i]; before += i < warp ? n : 0; all += n; }
-        if (here) {
-            const int row = at + before + __popc(votes & ((1u << lane) - 1u));
-            NM_ST(a.order + row, p / a.top_k, a.in_order, a.status);
-            NM_ST(a.place + p, row, a.in_place, a.status);
+    // Warp w: pairs [w, w + 1) of sixteen equal runs, 32 at a time.
+    const int run = ceil_div(ceil_div(a.pairs, 32), kPlanWarps) * 32, p0 = min(a.pairs, warp * run), p1 = min(a.pairs, p0 + run);
+    auto votes_at = [&](int p) { return __ballot_sync(0xffffffffu, p < p1 && (kept ? s_expert[p] : expert_of(p)) == mine); };
+    int n = 0;
+    for (int p = p0; p < p1; p += 32) n += __popc(votes_at(p + lane));
+    if (lane == 0) s_before[warp] = n;
+    __syncthreads();
+    int row = row0;
+    for (int i = 0; i < warp; ++i) row += s_before[i];
+    for (int p = p0; p < p1; p += 32) {
+        const unsigned votes = votes_at(p + lane);
+        if (votes >> lane & 1u) {
+            const int at = row + __popc(votes & ((1u << lane) - 1u));
+            NM_ST(a.order + at, (p + lane) / a.top_k, a.in_order, a.status);
+            NM_ST(a.place + p + lane, at, a.in_place, a.status);
         }
-        at += all;
+        row += __popc(votes);
     }
 }
 
@@ -297,15 +305,24 @@ __global__ void __launch_bounds__(256) hidden_terms_kernel(const float *h, uint1
     __shared__ float s_max[8];
     pdl_launch_dependents();
     pdl_wait_prior_grids();
+    constexpr int kKept = 8;                                       // values a thread keeps (rows of up to 2048); the others are read again
     for (int r = blockIdx.x; r < rows; r += gridDim.x) {
         const float *x = h + (size_t)r * n;
+        float kept[kKept];
         float m = 0.f;
-        for (int i = threadIdx.x; i < n; i += 256) {
-            const float v = fabsf(NM_LD(x + i, in_h, status));
-            if (v < INFINITY) m = fmaxf(m, v);
+#pragma unroll
+        for (int i = 0; i < kKept; ++i) {
+            const int at = i * 256 + threadIdx.x;
+            kept[i] = at < n ? NM_LD(x + at, in_h, status) : 0.f;
         }
 #pragma unroll
-        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        for (int i = 0; i < kKept; ++i)
+            if (fabsf(kept[i]) < INFINITY) m = fmaxf(m, fabsf(kept[i]));
+        for (int at = kKept * 256 + threadIdx.x; at < n; at += 256) {
+            const float v = fabsf(NM_LD(x + at, in_h, status));
+            if (v < INFINITY) m = fmaxf(m, v);
+        }
+        m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));      // (not negative: the bits order as the values)
         __syncthreads();
         if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
         __syncthreads();
@@ -313,14 +330,18 @@ __global__ void __launch_bounds__(256) hidden_terms_kernel(const float *h, uint1
         for (int i = 0; i < 8; ++i) m = fmaxf(m, s_max[i]);
         int e = 0;
         if (m > 0.f) { frexpf(m, &e); e = max(e - 15, -100); }   // (not below 2^-100: the factor back has to be a normal number)
-        for (int i = threadIdx.x; i < n; i += 256) {
-            const float v = scalbnf(NM_LD(x + i, in_h, status), -e);
+        auto put = [&](int at, float value) {
+            const float v = scalbnf(value, -e);
             const __half hi = __float2half_rn(v);
             const float rest = v - __half2float(hi);
-            uint16_t *to = terms + (size_t)r * n + i;
+            uint16_t *to = terms + (size_t)r * n + at;
             NM_ST(to, __half_as_ushort(hi), in_terms, status);
             NM_ST(to + (size_t)rows * n, fabsf(v) < INFINITY ? __half_as_ushort(__float2half_rn(rest)) : (uint16_t)0, in_terms, status);
-        }
+        };
+#pragma unroll
+        for (int i = 0; i < kKept; ++i)
+            if (i * 256 + (int)threadIdx.x < n) put(i * 256 + threadIdx.x, kept[i]);
+        for (int at = kKept * 256 + threadIdx.x; at < n; at += 256) put(at, NM_LD(x + at, in_h, status));
         if (threadIdx.x == 0) NM_ST(row_scale + r, scalbnf(1.f, e), in_scale, status);
     }
 }

@@ -33,6 +33,7 @@ namespace nm {
 namespace {
 
 constexpr int kMaxThreads = 64 + 32 * 8;
+constexpr int kGathered = 16;                   // token rows are gathered in tiles of up to so many (with 32 the eight tests a step alone cost 20%)
 constexpr int kQueue = 4;                       // chunks that the copies may be ahead of the epilogue
 constexpr int kKT = 64;                        // k of a stage
 constexpr int kSlab = 128;                     // outputs of a slab (the MMA's M)
@@ -215,7 +216,7 @@ struct Rows {
 };
 
 // How an item's token rows are copied: gathered (their tokens), or one box for each term; and the bytes of a step, weights and all.
-struct TokenCopy { int ids[16], boxes; uint32_t term_bytes, step_bytes; };
+struct TokenCopy { int ids[kGathered], boxes; uint32_t term_bytes, step_bytes; };
 __device__ __forceinline__ TokenCopy token_copy(const StreamArgs &a, const Item &t, int slabs)
 {
     TokenCopy x;
@@ -224,7 +225,7 @@ __device__ __forceinline__ TokenCopy token_copy(const StreamArgs &a, const Item 
     x.step_bytes = (uint32_t)slabs * kSlabBytes + (a.gather ? (uint32_t)ceil_div(t.rows, 4) * 512u : (uint32_t)(x.boxes * a.box_rows * a.terms) * 128u);
     if (a.gather) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x.ids[i] = i < t.rows ? NM_LD(a.plan.order + t.row0 + i, a.in_order, a.status) : 0;
+        for (int i = 0; i < kGathered; ++i) x.ids[i] = i < t.rows ? NM_LD(a.plan.order + t.row0 + i, a.in_order, a.status) : 0;
     }
     return x;
 }
@@ -314,7 +315,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
         const uint32_t dst = base + (uint32_t)s * a.stage_bytes + kSlabs * kSlabBytes, bar = full0 + 8 * s;
         if (a.gather) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
+            for (int g = 0; g < kGathered / 4; ++g)
                 if (4 * g < t.rows) tma_gather4(dst + g * 512, &maps_x.of[0], k * kKT, x.ids[4 * g], x.ids[4 * g + 1], x.ids[4 * g + 2], x.ids[4 * g + 3], bar, keep);
         } else {
             tma_load_3d(dst, &maps_x.of[x.boxes - 1], k * kKT, t.row0, 0, bar, keep);
@@ -675,18 +676,18 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     TokenMaps x;
     const uint16_t *W = static_cast<const uint16_t *>(p.W);
     bool ok = true;
-    for (int part = 0; part < parts; ++part) {
-        const cuuint64_t wide = (cuuint64_t)parts * p.N;
+    auto weight_map = [&](CUtensorMap *map, const uint16_t *W, long expert, int N, int K, int wide) {
         if (p.col) {
-            const cuuint64_t dims[3] = {(cuuint64_t)p.K, (cuuint64_t)p.N, (cuuint64_t)p.E}, strides[2] = {(cuuint64_t)p.K * 2, (cuuint64_t)p.w_expert * 2};
+            const cuuint64_t dims[3] = {(cuuint64_t)K, (cuuint64_t)N, (cuuint64_t)p.E}, strides[2] = {(cuuint64_t)K * 2, (cuuint64_t)expert * 2};
             const cuuint32_t box[3] = {kKT, kSlab, 1};
-            ok = ok && encode_map(&w[part], W + (size_t)part * p.N * p.K, p.f16, 3, dims, strides, box);
-        } else {
-            const cuuint64_t dims[3] = {(cuuint64_t)p.N, (cuuint64_t)p.K, (cuuint64_t)p.E}, strides[2] = {wide * 2, (cuuint64_t)p.w_expert * 2};
-            const cuuint32_t box[3] = {64, kKT, 1};
-            ok = ok && encode_map(&w[part], W + (size_t)part * p.N, p.f16, 3, dims, strides, box);
+            return encode_map(map, W, p.f16, 3, dims, strides, box);
         }
-    }
+        const cuuint64_t dims[3] = {(cuuint64_t)N, (cuuint64_t)K, (cuuint64_t)p.E}, strides[2] = {(cuuint64_t)wide * 2, (cuuint64_t)expert * 2};
+        const cuuint32_t box[3] = {64, kKT, 1};
+        return encode_map(map, W, p.f16, 3, dims, strides, box);
+    };
+    for (int part = 0; part < parts; ++part) ok = ok && weight_map(&w[part], W + (size_t)part * p.N * (p.col ? p.K : 1), p.w_expert, p.N, p.K, parts * p.N);
+    if (!gated) w[1] = w[0];
     if (p.gather) {
         const cuuint64_t dims[2] = {(cuuint64_t)p.K, (cuuint64_t)p.x_rows}, strides[1] = {(cuuint64_t)p.ldx * 2};
         const cuuint32_t box[2] = {kKT, 1};
@@ -702,7 +703,6 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     if (!a.status) { *what = "device status word"; return cudaErrorInvalidValue; }
     *what = "streamed product launch";
     const long ctas = p.planned ? kSMs : std::min(kSMs, a.schedule.chunks);
-    if (!gated) w[1] = w[0];
     auto launch = [&](auto mode_, auto gated_, auto slabs_) {
         constexpr int kM = decltype(mode_)::value, kS = decltype(slabs_)::value;
         constexpr bool kG = decltype(gated_)::value;
