@@ -46,7 +46,7 @@ std::atomic<int> g_forced_parts{0};             // nm_debug_set_ffn_cut
 struct StreamArgs {
     Schedule schedule;                          // where the rows are known on the host
     int kb, column_tiles, tile_n;               // steps of an item, column tiles of a row tile, outputs of one
-    int rows, N, R, box_rows, terms, nstage, stage_bytes;   // box_rows: the least of the box heights, the others its multiples
+    int rows, N, R, box_rows, nstage, stage_bytes;   // box_rows: the least of the box heights, the others its multiples
     int acc_columns;                            // of a slab: R, twice that where the terms have columns of their own
     bool apart;
     unsigned tmem_columns;
@@ -216,16 +216,20 @@ struct Rows {
 };
 
 // How an item's token rows are copied: gathered (their tokens), or one box for each term; and the bytes of a step, weights and all.
-struct TokenCopy { int ids[kGathered], boxes; uint32_t term_bytes, step_bytes; };
-__device__ __forceinline__ TokenCopy token_copy(const StreamArgs &a, const Item &t, int slabs)
+// What only one kind of product does: the first gathers rows, the second has two terms.
+template <int kMode> constexpr bool kGathers = kMode == kOutHidden;
+template <int kMode> constexpr int kTerms = kMode == kOutDown ? 2 : 1;
+template <bool kGather> struct TokenCopy { int ids[kGather ? kGathered : 1], boxes; uint32_t term_bytes, step_bytes; };
+template <int kMode>
+__device__ __forceinline__ TokenCopy<kGathers<kMode>> token_copy(const StreamArgs &a, const Item &t, int slabs)
 {
-    TokenCopy x;
+    TokenCopy<kGathers<kMode>> x;
     x.boxes = ceil_div(t.rows, a.box_rows);
     x.term_bytes = (uint32_t)((a.apart ? x.boxes * a.box_rows : a.R) * 128);
-    x.step_bytes = (uint32_t)slabs * kSlabBytes + (a.gather ? (uint32_t)ceil_div(t.rows, 4) * 512u : (uint32_t)(x.boxes * a.box_rows * a.terms) * 128u);
-    if (a.gather) {
+    x.step_bytes = (uint32_t)slabs * kSlabBytes + (kGathers<kMode> && a.gather ? (uint32_t)ceil_div(t.rows, 4) * 512u : (uint32_t)(x.boxes * a.box_rows * kTerms<kMode>) * 128u);
+    if (kGathers<kMode> && a.gather) {
 #pragma unroll
-        for (int i = 0; i < kGathered; ++i) x.ids[i] = i < t.rows ? NM_LD(a.plan.order + t.row0 + i, a.in_order, a.status) : 0;
+        for (int i = 0; i < (kGathers<kMode> ? kGathered : 0); ++i) x.ids[i] = i < t.rows ? NM_LD(a.plan.order + t.row0 + i, a.in_order, a.status) : 0;
     }
     return x;
 }
@@ -295,7 +299,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
         __syncwarp();
     }
     const int first_id = blockIdx.x;
-    int filled = 0, head = 0;                                  // stages filled so far, of them before the others were ready (lane 0 of warp 0)
+    int head = 0;                                              // stages that are filled before the warps part
     const uint64_t stream = l2_policy_evict_first(), keep = l2_policy_evict_last();
     auto weights = [&](const Item &t, int k, int s) {
         const uint32_t dst = base + (uint32_t)s * a.stage_bytes, bar = full0 + 8 * s;
@@ -311,46 +315,50 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             }
         }
     };
-    auto tokens = [&](const Item &t, const TokenCopy &x, int k, int s) {
+    auto tokens = [&](const Item &t, const TokenCopy<kGathers<kMode>> &x, int k, int s) {
         const uint32_t dst = base + (uint32_t)s * a.stage_bytes + kSlabs * kSlabBytes, bar = full0 + 8 * s;
-        if (a.gather) {
+        if constexpr (kGathers<kMode>) {
+            if (a.gather) {
 #pragma unroll
-            for (int g = 0; g < kGathered / 4; ++g)
-                if (4 * g < t.rows) tma_gather4(dst + g * 512, &maps_x.of[0], k * kKT, x.ids[4 * g], x.ids[4 * g + 1], x.ids[4 * g + 2], x.ids[4 * g + 3], bar, keep);
-        } else {
-            tma_load_3d(dst, &maps_x.of[x.boxes - 1], k * kKT, t.row0, 0, bar, keep);
-            if (a.terms == 2) tma_load_3d(dst + x.term_bytes, &maps_x.of[x.boxes - 1], k * kKT, t.row0, 1, bar, keep);
+                for (int g = 0; g < kGathered / 4; ++g)
+                    if (4 * g < t.rows) tma_gather4(dst + g * 512, &maps_x.of[0], k * kKT, x.ids[4 * g], x.ids[4 * g + 1], x.ids[4 * g + 2], x.ids[4 * g + 3], bar, keep);
+                return;
+            }
         }
+        tma_load_3d(dst, &maps_x.of[x.boxes - 1], k * kKT, t.row0, 0, bar, keep);
+        if constexpr (kTerms<kMode> == 2) tma_load_3d(dst + x.term_bytes, &maps_x.of[x.boxes - 1], k * kKT, t.row0, 1, bar, keep);
     };
-    auto schedule = [&] { return a.planned ? *a.plan.schedule : a.schedule; };
+    if (warp == 1) tmem_alloc(&s_tmem, a.tmem_columns);
+    __syncthreads();                                           // (the barriers are there)
     // The plan of a programmatic chain is two kernels back and complete (the kernel before waited for it): only what the kernel before wrote has to
-    // be waited for.  Without early_weights everything is behind the wait.  The copies begin while tensor memory is still being allocated.
+    // be waited for.  Without early_weights everything is behind the wait.
     if (!a.early_weights) pdl_wait_prior_grids();
     if (a.programmatic) pdl_launch_dependents();
-    if (warp == 0 && lane == 0) {
-        const Schedule sc = schedule();
-        if (first_id < sc.chunks) {
-            const Chunk c = chunk_of(sc, a.kb, first_id);
+    // The first fills are dealt out to all of the warps: a request costs the thread that makes it 100 clocks and more, so one thread took 2 us for a ring of twelve stages.
+    const Schedule sched = a.planned ? *a.plan.schedule : a.schedule;
+    if (first_id < sched.chunks) {
+        const Chunk c = chunk_of(sched, a.kb, first_id);
+        head = min(NS, c.k1 - c.k0);
+        if (lane == 0 && warp < head) {
+            const int warps = (int)blockDim.x / 32;
             const Item t = item_of(a, c.item);
-            const TokenCopy x = token_copy(a, t, kSlabs);
-            head = min(NS, c.k1 - c.k0);
-            for (int i = 0; i < head; ++i) {
+            const auto x = token_copy<kMode>(a, t, kSlabs);
+            for (int i = warp; i < head; i += warps) {
                 mbar_arrive_expect_tx(full0 + 8 * i, x.step_bytes);
                 weights(t, c.k0 + i, i);
+                if (!a.early_weights) tokens(t, x, c.k0 + i, i);
             }
-            if (a.early_weights) pdl_wait_prior_grids();
-            for (int i = 0; i < head; ++i) tokens(t, x, c.k0 + i, i);
-            filled = head;
-        } else if (a.early_weights) {
-            pdl_wait_prior_grids();
+            if (a.early_weights) {
+                pdl_wait_prior_grids();
+                for (int i = warp; i < head; i += warps) tokens(t, x, c.k0 + i, i);
+            }
         }
     }
-    if (warp == 1) tmem_alloc(&s_tmem, a.tmem_columns);
+    int filled = head;                                         // (where a wait runs out, the copies begun are known by it: lane 0 of warp 0)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = s_tmem;
-    const Schedule sched = schedule();
     const bool more_than_one = sched.chunks > (int)gridDim.x;
 
     if (warp == 0) {
@@ -365,7 +373,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             if (first_id < sched.chunks) t = item_of(a, chunk_of(sched, a.kb, first_id).item);
             for (int id = first_id; ok && id < sched.chunks;) {
                 const Chunk c = chunk_of(sched, a.kb, id);
-                const TokenCopy x = token_copy(a, t, kSlabs);
+                const auto x = token_copy<kMode>(a, t, kSlabs);
                 const int ask_at = max(c.k0, c.k1 - 8), read_at = max(c.k0, c.k1 - 3);
                 id = sched.chunks;
                 for (int k = c.k0; k < c.k1; ++k, ++n) {
@@ -408,9 +416,9 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
         for (int id = first_id; id < sched.chunks;) {
             const Chunk c = chunk_of(sched, a.kb, id);
             const Item t = item_of(a, c.item);
-            const int columns = a.apart ? 2 * ceil_div(t.rows, a.box_rows) * a.box_rows : (t.rows + 15) & ~15;
+            const int columns = kTerms<kMode> == 2 && a.apart ? 2 * ceil_div(t.rows, a.box_rows) * a.box_rows : (t.rows + 15) & ~15;
             const uint32_t idesc = kF16 ? instr_desc_f16(kSlab, columns, !kCol, false) : instr_desc(kSlab, columns, !kCol, false);
-            const bool twice = a.terms == 2 && !a.apart;
+            const bool twice = kTerms<kMode> == 2 && !a.apart;
             ok = mbar_try_wait(acc_empty0 + 8 * acc, acc_ph) || mbar_wait(acc_empty0 + 8 * acc, acc_ph, &s_abort, a.status);
             if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
@@ -644,7 +652,7 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     a.tile_n = gated ? kSlab : slabs * kSlab;
     a.column_tiles = m.column_tiles;
     a.box_rows = std::max(8, p.R / 4);
-    a.rows = p.rows; a.N = p.N; a.R = p.R; a.terms = p.terms;
+    a.rows = p.rows; a.N = p.N; a.R = p.R;
     if (!p.planned) {
         const int items = ceil_div(p.rows, p.R) * a.column_tiles, rest = items - whole_items(items);
         int best = 1;
