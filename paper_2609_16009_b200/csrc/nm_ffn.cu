@@ -367,8 +367,9 @@ bool ffn_dtype_ok(nm_dtype t) { return t == NM_BF16 || t == NM_F16; }
 bool ffn_layout_ok(nm_layout l) { return l == NM_ROW_MAJOR || l == NM_COL_MAJOR; }
 bool act_ok(nm_act act) { return act >= NM_ACT_NONE && act <= NM_ACT_GELU_TANH; }
 
-// Whether tensor maps can address rows of `pitch` 16-bit elements at p: both on 16 bytes.
-bool rows_on_16(const void *p, long pitch) { return !((uintptr_t)p & 15u) && pitch % 8 == 0; }
+// Whether tensor maps can address rows of `pitch` 16-bit elements at p: both on 16 bytes, and no stride of 2^40 bytes.
+bool stride_ok(long elements) { return elements < (1l << 39); }
+bool rows_on_16(const void *p, long pitch) { return !((uintptr_t)p & 15u) && pitch % 8 == 0 && stride_ok(pitch); }
 
 struct MoeLayout { size_t tiles, n_rows, schedules, order, place, partial, h, terms, scale, y, total; };
 MoeLayout moe_layout(long pairs, int d, int inter, int E, bool f16)
@@ -382,7 +383,9 @@ MoeLayout moe_layout(long pairs, int d, int inter, int E, bool f16)
     l.order = at; at += align256(4 * (size_t)pairs);
     l.place = at; at += align256(4 * (size_t)pairs);
     l.scale = at; at += align256(4 * (size_t)pairs);
-    l.partial = at; at += align256(std::max(stream_partial_bytes(R, inter, true), std::max(stream_partial_bytes(R, inter, false), stream_partial_bytes(R, d, false))));
+    const long tiles = E + pairs / R;
+    l.partial = at;
+    at += align256(std::max(stream_partial_bytes(R, inter, d, true, tiles), std::max(stream_partial_bytes(R, inter, d, false, tiles), stream_partial_bytes(R, d, inter, false, tiles))));
     l.h = at; at += align256(4 * (size_t)pairs * inter);
     l.terms = f16 ? at : l.h;
     if (f16) at += align256(4 * (size_t)pairs * inter);
@@ -402,8 +405,9 @@ extern "C" {
 
 size_t nm_matmul_act_workspace_bytes(int M, int N, int K, int gated, nm_dtype dtype)
 {
-    if (M < 1 || N < 1 || K < 1 || !ffn_dtype_ok(dtype)) return 0;
-    return NM_WS_COUNTER_BYTES + stream_partial_bytes(stream_tile_rows(M, M), N, gated != 0);
+    if (M < 1 || M > NM_MAX_FFN_ROWS || N < 1 || N > kMaxDim || K < 1 || K > kMaxDim || !ffn_dtype_ok(dtype)) return 0;
+    const int R = stream_tile_rows(M, M);
+    return NM_WS_COUNTER_BYTES + stream_partial_bytes(R, N, K, gated != 0, ceil_div(M, R));
 }
 
 int nm_matmul_act(const void *A, long lda, const void *B, const void *bias, const void *residual, long ld_residual, void *C, long ldc, int M,
@@ -418,9 +422,9 @@ int nm_matmul_act(const void *A, long lda, const void *B, const void *bias, cons
     const int parts = gated ? 2 : 1;
     cudaStream_t s = (cudaStream_t)stream;
     const bool col = layout_B == NM_COL_MAJOR, programmatic = programmatic_launch_enabled();
-    if (rows_on_16(A, lda) && rows_on_16(B, col ? K : N)) {
+    if (rows_on_16(A, lda) && rows_on_16(B, col ? K : N) && stride_ok((long)M * lda)) {
         ProductArgs p{};
-        p.rows = M; p.N = N; p.K = K; p.R = stream_tile_rows(M, M); p.terms = 1;
+        p.rows = M; p.N = N; p.K = K; p.R = stream_tile_rows(M, M); p.expected_rows = (float)std::min(M, p.R); p.row_tiles = ceil_div(M, p.R); p.terms = 1;
         p.col = col; p.f16 = dtype == NM_F16; p.early_weights = p.programmatic = programmatic;
         p.act = act;
         p.W = B; p.w_expert = (long)parts * N * K; p.E = 1;
@@ -451,7 +455,7 @@ int nm_matmul_act(const void *A, long lda, const void *B, const void *bias, cons
 
 size_t nm_moe_ffn_workspace_bytes(int T, int d, int inter, int E, int top_k, nm_dtype dtype)
 {
-    if (T < 1 || d < 1 || inter < 1 || E < 1 || top_k < 1 || (long)T * top_k > kMaxPairs || !ffn_dtype_ok(dtype)) return 0;
+    if (T < 1 || d < 1 || d > kMaxDim || inter < 1 || inter > kMaxDim || E < 1 || E > NM_MAX_EXPERTS || top_k < 1 || (long)T * top_k > kMaxPairs || !ffn_dtype_ok(dtype)) return 0;
     return moe_layout((long)T * top_k, d, inter, E, dtype == NM_F16).total;
 }
 
@@ -480,15 +484,16 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
     unsigned *const status = bounds_status_ptr();
     const char *what = "experts' products launch";
     cudaError_t e;
-    if (rows_on_16(x, ldx) && rows_on_16(W_up, col ? d : inter) && rows_on_16(W_down, col ? inter : d) && inter % 8 == 0) {
+    if (rows_on_16(x, ldx) && rows_on_16(W_up, col ? d : inter) && rows_on_16(W_down, col ? inter : d) && inter % 8 == 0 &&
+        stride_ok((long)parts * inter * d) && stride_ok(pairs * inter) && stride_ok(pairs * d)) {
         PlanArgs pl{};
         pl.experts = experts; pl.first = first_expert; pl.E = E; pl.pairs = (int)pairs; pl.top_k = top_k;
         pl.R = stream_tile_rows((double)pairs / E, (int)std::min<long>(pairs, 128));
         pl.tiles = reinterpret_cast<RowTile *>(ws + lay.tiles); pl.n_rows = reinterpret_cast<int *>(ws + lay.n_rows);
         pl.schedules = reinterpret_cast<Schedule *>(ws + lay.schedules);
         const float rows = (float)std::min<double>(pl.R, std::max(1.0, (double)pairs / E));
-        pl.model[0] = stream_cut_model(pl.R, rows, inter, d, gated != 0, 1);
-        pl.model[1] = stream_cut_model(pl.R, rows, d, inter, false, 2);
+        pl.model[0] = stream_cut_model(pl.R, rows, inter, d, gated != 0, 1, E + pairs / pl.R);
+        pl.model[1] = stream_cut_model(pl.R, rows, d, inter, false, 2, E + pairs / pl.R);
         pl.order = reinterpret_cast<int *>(ws + lay.order); pl.place = reinterpret_cast<int *>(ws + lay.place);
         pl.counters = reinterpret_cast<unsigned *>(ws);
         pl.in_experts = in_experts; pl.in_tiles = make_span(pl.tiles, sizeof(RowTile) * (E + (size_t)pairs / pl.R));
@@ -498,7 +503,7 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
         e = launch(plan_kernel, E, kPlanThreads, programmatic, s, pl);
 
         ProductArgs p{};
-        p.rows = (int)pairs; p.N = inter; p.K = d; p.R = pl.R; p.terms = 1;
+        p.rows = (int)pairs; p.N = inter; p.K = d; p.R = pl.R; p.expected_rows = rows; p.row_tiles = E + pairs / pl.R; p.terms = 1;
         p.col = col; p.f16 = f16; p.planned = p.programmatic = true;
         p.act = act;
         p.plan = RowPlan{pl.tiles, pl.schedules, pl.order};

@@ -83,6 +83,8 @@ struct ProductArgs {
     int rows;                          // token rows there are (kOutAct), or pairs
     int N, K;                          // outputs (of one of the two parts, where gated), inner dimension
     int R;                             // rows of a tile, the accumulator's columns: 16, 32, 64 or 128
+    float expected_rows;               // of a tile
+    long row_tiles;                    // there may be
     int terms;                         // 16-bit terms that a token value is the sum of
     bool col, f16;
     bool gather;                       // token rows by the plan's order (one term)
@@ -104,8 +106,8 @@ struct ProductArgs {
 // sums of chunks.
 int stream_tile_rows(double average, int most);
 int stream_slabs(int N, bool gated);
-size_t stream_partial_bytes(int R, int N, bool gated);
-CutModel stream_cut_model(int R, float rows, int N, int K, bool gated, int terms);
+size_t stream_partial_bytes(int R, int N, int K, bool gated, long row_tiles);
+CutModel stream_cut_model(int R, float rows, int N, int K, bool gated, int terms, long row_tiles);
 cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStream_t s, const char **what);
 
 }  // namespace nm

@@ -10,9 +10,9 @@
 //   chunk  an item, or for the last round or two one of `parts` runs of its steps; the cuts are a rule on sizes (schedule_of), the CTAs take chunks as they
 //          get done: with equal shares the fastest SMs were done after 652 us where the slowest took 870.  A chunk's fp32 sums wait in the workspace for
 //          the last of its item (a counter; nobody waits), which adds them in the order of k.  So results do not depend on who took what or came last.
-//   warps  0: copies, and the next chunk; 1: MMAs; from 2: the epilogue, from the other one of two accumulators.  Four to twelve warps by the rows of a
-//          tile: what an output costs is latency (tensor memory, exp, residual; 128 rows of 1536 x 24576 took 96 us with four warps, 48 with sixteen),
-//          and a launch of more warps costs a short call 1.5 us
+//   warps  0: copies, and the next chunk; 1: MMAs; from 2: the epilogue, from the other one of two accumulators.  Eight warps, two to a
+//          quarter of its lanes (16 rows of 18432 x 7168: 47.9 us, 49.9 with four), or four for up to four rows (they have nothing for more, and a launch of more
+//          threads takes longer)
 //
 // A step's token rows are ONE copy: of the four box heights there are a tensor map of, the least that holds the tile's rows.  A request costs the copy
 // engine and the thread that makes it 40 to 60 ns whatever its size, and requests made by several lanes at once take their turns (two boxes of 8 rows by two lanes: 0.2 us
@@ -48,7 +48,7 @@ struct StreamArgs {
     int kb, column_tiles, tile_n;               // steps of an item, column tiles of a row tile, outputs of one
     int rows, N, R, box_rows, nstage, stage_bytes;   // box_rows: the least of the box heights, the others its multiples
     int acc_columns;                            // of a slab: R, twice that where the terms have columns of their own
-    bool apart;
+    bool apart, few;                            // few: four rows or fewer in a tile, as far as that is known: four epilogue warps then
     unsigned tmem_columns;
     bool gather, planned, early_weights, programmatic;
     int act;
@@ -102,8 +102,9 @@ __device__ __forceinline__ Item item_of(const StreamArgs &a, int item)
 {
     const int tile = item / a.column_tiles, n0 = (item - tile * a.column_tiles) * a.tile_n;
     if (a.planned) {
-        const RowTile t = NM_LD(a.plan.tiles + tile, a.in_tiles, a.status);
-        return Item{t.expert, t.row0, t.rows, n0};
+        const RowTile *at = a.plan.tiles + tile;
+        const int4 t = NM_INSIDE(at, 16, a.in_tiles, a.status) ? __ldcg(reinterpret_cast<const int4 *>(at)) : make_int4(0, 0, 1, 0);
+        return Item{t.x, t.y, t.z, n0};
     }
     const int row0 = tile * a.R;
     return Item{0, row0, min(a.R, a.rows - row0), n0};
@@ -229,7 +230,7 @@ __device__ __forceinline__ TokenCopy<kGathers<kMode>> token_copy(const StreamArg
     x.step_bytes = (uint32_t)slabs * kSlabBytes + (kGathers<kMode> && a.gather ? (uint32_t)ceil_div(t.rows, 4) * 512u : (uint32_t)(x.boxes * a.box_rows * kTerms<kMode>) * 128u);
     if (kGathers<kMode> && a.gather) {
 #pragma unroll
-        for (int i = 0; i < (kGathers<kMode> ? kGathered : 0); ++i) x.ids[i] = i < t.rows ? NM_LD(a.plan.order + t.row0 + i, a.in_order, a.status) : 0;
+        for (int i = 0; i < (kGathers<kMode> ? kGathered : 0); ++i) x.ids[i] = i < t.rows && NM_INSIDE(a.plan.order + t.row0 + i, 4, a.in_order, a.status) ? __ldcg(a.plan.order + t.row0 + i) : 0;
     }
     return x;
 }
@@ -239,7 +240,7 @@ __device__ __forceinline__ TokenCopy<kGathers<kMode>> token_copy(const StreamArg
 template <int kSlabs, int kGroups>
 __device__ __forceinline__ void join(const StreamArgs &a, int j, int step, int first, int parts, int n_lane, float (&z)[kGroups][kSlabs][4])
 {
-    constexpr int kAhead = 8 / (kSlabs * kGroups);
+    constexpr int kAhead = 4 / kSlabs;                           // (more of them cost registers, and with those the rest of the epilogue)
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
@@ -335,7 +336,11 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
     if (!a.early_weights) pdl_wait_prior_grids();
     if (a.programmatic) pdl_launch_dependents();
     // The first fills are dealt out to all of the warps: a request costs the thread that makes it 100 clocks and more, so one thread took 2 us for a ring of twelve stages.
-    const Schedule sched = a.planned ? *a.plan.schedule : a.schedule;
+    Schedule sched = a.schedule;
+    if (a.planned) {
+        const int4 v = __ldcg(reinterpret_cast<const int4 *>(a.plan.schedule));
+        sched = Schedule{v.x, v.y, v.z, v.w};
+    }
     if (first_id < sched.chunks) {
         const Chunk c = chunk_of(sched, a.kb, first_id);
         head = min(NS, c.k1 - c.k0);
@@ -380,7 +385,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                     if (more_than_one) {
                         if (k == ask_at) ticket = ask_ticket(a.counters + a.ticket);
                         if (k == read_at) {
-                            id = (int)(gridDim.x + ticket);
+                            id = (int)min(gridDim.x + ticket, (unsigned)sched.chunks);
                             if (id < sched.chunks) t_next = item_of(a, chunk_of(sched, a.kb, id).item);
                         }
                     }
@@ -599,8 +604,7 @@ cudaError_t launch_stream(const CUtensorMap &w0, const CUtensorMap &w1, const To
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)ctas);
-    // four rows at a time for each warp of a quarter: one to four of them
-    cfg.blockDim = dim3(a.R <= 16 ? kMaxThreads - 128 : kMaxThreads);
+    cfg.blockDim = dim3(a.few ? kMaxThreads - 128 : kMaxThreads);
     cfg.dynamicSmemBytes = (size_t)a.nstage * a.stage_bytes + 1024;
     cfg.stream = s;
     cudaLaunchAttribute attr[1];
@@ -623,18 +627,23 @@ int stream_tile_rows(double average, int most)
 // Two slabs halve how often the token rows are read (and the MMAs that share them come in pairs); of a narrow matrix too much of the last tile would be empty.
 int stream_slabs(int N, bool gated) { return gated || N >= 2048 ? 2 : 1; }
 
-// Sums of chunks: as many as 64 MB hold, and no more than 1024.
-static int most_chunks(int R, int N, bool gated) { return (int)std::min<size_t>(1024, ((size_t)64 << 20) / ((size_t)R * stream_slabs(N, gated) * kSlab * sizeof(float))); }
-size_t stream_partial_bytes(int R, int N, bool gated) { return (size_t)most_chunks(R, N, gated) * R * stream_slabs(N, gated) * kSlab * sizeof(float); }
+// Sums of chunks: as many as 64 MB hold, no more than 1024, and no more than the items of the last rounds have steps.
+static size_t sum_bytes(int R, int N, bool gated) { return (size_t)R * stream_slabs(N, gated) * kSlab * sizeof(float); }
+static int most_chunks(int R, int N, int K, bool gated, long row_tiles)
+{
+    const long tile_n = gated ? kSlab : stream_slabs(N, gated) * kSlab, items = std::min<long>(2 * kSMs, row_tiles * ((N + tile_n - 1) / tile_n));
+    return (int)std::min<long>(std::min<long>(1024, items * ceil_div(K, kKT)), ((long)64 << 20) / (long)sum_bytes(R, N, gated));
+}
+size_t stream_partial_bytes(int R, int N, int K, bool gated, long row_tiles) { return (size_t)most_chunks(R, N, K, gated, row_tiles) * sum_bytes(R, N, gated); }
 
-CutModel stream_cut_model(int R, float rows, int N, int K, bool gated, int terms)
+CutModel stream_cut_model(int R, float rows, int N, int K, bool gated, int terms, long row_tiles)
 {
     const int slabs = stream_slabs(N, gated);
     const float step_bytes = slabs * kSlabBytes + terms * rows * 128;
     CutModel m;
     m.kb = ceil_div(K, kKT);
     m.column_tiles = ceil_div(N, gated ? kSlab : slabs * kSlab);
-    m.most_chunks = most_chunks(R, N, gated);
+    m.most_chunks = most_chunks(R, N, K, gated, row_tiles);
     m.alone_us = std::max(0.245f, step_bytes / 96e3f);
     m.busy_us = std::max(m.alone_us, kSMs * (float)(slabs * kSlabBytes) / 6.9e6f);
     m.sums_us = std::max(4.f, rows) * slabs * kSlab * 4 / 35e3f;
@@ -647,7 +656,7 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
 {
     StreamArgs a{};
     const int slabs = stream_slabs(p.N, gated);
-    const CutModel m = stream_cut_model(p.R, (float)std::min(p.rows, p.R), p.N, p.K, gated, p.terms);
+    const CutModel m = stream_cut_model(p.R, p.expected_rows, p.N, p.K, gated, p.terms, p.row_tiles);
     a.kb = m.kb;
     a.tile_n = gated ? kSlab : slabs * kSlab;
     a.column_tiles = m.column_tiles;
@@ -663,6 +672,7 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     a.stage_bytes = slabs * kSlabBytes + p.terms * p.R * 128;
     a.nstage = std::min(kMaxStages, kRingBytes / a.stage_bytes);
     a.apart = p.terms == 2 && p.R <= 64;
+    a.few = p.expected_rows <= 4.f;
     a.acc_columns = a.apart ? 2 * p.R : p.R;
     a.tmem_columns = std::max(32, 2 * slabs * a.acc_columns);
     a.gather = p.gather; a.planned = p.planned; a.early_weights = p.early_weights; a.programmatic = p.programmatic;
@@ -675,7 +685,7 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     a.in_residual = make_span(p.residual, p.residual ? 2 * ((size_t)(p.rows - 1) * p.ld_residual + p.N) : 0);
     a.in_out = make_span(p.out, mode == kOutAct ? 2 * ((size_t)(p.rows - 1) * p.ldo + p.N) : 4 * (size_t)p.rows * p.ldo);
     a.in_scale = make_span(p.row_scale, p.row_scale ? 4 * (size_t)p.rows : 0);
-    a.in_partial = make_span(p.partial, stream_partial_bytes(p.R, p.N, gated));
+    a.in_partial = make_span(p.partial, stream_partial_bytes(p.R, p.N, p.K, gated, p.row_tiles));
     a.in_tiles = make_span(p.plan.tiles, sizeof(RowTile) * ((size_t)p.E + p.rows / p.R));
     a.in_order = make_span(p.plan.order, 4 * (size_t)p.rows);
     a.status = device_status_ptr();
