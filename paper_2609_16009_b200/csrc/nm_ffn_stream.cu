@@ -664,9 +664,16 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     a.rows = p.rows; a.N = p.N; a.R = p.R;
     if (!p.planned) {
         const int items = ceil_div(p.rows, p.R) * a.column_tiles, rest = items - whole_items(items);
+        // (one number of parts for each length that a chunk can have)
+        const int most = std::min(std::min(a.kb, kSMs), m.most_chunks / rest);
         int best = 1;
-        for (int parts = 2; parts <= std::min(a.kb, kSMs) && rest * parts <= m.most_chunks; ++parts)
-            if (cut_cost(m, rest, parts) < cut_cost(m, rest, best)) best = parts;
+        float least = cut_cost(m, rest, 1);
+        for (int parts = 2; parts <= most;) {
+            const float cost = cut_cost(m, rest, parts);
+            if (cost < least) { least = cost; best = parts; }
+            const int kc = ceil_div(a.kb, parts);
+            parts = kc > 1 ? std::max(parts + 1, ceil_div(a.kb, kc - 1)) : most + 1;
+        }
         a.schedule = schedule_of(items, a.kb, best);
     }
     a.stage_bytes = slabs * kSlabBytes + p.terms * p.R * 128;
@@ -712,7 +719,10 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
         ok = ok && encode_map(&x.of[0], p.x, p.f16, 2, dims, strides, box);
     } else {
         const cuuint64_t dims[3] = {(cuuint64_t)p.K, (cuuint64_t)p.x_rows, (cuuint64_t)p.terms}, strides[2] = {(cuuint64_t)p.ldx * 2, (cuuint64_t)p.x_term * 2};
-        for (int i = 0; (i + 1) * a.box_rows <= p.R; ++i) {
+        // (only the heights that there can be: of a full tile and of the last one, where the rows are known)
+        const int whole_box = p.R / a.box_rows - 1, last_box = p.planned ? 0 : (p.rows - 1) % p.R / a.box_rows;
+        for (int i = 0; i <= whole_box; ++i) {
+            if (!p.planned && i != last_box && (i != whole_box || p.rows < p.R)) continue;
             const cuuint32_t box[3] = {kKT, (cuuint32_t)((i + 1) * a.box_rows), 1};
             ok = ok && encode_map(&x.of[i], p.x, p.f16, 3, dims, strides, box);
         }
