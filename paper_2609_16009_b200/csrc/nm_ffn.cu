@@ -160,14 +160,13 @@ __global__ void __launch_bounds__(256) combine_kernel(const CombineArgs a)
                     float v[8][kV];
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {
-                        const int row = j + q < here ? s_row[j + q] : -1;
-                        const float *y = a.y + (long)row * a.d + n;
+                        // (some row where there is none: a load under a condition would wait for the one before it)
+                        const float *y = a.y + (long)max(s_row[min(j + q, here - 1)], 0) * a.d + n;
                         if constexpr (kV == 4) {
-                            float4 f = make_float4(0.f, 0.f, 0.f, 0.f);
-                            if (row >= 0) f = NM_LD(reinterpret_cast<const float4 *>(y), a.in_y, a.status);
+                            const float4 f = NM_LD(reinterpret_cast<const float4 *>(y), a.in_y, a.status);
                             v[q][0] = f.x; v[q][1] = f.y; v[q][2] = f.z; v[q][3] = f.w;
                         } else {
-                            v[q][0] = row >= 0 ? NM_LD(y, a.in_y, a.status) : 0.f;
+                            v[q][0] = NM_LD(y, a.in_y, a.status);
                         }
                     }
 #pragma unroll

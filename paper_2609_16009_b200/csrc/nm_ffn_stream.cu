@@ -236,11 +236,10 @@ __device__ __forceinline__ TokenCopy<kGathers<kMode>> token_copy(const StreamArg
 }
 
 // Sums of a chunk lie in groups of four rows, [group][slab][128 outputs][4 rows]: a thread moves 16 bytes at a time.  Adds up the `parts` chunks of an
-// item from slot `first` on for the groups from rows j, j + step .. on, in the order of k; several chunks are asked for at once.
-template <int kSlabs, int kGroups>
+// item from slot `first` on for the groups from rows j, j + step .. on, in the order of k; kAhead chunks are asked for at once.
+template <int kSlabs, int kGroups, int kAhead>
 __device__ __forceinline__ void join(const StreamArgs &a, int j, int step, int first, int parts, int n_lane, float (&z)[kGroups][kSlabs][4])
 {
-    constexpr int kAhead = 4 / kSlabs;                           // (more of them cost registers, and with those the rest of the epilogue)
 #pragma unroll
     for (int g = 0; g < kGroups; ++g)
 #pragma unroll
@@ -252,16 +251,16 @@ __device__ __forceinline__ void join(const StreamArgs &a, int j, int step, int f
     const int further = step / 4 * (kSlabs * kSlab);
     for (int p0 = 0; p0 < parts; p0 += kAhead) {
         float4 v[kAhead][kGroups][kSlabs];
+        // (the last chunk again where there are no more: a load under a condition would wait for the one before it)
 #pragma unroll
         for (int q = 0; q < kAhead; ++q)
-            if (p0 + q < parts)
 #pragma unroll
-                for (int g = 0; g < kGroups; ++g)
+            for (int g = 0; g < kGroups; ++g)
 #pragma unroll
-                    for (int sl = 0; sl < kSlabs; ++sl) {
-                        const float4 *at = from + (p0 + q) * piece + g * further + sl * kSlab;
-                        v[q][g][sl] = NM_INSIDE(at, 16, a.in_partial, a.status) ? __ldcg(at) : make_float4(0.f, 0.f, 0.f, 0.f);
-                    }
+                for (int sl = 0; sl < kSlabs; ++sl) {
+                    const float4 *at = from + min(p0 + q, parts - 1) * piece + g * further + sl * kSlab;
+                    v[q][g][sl] = NM_INSIDE(at, 16, a.in_partial, a.status) ? __ldcg(at) : make_float4(0.f, 0.f, 0.f, 0.f);
+                }
 #pragma unroll
         for (int q = 0; q < kAhead; ++q)
             if (p0 + q < parts)
@@ -540,13 +539,14 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                     int j = 4 * turn;
                     for (; j + step < t.rows; j += 2 * step) {
                         float z[2][kSlabs][4];
-                        join<kSlabs, 2>(a, j, step, c.first_slot, sched.parts, n_lane, z);
+                        // (items of the experts' products are cut into few parts; asking for more of them cost 67 tokens through 3 of 24 experts 4 us of 72)
+                        join<kSlabs, 2, (kMode == kOutAct ? 8 : 4) / kSlabs>(a, j, step, c.first_slot, sched.parts, n_lane, z);
                         put_next(z[0], j);
                         put_next(z[1], j + step);
                     }
                     if (j < t.rows) {
                         float z[1][kSlabs][4];
-                        join<kSlabs, 1>(a, j, step, c.first_slot, sched.parts, n_lane, z);
+                        join<kSlabs, 1, 8 / kSlabs>(a, j, step, c.first_slot, sched.parts, n_lane, z);
                         put_next(z[0], j);
                     }
                 }
