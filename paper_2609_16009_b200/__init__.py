@@ -142,6 +142,25 @@ _lib.nm_debug_wait_probe.argtypes = [C.c_ulonglong, _vp, _vp]
 _lib.nm_debug_mma_probe.argtypes = [_i] * 8 + [_vp, _vp]
 
 
+try:
+    # The short calls' way into the library (csrc/nm_python.c): the same arguments without ctypes' marshalling.
+    from . import _nm_calls as _calls
+    _calls.bind(*(C.cast(getattr(_lib, n), _vp).value for n in ("nm_moe_route", "nm_matmul_act", "nm_moe_ffn")))
+except ImportError:
+    _calls = None
+_bound_lib = _lib
+
+
+def _call(name: str, *args) -> None:
+    """The entry point `name` with its arguments in order; tensors stand for their data."""
+    if _calls is not None and _lib is _bound_lib:
+        status = getattr(_calls, name)(*args)
+    else:
+        status = getattr(_lib, name)(*[a.data_ptr() if hasattr(a, "data_ptr") else a for a in args])
+    if status != 0:
+        raise NmError(status, name)
+
+
 def _check(status: int, where: str) -> None:
     if status != 0:
         raise NmError(status, where)
@@ -370,8 +389,8 @@ def nm_mla_attention_q8(Q, prefix, prefix_rows, cache, cache_stride, seq_lens, o
 def nm_moe_route(logits, bias, experts, weights, T, E, top_k, dtype, score=SCORE_SOFTMAX, groups=1, keep_groups=1, group_best=1, renormalise=True, scale=1.0,
                  ld_logits=None, stream=None) -> None:
     """bias (fp32) may be None; experts int32 and weights fp32, dense [T][top_k]; ld_logits defaults to dense rows."""
-    _check(_lib.nm_moe_route(_ptr(logits), E if ld_logits is None else ld_logits, _ptr(bias), _ptr(experts), _ptr(weights), T, E, top_k, dtype, score, groups,
-                             keep_groups, group_best, int(renormalise), scale, _stream(stream)), "nm_moe_route")
+    _call("nm_moe_route", logits, E if ld_logits is None else ld_logits, bias, experts, weights, T, E, top_k, dtype, score, groups, keep_groups, group_best, int(renormalise),
+          float(scale), _stream(stream))
 
 
 def nm_matmul_act_workspace_bytes(M, N, K, gated=False, dtype=BF16) -> int:
@@ -381,9 +400,8 @@ def nm_matmul_act_workspace_bytes(M, N, K, gated=False, dtype=BF16) -> int:
 def nm_matmul_act(A, B, C_out, M, N, K, act, dtype, layout_B, workspace, gated=False, bias=None, residual=None, lda=None, ldc=None, ld_residual=None,
                   stream=None) -> None:
     """N: columns of C; B has 2 N where gated.  lda, ldc and ld_residual default to dense rows."""
-    _check(_lib.nm_matmul_act(_ptr(A), K if lda is None else lda, _ptr(B), _ptr(bias), _ptr(residual), N if ld_residual is None else ld_residual, _ptr(C_out),
-                              N if ldc is None else ldc, M, N, K, act, int(gated), dtype, layout_B, _ptr(workspace),
-                              0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "nm_matmul_act")
+    _call("nm_matmul_act", A, K if lda is None else lda, B, bias, residual, N if ld_residual is None else ld_residual, C_out, N if ldc is None else ldc, M, N, K, act, int(gated),
+          dtype, layout_B, workspace, 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream))
 
 
 def nm_moe_ffn_workspace_bytes(T, d, inter, E, top_k, dtype=BF16) -> int:
@@ -393,9 +411,8 @@ def nm_moe_ffn_workspace_bytes(T, d, inter, E, top_k, dtype=BF16) -> int:
 def nm_moe_ffn(x, experts, weights, W_up, W_down, out, T, d, inter, E, top_k, act, dtype, layout, workspace, gated=True, residual=None, first_expert=0, ldx=None,
                ldo=None, ld_residual=None, stream=None) -> None:
     """weights and residual may be None; ldx, ldo and ld_residual default to dense rows."""
-    _check(_lib.nm_moe_ffn(_ptr(x), d if ldx is None else ldx, _ptr(experts), _ptr(weights), _ptr(W_up), _ptr(W_down), _ptr(residual),
-                           d if ld_residual is None else ld_residual, _ptr(out), d if ldo is None else ldo, T, d, inter, E, top_k, first_expert, act, int(gated),
-                           dtype, layout, _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream)), "nm_moe_ffn")
+    _call("nm_moe_ffn", x, d if ldx is None else ldx, experts, weights, W_up, W_down, residual, d if ld_residual is None else ld_residual, out, d if ldo is None else ldo, T, d, inter, E,
+          top_k, first_expert, act, int(gated), dtype, layout, workspace, 0 if workspace is None else workspace.numel() * workspace.element_size(), _stream(stream))
 
 
 def mla_params(dims: dict, seq_len: int, tensors: dict, rms_eps=1e-6, softmax_scale=None, layout_dense=ROW_MAJOR,

@@ -11,6 +11,7 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
@@ -18,6 +19,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OBJ = os.path.join(ROOT, "build", "nm")
 LIB = os.path.join(PKG, "libnm.so")
+CALLS_SRC = os.path.join(CSRC, "nm_python.c")
+CALLS = os.path.join(PKG, "_nm_calls" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden", "--threads", "2"]
@@ -28,6 +31,21 @@ def _nvcc() -> str:
         if c and (os.path.isabs(c) and os.path.exists(c) or not os.path.isabs(c)):
             return c
     raise RuntimeError("nvcc not found")
+
+
+def build_calls() -> str | None:
+    """The extension module through which the binding makes its short calls (csrc/nm_python.c); None where Python's headers are missing: they go through ctypes then."""
+    include = sysconfig.get_paths()["include"]
+    if not os.path.exists(os.path.join(include, "Python.h")):
+        return None
+    if not os.path.exists(CALLS) or os.path.getmtime(CALLS) < os.path.getmtime(CALLS_SRC):
+        tmp = CALLS + f".tmp{os.getpid()}"
+        r = subprocess.run([os.environ.get("CC", "gcc"), "-O2", "-Wall", "-shared", "-fPIC", "-I", include, CALLS_SRC, "-o", tmp], capture_output=True, text=True)
+        if r.returncode != 0:
+            sys.stderr.write(r.stdout + r.stderr)
+            raise RuntimeError("gcc failed on nm_python.c")
+        os.replace(tmp, CALLS)
+    return CALLS
 
 
 def build(verbose: bool = False, force: bool = False, ptxas_info: bool = False, check: bool = False) -> str:
@@ -70,6 +88,8 @@ def build(verbose: bool = False, force: bool = False, ptxas_info: bool = False, 
             sys.stderr.write(r.stdout + r.stderr)
             raise RuntimeError("link failed")
         os.replace(tmp, LIB)
+    if not check:
+        build_calls()
     return LIB
 
 
