@@ -15,6 +15,7 @@ namespace nm {
 
 namespace {
 
+static_assert(kCounterWords * sizeof(unsigned) <= NM_WS_COUNTER_BYTES, "the counters have a place of their own");
 constexpr int kMaxPairs = 1 << 22, kMaxDim = 1 << 20;  // (items and chunks are then counted in 32 bits)
 
 // ---- products of operands of any alignment -----------------------------------------------------------------------------------
@@ -249,13 +250,8 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a)
     if (mine == a.E - 1) {
         if (tid == 0) *a.n_rows = row0 + count;
         if (warp < 2) {                                           // a warp a product: a lane for each number of parts
-            const CutModel &m = a.model[warp];
-            const int items = (tile0 + own) * m.column_tiles, rest = items - whole_items(items), parts = lane + 1;
-            const bool may = parts == 1 || (parts <= m.kb && (long)rest * parts <= m.most_chunks);
-            const float cost = may ? cut_cost(m, rest, parts) : INFINITY;
-            const unsigned least = __reduce_min_sync(0xffffffffu, __float_as_uint(cost));       // (costs are not negative: their bits order as they do)
-            const int best = __ffs((int)__ballot_sync(0xffffffffu, __float_as_uint(cost) == least));
-            if (lane == 0) a.schedules[warp] = schedule_of(items, m.kb, best);
+            const Schedule best = best_schedule(a.model[warp], tile0 + own, lane);
+            if (lane == 0) a.schedules[warp] = best;
         }
     }
     if (mine == 0) for (int i = tid; i < kCounterWords; i += kPlanThreads) a.counters[i] = 0u;
@@ -375,7 +371,7 @@ MoeLayout moe_layout(long pairs, int d, int inter, int E, bool f16)
 {
     const int R = stream_tile_rows((double)pairs / E, (int)std::min<long>(pairs, 128));
     MoeLayout l{};
-    size_t at = align256(kCounterWords * sizeof(unsigned));
+    size_t at = NM_WS_COUNTER_BYTES;
     l.n_rows = at; at += 256;
     l.schedules = at; at += 256;
     l.tiles = at; at += align256((E + pairs / 16) * sizeof(RowTile));
@@ -499,13 +495,14 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
         pl.in_order = make_span(pl.order, 4 * (size_t)pairs); pl.in_place = make_span(pl.place, 4 * (size_t)pairs);
         pl.status = status;
         place = pl.place;
-        e = launch(plan_kernel, E, kPlanThreads, programmatic, s, pl);
+        const bool own_plan = pl.R <= 16 && pairs <= kOwnPairs;
+        e = own_plan ? cudaSuccess : launch(plan_kernel, E, kPlanThreads, programmatic, s, pl);
 
         ProductArgs p{};
         p.rows = (int)pairs; p.N = inter; p.K = d; p.R = pl.R; p.expected_rows = rows; p.row_tiles = E + pairs / pl.R; p.terms = 1;
-        p.col = col; p.f16 = f16; p.planned = p.programmatic = true;
+        p.col = col; p.f16 = f16; p.planned = true; p.programmatic = own_plan ? programmatic : true;
         p.act = act;
-        p.plan = RowPlan{pl.tiles, pl.schedules, pl.order};
+        p.plan = RowPlan{pl.tiles, pl.schedules, pl.order, own_plan ? (int)pairs : 0, experts, first_expert, E, top_k, pl.place};
         p.W = W_up; p.w_expert = (long)parts * inter * d; p.E = E;
         p.gather = pl.R <= 16;
         if (p.gather) {
@@ -529,7 +526,7 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
 
         ProductArgs q = p;
         q.N = d; q.K = inter; q.terms = 2; q.gather = false; q.early_weights = true; q.act = NM_ACT_NONE;
-        q.plan.schedule = pl.schedules + 1; q.ticket = kTicketDown;
+        q.programmatic = true; q.plan.schedule = pl.schedules + 1; q.ticket = kTicketDown;
         q.W = W_down; q.w_expert = (long)inter * d;
         q.x = terms; q.ldx = inter; q.x_rows = pairs; q.x_term = pairs * inter;
         q.row_scale = f16 ? row_scale : nullptr;

@@ -49,7 +49,12 @@ struct RowPlan {
     const RowTile *tiles;
     const Schedule *schedule;          // of this product
     const int *order;                  // [sorted row] -> token
+    // Few pairs (up to kOwnPairs, in gathered tiles): every CTA makes the plan itself, in shared memory, and no kernel has to come first.  0: it is there.
+    int own_pairs;
+    const int32_t *experts; int first, E, top_k;
+    int *place;                        // [pair] -> sorted row, for the weighted sum
 };
+constexpr int kOwnPairs = 128;
 
 // Words of the counter area: a ticket for each product of a call (the chunks dealt out beyond one for each CTA), CTAs that are done, and the chunks there
 // are of an item that is cut.
@@ -75,6 +80,16 @@ __host__ __device__ inline Schedule schedule_of(int items, int kb, int parts)
 {
     const int whole = whole_items(items), kc = (kb + parts - 1) / parts, p = (kb + kc - 1) / kc;
     return p > 1 ? Schedule{whole, p, kc, whole + (items - whole) * p} : Schedule{items, 1, kb, items};
+}
+
+// The best schedule for `tiles` row tiles: by a warp, a lane for each number of parts.
+__device__ __forceinline__ Schedule best_schedule(const CutModel &m, int tiles, int lane)
+{
+    const int items = tiles * m.column_tiles, rest = items - whole_items(items), parts = lane + 1;
+    const bool may = parts == 1 || (parts <= m.kb && (long)rest * parts <= m.most_chunks);
+    const float cost = may ? cut_cost(m, rest, parts) : INFINITY;
+    const unsigned least = __reduce_min_sync(0xffffffffu, __float_as_uint(cost));                // (costs are not negative: their bits order as they do)
+    return schedule_of(items, m.kb, __ffs((int)__ballot_sync(0xffffffffu, __float_as_uint(cost) == least)));
 }
 
 // One product of the streaming kernel (nm_ffn_stream.cu): rows of a token operand against weights of their expert.

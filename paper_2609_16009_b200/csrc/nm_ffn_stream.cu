@@ -50,14 +50,15 @@ struct StreamArgs {
     int acc_columns;                            // of a slab: R, twice that where the terms have columns of their own
     bool apart, few;                            // few: four rows or fewer in a tile, as far as that is known: four epilogue warps then
     unsigned tmem_columns;
-    bool gather, planned, early_weights, programmatic;
+    bool gather, clears, early_weights, programmatic;   // clears: the tickets, for the call that follows
     int act;
     RowPlan plan;
+    CutModel model;                             // (of a plan made here)
     const uint16_t *bias, *residual; long ld_residual;
     void *out; long ldo; long out_term;
     const float *row_scale;
     float *partial; unsigned *counters; int ticket;
-    Span in_bias, in_residual, in_out, in_scale, in_partial, in_tiles, in_order;
+    Span in_bias, in_residual, in_out, in_scale, in_partial, in_tiles, in_order, in_experts, in_place;
     unsigned *status;
 };
 
@@ -96,12 +97,65 @@ __device__ __forceinline__ Chunk chunk_of(const Schedule &s, int kb, int id)
     return Chunk{s.whole + cut, k0, min(kb, k0 + s.kc), at, cut * s.parts, cut};
 }
 
+// A plan made by the CTA itself, see RowPlan: tiles as (expert and rows, first row), the tokens of the sorted rows, the schedule.
+struct OwnPlan {
+    Schedule schedule;
+    uint2 tiles[kOwnPairs];
+    uint16_t order[kOwnPairs], expert[kOwnPairs], tiles_of[kOwnPairs];
+};
+// By all threads of the CTA (at least kOwnPairs of them).  A thread a pair: how many pairs have lower experts, and how many of its own come before, is where its row lies;
+// the first pair of an expert stands for it.
+__device__ __forceinline__ void make_plan(const StreamArgs &a, OwnPlan &own, bool place_too)
+{
+    const int p = threadIdx.x, pairs = a.plan.own_pairs, lane = p & 31;
+    int e = 0xffff;                                               // not held here
+    if (p < pairs) {
+        const long v = (long)NM_LD(a.plan.experts + p, a.in_experts, a.status) - a.plan.first;
+        if (v >= 0 && v < a.plan.E) e = (int)v;
+        own.expert[p] = (uint16_t)e;
+    }
+    __syncthreads();
+    int lower = 0, before = 0, all = 0;
+    if (e != 0xffff)
+        for (int q = 0; q < pairs; ++q) {
+            const int other = own.expert[q];
+            lower += other < e;
+            before += other == e && q < p;
+            all += other == e;
+        }
+    const int tiles = e != 0xffff && before == 0 ? ceil_div(all, a.R) : 0;
+    if (p < pairs) own.tiles_of[p] = (uint16_t)tiles;
+    if (e != 0xffff) {
+        own.order[lower + before] = (uint16_t)(p / a.plan.top_k);
+        if (place_too) NM_ST(a.plan.place + p, lower + before, a.in_place, a.status);
+    }
+    __syncthreads();
+    if (tiles > 0) {
+        int at = 0;
+        for (int q = 0; q < pairs; ++q) at += own.expert[q] < e ? own.tiles_of[q] : 0;
+        for (int i = 0; i < tiles; ++i) own.tiles[at + i] = make_uint2((unsigned)e | (unsigned)min(a.R, all - i * a.R) << 16, (unsigned)(lower + i * a.R));
+    }
+    if (p < 32) {                                                 // a lane for each number of parts
+        int total = 0;
+        for (int q = lane; q < pairs; q += 32) total += own.tiles_of[q];
+        total = __reduce_add_sync(0xffffffffu, total);
+        const Schedule s = best_schedule(a.model, total, lane);
+        if (lane == 0) own.schedule = s;
+    }
+    __syncthreads();
+}
+
 // One item: its rows and outputs.
 struct Item { int expert, row0, rows, n0; };
-__device__ __forceinline__ Item item_of(const StreamArgs &a, int item)
+template <int kMode>
+__device__ __forceinline__ Item item_of(const StreamArgs &a, const OwnPlan &own, int item)
 {
     const int tile = item / a.column_tiles, n0 = (item - tile * a.column_tiles) * a.tile_n;
-    if (a.planned) {
+    if constexpr (kMode != kOutAct) {
+        if (a.plan.own_pairs) {
+            const uint2 t = own.tiles[tile];
+            return Item{(int)(t.x & 0xffffu), (int)t.y, (int)(t.x >> 16), n0};
+        }
         const RowTile *at = a.plan.tiles + tile;
         const int4 t = NM_INSIDE(at, 16, a.in_tiles, a.status) ? __ldcg(reinterpret_cast<const int4 *>(at)) : make_int4(0, 0, 1, 0);
         return Item{t.x, t.y, t.z, n0};
@@ -222,7 +276,7 @@ template <int kMode> constexpr bool kGathers = kMode == kOutHidden;
 template <int kMode> constexpr int kTerms = kMode == kOutDown ? 2 : 1;
 template <bool kGather> struct TokenCopy { int ids[kGather ? kGathered : 1], boxes; uint32_t term_bytes, step_bytes; };
 template <int kMode>
-__device__ __forceinline__ TokenCopy<kGathers<kMode>> token_copy(const StreamArgs &a, const Item &t, int slabs)
+__device__ __forceinline__ TokenCopy<kGathers<kMode>> token_copy(const StreamArgs &a, const OwnPlan &own, const Item &t, int slabs)
 {
     TokenCopy<kGathers<kMode>> x;
     x.boxes = ceil_div(t.rows, a.box_rows);
@@ -230,7 +284,7 @@ __device__ __forceinline__ TokenCopy<kGathers<kMode>> token_copy(const StreamArg
     x.step_bytes = (uint32_t)slabs * kSlabBytes + (kGathers<kMode> && a.gather ? (uint32_t)ceil_div(t.rows, 4) * 512u : (uint32_t)(x.boxes * a.box_rows * kTerms<kMode>) * 128u);
     if (kGathers<kMode> && a.gather) {
 #pragma unroll
-        for (int i = 0; i < (kGathers<kMode> ? kGathered : 0); ++i) x.ids[i] = i < t.rows && NM_INSIDE(a.plan.order + t.row0 + i, 4, a.in_order, a.status) ? __ldcg(a.plan.order + t.row0 + i) : 0;
+        for (int i = 0; i < (kGathers<kMode> ? kGathered : 0); ++i) x.ids[i] = i >= t.rows ? 0 : a.plan.own_pairs ? own.order[t.row0 + i] : NM_INSIDE(a.plan.order + t.row0 + i, 4, a.in_order, a.status) ? __ldcg(a.plan.order + t.row0 + i) : 0;
     }
     return x;
 }
@@ -284,6 +338,8 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
     __shared__ uint32_t s_tmem;
     __shared__ int s_abort, s_queue[kQueue], s_next[2];
     __shared__ unsigned s_last;
+    __shared__ typename std::conditional<kMode == kOutAct, char, OwnPlan>::type s_plan;
+    const OwnPlan &own = reinterpret_cast<const OwnPlan &>(s_plan);
     const uint32_t full0 = smem_u32(s_bars), empty0 = full0 + 8 * kMaxStages, queued0 = empty0 + 8 * kMaxStages, taken0 = queued0 + 8 * kQueue,
                    acc_full0 = taken0 + 8 * kQueue, acc_empty0 = acc_full0 + 16, drained = acc_empty0 + 16;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -330,23 +386,28 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
     };
     if (warp == 1) tmem_alloc(&s_tmem, a.tmem_columns);
     __syncthreads();                                           // (the barriers are there)
-    // The plan of a programmatic chain is two kernels back and complete (the kernel before waited for it): only what the kernel before wrote has to
-    // be waited for.  Without early_weights everything is behind the wait.
+    // The plan of a programmatic chain (or the experts it is made of) is two kernels back and complete, as the kernel before waited for it: only what the kernel
+    // before wrote has to be waited for.  Without early_weights everything is behind the wait.
     if (!a.early_weights) pdl_wait_prior_grids();
-    if (a.programmatic) pdl_launch_dependents();
+    pdl_launch_dependents();
     // The first fills are dealt out to all of the warps: a request costs the thread that makes it 100 clocks and more, so one thread took 2 us for a ring of twelve stages.
     Schedule sched = a.schedule;
-    if (a.planned) {
-        const int4 v = __ldcg(reinterpret_cast<const int4 *>(a.plan.schedule));
-        sched = Schedule{v.x, v.y, v.z, v.w};
+    if constexpr (kMode != kOutAct) {
+        if (a.plan.own_pairs) {
+            make_plan(a, s_plan, kMode == kOutHidden && blockIdx.x == 0);
+            sched = own.schedule;
+        } else {
+            const int4 v = __ldcg(reinterpret_cast<const int4 *>(a.plan.schedule));
+            sched = Schedule{v.x, v.y, v.z, v.w};
+        }
     }
     if (first_id < sched.chunks) {
         const Chunk c = chunk_of(sched, a.kb, first_id);
         head = min(NS, c.k1 - c.k0);
         if (lane == 0 && warp < head) {
             const int warps = (int)blockDim.x / 32;
-            const Item t = item_of(a, c.item);
-            const auto x = token_copy<kMode>(a, t, kSlabs);
+            const Item t = item_of<kMode>(a, own, c.item);
+            const auto x = token_copy<kMode>(a, own, t, kSlabs);
             for (int i = warp; i < head; i += warps) {
                 mbar_arrive_expect_tx(full0 + 8 * i, x.step_bytes);
                 weights(t, c.k0 + i, i);
@@ -374,10 +435,10 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             // (a ticket takes 1 to 2 us), and late enough that whoever is done first takes what is left.
             Item t{}, t_next{};
             unsigned ticket = 0u;
-            if (first_id < sched.chunks) t = item_of(a, chunk_of(sched, a.kb, first_id).item);
+            if (first_id < sched.chunks) t = item_of<kMode>(a, own, chunk_of(sched, a.kb, first_id).item);
             for (int id = first_id; ok && id < sched.chunks;) {
                 const Chunk c = chunk_of(sched, a.kb, id);
-                const auto x = token_copy<kMode>(a, t, kSlabs);
+                const auto x = token_copy<kMode>(a, own, t, kSlabs);
                 const int ask_at = max(c.k0, c.k1 - 8), read_at = max(c.k0, c.k1 - 3);
                 id = sched.chunks;
                 for (int k = c.k0; k < c.k1; ++k, ++n) {
@@ -385,7 +446,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                         if (k == ask_at) ticket = ask_ticket(a.counters + a.ticket);
                         if (k == read_at) {
                             id = (int)min(gridDim.x + ticket, (unsigned)sched.chunks);
-                            if (id < sched.chunks) t_next = item_of(a, chunk_of(sched, a.kb, id).item);
+                            if (id < sched.chunks) t_next = item_of<kMode>(a, own, chunk_of(sched, a.kb, id).item);
                         }
                     }
                     if (n >= head) {
@@ -406,7 +467,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                 }
             }
             // Every CTA has had its last ticket (the value is looked at, so it has come): whoever is last to say so clears them for the next call.
-            if (more_than_one && !a.planned && ticket != 0xffffffffu && atomicAdd(a.counters + kDone, 1u) == gridDim.x - 1) {
+            if (more_than_one && a.clears && ticket != 0xffffffffu && atomicAdd(a.counters + kDone, 1u) == gridDim.x - 1) {
                 a.counters[a.ticket] = 0u;
                 a.counters[kDone] = 0u;
             }
@@ -419,7 +480,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
         bool ok = true;
         for (int id = first_id; id < sched.chunks;) {
             const Chunk c = chunk_of(sched, a.kb, id);
-            const Item t = item_of(a, c.item);
+            const Item t = item_of<kMode>(a, own, c.item);
             const int columns = kTerms<kMode> == 2 && a.apart ? 2 * ceil_div(t.rows, a.box_rows) * a.box_rows : (t.rows + 15) & ~15;
             const uint32_t idesc = kF16 ? instr_desc_f16(kSlab, columns, !kCol, false) : instr_desc(kSlab, columns, !kCol, false);
             const bool twice = kTerms<kMode> == 2 && !a.apart;
@@ -469,7 +530,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
         uint32_t ph = 0, queue_ph = 0;
         for (int id = first_id; id < sched.chunks; round ^= 1) {
             const Chunk c = chunk_of(sched, a.kb, id);
-            const Item t = item_of(a, c.item);
+            const Item t = item_of<kMode>(a, own, c.item);
             Rows<kMode, kGated, kSlabs, kF16> rows(a, t, 4 * turn, step, n_lane);
             if (kMode == kOutAct && a.residual) {
                 // (a lane a row: this warp's rows are four of every `step`)
@@ -682,8 +743,8 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     a.few = p.expected_rows <= 4.f;
     a.acc_columns = a.apart ? 2 * p.R : p.R;
     a.tmem_columns = std::max(32, 2 * slabs * a.acc_columns);
-    a.gather = p.gather; a.planned = p.planned; a.early_weights = p.early_weights; a.programmatic = p.programmatic;
-    a.act = p.act; a.plan = p.plan;
+    a.gather = p.gather; a.clears = !p.planned || p.plan.own_pairs; a.early_weights = p.early_weights; a.programmatic = p.programmatic;
+    a.act = p.act; a.plan = p.plan; a.model = m;
     a.bias = static_cast<const uint16_t *>(p.bias); a.residual = static_cast<const uint16_t *>(p.residual); a.ld_residual = p.ld_residual;
     a.out = p.out; a.ldo = p.ldo; a.out_term = (long)p.rows * p.ldo; a.row_scale = p.row_scale;
     a.partial = p.partial; a.counters = p.counters; a.ticket = p.ticket;
@@ -695,6 +756,7 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     a.in_partial = make_span(p.partial, stream_partial_bytes(p.R, p.N, p.K, gated, p.row_tiles));
     a.in_tiles = make_span(p.plan.tiles, sizeof(RowTile) * ((size_t)p.E + p.rows / p.R));
     a.in_order = make_span(p.plan.order, 4 * (size_t)p.rows);
+    a.in_experts = make_span(p.plan.experts, 4 * (size_t)p.plan.own_pairs); a.in_place = make_span(p.plan.place, 4 * (size_t)p.plan.own_pairs);
     a.status = device_status_ptr();
 
     CUtensorMap w[2];

@@ -56,6 +56,32 @@ def test_many_pairs():
     assert_within(moe_tests.run(c, SILU, True, BF16, COL), *moe_tests.expected(c, SILU, True, BF16))
 
 
+@pytest.mark.parametrize("T,E,k", [(1, 40, 6), (20, 40, 6), (21, 40, 6), (22, 40, 6), (128, 64, 1), (129, 64, 1), (64, 64, 2), (2, 200, 64), (43, 1000, 3)])
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_plans_around_the_pairs_a_block_plans_itself(T, E, k, dtype):
+    c = moe_tests.make(T, 136, 72, E, k, dtype, T + E)
+    c["experts"][T // 2] = -1
+    c["experts"][-1, 0] = E
+    for skewed in (False, True):
+        if skewed:
+            c["experts"][: 3 * T // 4 + 1, 0] = E - 1              # several tiles of one expert
+        assert_within(moe_tests.run(c, SILU, True, dtype, COL), *moe_tests.expected(c, SILU, True, dtype))
+
+
+def test_one_workspace_for_experts_of_all_sizes(cut):
+    """Calls that plan themselves and calls that do not, cut and whole, through one workspace: the counters are left as they were found."""
+    import paper_2609_16009_b200 as nm
+    ws = nm.new_workspace(128 << 20)
+    for i, (T, d, inter, E, k, parts) in enumerate([(1, 1024, 264, 8, 2, 3), (300, 256, 136, 5, 2, 2), (2, 4096, 128, 50, 6, 0), (20, 264, 520, 40, 6, 5), (40, 264, 136, 3, 3, 0), (1, 72, 64, 4, 1, 0)]):
+        cut(parts)
+        c = moe_tests.make(T, d, inter, E, k, BF16, 80 + i)
+        out = torch.zeros(T, d, dtype=torch.bfloat16, device="cuda")
+        for _ in range(3):
+            moe_tests.call(nm, c, SILU, True, BF16, COL, out, ws)
+        assert_within(out, *moe_tests.expected(c, SILU, True, BF16))
+        assert int(ws[:65536].count_nonzero()) == 0
+
+
 def test_many_experts_few_tokens():
     c = moe_tests.make(3, 72, 64, 1024, 32, BF16, 4)
     assert_within(moe_tests.run(c, SILU, True, BF16, ROW), *moe_tests.expected(c, SILU, True, BF16))
@@ -72,7 +98,7 @@ def test_weights_of_experts_beyond_32_bit_offsets():
     down[-1] = torch.randn(d, inter, generator=g, device="cuda").bfloat16() * inter ** -0.5
     y = torch.zeros(T, d, dtype=torch.bfloat16, device="cuda")
     nm.nm_moe_ffn(x, torch.full((T, 1), E - 1, dtype=torch.int32, device="cuda"), None, up, down, y, T, d, inter, E, k, SILU, BF16, COL,
-                  torch.empty(nm.nm_moe_ffn_workspace_bytes(T, d, inter, E, k), dtype=torch.uint8, device="cuda"))
+                  nm.new_workspace(nm.nm_moe_ffn_workspace_bytes(T, d, inter, E, k)))
     c = dict(x=x.cpu(), up=up[-1:].transpose(1, 2).cpu(), down=down[-1:].transpose(1, 2).cpu(), experts=torch.zeros(T, 1, dtype=torch.int32), weights=None, residual=None)
     assert_within(y, *moe_tests.expected(c, SILU, True, BF16, residual=False))
 

@@ -50,7 +50,9 @@ def place(c, layout):
 def workspace(nm, c, dtype):
     T, k = c["experts"].shape
     E, inter, d = c["down"].shape
-    return torch.full((nm.nm_moe_ffn_workspace_bytes(T, d, inter, E, k, dtype),), 0xFF, dtype=torch.uint8, device="cuda")     # nothing in it has to be cleared
+    ws = torch.full((nm.nm_moe_ffn_workspace_bytes(T, d, inter, E, k, dtype),), 0xFF, dtype=torch.uint8, device="cuda")
+    nm.nm_workspace_init(ws[:nm.WS_COUNTER_BYTES])                 # the counters; the rest may hold anything
+    return ws
 
 
 def run(c, act, gated, dtype, layout, first=0, residual=True):
