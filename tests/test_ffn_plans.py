@@ -48,6 +48,15 @@ def test_every_number_of_rows_of_an_expert(rows):
     assert_within(act_tests.run(A, W, b, r, SILU, False, BF16, ROW), *act_tests.expected(A, W, b, r, SILU, False, BF16))
 
 
+@pytest.mark.parametrize("K", [63, 1001, 2050])
+def test_one_row_of_any_length(K):
+    """The pitch of a single row is no pitch: row-major weights take the tensor-core kernel with any K."""
+    A, W, b, r = act_tests.make(1, 264, K, BF16, True, K)
+    assert_within(act_tests.run(A, W, b, r, SILU, True, BF16, ROW), *act_tests.expected(A, W, b, r, SILU, True, BF16))
+    c = moe_tests.make(1, K, 72, 5, 2, BF16, K)
+    assert_within(moe_tests.run(c, SILU, True, BF16, ROW), *moe_tests.expected(c, SILU, True, BF16))
+
+
 def test_many_pairs():
     """More pairs than a plan keeps in shared memory, and an expert that takes most of them."""
     T, d, inter, E, k = 5000, 64, 64, 20, 2
