@@ -22,6 +22,10 @@ int nm_debug_set_plan(int tile_n, int nsplit);
 /* Feed-forward products (nm_matmul_act, nm_moe_ffn): the chunks that an item of the last rounds is cut into, or as near to it as the workspace and the inner
  * dimension allow; 0 gives it back to the model.  Results of equal cuts have equal bits. */
 int nm_debug_set_ffn_cut(int parts);
+/* Debug build only (NM_ERR_UNSUPPORTED otherwise): hold threads of the feed-forward products up for `ns` (up to 2 s) each time they come to a place: 1 the copying
+ * thread before a copy, 2 the same before it passes the next chunk on, 3 the warp that issues products before a chunk's, 4 the epilogue before it gives an accumulator back, 5 half of it
+ * before an item's chunks are counted, 6 a warp of it before the next chunk is taken; 0 ends it.  Not once a wait of the CTA has expired, which a pause of more than a second brings about. */
+int nm_debug_set_ffn_pause(int where, unsigned ns);
 /* Force the kernel family for row-major bf16 weights (-1 heuristic; 0 plain-load kernel; 3 TMA-ring
  * CUDA-core kernel; 4 swap-AB tensor-core kernel) and the ring depth in stages (0 heuristic). */
 int nm_debug_set_kernel(int kind, int stages);

@@ -43,6 +43,7 @@ constexpr int kMaxStages = 12;
 constexpr int kRingBytes = 216 * 1024;
 
 std::atomic<int> g_forced_parts{0};             // nm_debug_set_ffn_cut
+std::atomic<unsigned long long> g_pause{0};     // nm_debug_set_ffn_pause: place | nanoseconds, from the top
 
 struct StreamArgs {
     Schedule schedule;                          // where the rows are known on the host
@@ -61,6 +62,7 @@ struct StreamArgs {
     float *partial; unsigned *counters; int ticket;
     Span in_bias, in_residual, in_out, in_scale, in_partial, in_tiles, in_order, in_experts, in_place;
     unsigned *status;
+    int pause_where; unsigned pause_ns;         // see nm_debug_set_ffn_pause
 };
 
 __device__ __forceinline__ bool elect_one()
@@ -69,6 +71,19 @@ __device__ __forceinline__ bool elect_one()
     asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
     return r != 0;
 }
+
+// Debug build: the CTAs' threads can be held up at named places (nm_debug_set_ffn_pause), to show that nothing depends on their pace.
+constexpr int kPausePlaces = 6;
+#ifdef NM_BOUNDS_CHECK
+__device__ __noinline__ void pause_here(unsigned ns)
+{
+    const uint64_t t0 = global_timer_ns();
+    while (global_timer_ns() - t0 < ns) __nanosleep(1000);
+}
+#define NM_PAUSE(where) do { if (a.pause_where == (where) && !*static_cast<volatile int *>(&s_abort)) pause_here(a.pause_ns); } while (0)
+#else
+#define NM_PAUSE(where) do { } while (0)
+#endif
 
 // Four rows of a 2-D tensor, 64 k each, to consecutive 128-byte rows of shared memory.
 __device__ __forceinline__ void tma_gather4(uint32_t dst, const CUtensorMap *map, int x, int r0, int r1, int r2, int r3, uint32_t bar, uint64_t policy)
@@ -454,6 +469,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                         }
                     }
                     if (n >= head) {
+                        NM_PAUSE(1);                              // before a copy
                         ok = mbar_try_wait(empty0 + 8 * s, ph) || mbar_wait(empty0 + 8 * s, ph, &s_abort, a.status);
                         if (!ok) break;
                         mbar_arrive_expect_tx(full0 + 8 * s, x.step_bytes);
@@ -464,6 +480,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                     if (++s == NS) { s = 0; ph ^= 1; }
                 }
                 t = t_next;
+                NM_PAUSE(2);                                      // before the next chunk is passed on
                 if (ok && more_than_one) {
                     ok = mbar_try_wait(taken0 + 8 * queue, queue_ph) || mbar_wait(taken0 + 8 * queue, queue_ph, &s_abort, a.status);
                     if (ok) { s_queue[queue] = id; mbar_arrive(queued0 + 8 * queue); }
@@ -492,6 +509,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
             const uint32_t d = tmem + (uint32_t)acc * kSlabs * a.acc_columns;
+            NM_PAUSE(3);                                          // before a chunk's products
             for (int k = c.k0; k < c.k1; ++k) {
                 ok = mbar_try_wait(full0 + 8 * s, ph) || mbar_wait(full0 + 8 * s, ph, &s_abort, a.status);
                 ok = __all_sync(0xffffffffu, ok);
@@ -580,6 +598,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                         NM_ST(mine + (j / 4 * kSlabs + sl) * kSlab + n_lane, make_float4(z[sl][0], z[sl][1], z[sl][2], z[sl][3]), a.in_partial, a.status);
                 }
             }
+            NM_PAUSE(4);                                          // before an accumulator is given back
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(acc_empty0 + 8 * acc);
@@ -587,6 +606,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             acc ^= 1;
 
             if (c.cut >= 0) {
+                if (turn == 0) NM_PAUSE(5);                       // (half of the warps) before an item's chunks are counted
                 named_barrier_sync(1, finishers);
                 if (thread == 0) {
                     __threadfence();                             // (all of the CTA's sums: the barrier comes first)
@@ -618,6 +638,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
             }
             if (!more_than_one) break;
             // One thread takes the next chunk for all, so that they agree where a wait runs out.
+            if (turn == 0 && quad == 1) NM_PAUSE(6);              // (a warp) before the next chunk is taken
             if (thread == 0) {
                 const bool ok = mbar_wait(queued0 + 8 * queue, queue_ph, &s_abort, a.status);
                 s_next[round] = ok ? *static_cast<volatile int *>(s_queue + queue) : sched.chunks;
@@ -762,6 +783,8 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     a.in_order = make_span(p.plan.order, 4 * (size_t)p.rows);
     a.in_experts = make_span(p.plan.experts, 4 * (size_t)p.plan.own_pairs); a.in_place = make_span(p.plan.place, 4 * (size_t)p.plan.own_pairs);
     a.status = device_status_ptr();
+    const unsigned long long pause = g_pause.load(std::memory_order_relaxed);
+    a.pause_ns = (unsigned)pause; a.pause_where = (int)(pause >> 32);
 
     CUtensorMap w[2];
     TokenMaps x;
@@ -819,6 +842,18 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
 
 extern "C" {
 #pragma GCC visibility push(default)
+
+int nm_debug_set_ffn_pause(int where, unsigned ns)
+{
+#ifdef NM_BOUNDS_CHECK
+    if (where < 0 || where > nm::kPausePlaces || ns > 2000000000u) return NM_ERR_INVALID_ARG;
+    nm::g_pause.store(((unsigned long long)where << 32) | ns, std::memory_order_relaxed);
+    return NM_OK;
+#else
+    (void)where; (void)ns;
+    return NM_ERR_UNSUPPORTED;
+#endif
+}
 
 int nm_debug_set_ffn_cut(int parts)
 {
