@@ -203,7 +203,6 @@ struct PlanArgs {
     int *n_rows;                                // rows there are in all
     Schedule *schedules;                        // of the two products
     CutModel model[2];
-    unsigned *counters;                         // cleared for the products that follow
     Span in_experts, in_tiles, in_order, in_place;
     unsigned *status;
 };
@@ -254,7 +253,6 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs a)
             if (lane == 0) a.schedules[warp] = best;
         }
     }
-    if (mine == 0) for (int i = tid; i < kCounterWords; i += kPlanThreads) a.counters[i] = 0u;
     for (int i = tid; i < own; i += kPlanThreads) NM_ST(a.tiles + tile0 + i, (RowTile{mine, row0 + i * a.R, min(a.R, count - i * a.R), 0}), a.in_tiles, a.status);
     if (count == 0) return;
     // Warp w: pairs [w, w + 1) of sixteen equal runs, 32 at a time.
@@ -492,7 +490,6 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
         pl.model[0] = stream_cut_model(pl.R, rows, inter, d, gated != 0, 1, E + pairs / pl.R);
         pl.model[1] = stream_cut_model(pl.R, rows, d, inter, false, 2, E + pairs / pl.R);
         pl.order = reinterpret_cast<int *>(ws + lay.order); pl.place = reinterpret_cast<int *>(ws + lay.place);
-        pl.counters = reinterpret_cast<unsigned *>(ws);
         pl.in_experts = in_experts; pl.in_tiles = make_span(pl.tiles, sizeof(RowTile) * (E + (size_t)pairs / pl.R));
         pl.in_order = make_span(pl.order, 4 * (size_t)pairs); pl.in_place = make_span(pl.place, 4 * (size_t)pairs);
         pl.status = status;
@@ -517,7 +514,7 @@ int nm_moe_ffn(const void *x, long ldx, const int32_t *experts, const float *wei
             p.x = sorted; p.ldx = d; p.x_rows = pairs; p.x_term = pairs * d;
         }
         p.out = h; p.ldo = inter;
-        p.counters = pl.counters; p.ticket = kTicketUp; p.partial = reinterpret_cast<float *>(ws + lay.partial);
+        p.counters = reinterpret_cast<unsigned *>(ws); p.ticket = kTicketUp; p.partial = reinterpret_cast<float *>(ws + lay.partial);
         if (e == cudaSuccess) e = launch_product(kOutHidden, gated != 0, p, s, &what);
 
         float *row_scale = reinterpret_cast<float *>(ws + lay.scale);

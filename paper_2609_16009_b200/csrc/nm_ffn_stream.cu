@@ -52,7 +52,7 @@ struct StreamArgs {
     int acc_columns;                            // of a slab: R, twice that where the terms have columns of their own
     bool apart, few;                            // few: four rows or fewer in a tile, as far as that is known: four epilogue warps then
     unsigned tmem_columns;
-    bool gather, clears, early_weights, programmatic;   // clears: the tickets, for the call that follows
+    bool gather, early_weights, programmatic;
     int act;
     RowPlan plan;
     CutModel model;                             // (of a plan made here)
@@ -487,8 +487,9 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
                     if (++queue == kQueue) { queue = 0; queue_ph ^= 1; }
                 }
             }
-            // Every CTA has had its last ticket (the value is looked at, so it has come): whoever is last to say so clears them for the next call.
-            if (more_than_one && a.clears && ticket != 0xffffffffu && atomicAdd(a.counters + kDone, 1u) == gridDim.x - 1) {
+            // Every CTA has had its last ticket (the value is looked at, so it has come): whoever is last to say so clears them.  Every product leaves the counters
+            // at zero, whoever made its plan: what uses the workspace next may be any call that has counters there.
+            if (more_than_one && ticket != 0xffffffffu && atomicAdd(a.counters + kDone, 1u) == gridDim.x - 1) {
                 a.counters[a.ticket] = 0u;
                 a.counters[kDone] = 0u;
             }
@@ -768,7 +769,7 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     a.few = p.expected_rows <= 4.f;
     a.acc_columns = a.apart ? 2 * p.R : p.R;
     a.tmem_columns = std::max(32, 2 * slabs * a.acc_columns);
-    a.gather = p.gather; a.clears = !p.planned || p.plan.own_pairs; a.early_weights = p.early_weights; a.programmatic = p.programmatic;
+    a.gather = p.gather; a.early_weights = p.early_weights; a.programmatic = p.programmatic;
     a.act = p.act; a.plan = p.plan; a.model = m;
     a.bias = static_cast<const uint16_t *>(p.bias); a.residual = static_cast<const uint16_t *>(p.residual); a.ld_residual = p.ld_residual;
     a.out = p.out; a.ldo = p.ldo; a.out_term = (long)p.rows * p.ldo; a.row_scale = p.row_scale;
