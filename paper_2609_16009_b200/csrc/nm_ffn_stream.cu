@@ -49,6 +49,7 @@ struct StreamArgs {
     Schedule schedule;                          // where the rows are known on the host
     int kb, column_tiles, tile_n;               // steps of an item, column tiles of a row tile, outputs of one
     int rows, N, R, box_rows, nstage, stage_bytes;   // box_rows: the least of the box heights, the others its multiples
+    int first_map;                              // of the token maps: one that there is, and that of the first tile where its rows are known
     int acc_columns;                            // of a slab: R, twice that where the terms have columns of their own
     bool apart, few;                            // few: four rows or fewer in a tile, as far as that is known: four epilogue warps then
     unsigned tmem_columns;
@@ -103,6 +104,21 @@ __device__ __forceinline__ unsigned ask_ticket(unsigned *counter)
 
 // Token rows: boxes of 1, 2, 3 and 4 times box_rows rows (the first alone for gathered rows).
 struct TokenMaps { CUtensorMap of[4]; };
+
+// Debug build: a token map is looked at before it is used, as an address is; one that was not made is all zeros.
+#ifdef NM_BOUNDS_CHECK
+__device__ __noinline__ bool map_made(const CUtensorMap *map, unsigned *status)
+{
+    const uint32_t *words = reinterpret_cast<const uint32_t *>(map);
+    uint32_t any = 0u;
+    for (unsigned i = 0; i < sizeof(CUtensorMap) / 4; ++i) any |= words[i];
+    if (!any && status) atomicOr(status, kStatusOutOfBounds);
+    return any != 0u;
+}
+#define NM_MAP_MADE(map, st) map_made((map), (st))
+#else
+#define NM_MAP_MADE(map, st) true
+#endif
 
 // A chunk: steps [k0, k1) of an item; where that is not all of it, the place of its sums and of the item's first chunk's, and the item's counter.
 struct Chunk { int item, k0, k1, slot, first_slot, cut; };
@@ -365,7 +381,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_w0, const __grid_constant_
     const int NS = a.nstage, finishers = (int)blockDim.x - 64;
 
     if (warp == 0) {
-        if (lane == 0) { tma_prefetch_descriptor(&map_w0); if (kGated) tma_prefetch_descriptor(&map_w1); tma_prefetch_descriptor(&maps_x.of[0]); s_abort = 0; }
+        if (lane == 0) { tma_prefetch_descriptor(&map_w0); if (kGated) tma_prefetch_descriptor(&map_w1); if (NM_MAP_MADE(&maps_x.of[a.first_map], a.status)) tma_prefetch_descriptor(&maps_x.of[a.first_map]); s_abort = 0; }
         if (lane < NS) { mbar_init(full0 + 8 * lane, 1); mbar_init(empty0 + 8 * lane, 1); }
         if (lane < kQueue) { mbar_init(queued0 + 8 * lane, 1); mbar_init(taken0 + 8 * lane, 2); }      // (taken by the MMA warp and the epilogue)
         if (lane < 2) { mbar_init(acc_full0 + 8 * lane, 1); mbar_init(acc_empty0 + 8 * lane, (uint32_t)finishers / 32); }
@@ -788,7 +804,7 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
     a.pause_ns = (unsigned)pause; a.pause_where = (int)(pause >> 32);
 
     CUtensorMap w[2];
-    TokenMaps x;
+    TokenMaps x{};                              // (heights that there cannot be stay zero)
     const uint16_t *W = static_cast<const uint16_t *>(p.W);
     bool ok = true;
     auto weight_map = [&](CUtensorMap *map, const uint16_t *W, long expert, int N, int K, int wide) {
@@ -811,6 +827,7 @@ cudaError_t launch_product(int mode, bool gated, const ProductArgs &p, cudaStrea
         const cuuint64_t dims[3] = {(cuuint64_t)p.K, (cuuint64_t)p.x_rows, (cuuint64_t)p.terms}, strides[2] = {(cuuint64_t)p.ldx * 2, (cuuint64_t)p.x_term * 2};
         // (only the heights that there can be: of a full tile and of the last one, where the rows are known)
         const int whole_box = p.R / a.box_rows - 1, last_box = p.planned ? 0 : (p.rows - 1) % p.R / a.box_rows;
+        a.first_map = p.planned ? 0 : p.rows < p.R ? last_box : whole_box;
         for (int i = 0; i <= whole_box; ++i) {
             if (!p.planned && i != last_box && (i != whole_box || p.rows < p.R)) continue;
             const cuuint32_t box[3] = {kKT, (cuuint32_t)((i + 1) * a.box_rows), 1};
