@@ -6,8 +6,15 @@
 namespace nm {
 
 // ---- activations, fp32 -------------------------------------------------------------------------------------------------------
-// Of n values at once: one branch.  __expf is within 2 + |1.2 x| steps of exp(x) and the quotient within 2, which the 16 or 17 bits that are kept do not see;
-// a denominator beyond 2^126 makes the quotient 0, as near as fp32 gets.
+// Of n values at once: one branch.  __expf is within 2 + |1.2 x| steps of exp(x) and the quotient within 2, which the 16 bits that are kept do not see.
+// x / (1 + exp(-2 s)), s half of the exponent (of x itself, or of the tanh form's polynomial).  From h = exp(-|s|): the quotient is x / (1 + h h) for s >= 0 and
+// x h h / (1 + h h) below, so the denominator stays in [1, 2] and h is a normal number as long as the result is one.  (exp(-2 s) itself leaves fp32 at -89, and
+// __fdividef gives 0 from a denominator of 2^126 on: silu(-87.5) = -8.7e-37 is a normal number in fp32 and in bf16.)  Below 2^-126 the result is within steps of 2^-149.
+__device__ __forceinline__ float gated_by_exp(float x, float s)
+{
+    const float h = __expf(-fabsf(s));
+    return __fdividef(s < 0.f ? x * h * h : x, fmaf(h, h, 1.f));
+}
 template <int n>
 __device__ __forceinline__ void activate(int act, float (&v)[n])
 {
@@ -18,7 +25,7 @@ __device__ __forceinline__ void activate(int act, float (&v)[n])
         break;
     case NM_ACT_SILU:
 #pragma unroll
-        for (int i = 0; i < n; ++i) v[i] = __fdividef(v[i], 1.f + __expf(-v[i]));
+        for (int i = 0; i < n; ++i) v[i] = gated_by_exp(v[i], 0.5f * v[i]);
         break;
     case NM_ACT_GELU:
 #pragma unroll
@@ -26,7 +33,7 @@ __device__ __forceinline__ void activate(int act, float (&v)[n])
         break;
     case NM_ACT_GELU_TANH:                                                              // 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z))
 #pragma unroll
-        for (int i = 0; i < n; ++i) v[i] = __fdividef(v[i], 1.f + __expf(-1.59576912f * (v[i] + 0.044715f * v[i] * v[i] * v[i])));
+        for (int i = 0; i < n; ++i) v[i] = gated_by_exp(v[i], 0.79788456f * (v[i] + 0.044715f * v[i] * v[i] * v[i]));
         break;
     default: break;
     }
