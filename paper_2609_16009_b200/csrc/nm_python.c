@@ -15,10 +15,11 @@ static act_fn g_act;
 static moe_fn g_moe;
 static PyObject *g_data_ptr;                     /* "data_ptr" */
 
-/* Errors are looked for once, after all of the arguments: PyErr_Occurred. */
+/* The first error stands: what is behind it is not looked at (nothing of Python may be called with an error set), and the caller asks once, after all of the
+ * arguments. */
 static void *ptr(PyObject *o)
 {
-    if (o == Py_None) return NULL;
+    if (o == Py_None || PyErr_Occurred()) return NULL;
     if (PyLong_Check(o)) return PyLong_AsVoidPtr(o);
     PyObject *p = PyObject_CallMethodNoArgs(o, g_data_ptr);
     if (!p) return NULL;
