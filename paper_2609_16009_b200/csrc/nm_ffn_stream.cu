@@ -142,7 +142,9 @@ __device__ __forceinline__ void make_plan(const StreamArgs &a, OwnPlan &own, boo
     const int p = threadIdx.x, pairs = a.plan.own_pairs, lane = p & 31;
     int e = 0xffff;                                               // not held here
     if (p < pairs) {
-        const long v = (long)NM_LD(a.plan.experts + p, a.in_experts, a.status) - a.plan.first;
+        // (past L1, as all that is read ahead of the wait: the kernel that wrote it is two back, and no wait of this one makes its lines new)
+        const int32_t *at = a.plan.experts + p;
+        const long v = (long)(NM_INSIDE(at, 4, a.in_experts, a.status) ? __ldcg(at) : 0) - a.plan.first;
         if (v >= 0 && v < a.plan.E) e = (int)v;
         own.expert[p] = (uint16_t)e;
     }
