@@ -363,16 +363,16 @@ cudaError_t launch_route(const RouteArgs &a, cudaStream_t stream)
     return cudaLaunchKernelEx(&cfg, route_kernel<TL, kPer>, a);
 }
 
-template <typename TL>
+// Experts a lane: the least of 2, 4, .. 16, 20, 24 and 32 that holds them all.  Two more than needed cost 4 to 13% (8192 tokens, sigmoid and bias, no groups, us: 64 experts
+// with two or four 11.2, 11.9; 160 with six or eight 13.9, 15.0; 256 with eight or ten 16.8, 17.9; 320 with ten or twelve 20.2, 22.8; 448 with fourteen or
+// sixteen 25.6, 27.3; 640 with twenty or twenty-four 38.9, 44.0, with thirty-two 51.8; 768 with twenty-four or thirty-two 50.6, 58.3).  Wider steps from sixteen on, where
+// the kernel is at its registers' bound (sixteen: 72, twenty 91, twenty-four 101, thirty-two 128): twenty-eight is no faster than thirty-two (896 without a bias 38.8 and
+// 36.6, 16 tokens 9.2 and 8.5).
+template <typename TL, int kPer>
 cudaError_t launch_by_width(const RouteArgs &a, cudaStream_t s)
 {
-    if (a.E <= 64) return launch_route<TL, 2>(a, s);
-    if (a.E <= 128) return launch_route<TL, 4>(a, s);
-    if (a.E <= 256) return launch_route<TL, 8>(a, s);
-    if (a.E <= 320) return launch_route<TL, 10>(a, s);
-    if (a.E <= 384) return launch_route<TL, 12>(a, s);
-    if (a.E <= 512) return launch_route<TL, 16>(a, s);
-    return launch_route<TL, 32>(a, s);
+    if constexpr (32 * kPer >= kMaxE) return launch_route<TL, kPer>(a, s);
+    else return a.E <= 32 * kPer ? launch_route<TL, kPer>(a, s) : launch_by_width<TL, kPer + (kPer < 16 ? 2 : kPer < 24 ? 4 : 8)>(a, s);
 }
 
 }  // namespace
@@ -407,7 +407,7 @@ int nm_moe_route(const void *logits, long ld_logits, const float *bias, int32_t 
     a.in_weights = make_span(weights, 4 * (size_t)T * top_k);
     a.status = bounds_status_ptr();
     cudaStream_t s = (cudaStream_t)stream;
-    const cudaError_t e = dtype == NM_F32 ? launch_by_width<float>(a, s) : dtype == NM_BF16 ? launch_by_width<bf16_t>(a, s) : launch_by_width<f16_t>(a, s);
+    const cudaError_t e = dtype == NM_F32 ? launch_by_width<float, 2>(a, s) : dtype == NM_BF16 ? launch_by_width<bf16_t, 2>(a, s) : launch_by_width<f16_t, 2>(a, s);
     return e == cudaSuccess ? NM_OK : record_cuda_error(e, "expert routing launch");
 }
 
