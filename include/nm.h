@@ -280,7 +280,8 @@ int nm_matmul_act(const void *A, long lda, const void *B, const void *bias, cons
  *   dtype              NM_BF16 or NM_F16, of x, the weights, residual and out alike; NM_ERR_UNSUPPORTED otherwise
  *   T * top_k          up to 2^22; d and inter up to 2^20; E up to NM_MAX_EXPERTS
  * Sums and activations are fp32, h is kept to 16 bits or more, the result is rounded once.  The weights of an expert that no token chose
- * are not read.  Equal calls give equal bits.  Operands whose rows all start on 16 bytes (d and inter multiples of 8) take the tensor-core kernels, any others simple ones.
+ * are not read.  Tiles are laid out for T * top_k / E rows an expert, as if all choices were held here: where most are not, a call is right and up to a tenth slower than
+ * one of the held choices alone.  Equal calls give equal bits.  Operands whose rows all start on 16 bytes (d and inter multiples of 8) take the tensor-core kernels, any others simple ones.
  * Workspace: nm_moe_ffn_workspace_bytes, counters cleared once by nm_workspace_init (and again after NM_ERR_TIMEOUT); the rest may hold anything, and nothing is kept from
  * one call for the next.  Calls that overlap on the GPU (two captured graphs among them) need workspaces of their own.  Honours nm_set_programmatic_launch.
  */

@@ -5,8 +5,8 @@
 //
 // What bounds them: the weights of every expert that some token chose, read once from HBM.  The products are in nm_ffn_stream.cu; here is what stands around them - rows by
 // expert, rows sorted, fp16 hidden values scaled into range, the weighted sum of a token's experts - the host side, and the products for operands that tensor
-// maps cannot address (rows that do not start on 16 bytes): fp32 sums on CUDA cores, a hundred times as long for many rows (1024 tokens through 6 of
-// 64 experts of 7168 x 1536 138 ms).
+// maps cannot address (rows that do not start on 16 bytes): fp32 sums on CUDA cores, four times as long for one row of 2048 x 4004, 13 times for 100, a hundred
+// and more for many (1024 tokens through 6 of 64 experts of 7168 x 1536 138 ms).
 #include <algorithm>
 
 #include "nm_ffn.cuh"
@@ -20,8 +20,8 @@ constexpr int kMaxPairs = 1 << 22, kMaxDim = 1 << 20;  // (items and chunks are 
 
 // ---- products of operands of any alignment -----------------------------------------------------------------------------------
 // A block of four warps computes 32 outputs of one row.  Column-major weights: a warp per output in turn, lanes along k.  Row-major: a lane
-// per output, the warps along k, their sums joined in shared memory.  What is read is read element by element; there is nothing to reuse but
-// the row itself, which stays in L1.
+// per output, the warps along k, their sums joined in shared memory.  What is read is read element by element.  One row a block: the row stays in L1, and the weights are
+// read again for every row, from L2 as far as they fit (100 rows of 2048 x 4004: 328 us, 70 for one).  It is there to be right for operands that are laid out so, not for many rows.
 constexpr int kSimpleN = 32, kSimpleThreads = 128;
 
 struct SimpleArgs {
@@ -292,7 +292,8 @@ __global__ void __launch_bounds__(256) sort_rows_kernel(const uint16_t *x, long 
 
 // ---- fp16: hidden values beyond the type's range ---------------------------------------------------------------------------------
 // act(g) * u may leave fp16 at either end, so a row is scaled by a power of two that brings its largest value to 2^14 .. 2^15, and the product's
-// row is scaled back (fp32, exact).  Two terms: 22 bits, down to 2^-40 of the row's largest.
+// row is scaled back (fp32, exact).  Two terms: 22 bits, down to 2^-40 of the row's largest.  All pairs' rows are walked over, those of choices held elsewhere too, although nobody
+// wrote them: what comes of these is not read (the number of rows there are would be one more load before the first).
 __global__ void __launch_bounds__(256) hidden_terms_kernel(const float *h, uint16_t *terms, float *row_scale, int rows, int n, unsigned *status, Span in_h, Span in_terms, Span in_scale)
 {
     __shared__ float s_max[8];

@@ -268,7 +268,7 @@ struct Rows {
                 } else if constexpr (kF16) {
                     NM_ST(reinterpret_cast<float *>(out[i]) + sl * kSlab, v, a.in_out, a.status);
                 } else {
-                    // The upper half of the word and what is left of it, rounded: 2^-17 of the value.  (Cut off, not rounded, so that no finite
+                    // The upper half of the word (8 bits) and what is left of it (16), rounded to 8: 2^-16 of the value.  (Cut off, not rounded, so that no finite
                     // value becomes an infinite term; an infinity or a NaN is the first term alone.)
                     const uint32_t hi = __float_as_uint(v) & 0xffff0000u;
                     const float rest = v - __uint_as_float(hi);
